@@ -58,10 +58,13 @@ typedef enum {
     LUVC_ERR_WORKSPACE = 8,  /* caller workspace too small or misaligned */
     LUVC_ERR_CUDA = 9,       /* a CUDA call failed (allocation, copy, launch) */
     LUVC_ERR_TIMEOUT = 10,   /* a bounded device-side wait gave up */
-    LUVC_ERR_INTERNAL = 11
+    LUVC_ERR_INTERNAL = 11,
+    LUVC_ERR_PAGES = 12      /* not enough free pages, or table entries, in a key-value cache */
 } luvc_status;
 
-typedef enum { LUVC_BF16 = 0, LUVC_F32 = 1 } luvc_dtype;
+/* LUVC_E4M3 (8-bit floats, 4 exponent and 3 mantissa bits, no infinities) is a type of
+ * key-value caches only. */
+typedef enum { LUVC_BF16 = 0, LUVC_F32 = 1, LUVC_E4M3 = 2 } luvc_dtype;
 
 /* Cutoff used when the caller passes cutoff <= 0.  The paper never states the
  * value of its sigma_t; 1/8 of the band is this library's choice. */
@@ -368,6 +371,142 @@ int luvc_spu_prune_static(const void* hidden, int B, int N, int D, float cutoff,
  * LUVC_ERR_TIMEOUT when a bounded wait gave up); the next call clears it.  Allocates nothing.
  * (No counterpart in the paper.) */
 int luvc_spu_static_status(void* cuda_stream);
+
+/* ---- paged key-value cache ------------------------------------------------ */
+
+/*
+ * The tokens that OIM and SPU leave end as rows of the language model's key-value cache.  (The paper
+ * stops at the pruned hidden states; these operators are what a decoder does with them next.)  A cache
+ * belongs to a group of `layers` decoder layers that hold the same tokens: the layers before a prune and
+ * those after it hold different ones, so each group has a cache of its own.  Its tokens live in pages of
+ * page_size tokens of a pool; a sequence is a slot with a length and a list of pages.
+ *
+ * All arrays are DEVICE memory of the caller (16-byte aligned pools, 4-byte aligned books); the struct
+ * itself is host memory and is read during the call only.  The books of a new cache are lengths = 0,
+ * refs = 0, table = -1; only the functions below write them, entirely on the device, so that a call's
+ * page numbers need no host round trip and the calls can be captured in a CUDA graph (after a warm-up
+ * call has grown the library's scratch, or with a workspace of the caller's).
+ */
+typedef struct {
+    void* k;                 /* [layers, pages, heads, page_size, D] of element type dtype */
+    void* v;                 /* the same shape */
+    int32_t* lengths;        /* [slots] tokens of each sequence; 0: the slot is empty */
+    int32_t* refs;           /* [pages] sequences that hold the page; 0: the page is free */
+    int32_t* table;          /* [slots, max_pages] page of each run of page_size tokens, -1 past the sequence */
+    const float* k_scale;    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; else NULL */
+    const float* v_scale;    /* the same for the values */
+    int layers, pages, heads, page_size, D, slots, max_pages;
+    int dtype;               /* LUVC_BF16, LUVC_F32 or LUVC_E4M3 */
+} luvc_kv_cache;
+
+/*
+ * Limits: page_size a multiple of 16; D a multiple of 8 (of 16 for LUVC_E4M3, of 4 for LUVC_F32) up to
+ * 256; at most 4096 sequences per call; layers * heads <= 65536; at most 2^31 - 1 token rows
+ * (pages * heads * page_size) per layer and 2^31 - 1 tokens per sequence.  Offsets into the pools are 64-bit.
+ */
+typedef struct {
+    void* stream;            /* cudaStream_t; NULL = legacy default stream */
+    void* workspace;         /* device, 256-byte aligned; NULL = library-owned scratch */
+    size_t workspace_bytes;
+    int32_t* device_status;  /* optional device block of LUVC_STATUS_BYTES (see luvc_read_status);
+                                NULL = the library-owned word of the current device */
+} luvc_kv_opts;
+
+/* Bytes of workspace luvc_kv_fork and luvc_kv_compact need for n sequences of this cache (the other
+ * luvc_kv_* calls need none).  0 for invalid arguments. */
+size_t luvc_kv_workspace_bytes(const luvc_kv_cache* cache, int n);
+
+/*
+ * Common to the calls below: `seqs` is a DEVICE array of n distinct slots, NULL = slots 0 .. n-1; opts may
+ * be NULL (default stream, library-owned scratch and status word).  Free pages are handed out lowest
+ * number first, in the order of the call's sequences.  What only the device can see is written to the
+ * status word and leaves the cache as it was: LUVC_ERR_PAGES (too few free pages, or max_pages exceeded),
+ * LUVC_ERR_SHAPE (a slot out of range or named twice, a negative count), LUVC_ERR_KEEP (compact: a block
+ * outside its sequence, more kept tokens than block), LUVC_ERR_TARGET (fork: dst not empty).  Calls that
+ * find a set word do nothing.
+ */
+
+/* Room for counts[i] (DEVICE, n entries, >= 0) further tokens at the end of each sequence: pages are
+ * taken, table and lengths extended.  luvc_kv_write then fills the rows, layer by layer. */
+int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, const int32_t* counts,
+                    const luvc_kv_opts* opts);
+
+/*
+ * Writes the key and value rows of the LAST tokens of n sequences into one layer.
+ *
+ * k, v        [tokens, heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or E4M3 cache, LUVC_F32 for
+ *             an f32 cache.  k_stride / v_stride: elements from one token to the next (rows of a fused
+ *             projection need no copy); a token's heads * D elements are contiguous
+ * starts      DEVICE [n + 1], ascending: sequence i owns rows starts[i] .. starts[i+1]-1, which are its
+ *             last starts[i+1] - starts[i] tokens; starts[0] = 0, starts[n] = tokens.  NULL: one token each
+ *             (tokens = n)
+ * sizes       optional DEVICE [tokens] int32, the out_sizes of luvc_oim_merge*: the values are written
+ *             enhanced, V + log(size) (Eq. 2), formed in fp32 and rounded once
+ * An E4M3 cache stores x / scale, saturated at +-448, rounded to nearest even.  Rows that would fall before
+ * the start of their sequence are not written (LUVC_ERR_SHAPE in the status word).
+ */
+int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,
+                  long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes,
+                  int dtype, const luvc_kv_opts* opts);
+
+/* Sequence dst[i] (DEVICE, n distinct empty slots) becomes a copy of sequence src[i] (DEVICE; the same
+ * source may be named several times) in all layers.  Full pages are shared and counted in refs; the
+ * rows of a partly filled last page are copied to a page of its own, so that either sequence may grow. */
+int luvc_kv_fork(const luvc_kv_cache* cache, const int32_t* src, const int32_t* dst, int n, const luvc_kv_opts* opts);
+
+/* Empties the slots; pages that no sequence holds any more are free again.  (A slot named twice is freed once.) */
+int luvc_kv_free(const luvc_kv_cache* cache, const int32_t* seqs, int n, const luvc_kv_opts* opts);
+
+/*
+ * Drops pruned tokens from n sequences, in all layers: of the block of span[i] tokens from first[i] on,
+ * only the tokens idx[i][0 .. count-1] (relative to the block, strictly ascending) stay, together with all
+ * tokens before and after the block.  idx is the out_idx of luvc_spu_prune* as it is.
+ *
+ * first, span DEVICE [n]; idx DEVICE [n, keep]; counts optional DEVICE [n], entries of idx that count
+ *             (NULL: keep)
+ * The kept tokens close up in order.  Leading full pages of which nothing moves stay where they are
+ * (and stay shared); all other rows are copied to newly taken pages and the old pages are given back
+ * afterwards, so sequences that share pages with this one are not touched, and the pool needs the new pages
+ * free at the call.  An idx entry outside the block is replaced by the nearest one inside
+ * (LUVC_ERR_KEEP in the status word, after the fact).
+ */
+int luvc_kv_compact(const luvc_kv_cache* cache, const int32_t* seqs, int n, const int32_t* first, const int32_t* span,
+                    const int32_t* idx, int keep, const int32_t* counts, const luvc_kv_opts* opts);
+
+/* ---- attention of one new token ------------------------------------------- */
+
+/* Bytes of workspace luvc_attn_decode needs on the current device, whatever the sequences; 0 on error. */
+size_t luvc_attn_workspace_bytes(void);
+
+typedef struct {
+    void* stream;            /* cudaStream_t; NULL = legacy default stream */
+    void* workspace;         /* device, 256-byte aligned, ZEROED by the caller before its first use (a call leaves
+                                what must be zero zeroed); NULL = library-owned scratch */
+    size_t workspace_bytes;
+    int32_t* device_status;  /* as in luvc_kv_opts */
+    float scale;             /* factor of the scores; 0 = 1 / sqrt(D) */
+    const float* key_bias;   /* optional DEVICE [n, bias_stride] fp32, added to the scores: log(size) of merged tokens,
+                                or a mask (-inf, or the lowest finite value).  Keys at and past bias_width get 0 */
+    int bias_width;          /* entries per row that may be read */
+    long long bias_stride;   /* elements from one row to the next, >= bias_width */
+    float* lse;              /* optional DEVICE [n, q_heads] fp32: log of the sum of exp(score), -inf where no key is left */
+} luvc_attn_opts;
+
+/*
+ * out[i, h, :] = sum_t p_t V[t] / sum_t p_t,  p_t = exp(scale * <q[i, h], K[t]> + key_bias[i, t]),
+ * over the tokens t < lengths[seqs[i]] of one layer; query head h reads key head h / (q_heads / heads).
+ *
+ * q, out      [n, q_heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or E4M3 cache, LUVC_F32 for an
+ *             f32 cache; q_stride: elements from one sequence's queries to the next (a sequence's q_heads * D
+ *             elements are contiguous); out is dense
+ * seqs        DEVICE [n] slots, NULL = 0 .. n-1; a slot may be named several times.  A slot out of range
+ *             reads as empty (LUVC_ERR_SHAPE in the status word)
+ * A sequence without tokens, or whose keys are all masked by -inf, gives a row of zeros.  A key masked
+ * by -inf contributes nothing, whatever its rows hold; rows past the length are never used.  Scores,
+ * softmax and sums are fp32; results do not depend on timing or on other streams.
+ */
+int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,
+                     int q_heads, int dtype, void* out, const luvc_attn_opts* opts);
 
 #ifdef __cplusplus
 }

@@ -1,8 +1,8 @@
 """Python binding of the LUVC C-ABI library (``include/luvc.h``).
 
-Argument marshalling only: every step of OIM (Section 3.2 of arXiv 2512.09010) and
-SPU (Section 3.3, Algorithm 2) runs inside ``libluvc.so``'s CUDA kernels.  PyTorch
-is used for device memory and streams.  There is no CPU fallback: if the shared
+Argument marshalling only: every step of OIM (Section 3.2 of arXiv 2512.09010), of
+SPU (Section 3.3, Algorithm 2) and of the paged key-value cache that takes their tokens
+runs inside ``libluvc.so``'s CUDA kernels.  PyTorch is used for device memory and streams.  There is no CPU fallback: if the shared
 library cannot be built or loaded, importing this package fails.
 """
 from __future__ import annotations
@@ -14,13 +14,14 @@ import torch
 
 from . import _build
 
-BF16, F32 = 0, 1
+BF16, F32, E4M3 = 0, 1, 2
 DEFAULT_CUTOFF = 0.125
 
 STATUS_NAMES = {
     0: "LUVC_OK", 1: "LUVC_ERR_NULL", 2: "LUVC_ERR_SHAPE", 3: "LUVC_ERR_TARGET", 4: "LUVC_ERR_KEEP",
     5: "LUVC_ERR_CUTOFF", 6: "LUVC_ERR_ALIGN", 7: "LUVC_ERR_DTYPE", 8: "LUVC_ERR_WORKSPACE",
     9: "LUVC_ERR_CUDA", 10: "LUVC_ERR_TIMEOUT", 11: "LUVC_ERR_INTERNAL",
+    12: "LUVC_ERR_PAGES",
 }
 
 # every symbol include/luvc.h declares
@@ -30,7 +31,8 @@ EXPORTS = (
     "luvc_oim_plan", "luvc_oim_plan_anyres", "luvc_oim_workspace_bytes", "luvc_oim_workspace_bytes_ex", "luvc_oim_merge", "luvc_oim_merge_f32", "luvc_oim_merge_ex",
     "luvc_oim_merge_host", "luvc_oim_value_enhance", "luvc_spu_sigma", "luvc_spu_workspace_bytes", "luvc_spu_prune",
     "luvc_spu_prune_f32", "luvc_spu_prune_ex", "luvc_spu_prune_host", "luvc_spu_prune_static", "luvc_spu_static_status",
-    "luvc_spu_cascade",
+    "luvc_spu_cascade", "luvc_kv_workspace_bytes", "luvc_kv_reserve", "luvc_kv_write", "luvc_kv_fork", "luvc_kv_free",
+    "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode",
 )
 
 
@@ -56,6 +58,30 @@ class SpuOpts(ctypes.Structure):
         ("dtype", ctypes.c_int), ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_size_t), ("no_window", ctypes.c_int), ("out_scores", ctypes.c_void_p),
         ("device_status", ctypes.c_void_p),
+    ]
+
+
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+        ("table", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("layers", ctypes.c_int),
+        ("pages", ctypes.c_int), ("heads", ctypes.c_int), ("page_size", ctypes.c_int), ("D", ctypes.c_int),
+        ("slots", ctypes.c_int), ("max_pages", ctypes.c_int), ("dtype", ctypes.c_int),
+    ]
+
+
+class KvOpts(ctypes.Structure):
+    _fields_ = [
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("device_status", ctypes.c_void_p),
+    ]
+
+
+class AttnOpts(ctypes.Structure):
+    _fields_ = [
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("device_status", ctypes.c_void_p), ("scale", ctypes.c_float), ("key_bias", ctypes.c_void_p),
+        ("bias_width", ctypes.c_int), ("bias_stride", ctypes.c_longlong), ("lse", ctypes.c_void_p),
     ]
 
 
@@ -100,6 +126,17 @@ def _load() -> ctypes.CDLL:
     L.luvc_spu_prune_host.argtypes = [p, i, i, i, f, i, i, p, p]
     L.luvc_spu_prune_static.argtypes = [p, i, i, i, f, i, i, p, p, p]
     L.luvc_spu_cascade.argtypes = [p, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(f), i, p, p, p]
+    cache, kv, ll = ctypes.POINTER(KvCacheStruct), ctypes.POINTER(KvOpts), ctypes.c_longlong
+    L.luvc_kv_workspace_bytes.restype = sz
+    L.luvc_kv_workspace_bytes.argtypes = [cache, i]
+    L.luvc_kv_reserve.argtypes = [cache, p, i, p, kv]
+    L.luvc_kv_write.argtypes = [cache, i, p, i, p, p, ll, ll, i, p, p, i, kv]
+    L.luvc_kv_fork.argtypes = [cache, p, p, i, kv]
+    L.luvc_kv_free.argtypes = [cache, p, i, kv]
+    L.luvc_kv_compact.argtypes = [cache, p, i, p, p, p, i, p, kv]
+    L.luvc_attn_workspace_bytes.restype = sz
+    L.luvc_attn_workspace_bytes.argtypes = []
+    L.luvc_attn_decode.argtypes = [p, ll, cache, i, p, i, i, i, p, ctypes.POINTER(AttnOpts)]
     return L
 
 
@@ -356,3 +393,180 @@ def spu_prune_host(hidden: torch.Tensor, keep: int, cutoff: float, out_idx: torc
     _check(lib.luvc_set_stream(_stream_ptr(None)), "luvc_set_stream")
     _check(lib.luvc_spu_prune_host(hidden.data_ptr(), B, N, D, float(cutoff), int(keep), _dtype_code(hidden),
                                    out_idx.data_ptr(), out_hidden.data_ptr()), "luvc_spu_prune_host")
+
+
+# ---- paged key-value cache and the attention over it ---------------------------------------------
+
+
+class KvCache:
+    """A paged key-value cache of a group of decoder layers that hold the same tokens (luvc_kv_cache).
+
+    k, v: the caller's pools, CUDA tensors [layers, pages, heads, page_size, D] in bfloat16, float32 or
+    float8_e4m3fn (then with k_scale / v_scale, float32 [layers, heads]: a stored x stands for x * scale).
+    slots: sequences; max_pages: pages a sequence may have.  meta: optional int32 tensor of
+    slots + pages + slots * max_pages entries that holds the books (made empty if not given); `lengths`, `refs`
+    and `table` are views of it, so that one copy of `meta` is a snapshot of all three."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, slots: int, max_pages: int, *, meta: torch.Tensor | None = None,
+                 k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        if not (k.is_cuda and v.is_cuda and k.device == v.device):
+            raise ValueError("the pools must live on one CUDA device")
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v must be contiguous [layers, pages, heads, page_size, D] tensors of one shape and type")
+        if k.dtype not in _CACHE_DTYPES:
+            raise TypeError("a key-value cache holds bfloat16, float32 or float8_e4m3fn, got %s" % k.dtype)
+        layers, pages, heads, page_size, D = k.shape
+        size = slots + pages + slots * max_pages
+        if meta is None:
+            meta = torch.zeros(size, dtype=torch.int32, device=k.device)
+            meta[slots + pages:] = -1
+        if meta.dtype != torch.int32 or meta.shape != (size,) or not meta.is_contiguous() or meta.device != k.device:
+            raise ValueError("meta must be a contiguous int32 tensor of %d entries on the pools' device" % size)
+        for s in (k_scale, v_scale):
+            if (s is not None) != (k.dtype == torch.float8_e4m3fn):
+                raise ValueError("k_scale and v_scale go with float8_e4m3fn pools, and only with them")
+            if s is not None and (s.dtype != torch.float32 or s.shape != (layers, heads) or not s.is_contiguous()
+                                  or s.device != k.device):
+                raise ValueError("scales must be contiguous float32 [layers, heads] tensors on the pools' device")
+        self.k, self.v, self.meta, self.k_scale, self.v_scale = k, v, meta, k_scale, v_scale
+        self.lengths = meta[:slots]
+        self.refs = meta[slots:slots + pages]
+        self.table = meta[slots + pages:].view(slots, max_pages)
+        self.device, self.dtype = k.device, k.dtype
+        self.layers, self.pages, self.heads, self.page_size, self.head_dim = layers, pages, heads, page_size, D
+        self.slots, self.max_pages = slots, max_pages
+        self.io_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16    # of queries, new rows, outputs
+        self.struct = KvCacheStruct(
+            k.data_ptr(), v.data_ptr(), self.lengths.data_ptr(), self.refs.data_ptr(), self.table.data_ptr(),
+            k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None,
+            layers, pages, heads, page_size, D, slots, max_pages, _CACHE_DTYPES[k.dtype])
+
+
+_CACHE_DTYPES = {torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: E4M3}
+
+
+def _ints(t: torch.Tensor | None, cache: KvCache, shape, name: str):
+    """Address of a contiguous int32 tensor of the given shape on the cache's device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != cache.device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on %s" % (name, tuple(shape), cache.device))
+    return t.data_ptr()
+
+
+def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
+    o = KvOpts(stream=_stream_ptr(cache.device))
+    if workspace is not None:
+        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if device_status is not None:
+        o.device_status = device_status.data_ptr()
+    return o
+
+
+def kv_workspace_bytes(cache: KvCache, n: int) -> int:
+    return int(lib.luvc_kv_workspace_bytes(cache.struct, n))
+
+
+def attn_workspace_bytes() -> int:
+    return int(lib.luvc_attn_workspace_bytes())
+
+
+def kv_reserve(cache: KvCache, counts: torch.Tensor, *, seqs: torch.Tensor | None = None,
+               device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_reserve: room for counts[i] further tokens of each sequence (int32 [n]); seqs: slots (None: 0 .. n-1)."""
+    n = counts.numel()
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_kv_reserve(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _ints(counts, cache, (n,), "counts"),
+                                   _kv_opts(cache, None, device_status)), "luvc_kv_reserve")
+
+
+def _token_stride(t: torch.Tensor, cache: KvCache, heads: int, name: str) -> int:
+    """Elements from one token to the next of a [tokens, heads, D] tensor whose tokens are contiguous."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.head_dim or t.device != cache.device:
+        raise ValueError("%s must be [tokens, %d, %d] on %s" % (name, heads, cache.head_dim, cache.device))
+    if t.dtype != cache.io_dtype:
+        raise TypeError("%s must be %s for a %s cache, got %s" % (name, cache.io_dtype, cache.dtype, t.dtype))
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (heads > 1 and s1 != cache.head_dim):
+        raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
+    return s0 if t.shape[0] > 1 else max(s0, heads * cache.head_dim)
+
+
+def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0, starts: torch.Tensor | None = None,
+             seqs: torch.Tensor | None = None, sizes: torch.Tensor | None = None,
+             device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_write: the rows k, v [tokens, heads, D] become the last tokens of the sequences in `layer`.
+    starts: int32 [n+1], rows starts[i] .. starts[i+1]-1 belong to sequence i (None: one row each); sizes: int32
+    [tokens], the values are written as v + log(size) (Eq. 2).  k and v may be parts of a wider tensor."""
+    tokens = k.shape[0]
+    n = tokens if starts is None else starts.numel() - 1
+    if v.shape != k.shape:
+        raise ValueError("k and v must have one shape")
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_kv_write(cache.struct, layer, _ints(seqs, cache, (n,), "seqs"), n, k.data_ptr(), v.data_ptr(),
+                                 _token_stride(k, cache, cache.heads, "k"), _token_stride(v, cache, cache.heads, "v"), tokens,
+                                 _ints(starts, cache, (n + 1,), "starts"), _ints(sizes, cache, (tokens,), "sizes"),
+                                 F32 if k.dtype == torch.float32 else BF16, _kv_opts(cache, None, device_status)),
+               "luvc_kv_write")
+
+
+def kv_fork(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, *, workspace: torch.Tensor | None = None,
+            device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_fork: the empty slots dst (int32 [n]) become copies of the sequences src (int32 [n]); full pages are shared."""
+    n = dst.numel()
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_kv_fork(cache.struct, _ints(src, cache, (n,), "src"), _ints(dst, cache, (n,), "dst"), n,
+                                _kv_opts(cache, workspace, device_status)), "luvc_kv_fork")
+
+
+def kv_free(cache: KvCache, seqs: torch.Tensor, *, device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_free: empties the slots seqs (int32 [n]); pages nobody holds any more are free again."""
+    n = seqs.numel()
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_kv_free(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _kv_opts(cache, None, device_status)),
+               "luvc_kv_free")
+
+
+def kv_compact(cache: KvCache, first: torch.Tensor, span: torch.Tensor, idx: torch.Tensor, *,
+               counts: torch.Tensor | None = None, seqs: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+               device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_compact: of the block of span[i] tokens from first[i] on, sequence i keeps the tokens idx[i] (int32
+    [n, keep], relative to the block, ascending: the out_idx of spu_prune) and everything outside the block."""
+    n, keep = idx.shape
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_kv_compact(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _ints(first, cache, (n,), "first"),
+                                   _ints(span, cache, (n,), "span"), _ints(idx, cache, (n, keep), "idx") if keep else None, keep,
+                                   _ints(counts, cache, (n,), "counts"), _kv_opts(cache, workspace, device_status)),
+               "luvc_kv_compact")
+
+
+def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.Tensor | None = None, scale: float = 0.0,
+                key_bias: torch.Tensor | None = None, want_lse: bool = False, out: torch.Tensor | None = None,
+                workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None):
+    """luvc_attn_decode: attention of the queries q [n, q_heads, D], one new token per sequence, over the cached tokens of
+    `layer`.  key_bias: float32 [n, width], added to the scores of the first `width` tokens; scale 0: 1/sqrt(D).
+    Returns out [n, q_heads, D] and, with want_lse, the log-sum-exp of the scores [n, q_heads] float32."""
+    n, q_heads = q.shape[0], q.shape[1]
+    stride = _token_stride(q, cache, q_heads, "q")
+    if out is None:
+        out = torch.empty((n, q_heads, cache.head_dim), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or out.device != q.device:
+        raise ValueError("out must be a contiguous tensor of q's shape and type")
+    lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device) if want_lse else None
+    o = AttnOpts(stream=_stream_ptr(cache.device), scale=scale)
+    if workspace is not None:
+        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if device_status is not None:
+        o.device_status = device_status.data_ptr()
+    if key_bias is not None:
+        if key_bias.dtype != torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n or key_bias.device != cache.device \
+                or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):
+            raise ValueError("key_bias must be a float32 [n, width] tensor on the cache's device, its rows contiguous")
+        o.key_bias, o.bias_width = key_bias.data_ptr(), key_bias.shape[1]
+        o.bias_stride = key_bias.stride(0) if n > 1 else max(key_bias.stride(0), key_bias.shape[1])
+    if lse is not None:
+        o.lse = lse.data_ptr()
+    with torch.cuda.device(cache.device):
+        _check(lib.luvc_attn_decode(q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, (n,), "seqs"), n, q_heads,
+                                    F32 if q.dtype == torch.float32 else BF16, out.data_ptr(), o), "luvc_attn_decode")
+    return (out, lse) if want_lse else out

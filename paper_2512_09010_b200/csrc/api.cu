@@ -1,5 +1,5 @@
 // C ABI of the library: argument checks, stream and scratch handling, and the
-// host-buffer variants.  All arithmetic lives in oim.cu and spu.cu.
+// host-buffer variants.  All arithmetic lives in oim.cu, spu.cu, kv_cache.cu and attn_decode.cu.
 
 #include <atomic>
 #include <cmath>
@@ -42,7 +42,7 @@ thread_local cudaStream_t t_stream = nullptr;
 // Library-owned scratch: one growing buffer per purpose and per device (keyed by the ordinal of the
 // device that is current at the call), shared by all threads and streams of the process.  Calls
 // whose GPU work overlaps race on it (documented in luvc.h); the lock only covers (re)allocation.
-enum Slot { kOimWs = 0, kSpuWs, kIoIn, kIoOut, kStatus, kCascade, kIoInSpu, kIoOutSpu, kSlots };
+enum Slot { kOimWs = 0, kSpuWs, kIoIn, kIoOut, kStatus, kCascade, kIoInSpu, kIoOutSpu, kKvWs, kAttnWs, kSlots };
 constexpr int kMaxDevices = 64;
 struct Scratch { void* ptr = nullptr; size_t bytes = 0; };
 Scratch g_scratch[kMaxDevices][kSlots];
@@ -78,6 +78,20 @@ int* status_word() {
     void* p = scratch(kStatus, 256);
     if (p && cudaMemset(p, 0, 256) != cudaSuccess) return nullptr;
     return static_cast<int*>(p);
+}
+
+// The current device's attention workspace: allocated and zeroed once (the kernel leaves it zeroed where it must be).
+void* attn_scratch() {
+    const int dev = current_device();
+    if (dev < 0) return nullptr;
+    {
+        std::lock_guard<std::mutex> lock(g_mutex);
+        if (g_scratch[dev][kAttnWs].ptr) return g_scratch[dev][kAttnWs].ptr;
+    }
+    const size_t bytes = attn_workspace_bytes();
+    void* p = bytes ? scratch(kAttnWs, bytes) : nullptr;
+    if (p && cudaMemset(p, 0, bytes) != cudaSuccess) return nullptr;
+    return p;
 }
 
 // Reads (after synchronising the stream) and clears the first word of a status block.
@@ -142,6 +156,46 @@ int check_spu(const void* hidden, int B, int N, int D, float cutoff, int keep, c
     return LUVC_OK;
 }
 
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int check_cache(const luvc_kv_cache* c) {
+    if (!c || !c->k || !c->v || !c->lengths || !c->refs || !c->table) return LUVC_ERR_NULL;
+    if (c->dtype != LUVC_BF16 && c->dtype != LUVC_F32 && c->dtype != LUVC_E4M3) return LUVC_ERR_DTYPE;
+    if ((c->dtype == LUVC_E4M3) != (c->k_scale != nullptr) || (c->dtype == LUVC_E4M3) != (c->v_scale != nullptr)) return LUVC_ERR_NULL;
+    if (c->layers < 1 || c->pages < 1 || c->heads < 1 || c->page_size < 1 || c->D < 1 || c->slots < 1 || c->max_pages < 1)
+        return LUVC_ERR_SHAPE;
+    if (c->page_size % 16 || c->D > 256 || (long long)c->layers * c->heads > 65536) return LUVC_ERR_SHAPE;
+    const long long most = (1ll << 31) - 1;
+    if ((long long)c->page_size * c->heads > most || (long long)c->pages * c->page_size * c->heads > most ||
+        (long long)c->max_pages * c->page_size > most)
+        return LUVC_ERR_SHAPE;
+    if ((c->D * kv_elem_size(c->dtype)) % 16 || !aligned16(c->k) || !aligned16(c->v) || !aligned4(c->lengths) ||
+        !aligned4(c->refs) || !aligned4(c->table) || !aligned4(c->k_scale) || !aligned4(c->v_scale))
+        return LUVC_ERR_ALIGN;
+    return LUVC_OK;
+}
+
+// Sequences of a call and the status word: the rules common to the cache's entry points.
+int check_kv_call(const luvc_kv_cache* c, const int32_t* seqs, int n, const int32_t* device_status) {
+    const int rc = check_cache(c);
+    if (rc) return rc;
+    if (n < 1 || n > kKvMaxSeqs || (!seqs && n > c->slots)) return LUVC_ERR_SHAPE;
+    if (!aligned4(seqs) || (device_status && !aligned16(device_status))) return LUVC_ERR_ALIGN;
+    return LUVC_OK;
+}
+
+// Workspace of a fork or a compaction: the caller's, or the library's.
+int kv_workspace(const luvc_kv_cache& c, int n, const luvc_kv_opts& o, void** ws) {
+    const size_t need = kv_workspace_bytes(c, n);
+    if (o.workspace) {
+        if (o.workspace_bytes < need || (reinterpret_cast<uintptr_t>(o.workspace) & 255u)) return LUVC_ERR_WORKSPACE;
+        *ws = o.workspace;
+        return LUVC_OK;
+    }
+    *ws = scratch(kKvWs, need);
+    return *ws ? LUVC_OK : LUVC_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace luvc
 
@@ -165,6 +219,7 @@ const char* luvc_status_string(int status) {
         case LUVC_ERR_CUDA: return "a CUDA call failed";
         case LUVC_ERR_TIMEOUT: return "a bounded device-side wait gave up";
         case LUVC_ERR_INTERNAL: return "internal error";
+        case LUVC_ERR_PAGES: return "not enough free pages or table entries in the key-value cache";
         default: return "unknown status";
     }
 }
@@ -510,6 +565,120 @@ int luvc_spu_prune_host(const void* hidden, int B, int N, int D, float cutoff, i
     cudaMemcpyAsync(out_hidden, dout, (size_t)B * keep * D * es, cudaMemcpyDeviceToHost, st);
     cudaMemcpyAsync(out_idx, didx, (size_t)B * keep * 4, cudaMemcpyDeviceToHost, st);
     return cudaStreamSynchronize(st) == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+}
+
+// ---- paged key-value cache -----------------------------------------------------
+
+size_t luvc_kv_workspace_bytes(const luvc_kv_cache* cache, int n) {
+    if (check_cache(cache) || n < 1 || n > kKvMaxSeqs) return 0;
+    return kv_workspace_bytes(*cache, n);
+}
+
+int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, const int32_t* counts, const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    const int rc = check_kv_call(cache, seqs, n, o.device_status);
+    if (rc) return rc;
+    if (!counts) return LUVC_ERR_NULL;
+    if (!aligned4(counts)) return LUVC_ERR_ALIGN;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    return kv_reserve(*cache, seqs, n, counts, status, static_cast<cudaStream_t>(o.stream));
+}
+
+int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,
+                  long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes, int dtype,
+                  const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    const int rc = check_kv_call(cache, seqs, n, o.device_status);
+    if (rc) return rc;
+    if ((!k || !v) && tokens > 0) return LUVC_ERR_NULL;
+    if (dtype != (cache->dtype == LUVC_F32 ? LUVC_F32 : LUVC_BF16)) return LUVC_ERR_DTYPE;
+    const long long row = (long long)cache->heads * cache->D;
+    if (layer < 0 || layer >= cache->layers || tokens < 0 || (!starts && tokens != n) || k_stride < row || v_stride < row)
+        return LUVC_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if (!aligned16(k) || !aligned16(v) || (k_stride * es) % 16 || (v_stride * es) % 16 || !aligned4(starts) || !aligned4(sizes))
+        return LUVC_ERR_ALIGN;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    if (tokens == 0) return LUVC_OK;
+    return kv_write(*cache, layer, seqs, n, k, v, k_stride, v_stride, tokens, starts, sizes, status,
+                    static_cast<cudaStream_t>(o.stream));
+}
+
+int luvc_kv_fork(const luvc_kv_cache* cache, const int32_t* src, const int32_t* dst, int n, const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    if (!src || !dst) return LUVC_ERR_NULL;
+    int rc = check_kv_call(cache, dst, n, o.device_status);
+    if (rc) return rc;
+    if (!aligned4(src)) return LUVC_ERR_ALIGN;
+    void* ws = nullptr;
+    rc = kv_workspace(*cache, n, o, &ws);
+    if (rc) return rc;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    return kv_fork(*cache, src, dst, n, ws, status, static_cast<cudaStream_t>(o.stream));
+}
+
+int luvc_kv_free(const luvc_kv_cache* cache, const int32_t* seqs, int n, const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    const int rc = check_kv_call(cache, seqs, n, o.device_status);
+    if (rc) return rc;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    return kv_free(*cache, seqs, n, status, static_cast<cudaStream_t>(o.stream));
+}
+
+int luvc_kv_compact(const luvc_kv_cache* cache, const int32_t* seqs, int n, const int32_t* first, const int32_t* span,
+                    const int32_t* idx, int keep, const int32_t* counts, const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    int rc = check_kv_call(cache, seqs, n, o.device_status);
+    if (rc) return rc;
+    if (!first || !span || (!idx && keep > 0)) return LUVC_ERR_NULL;
+    if (keep < 0) return LUVC_ERR_KEEP;
+    if (!aligned4(first) || !aligned4(span) || !aligned4(idx) || !aligned4(counts)) return LUVC_ERR_ALIGN;
+    void* ws = nullptr;
+    rc = kv_workspace(*cache, n, o, &ws);
+    if (rc) return rc;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    return kv_compact(*cache, seqs, n, first, span, idx, keep, counts, ws, status, static_cast<cudaStream_t>(o.stream));
+}
+
+// ---- attention of one new token ---------------------------------------------------
+
+size_t luvc_attn_workspace_bytes(void) { return attn_workspace_bytes(); }
+
+int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,
+                     int q_heads, int dtype, void* out, const luvc_attn_opts* opts) {
+    const luvc_attn_opts o = opts ? *opts : luvc_attn_opts{};
+    int rc = check_cache(cache);
+    if (rc) return rc;
+    if (!q || !out) return LUVC_ERR_NULL;
+    if (dtype != (cache->dtype == LUVC_F32 ? LUVC_F32 : LUVC_BF16)) return LUVC_ERR_DTYPE;
+    if (n < 1 || n > kKvMaxSeqs || (!seqs && n > cache->slots) || layer < 0 || layer >= cache->layers || q_heads < 1 ||
+        q_heads > 65536 || q_heads % cache->heads || q_stride < (long long)q_heads * cache->D || !(o.scale == o.scale))
+        return LUVC_ERR_SHAPE;
+    if (o.key_bias && (o.bias_width < 0 || o.bias_stride < o.bias_width)) return LUVC_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if (!aligned16(q) || !aligned16(out) || (cache->D * es) % 16 || (q_stride * es) % 16 || !aligned4(seqs) ||
+        !aligned4(o.key_bias) || !aligned4(o.lse) || (o.device_status && !aligned16(o.device_status)))
+        return LUVC_ERR_ALIGN;
+    AttnProblem p;
+    p.workspace = o.workspace;
+    if (p.workspace) {
+        if (o.workspace_bytes < attn_workspace_bytes() || (reinterpret_cast<uintptr_t>(p.workspace) & 255u)) return LUVC_ERR_WORKSPACE;
+    } else if (!(p.workspace = attn_scratch())) {
+        return LUVC_ERR_CUDA;
+    }
+    p.status = o.device_status ? o.device_status : status_word();
+    if (!p.status) return LUVC_ERR_CUDA;
+    p.c = *cache; p.q = q; p.q_stride = q_stride; p.seqs = seqs; p.bias = o.key_bias; p.bias_stride = o.bias_stride;
+    p.bias_width = o.key_bias ? o.bias_width : 0;
+    p.out = out; p.lse = o.lse; p.layer = layer; p.n = n; p.q_heads = q_heads;
+    p.scale = o.scale != 0.f ? o.scale : 1.f / std::sqrt((float)cache->D);
+    p.stream = static_cast<cudaStream_t>(o.stream);
+    return attn_decode(p);
 }
 
 }  // extern "C"

@@ -176,4 +176,35 @@ SpuInv2Plan spu_inv2_plan(int B, int N, int D, int sigma);
 int spu_inv2_run(const float* Y, float* part, int B, int N, int D, int sigma, int* status, cudaStream_t stream, void* img,
                  bool img_ready = false);
 
+// ---- paged key-value cache (kv_cache.cu) and the attention over it (attn_decode.cu) ---------------
+
+constexpr int kKvMaxSeqs = 4096;    // sequences of one call
+size_t kv_elem_size(int dtype);
+size_t kv_workspace_bytes(const luvc_kv_cache& c, int n);
+int kv_reserve(const luvc_kv_cache& c, const int32_t* seqs, int n, const int32_t* counts, int* status, cudaStream_t stream);
+int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, const void* k, const void* v, long long k_stride,
+             long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes, int* status, cudaStream_t stream);
+int kv_fork(const luvc_kv_cache& c, const int32_t* src, const int32_t* dst, int n, void* ws, int* status, cudaStream_t stream);
+int kv_free(const luvc_kv_cache& c, const int32_t* seqs, int n, int* status, cudaStream_t stream);
+int kv_compact(const luvc_kv_cache& c, const int32_t* seqs, int n, const int32_t* first, const int32_t* span, const int32_t* idx,
+               int keep, const int32_t* counts, void* ws, int* status, cudaStream_t stream);
+
+struct AttnProblem {
+    luvc_kv_cache c;
+    const void* q;
+    long long q_stride;
+    const int32_t* seqs;
+    const float* bias;
+    long long bias_stride;
+    void* out;
+    float* lse;
+    int layer, n, q_heads, bias_width;
+    float scale;
+    void* workspace;
+    int* status;
+    cudaStream_t stream;
+};
+size_t attn_workspace_bytes();      // 0: no device
+int attn_decode(const AttnProblem& p);
+
 }  // namespace luvc

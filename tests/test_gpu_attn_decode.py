@@ -1,0 +1,255 @@
+"""Attention of one new token over the paged cache against the formula in 64 bits.
+
+The bound of an output element, worked out from the inputs before anything is run: scores are fp32 sums of D products (each
+product and each of the at most D additions may lose 2^-23 of the largest partial sum, and an 8-bit cache's queries lose
+2^-25 of their largest element when they are brought to half precision); a weight exp(score) is off by that times
+its own size, in the numerator and in the denominator; weights enter their product with the values with at least 16 bits;
+sums over t tokens may lose 2^-23 per 16 tokens; the result is rounded once to its type."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+
+
+@pytest.fixture(scope="module")
+def luvc():
+    import paper_2512_09010_b200 as luvc
+    assert torch.cuda.is_available()
+    luvc.check_status()
+    return luvc
+
+
+def build(luvc, dtype, lengths, heads, D, page, layers=1, seed=0, nan=True, spare=3):
+    """A cache whose sequences lie on scattered pages; everything no sequence holds is NaN."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    need = [-(-n // page) for n in lengths]
+    pages = sum(need) + spare
+    k = torch.randn((layers, pages, heads, page, D), generator=g, device="cuda")
+    v = torch.randn((layers, pages, heads, page, D), generator=g, device="cuda")
+    k += 1.5 * torch.randn((layers, 1, heads, 1, D), generator=g, device="cuda")
+    order = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).tolist()
+    held = torch.zeros((pages, page), dtype=torch.bool)
+    max_pages = max(need + [1]) + 1
+    table, at = torch.full((len(lengths), max_pages), -1, dtype=torch.int32), 0
+    for b, n in enumerate(lengths):
+        mine = order[at:at + need[b]]
+        at += need[b]
+        table[b, :need[b]] = torch.tensor(mine, dtype=torch.int32)
+        for j, p in enumerate(mine):
+            held[p, :max(0, min(page, n - j * page))] = True
+    scales = {}
+    if dtype == "e4m3":
+        scales = {"k_scale": 0.01 + 0.02 * torch.rand((layers, heads), generator=g, device="cuda"),
+                  "v_scale": 0.01 + 0.02 * torch.rand((layers, heads), generator=g, device="cuda")}
+        k /= scales["k_scale"][:, None, :, None, None]
+        v /= scales["v_scale"][:, None, :, None, None]
+        k.clamp_(-448, 448), v.clamp_(-448, 448)
+    if nan:
+        gone = ~held.cuda()[None, :, None, :, None]
+        k.masked_fill_(gone, math.nan), v.masked_fill_(gone, math.nan)
+    c = luvc.KvCache(k.to(TYPES[dtype]), v.to(TYPES[dtype]), len(lengths), max_pages, **scales)
+    c.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+    c.table.copy_(table)
+    return c
+
+
+def rows(cache, slot, layer, n):
+    out = []
+    for pool, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        pages = cache.table[slot, :-(-n // cache.page_size)].long()
+        x = pool.float()[layer][pages].transpose(1, 2).reshape(-1, cache.heads, cache.head_dim)[:n].double()
+        out.append(x if scale is None else x * scale[layer].double()[:, None])
+    return out
+
+
+def check(luvc, cache, q, got, lse, layer=0, seqs=None, scale=None, bias=None):
+    n, hq, D = q.shape
+    group = hq // cache.heads
+    scale = scale or D ** -0.5
+    u = 2.0 ** -24 if q.dtype == torch.float32 else 2.0 ** -8
+    for i in range(n):
+        slot = i if seqs is None else seqs[i]
+        t = int(cache.lengths[slot])
+        if t == 0:
+            assert not got[i].any()
+            assert lse is None or bool((lse[i] == -math.inf).all())
+            continue
+        k, v = rows(cache, slot, layer, t)
+        k, v = k.repeat_interleave(group, 1), v.repeat_interleave(group, 1)
+        qi = q[i].double()
+        s = torch.einsum("hd,thd->ht", qi, k) * scale
+        size = torch.einsum("hd,thd->ht", qi.abs(), k.abs()) * scale
+        off = size * (D + 2) * 2.0 ** -23 + s.abs() * 2.0 ** -23
+        if cache.dtype == torch.float8_e4m3fn:
+            off = off + scale * 2.0 ** -25 * qi.abs().amax(1)[:, None] * k.abs().sum(2).t()
+        if bias is not None:
+            w = min(t, bias.shape[1])
+            b = torch.zeros(t, dtype=torch.float64, device="cuda")
+            b[:w] = bias[i, :w].double()
+            s = s + b
+            off = off + torch.where(b.isfinite(), b.abs(), 0.0) * 2.0 ** -23
+        keep = s > -math.inf
+        s, v = torch.where(keep, s, -math.inf), torch.where(keep.t()[:, :, None], v, 0.0)
+        top = s.amax(1, keepdim=True)
+        if not keep.any():
+            assert not got[i].any()
+            continue
+        p = torch.exp(s - top)
+        total = p.sum(1, keepdim=True)
+        p = p / total
+        want = torch.einsum("ht,thd->hd", p, v)
+        spread = torch.einsum("ht,thd->hd", p, v.abs())
+        wrong = torch.where(keep, off, 0.0).amax(1, keepdim=True)
+        rel = 2 * wrong + 2 * 2.0 ** -17 * (q.dtype != torch.float32) + (t / 16 + D + 64) * 2.0 ** -23
+        bound = spread * rel * 1.01 + u * want.abs()
+        diff = (got[i].double() - want).abs()
+        assert bool((diff <= bound).all()), (i, t, float((diff / bound).max()))
+        if lse is not None:
+            ref = (top + total.log())[:, 0]
+            assert bool(((lse[i].double() - ref).abs() <= wrong[:, 0] + (t / 16 + 64) * 2.0 ** -23 + ref.abs() * 2.0 ** -22).all())
+
+
+SHAPES = [  # type, query heads, key heads, D, page
+    ("bf16", 28, 4, 128, 16), ("bf16", 32, 8, 128, 64), ("bf16", 8, 8, 64, 16), ("bf16", 16, 2, 80, 48), ("bf16", 24, 1, 256, 32),
+    ("bf16", 17, 1, 8, 16), ("bf16", 10, 2, 104, 16), ("bf16", 32, 1, 192, 16), ("bf16", 66, 2, 64, 16),
+    ("e4m3", 28, 4, 128, 16), ("e4m3", 8, 8, 64, 32), ("e4m3", 12, 1, 256, 64), ("e4m3", 6, 3, 80, 16), ("e4m3", 40, 2, 48, 16),
+    ("e4m3", 3, 1, 144, 16),
+    ("f32", 16, 16, 64, 16), ("f32", 28, 4, 128, 48), ("f32", 4, 2, 20, 16), ("f32", 9, 1, 256, 16), ("f32", 34, 2, 68, 32),
+]
+LENGTHS = [[1], [0, 1, 15, 16, 17, 0], [31, 32, 33, 100, 2, 5, 64, 63], [700, 1, 0, 1297], [4100]]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("lengths", LENGTHS, ids=lambda x: "x".join(map(str, x))[:20])
+def test_ragged_sequences(luvc, shape, lengths):
+    dtype, hq, heads, D, page = shape
+    c = build(luvc, dtype, lengths, heads, D, page, seed=len(lengths) + D)
+    q = torch.randn((len(lengths), hq, D), generator=torch.Generator().manual_seed(D)).to(c.io_dtype).cuda()
+    out, lse = luvc.attn_decode(q, c, want_lse=True)
+    assert luvc.check_status() == 0
+    check(luvc, c, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype,heads,D", [("bf16", 8, 128), ("e4m3", 4, 128), ("f32", 2, 64), ("bf16", 1, 64)])
+def test_long_and_many(luvc, dtype, heads, D):
+    lengths = [16451, 3, 9000, 1] if heads > 1 else [40000]
+    c = build(luvc, dtype, lengths, heads, D, 64, seed=5, nan=True)
+    q = torch.randn((len(lengths), 4 * heads, D), generator=torch.Generator().manual_seed(1)).to(c.io_dtype).cuda()
+    check(luvc, c, q, *luvc.attn_decode(q, c, want_lse=True))
+    lengths = [(37 * i) % 90 for i in range(600)]
+    c = build(luvc, dtype, lengths, heads, D, 16, seed=6)
+    q = torch.randn((600, 4 * heads, D), generator=torch.Generator().manual_seed(2)).to(c.io_dtype).cuda()
+    check(luvc, c, q, *luvc.attn_decode(q, c, want_lse=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3", "f32"])
+def test_biases_and_masks(luvc, dtype):
+    lengths = [200, 33, 16, 70, 40]
+    c = build(luvc, dtype, lengths, 2, 64, 16, seed=9)
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn((5, 6, 64), generator=g).to(c.io_dtype).cuda()
+    wide = torch.randn((5, 300), generator=g).cuda()
+    bias = wide[:, :130]                                          # a part of a wider tensor; tokens from 130 on get 0
+    check(luvc, c, q, *luvc.attn_decode(q, c, key_bias=bias, want_lse=True), bias=bias)
+    bias = bias.clone()
+    bias[0, ::3] = -math.inf
+    bias[1, :] = -math.inf                                        # nothing is left: a row of zeros
+    bias[2, 1:] = -math.inf
+    bias[3, :] = torch.finfo(torch.float32).min                   # the lowest value everywhere: equal weights, not none
+    bias[4, :39] = torch.finfo(torch.float32).min
+    for page in c.table[0, :13].tolist():                         # rows under a mask may hold anything
+        rowsel = [j for j in range(16) if (c.table[0].tolist().index(page) * 16 + j) % 3 == 0]
+        for pool, what in ((c.k, math.nan), (c.v, math.inf if dtype != "e4m3" else math.nan)):
+            flat = pool.float()
+            flat[0, page, :, [j for j in rowsel if c.table[0].tolist().index(page) * 16 + j < 130]] = what
+            pool.copy_(flat.to(pool.dtype))
+    out, lse = luvc.attn_decode(q, c, key_bias=bias, want_lse=True)
+    clean = build(luvc, dtype, lengths, 2, 64, 16, seed=9)
+    check(luvc, clean, q, out, lse, bias=bias)
+    assert not out[1].any() and bool((lse[1] == -math.inf).all())
+    mean = rows(clean, 3, 0, 70)[1].mean(0).repeat_interleave(3, 0)
+    assert ((out[3].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 1e-4).all()
+    last = rows(clean, 4, 0, 40)[1][39].repeat_interleave(3, 0)   # the one token that is not masked
+    assert ((out[4].double() - last).abs() <= 2.0 ** -8 * last.abs() + 1e-6).all()
+
+
+def test_large_scores_and_a_scale(luvc):
+    c = build(luvc, "bf16", [500, 77], 2, 128, 16, seed=11)
+    q = 20 * torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    check(luvc, c, q, *luvc.attn_decode(q, c, scale=0.5, want_lse=True), scale=0.5)
+    big = build(luvc, "e4m3", [500, 77], 2, 128, 16, seed=11)
+    q = (1e30 * torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(4))).bfloat16().cuda()   # beyond half precision's range
+    check(luvc, big, q, *luvc.attn_decode(q, big, scale=1e-31, want_lse=True), scale=1e-31)
+
+
+def test_a_nan_in_a_row_that_counts_is_seen(luvc):
+    c = build(luvc, "bf16", [100], 1, 64, 16, seed=12)
+    q = torch.randn((1, 2, 64), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    c.k[0, int(c.table[0, 2]), 0, 5, 7] = math.nan
+    assert bool(luvc.attn_decode(q, c).isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_layers_slots_strides_and_streams(luvc, dtype):
+    c = build(luvc, dtype, [100, 0, 45, 300], 2, 64, 16, layers=3, seed=13)
+    g = torch.Generator().manual_seed(5)
+    wide = torch.randn((5, 3 * 8 * 64), generator=g).to(c.io_dtype).cuda()
+    q = wide[:, 8 * 64:16 * 64].view(5, 8, 64)                    # the middle part of a projection's rows
+    seqs = torch.tensor([3, 0, 3, 1, 2], dtype=torch.int32, device="cuda")
+    side, ws = torch.cuda.Stream(), torch.zeros(luvc.attn_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        out, lse = luvc.attn_decode(q, c, layer=2, seqs=seqs, want_lse=True, workspace=ws)
+    side.synchronize()
+    check(luvc, c, q, out, lse, layer=2, seqs=seqs.tolist())
+    again = torch.empty_like(out)
+    for _ in range(3):                                            # the same bits every time
+        assert torch.equal(luvc.attn_decode(q, c, layer=2, seqs=seqs, out=again, workspace=ws), out)
+    bad = seqs.clone()
+    bad[1] = 4                                                    # no such slot: empty, and reported
+    got = luvc.attn_decode(q, c, layer=2, seqs=bad)
+    assert luvc.check_status() == 2 and not got[1].any() and torch.equal(got[2], out[2])
+
+
+def test_results_repeat_bit_for_bit(luvc):
+    c = build(luvc, "bf16", [9000, 100, 2500], 4, 128, 16, seed=14)
+    q = torch.randn((3, 28, 128), generator=torch.Generator().manual_seed(6)).bfloat16().cuda()
+    first = luvc.attn_decode(q, c)
+    for _ in range(20):
+        assert torch.equal(luvc.attn_decode(q, c), first)
+
+
+def test_offsets_past_32_bits(luvc):
+    # the last pages of a pool of more than 2^32 elements per tensor (8 GB of one byte each)
+    heads, D, page = 8, 256, 64
+    pages = (1 << 32) // (heads * D * page) + 40
+    k = torch.zeros((1, pages, heads, page, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    v = torch.zeros((1, pages, heads, page, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    one = torch.ones((1, heads), device="cuda")
+    c = luvc.KvCache(k, v, 2, 40, k_scale=one, v_scale=one)
+    c.refs[:pages - 40].fill_(1)                                  # only the far end is free
+    n = 30 * page + 5
+    g = torch.Generator(device="cuda").manual_seed(8)
+    new = torch.randn((2, n, heads, D), generator=g, device="cuda").bfloat16()
+    count = torch.tensor([n], dtype=torch.int32, device="cuda")
+    luvc.kv_reserve(c, count)
+    assert c.table[0, :2].tolist() == [pages - 40, pages - 39]
+    luvc.kv_write(c, new[0], new[1], starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    q = torch.randn((1, heads * 2, D), generator=g, device="cuda").bfloat16()
+    k8, v8 = (x.float().to(torch.float8_e4m3fn).double() for x in new)
+    s = torch.einsum("hd,thd->ht", q[0].double(), k8.repeat_interleave(2, 1)) / 16
+    want = torch.einsum("ht,thd->hd", torch.softmax(s, 1), v8.repeat_interleave(2, 1))
+    got = luvc.attn_decode(q, c)[0].double()
+    assert luvc.check_status() == 0
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 2e-3).all()
+    # dropping the first two thirds of its tokens moves rows within the far end
+    idx = torch.arange(2 * n // 3, n, dtype=torch.int32, device="cuda")[None, :8 * page]
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    luvc.kv_compact(c, zero, count, idx.contiguous())
+    assert luvc.check_status() == 0 and c.lengths[0] == 8 * page and int(c.table[0, 0]) >= pages - 9
+    moved = c.k[0][c.table[0, :8].long().tolist()[0]].float().transpose(0, 1)
+    assert torch.equal(moved, k8[2 * n // 3:2 * n // 3 + page].float())

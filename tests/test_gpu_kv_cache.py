@@ -1,0 +1,372 @@
+"""The paged key-value cache against a plain model of its books and rows: every page number, every reference count and
+every row has to be the model's (integers and copies: exact).  Rows that are computed on the way (V + log size, the 8-bit
+form) are compared with the definition."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+
+
+@pytest.fixture(scope="module")
+def luvc():
+    import paper_2512_09010_b200 as luvc
+    assert torch.cuda.is_available()
+    luvc.check_status()
+    return luvc
+
+
+class Model:
+    """The books in plain Python, and for every sequence the id of the token in each position."""
+
+    def __init__(self, pages, page, slots, max_pages):
+        self.page, self.max_pages = page, max_pages
+        self.refs, self.table, self.ids = [0] * pages, [[] for _ in range(slots)], [[] for _ in range(slots)]
+
+    def take(self):
+        p = self.refs.index(0)
+        self.refs[p] = 1
+        return p
+
+    def reserve(self, slot, ids):
+        self.ids[slot] = self.ids[slot] + list(ids)
+        while len(self.table[slot]) * self.page < len(self.ids[slot]):
+            self.table[slot].append(self.take())
+
+    def fork(self, src, dst):
+        full = len(self.ids[src]) // self.page
+        self.ids[dst] = list(self.ids[src])
+        self.table[dst] = self.table[src][:full]
+        if len(self.ids[src]) % self.page:
+            self.table[dst].append(self.take())
+
+    def share(self, dst):                       # references of shared pages, counted after every page of the call is taken
+        for p in self.table[dst][:len(self.ids[dst]) // self.page]:
+            self.refs[p] += 1
+
+    def free(self, slot):
+        for p in self.table[slot]:
+            self.refs[p] -= 1
+        self.table[slot], self.ids[slot] = [], []
+
+    def compact(self, slot, first, span, idx):
+        order = list(range(first)) + [first + j for j in idx] + list(range(first + span, len(self.ids[slot])))
+        still = 0
+        while (still + 1) * self.page <= len(order) and order[(still + 1) * self.page - 1] == (still + 1) * self.page - 1:
+            still += 1
+        old = self.table[slot][still:]
+        self.table[slot] = self.table[slot][:still] + [self.take() for _ in range(-(-len(order) // self.page) - still)]
+        self.ids[slot] = [self.ids[slot][j] for j in order]
+        return old                              # given back after every page of the call is taken
+
+    def drop(self, pages):
+        for p in pages:
+            self.refs[p] -= 1
+
+
+def rows_for(ids, layer, heads, D, kind, dtype):
+    """The row of a token id: small whole numbers, exact in every type, different for neighbouring ids, layers, heads, K and V."""
+    i = torch.as_tensor(ids, dtype=torch.long, device="cuda")[:, None, None]
+    h = torch.arange(heads, device="cuda")[None, :, None]
+    d = torch.arange(D, device="cuda")[None, None, :]
+    return ((i * 7 + layer * 5 + h * 3 + d + 4 * kind) % 13 - 6).to(dtype)
+
+
+class Rig:
+    def __init__(self, luvc, dtype, pages, page, slots, max_pages, layers=2, heads=2, D=64):
+        self.luvc, self.model = luvc, Model(pages, page, slots, max_pages)
+        shape = (layers, pages, heads, page, D)
+        self.layers, self.heads, self.D, self.dtype = layers, heads, D, TYPES[dtype]
+        k = torch.full(shape, float("nan"), device="cuda").to(self.dtype)
+        scale = torch.ones((layers, heads), device="cuda") if dtype == "e4m3" else None
+        self.cache = luvc.KvCache(k, k.clone(), slots, max_pages, k_scale=scale, v_scale=scale)
+        self.next_id = 1
+
+    def ints(self, values):
+        return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+    def append(self, slots, counts):
+        self.luvc.kv_reserve(self.cache, self.ints(counts), seqs=self.ints(slots))
+        ids = []
+        for s, c in zip(slots, counts):
+            new = list(range(self.next_id, self.next_id + c))
+            self.next_id += c
+            self.model.reserve(s, new)
+            ids += new
+        starts = self.ints(np.concatenate(([0], np.cumsum(counts))))
+        for layer in range(self.layers):
+            k, v = (rows_for(ids, layer, self.heads, self.D, kind, self.cache.io_dtype) for kind in (0, 1))
+            self.luvc.kv_write(self.cache, k, v, layer=layer, starts=starts, seqs=self.ints(slots))
+
+    def check(self):
+        assert self.luvc.check_status() == 0
+        m, c = self.model, self.cache
+        assert c.lengths.tolist() == [len(x) for x in m.ids]
+        assert c.refs.tolist() == m.refs
+        assert c.table.tolist() == [t + [-1] * (m.max_pages - len(t)) for t in m.table]
+        for slot, ids in enumerate(m.ids):
+            if not ids:
+                continue
+            pages = torch.tensor(m.table[slot], device="cuda")
+            for layer in range(self.layers):
+                for kind, pool in enumerate((c.k, c.v)):
+                    got = pool.float()[layer][pages].transpose(1, 2).reshape(-1, self.heads, self.D)[:len(ids)]
+                    assert torch.equal(got, rows_for(ids, layer, self.heads, self.D, kind, torch.float32)), (slot, layer, kind)
+
+
+@pytest.mark.parametrize("dtype,page,D,heads", [("bf16", 16, 64, 2), ("f32", 16, 20, 3), ("e4m3", 32, 80, 1), ("bf16", 48, 128, 7),
+                                                ("bf16", 16, 8, 1), ("e4m3", 64, 256, 2)])
+def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
+    rng = np.random.default_rng(1234 + page + D)
+    r = Rig(luvc, dtype, pages=150, page=page, slots=12, max_pages=9, heads=heads, D=D)
+    most = 9 * page
+    for step in range(40):
+        m = r.model
+        used = [s for s in range(12) if m.ids[s]]
+        empty = [s for s in range(12) if not m.ids[s]]
+        what = rng.choice(["append", "fork", "compact", "free"], p=[0.4, 0.2, 0.3, 0.1])
+        if what == "append":
+            slots = rng.permutation(12)[:rng.integers(1, 7)].tolist()
+            counts = [int(min(most - len(m.ids[s]), rng.choice([0, 1, 2, 15, 16, 17, int(rng.integers(0, 3 * page))]))) for s in slots]
+            r.append(slots, counts)
+        elif what == "fork" and used and empty:
+            n = int(rng.integers(1, len(empty) + 1))
+            src, dst = rng.choice(used, n).tolist(), rng.permutation(empty)[:n].tolist()
+            luvc.kv_fork(r.cache, r.ints(src), r.ints(dst))
+            for s, d in zip(src, dst):
+                m.fork(s, d)
+            for d in dst:
+                m.share(d)
+        elif what == "compact" and used:
+            slots = rng.permutation(used)[:4].tolist()
+            first, span, idx, width = [], [], [], 0
+            for s in slots:
+                n = len(m.ids[s])
+                f = int(rng.integers(0, n + 1))
+                sp = int(rng.integers(0, n - f + 1))
+                keep = int(rng.choice([0, sp, int(rng.integers(0, sp + 1))]))
+                first.append(f), span.append(sp)
+                chosen = np.sort(rng.permutation(sp)[:keep])
+                if keep and rng.random() < 0.4:                     # a prefix, of which nothing moves
+                    chosen = np.arange(keep)
+                idx.append(chosen.tolist())
+                width = max(width, keep)
+            table = torch.full((len(slots), width), 1 << 30, dtype=torch.int32)      # what is past counts[i] is not read
+            for row, chosen in zip(table, idx):
+                row[:len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
+            luvc.kv_compact(r.cache, r.ints(first), r.ints(span), table.cuda(), counts=r.ints([len(x) for x in idx]), seqs=r.ints(slots))
+            old = [m.compact(s, f, sp, x) for s, f, sp, x in zip(slots, first, span, idx)]
+            for pages in old:
+                m.drop(pages)
+        elif what == "free" and used:
+            slots = rng.permutation(used)[:2].tolist()
+            luvc.kv_free(r.cache, r.ints(slots + slots[:1]))                          # named twice: freed once
+            for s in slots:
+                m.free(s)
+        r.check()
+
+
+def test_a_large_pool_and_many_sequences(luvc):
+    # more pages than one sweep of the scan covers (16384), more sequences than threads of its CTA, free pages far up
+    r = Rig(luvc, "bf16", pages=40000, page=16, slots=2100, max_pages=40, layers=1, heads=1, D=8)
+    r.append(list(range(500)), [16 * 40 - 3] * 500)
+    r.check()
+    luvc.kv_free(r.cache, r.ints(list(range(0, 500, 7))))
+    for s in range(0, 500, 7):
+        r.model.free(s)
+    r.append(list(range(2099, 499, -1)), [(5 * s) % 37 for s in range(2099, 499, -1)])
+    r.append(list(range(0, 500, 7)), [16 * 20 + 1] * 72)
+    r.check()
+
+
+def test_seqs_may_be_left_out(luvc):
+    r = Rig(luvc, "bf16", pages=20, page=16, slots=3, max_pages=4)
+    luvc.kv_reserve(r.cache, r.ints([20, 0, 3]))
+    for s, c in enumerate([20, 0, 3]):
+        r.model.reserve(s, range(100 * s, 100 * s + c))
+    ids = r.model.ids[0] + r.model.ids[2]
+    for layer in range(2):
+        luvc.kv_write(r.cache, *(rows_for(ids, layer, 2, 64, kind, torch.bfloat16) for kind in (0, 1)), layer=layer,
+                      starts=r.ints([0, 20, 20, 23]))
+    r.check()
+    luvc.kv_compact(r.cache, r.ints([2, 0, 0]), r.ints([17, 0, 3]), r.ints([[0, 5], [0, 0], [0, 2]]), counts=r.ints([2, 0, 2]))
+    for p in [r.model.compact(0, 2, 17, [0, 5]), r.model.compact(1, 0, 0, []), r.model.compact(2, 0, 3, [0, 2])]:
+        r.model.drop(p)
+    r.check()
+
+
+@pytest.mark.parametrize("case", ["pages", "table", "slot", "twice", "negative", "fork full", "fork same", "block", "count"])
+def test_what_only_the_device_can_see_leaves_the_cache_as_it_was(luvc, case):
+    r = Rig(luvc, "bf16", pages=12, page=16, slots=5, max_pages=6)
+    r.append([0, 1], [60, 35])
+    before = r.cache.meta.clone()
+    i, c = r.ints, r.cache
+    word = torch.zeros(4, dtype=torch.int32, device="cuda")
+    if case == "pages":           # 7 pages are in use, 5 are free: the first sequence fits, both do not
+        luvc.kv_reserve(c, i([48, 48]), seqs=i([2, 3]), device_status=word)
+    elif case == "table":
+        luvc.kv_reserve(c, i([1, 37]), seqs=i([1, 0]), device_status=word)
+    elif case == "slot":
+        luvc.kv_reserve(c, i([1, 1]), seqs=i([1, 5]), device_status=word)
+    elif case == "twice":
+        luvc.kv_reserve(c, i([1, 1]), seqs=i([1, 1]), device_status=word)
+    elif case == "negative":
+        luvc.kv_reserve(c, i([1, -1]), seqs=i([1, 0]), device_status=word)
+    elif case == "fork full":
+        luvc.kv_fork(c, i([0, 0]), i([2, 1]), device_status=word)
+    elif case == "fork same":
+        luvc.kv_fork(c, i([0, 0]), i([2, 2]), device_status=word)
+    elif case == "block":
+        luvc.kv_compact(c, i([0, 20]), i([60, 16]), i([[0], [1]]), device_status=word)
+    else:
+        luvc.kv_compact(c, i([0, 20]), i([1, 15]), i([[0, 1], [1, 2]]), device_status=word)
+    status = {"pages": 12, "table": 12, "fork full": 3, "block": 4, "count": 4}.get(case, 2)
+    luvc.kv_free(c, i([0]), device_status=word)                   # a set word stops the calls that follow
+    assert torch.equal(c.meta, before)
+    assert luvc.read_status(word) == status
+    assert luvc.read_status(word) == 0
+    r.append([0, 4], [3, 0])
+    r.check()
+
+
+def test_an_index_outside_its_block_is_replaced_and_reported(luvc):
+    r = Rig(luvc, "bf16", pages=12, page=16, slots=2, max_pages=4)
+    r.append([0], [40])
+    luvc.kv_compact(r.cache, r.ints([4]), r.ints([20]), r.ints([[3, 9, 400]]))
+    assert luvc.check_status() == 4
+    r.model.drop(r.model.compact(0, 4, 20, [3, 9, 19]))
+    r.check()
+
+
+def test_rows_before_the_sequence_are_not_written(luvc):
+    r = Rig(luvc, "bf16", pages=4, page=16, slots=2, max_pages=2)
+    r.append([0, 1], [3, 2])
+    rows = torch.ones((5, 2, 64), dtype=torch.bfloat16, device="cuda")
+    luvc.kv_write(r.cache, rows, rows, layer=0, starts=r.ints([0, 5, 5]))            # five rows, three tokens
+    assert luvc.check_status() == 2
+    assert bool((r.cache.k[0, r.model.table[0][0], :, :3] == 1).all())
+    assert bool(r.cache.k[0, r.model.table[0][0], :, 3:].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("heads,D", [(4, 128), (3, 80), (1, 16)])
+def test_written_rows_are_enhanced_and_rounded_once(luvc, dtype, heads, D):
+    g = torch.Generator(device="cuda").manual_seed(7)
+    counts = [1, 33, 0, 18]
+    T, layers = sum(counts), 2
+    wide = torch.float32 if dtype == "f32" else torch.bfloat16
+    qkv = torch.randn((T, 5 * heads * D), generator=g, device="cuda").to(wide) * 3
+    qkv[5, :] *= 1e4                                             # saturates the 8-bit form
+    k = qkv[:, 2 * heads * D:3 * heads * D].view(T, heads, D)    # parts of a wider row
+    v = qkv[:, 4 * heads * D:].view(T, heads, D)
+    sizes = torch.randint(1, 9, (T,), generator=g, device="cuda", dtype=torch.int32)
+    scale = (0.5 + torch.rand((layers, heads), generator=g, device="cuda")) * 0.02 if dtype == "e4m3" else None
+    pool = torch.zeros((layers, 9, heads, 16, D), device="cuda").to(TYPES[dtype])
+    cache = luvc.KvCache(pool, pool.clone(), 4, 4, k_scale=scale, v_scale=scale.flip(0) if scale is not None else None)
+    c = torch.tensor(counts, dtype=torch.int32, device="cuda")
+    starts = torch.cat((c.new_zeros(1), c.cumsum(0).int()))
+    luvc.kv_reserve(cache, c)
+    luvc.kv_write(cache, k, v, layer=1, starts=starts, sizes=sizes)
+    assert luvc.check_status() == 0
+    assert not cache.k[0].float().any()
+    got = []
+    for p in (cache.k, cache.v):
+        rows = [p.float()[1][cache.table[s, :(n + 15) // 16].long()].transpose(1, 2).reshape(-1, heads, D)[:n] for s, n in enumerate(counts) if n]
+        got.append(torch.cat(rows))
+    want = (k.double(), v.double() + sizes.double().log()[:, None, None])
+    if dtype == "e4m3":
+        # the quotient in fp32, to the nearest 8-bit value: exact for keys; log's last bit may tip a tie of the values by one step
+        q = [(w.float() / s[1][:, None]).clamp(-448, 448).to(torch.float8_e4m3fn).float() for w, s in zip(want, (cache.k_scale, cache.v_scale))]
+        assert torch.equal(got[0], q[0])
+        assert ((got[1] - q[1]).abs() <= q[1].abs() / 8 + 2.0 ** -9).all() and (got[1] != q[1]).float().mean() < 1e-3
+        assert got[0].abs().max() == 448
+    else:
+        assert torch.equal(got[0].double(), want[0])
+        # unit roundoff of the type, and log's and the sum's rounding in fp32
+        u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+        assert ((got[1].double() - want[1]).abs() <= u * want[1].abs() + 4 * 2.0 ** -24 * (v.double().abs() + 3)).all()
+
+
+def test_a_step_can_be_captured_and_replayed(luvc):
+    """A decode step (room, rows, attention) in a CUDA graph: page numbers are worked out on the device at every replay."""
+    r = Rig(luvc, "bf16", pages=16, page=16, slots=2, max_pages=5, layers=1)
+    r.append([0, 1], [14, 3])
+    c, one = r.cache, r.ints([1, 1])
+    k = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")       # equal scores: the mean of the values
+    out = torch.empty_like(q)
+    word = torch.zeros(4, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(luvc.attn_workspace_bytes(), dtype=torch.uint8, device="cuda")
+
+    def step():
+        luvc.kv_reserve(c, one, device_status=word)
+        luvc.kv_write(c, k, v, device_status=word)
+        luvc.attn_decode(q, c, out=out, workspace=ws, device_status=word)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        luvc.kv_write(c, k, v, device_status=word)                         # loads the kernels; rewritten below
+        luvc.attn_decode(q, c, out=out, workspace=ws, device_status=word)
+        luvc.kv_reserve(c, r.ints([0, 0]), device_status=word)
+    side.synchronize()
+    for s in (0, 1):                                                       # the rows the warm-up overwrote
+        last = r.model.ids[s][-1:]
+        kk, vv = (rows_for(last, 0, 2, 64, kind, torch.bfloat16) for kind in (0, 1))
+        luvc.kv_write(c, kk, vv, seqs=r.ints([s]))
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(20):
+        ids = [r.next_id, r.next_id + 1]
+        r.next_id += 2
+        for s in (0, 1):
+            r.model.reserve(s, [ids[s]])
+        k.copy_(rows_for(ids, 0, 2, 64, 0, torch.bfloat16))
+        v.copy_(rows_for(ids, 0, 2, 64, 1, torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        for s in (0, 1):
+            mean = rows_for(r.model.ids[s], 0, 2, 64, 1, torch.float64).mean(0).repeat_interleave(2, 0)
+            assert ((out[s].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 1e-5).all()
+    assert luvc.read_status(word) == 0
+    r.check()
+
+
+def test_python_refusals(luvc):
+    pool = torch.zeros((1, 4, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(TypeError):
+        luvc.KvCache(pool.half(), pool.half(), 2, 2)
+    with pytest.raises(ValueError):
+        luvc.KvCache(pool, pool[:, :3], 2, 2)
+    with pytest.raises(ValueError):
+        luvc.KvCache(pool.cpu(), pool.cpu(), 2, 2)
+    with pytest.raises(ValueError):
+        luvc.KvCache(pool, pool.clone(), 2, 2, meta=torch.zeros(9, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        luvc.KvCache(pool, pool.clone(), 2, 2, k_scale=torch.ones((1, 2), device="cuda"), v_scale=torch.ones((1, 2), device="cuda"))
+    with pytest.raises(ValueError):
+        luvc.KvCache(pool.to(torch.float8_e4m3fn), pool.to(torch.float8_e4m3fn), 2, 2)
+    c = luvc.KvCache(pool, pool.clone(), 2, 2)
+    with pytest.raises(ValueError):
+        luvc.kv_reserve(c, torch.ones(2, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        luvc.kv_reserve(c, torch.ones(2, dtype=torch.int32))
+    row = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(TypeError):
+        luvc.kv_write(c, row.float(), row.float())
+    with pytest.raises(ValueError):
+        luvc.kv_write(c, row.transpose(1, 2).contiguous().transpose(1, 2), row)
+    with pytest.raises(luvc.LuvcError) as e:
+        luvc.kv_write(c, row, row, layer=1)
+    assert e.value.status == 2
+    with pytest.raises(ValueError):
+        luvc.attn_decode(row[..., :32], c)
+    with pytest.raises(ValueError):
+        luvc.attn_decode(row, c, key_bias=torch.zeros((1, 4), device="cuda"))
+    with pytest.raises(luvc.LuvcError) as e:
+        luvc.attn_decode(torch.zeros((2, 3, 64), dtype=torch.bfloat16, device="cuda"), c)
+    assert e.value.status == 2
