@@ -480,8 +480,9 @@ size_t luvc_attn_workspace_bytes(void);
 
 typedef struct {
     void* stream;            /* cudaStream_t; NULL = legacy default stream */
-    void* workspace;         /* device, 256-byte aligned, ZEROED by the caller before its first use (a call leaves
-                                what must be zero zeroed); NULL = library-owned scratch */
+    void* workspace;         /* device, 256-byte aligned, ZEROED by the caller before its first use, and again
+                                after LUVC_ERR_TIMEOUT (a call leaves what must be zero zeroed);
+                                NULL = library-owned scratch */
     size_t workspace_bytes;
     int32_t* device_status;  /* as in luvc_kv_opts */
     float scale;             /* factor of the scores; 0 = 1 / sqrt(D) */
@@ -503,7 +504,8 @@ typedef struct {
  *             reads as empty (LUVC_ERR_SHAPE in the status word)
  * A sequence without tokens, or whose keys are all masked by -inf, gives a row of zeros.  A key masked
  * by -inf contributes nothing, whatever its rows hold; rows past the length are never used.  Scores,
- * softmax and sums are fp32; results do not depend on timing or on other streams.
+ * softmax and sums are fp32.  A call repeated gives the same bits; how the work is split, and with it the last bits,
+ * depends on all lengths of the call.  The call runs whatever the status word says.
  */
 int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,
                      int q_heads, int dtype, void* out, const luvc_attn_opts* opts);

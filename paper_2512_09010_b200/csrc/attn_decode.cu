@@ -1,98 +1,837 @@
 // Attention of one new token per sequence over its paged key-value cache.
 //
-// The simplest form: one CTA per (sequence, query head); its warps take every eighth token, keep a running maximum, sum and
-// weighted value row (the softmax in one pass: when the maximum grows, what has been summed is scaled down), and
-// join them through shared memory.
+//   out[i, h] = sum_t p_t V[t] / sum_t p_t,   p_t = exp(s_t - max s),   s_t = scale <q[i, h], K[t]> + bias[i, t]
+//
+// in one pass: a running maximum m, the sum l of the weights so far and their weighted sum O of value rows; when m grows,
+// l and O are scaled by exp(m_old - m_new).  Partial results of parts of a sequence join by the same rule.
+//
+// Bound.  Every cached row is read once, for all query heads that share it: 4 * G flops per element of K and V with G query
+// heads per key head, so HBM bounds it up to the largest G in use; what matters is to keep enough bytes in flight on every
+// SM, whatever the lengths.
+//
+// Split.  The work is the list of all tiles (KT tokens of one sequence and key head), sequence after sequence.  Each CTA (one per
+// SM) takes an equal part of that list, each of its warps an equal part of the CTA's, so no length leaves an SM idle and a
+// lone long sequence uses the whole GPU.  A warp works alone: it has a ring of stages in shared memory that TMA fills
+// (lane 0 issues; the page numbers of the next 32 pages are held one per lane), and it emits every
+// (sequence, head) that lies wholly in its part.  Of the others a warp has at most two, at the ends of its part; their
+// partial results stay in the ring stage that was read last (that stage is not filled again) and are joined by the CTA
+// when its warps are done, then, where a sequence crosses CTAs, through the workspace by the CTA that comes last (a counter that
+// wraps to zero; the parts are added in the order of the list, so results do not depend on which that is).
+//
+// Matrix instructions.  With one query token the product of a tile has up to 16 columns (the query heads of a key head), too few
+// rows for tcgen05 (its M is 64 at least, over rows that would have to be loaded for one token); at 4 G flops per element the
+// warp-level mma.sync, keys as the M of m16n8k16 and query heads as its N, is far from being the bound.  S^T = K Q^T with K from
+// ldmatrix, then O^T += V^T P^T with V from ldmatrix.trans and P^T from the scores' registers by movmatrix.
+// Roundings: Q and K are used as they are (an e4m3 cache goes to f16, which is exact; the query, scaled by a power of two so
+// that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
+// largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats (16 bits at least), because one
+// 16-bit float would cost as much again as the output's own rounding; tensor time is not the bound.  f32 caches use
+// tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 21 bits).  Sums, maxima and O are fp32.
 
+#include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "luvc_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace luvc {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxD = 256, kPer = kMaxD / 32;
+using namespace ptx;
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(__nv_fp8_e4m3 x) { return (float)x; }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
+constexpr int kMaxPartRows = 16, kMaxPartCols = 256;
+constexpr size_t kPartBytes = (size_t)kMaxPartRows * (kMaxPartCols + 2) * sizeof(float);
+constexpr int kMinTiles = 2;                    // tiles a warp takes at least: fewer CTAs, not smaller parts, for little work
+constexpr int kWaitProbes = 1 << 22;            // probes before a wait for a copy gives up (seconds)
 
-template <typename TQ, typename TC>
-__global__ void __launch_bounds__(kThreads) attn_decode_kernel(const __grid_constant__ AttnProblem a) {
-    __shared__ float part[kWarps][kMaxD], part_m[kWarps], part_s[kWarps];
-    const luvc_kv_cache& c = a.c;
-    if (__syncthreads_or(*reinterpret_cast<volatile int*>(a.status) != 0)) return;
-    const int i = blockIdx.y, hq = blockIdx.x, h = hq / (a.q_heads / c.heads);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = c.D, ps = c.page_size;
-    const int slot = a.seqs ? a.seqs[i] : i;
-    int len = 0;
-    if (slot >= 0 && slot < c.slots) len = max(0, min(c.lengths[slot], c.max_pages * ps));
-    else if (threadIdx.x == 0) *a.status = LUVC_ERR_SHAPE;
-    const float ks = c.k_scale ? c.k_scale[a.layer * c.heads + h] : 1.f;
-    const float vs = c.v_scale ? c.v_scale[a.layer * c.heads + h] : 1.f;
-    float q[kPer], o[kPer], m = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int d = lane + 32 * j;
-        q[j] = d < D ? to_float(static_cast<const TQ*>(a.q)[i * a.q_stride + (long long)hq * D + d]) : 0.f;
-        o[j] = 0.f;
-    }
-    for (int t = warp; t < len; t += kWarps) {
-        const int page = c.table[(long long)slot * c.max_pages + t / ps];
-        if (page < 0 || page >= c.pages) continue;
-        const float bias = t < a.bias_width ? a.bias[i * a.bias_stride + t] : 0.f;
-        if (bias == -INFINITY) continue;
-        const long long row = ((((long long)a.layer * c.pages + page) * c.heads + h) * ps + t % ps) * D;
-        float s = 0.f;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int d = lane + 32 * j;
-            if (d < D) s += q[j] * to_float(static_cast<const TC*>(c.k)[row + d]);
+// ---- the instructions of this file -----------------------------------------------------------------
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int x, int row) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(row) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t movm(uint32_t a) {      // transpose of an 8 x 8 matrix of 16-bit elements
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
+    uint32_t d;
+    asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(d) : "r"(two));
+    return d;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// the part of a float that a tf32 operand holds, and (exactly) the rest
+__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
+    hi = x & 0xffffe000u;
+    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) & 0xffffe000u;
+}
+
+// ---- shapes ---------------------------------------------------------------------------------------------
+
+// TC: element of the cache; DPB: bytes of a row in shared memory, a multiple of 128 (columns past D are filled with zeros by
+// TMA); NT: groups of 8 query heads per key head that one tile is multiplied with.
+template <typename TC, int DPB_, int NT_>
+struct Shape {
+    static constexpr int DPB = DPB_, NT = NT_, ES = sizeof(TC), DP = DPB / ES, SEGS = DPB / 128;
+    static constexpr int SUBK = 16 * DPB;                       // bytes of 16 rows
+    // 16-token parts of a tile.  A stage of 8 KB or more; it also has room for a partial result (8 NT rows of DP floats).
+    static constexpr int SUB = (2 * SUBK < 8192 || NT > ES) ? 2 : 1;
+    static constexpr int KT = 16 * SUB, STAGE = SUB * 2 * SUBK;
+    // warps and stages: up to 196,608 bytes of ring, three stages or more each
+    static constexpr int NW = STAGE <= 8192 ? 8 : STAGE <= 16384 ? 4 : 2, S = 3;
+    static constexpr int MT = DP / 16;                          // 16-row groups of O^T
+    static constexpr int ROWS = 8 * NT;
+    static_assert(ROWS * DP * 4 <= STAGE, "a partial result must fit a stage");
+    static_assert(NW * S * STAGE <= 196608, "ring too large");
+};
+
+struct Args {
+    AttnProblem p;
+    int group, groups;          // query heads per key head; head groups of ROWS
+    int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
+    unsigned* counters;         // [kMaxCtas]
+    float* parts;               // [kMaxCtas][2] of kPartBytes
+};
+
+// Results of a warp that are not final: its part of the list begins (0) or ends (1) inside a (sequence, head).
+struct Piece {
+    int off;                    // byte offset of O in the ring; -1: none
+    int seq, seg;
+};
+
+// Place of float d of row r of O in a stage: rows 2 t and 2 t + 1 of a lane quad start 8 banks apart.
+__device__ __forceinline__ int o_index(int r, int d, int dp) { return r * dp + (d ^ (((r >> 1) & 3) << 3)); }
+
+template <typename T> __device__ __forceinline__ void put4(T* p, float4 x);
+template <> __device__ __forceinline__ void put4<float>(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p, float4 x) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// Joins `count` partial results, given by get_o(k) (rows of floats), get_ml(k, row) and index(row, d), over nthr threads.
+// With `emit` the result is final and goes to out / lse, else to `part` (O rows of DP floats, then (m, l) pairs).
+template <typename TQ, int ROWS, int DP, typename GetO, typename GetMl, typename Index>
+__device__ __forceinline__ void join(const Args& a, int seq, int seg, int count, GetO get_o, GetMl get_ml, Index index, bool emit,
+                                     float* part, int tid, int nthr) {
+    const AttnProblem& p = a.p;
+    const int h = seg / a.groups, r0 = (seg % a.groups) * ROWS;
+    const int rows = min(ROWS, a.group - r0), quads = p.c.D / 4;
+    const long long head0 = (long long)seq * p.q_heads + (long long)h * a.group + r0;
+    const float vs = p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
+    for (int e = tid; e < rows * quads; e += nthr) {
+        const int r = e / quads, d = (e - r * quads) * 4;
+        float m = -INFINITY;
+        for (int k = 0; k < count; ++k) m = fmaxf(m, get_ml(k, r).x);
+        const float base = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < count; ++k) {
+            const float2 ml = get_ml(k, r);
+            const float w = exp2_fast((ml.x - base) * kLog2e);
+            const float4 x = *reinterpret_cast<const float4*>(get_o(k) + index(r, d));
+            l += w * ml.y;
+            o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
         }
-#pragma unroll
-        for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(~0u, s, x);
-        s = s * (a.scale * ks) + bias;
-        const float mn = fmaxf(m, s), base = mn == -INFINITY ? 0.f : mn;
-        const float f = expf(m - base), w = expf(s - base);
-        sum = sum * f + w;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int d = lane + 32 * j;
-            if (d < D) o[j] = o[j] * f + w * to_float(static_cast<const TC*>(c.v)[row + d]);
+        if (emit) {
+            const float f = l == 0.f ? 0.f : vs / l;
+            if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
+            o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+            put4(static_cast<TQ*>(p.out) + (head0 + r) * p.c.D + d, o);
+            if (p.lse && d == 0) p.lse[head0 + r] = l == 0.f ? -INFINITY : base + logf(l);
+        } else {
+            *reinterpret_cast<float4*>(part + r * DP + d) = o;
+            if (d == 0) *reinterpret_cast<float2*>(part + kMaxPartRows * kMaxPartCols + 2 * r) = make_float2(m, l);
         }
-        m = mn;
     }
+}
+
+template <typename TQ, typename TC, int DPB, int NT>
+__global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
+attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ Args a) {
+    using Sh = Shape<TC, DPB, NT>;
+    constexpr int NW = Sh::NW, S = Sh::S, MT = Sh::MT, DP = Sh::DP, ROWS = Sh::ROWS, KT = Sh::KT, NTHR = 32 * NW;
+    constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[NW * S];
+    __shared__ float2 ml_of[NW][2][ROWS];
+    __shared__ Piece piece[NW][2];
+    __shared__ int scan_warp[NW], last_flag;
+    unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
+
+    const AttnProblem& p = a.p;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n, ps = p.c.page_size;
+    const int g = lane >> 2, t4 = lane & 3;
+
+    // ---- the list of tiles ----
+    if (tid < NW * S) {
+        mbar_init(smem_u32(&bars[tid]), 1);
+        mbar_fence_init();
+    }
+    if (tid < 2 * NW) piece[tid >> 1][tid & 1].off = -1;
+    if (tid == 0) prefix[0] = 0;
+    auto slot_of = [&](int i) { return p.seqs ? p.seqs[i] : i; };
+    auto length_of = [&](int slot) {
+        return slot >= 0 && slot < p.c.slots ? max(0, min(p.c.lengths[slot], p.c.max_pages * ps)) : 0;
+    };
+    bool fits = true;
+    int base = 0;
+    for (int i0 = 0; i0 < n; i0 += NTHR) {
+        const int i = i0 + tid;
+        int v = 0;
+        if (i < n) {
+            const int slot = slot_of(i);
+            v = (length_of(slot) + KT - 1) / KT;
+            if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
+        }
+        int x = v;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) part[warp][lane + 32 * j] = o[j];
-    if (lane == 0) { part_m[warp] = m; part_s[warp] = sum; }
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(~0u, x, d);
+            if (lane >= d) x = (int)min(2147483647ll, (long long)x + y);
+        }
+        if (lane == 31) scan_warp[warp] = x;
+        __syncthreads();
+        long long before = base, all = base;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < warp) before += scan_warp[w];
+            all += scan_warp[w];
+        }
+        if (i < n) prefix[i + 1] = (int)min(2147483647ll, before + x);
+        fits = fits && all < 2147483647ll;
+        base = (int)min(2147483647ll, all);
+        __syncthreads();
+    }
+    if (!fits) {                                                // 2^31 tiles: the list's numbers do not reach
+        if (tid == 0) *p.status = LUVC_ERR_SHAPE;
+        return;
+    }
+    const int segs = p.c.heads * a.groups;
+    const long long total = (long long)base * segs;
+
+    // sequences without tokens
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+        if (prefix[i + 1] != prefix[i]) continue;
+        for (int e = tid; e < p.q_heads * (p.c.D / 4); e += NTHR)
+            put4(static_cast<TQ*>(p.out) + (long long)i * p.q_heads * p.c.D + 4 * e, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (p.lse)
+            for (int e = tid; e < p.q_heads; e += NTHR) p.lse[(long long)i * p.q_heads + e] = -INFINITY;
+    }
+
+    // ---- this CTA's part of the list, this warp's part of that ----
+    struct Place { int seq, seg, tile, tiles; long long first; };   // a tile; its (sequence, head) starts at `first` in the list
+    auto place_of = [&](long long x) {
+        int lo = 0, hi = n;                                     // prefix[lo] * segs <= x < prefix[hi] * segs
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((long long)prefix[mid] * segs <= x) lo = mid; else hi = mid;
+        }
+        Place q;
+        q.seq = lo;
+        q.tiles = prefix[lo + 1] - prefix[lo];
+        const long long in = x - (long long)prefix[lo] * segs;
+        q.seg = (int)(in / q.tiles);
+        q.tile = (int)(in - (long long)q.seg * q.tiles);
+        q.first = x - q.tile;
+        return q;
+    };
+    const long long per = max((total + gridDim.x - 1) / (long long)gridDim.x, (long long)NW * kMinTiles);
+    const int tol = (int)min(per / 4, 8ll);
+    auto bound_of = [&](long long c) {                          // start of CTA c's part, moved to a near (sequence, head) boundary
+        const long long x = c * per;
+        if (x <= 0) return 0ll;
+        if (x >= total) return total;
+        const Place q = place_of(x);
+        if (q.tile <= tol) return q.first;
+        if (q.tiles - q.tile <= tol) return q.first + q.tiles;
+        return x;
+    };
+    const long long cta_a = bound_of(blockIdx.x), cta_b = bound_of(blockIdx.x + 1ll);
+    if (cta_a >= cta_b) return;
+    const long long each = (cta_b - cta_a + NW - 1) / NW;
+    const long long wa = min(cta_a + warp * each, cta_b), wb = min(wa + each, cta_b);
+
+    unsigned char* const my_ring = ring + warp * S * Sh::STAGE;
+    const uint32_t my_ring_s = smem_u32(my_ring), my_bar = smem_u32(&bars[warp * S]);
+
+    if (wa < wb) {
+        // what is to be loaded next
+        Place ld = place_of(wa);
+        long long to_load = wb - wa;
+        int ld_len = 0, ld_page = 0, ld_off = 0, pg_first = 0, pg = -1;
+        const int32_t* ld_row = nullptr;
+        auto load_start = [&](bool new_seq) {                   // at a new (sequence, head), or at the warp's first tile
+            if (new_seq) {
+                const int slot = slot_of(ld.seq);
+                ld_len = length_of(slot);
+                ld_row = p.c.table + (long long)slot * p.c.max_pages;
+            }
+            const int token = ld.tile * KT;
+            ld_page = token / ps;
+            ld_off = token - ld_page * ps;
+            if (new_seq || ld_page < pg_first || ld_page >= pg_first + 32) {
+                pg_first = ld_page;
+                pg = ld_page + lane < p.c.max_pages ? ld_row[ld_page + lane] : -1;
+            }
+        };
+        auto load = [&](int stage) {
+            const uint32_t bar = my_bar + 8 * stage, dst = my_ring_s + stage * Sh::STAGE;
+            const int h = ld.seg / a.groups;
+            const int left = ld_len - ld.tile * KT;
+            if (lane == 0) mbar_arrive_expect_tx(bar, min(Sh::SUB, (left + 15) / 16) * 2 * Sh::SUBK);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < Sh::SUB; ++j) {
+                if (16 * j < left) {
+                    if (ld_page >= pg_first + 32) {
+                        pg_first = ld_page;
+                        pg = ld_page + lane < p.c.max_pages ? ld_row[ld_page + lane] : -1;
+                    }
+                    const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
+                    const int row = page >= 0 && page < p.c.pages ? (page * p.c.heads + h) * ps + ld_off : a.rows_total;
+                    if (lane == 0) {
+#pragma unroll
+                        for (int s = 0; s < Sh::SEGS; ++s) {
+                            tma_load_2d(dst + j * 2 * Sh::SUBK + s * 2048, &kmap, bar, s * (128 / Sh::ES), row);
+                            tma_load_2d(dst + j * 2 * Sh::SUBK + Sh::SUBK + s * 2048, &vmap, bar, s * (128 / Sh::ES), row);
+                        }
+                    }
+                    ld_off += 16;
+                    if (ld_off == ps) { ld_off = 0; ++ld_page; }
+                }
+            }
+            if (--to_load > 0 && ++ld.tile == ld.tiles) {       // the next (sequence, head)
+                ld.tile = 0;
+                bool new_seq = false;
+                if (++ld.seg == segs) {
+                    ld.seg = 0;
+                    new_seq = true;
+                    do { ++ld.seq; } while (prefix[ld.seq + 1] == prefix[ld.seq]);
+                    ld.tiles = prefix[ld.seq + 1] - prefix[ld.seq];
+                }
+                load_start(new_seq);
+            }
+        };
+        Place at = ld;
+        load_start(true);
+        unsigned order = 0, phases = 0;                         // stages in the order they were filled (4 bits each); their phases
+        int filled = 0;
+        for (; filled < S && to_load > 0; ++filled) {
+            load(filled);
+            order |= (unsigned)filled << (4 * filled);
+        }
+
+        long long left = wb - wa;
+        bool dead = false;                                      // a wait gave up
+        while (left > 0 && !dead) {
+            const int h = at.seg / a.groups, r0 = (at.seg % a.groups) * ROWS;
+            const int rows = min(ROWS, a.group - r0);
+            const int len = length_of(slot_of(at.seq));
+            const float scale = p.scale * (p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
+            // queries: B operand of S^T = K Q^T, head g of each group of 8
+            const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
+            constexpr int KS = DPB / 32;                        // steps of 32 bytes of a row
+            uint32_t q[NT][KS][2 * (kF8 ? 2 : 1)];
+            float qmul[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const TQ* const qh = qrow + (long long)(nt * 8 + g) * p.c.D;
+                const bool live = nt * 8 + g < rows;
+                if constexpr (kF32) {
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int d = 8 * k + 4 * b + t4;
+                            q[nt][k][b] = live && d < p.c.D ? reinterpret_cast<const uint32_t*>(qh)[d] : 0u;
+                        }
+                    qmul[nt][0] = qmul[nt][1] = scale;
+                } else if constexpr (!kF8) {
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int d = 16 * k + 8 * b + 2 * t4;
+                            q[nt][k][b] = live && d < p.c.D ? *reinterpret_cast<const uint32_t*>(qh + d) : 0u;
+                        }
+                    qmul[nt][0] = qmul[nt][1] = scale;
+                } else {
+                    // a 16-byte piece of a row is one k step; lane t4 holds its bytes 4 t4 .. 4 t4 + 3
+                    uint2 raw[2 * KS];
+                    float big = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 2 * KS; ++k) {
+                        const int d = 16 * k + 4 * t4;
+                        raw[k] = live && d < p.c.D ? *reinterpret_cast<const uint2*>(qh + d) : make_uint2(0u, 0u);
+                        big = fmaxf(big, fmaxf(fmaxf(fabsf(__uint_as_float(raw[k].x << 16)), fabsf(__uint_as_float(raw[k].x & 0xffff0000u))),
+                                               fmaxf(fabsf(__uint_as_float(raw[k].y << 16)), fabsf(__uint_as_float(raw[k].y & 0xffff0000u)))));
+                    }
+                    big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
+                    big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
+                    // 2^e <= big < 2^(e+1), kept where 2^e and 2^-e are normal floats
+                    const int e = big == 0.f ? 0 : max(-125, min(125, (int)(__float_as_uint(big) >> 23) - 127));
+                    const float down = __uint_as_float((unsigned)(127 - e) << 23), up = __uint_as_float((unsigned)(127 + e) << 23);
+#pragma unroll
+                    for (int k = 0; k < 2 * KS; ++k) {
+                        const __half2 x = __floats2half2_rn(__uint_as_float(raw[k].x << 16) * down, __uint_as_float(raw[k].x & 0xffff0000u) * down);
+                        const __half2 y = __floats2half2_rn(__uint_as_float(raw[k].y << 16) * down, __uint_as_float(raw[k].y & 0xffff0000u) * down);
+                        q[nt][k >> 1][2 * (k & 1)] = *reinterpret_cast<const uint32_t*>(&x);
+                        q[nt][k >> 1][2 * (k & 1) + 1] = *reinterpret_cast<const uint32_t*>(&y);
+                    }
+                    qmul[nt][0] = scale * __shfl_sync(~0u, up, 8 * t4);         // of heads 2 t4 and 2 t4 + 1
+                    qmul[nt][1] = scale * __shfl_sync(~0u, up, 8 * t4 + 4);
+                }
+            }
+
+            float m[NT][2], l[NT][2], o[MT][NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[mt][nt][c] = 0.f;
+
+            const int count = (int)min((long long)(at.tiles - at.tile), left);
+            const bool whole = at.tile == 0 && count == at.tiles;
+            int stage = 0;
+            for (int k = 0; k < count; ++k, ++at.tile) {
+                stage = order & 15;
+                order >>= 4;
+                --filled;
+                float bias[Sh::SUB][2];
+#pragma unroll
+                for (int j = 0; j < Sh::SUB; ++j)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int token = at.tile * KT + 16 * j + 8 * x + g;
+                        bias[j][x] = token < min(p.bias_width, len) ? p.bias[at.seq * p.bias_stride + token] : 0.f;
+                        if (token >= len) bias[j][x] = -INFINITY;
+                    }
+                {
+                    const uint32_t bar = my_bar + 8 * stage;
+                    int probes = 0;
+                    while (!mbar_try_wait(bar, (phases >> stage) & 1) && ++probes < kWaitProbes) {}
+                    if (__any_sync(~0u, probes >= kWaitProbes)) { dead = true; break; }
+                    phases ^= 1u << stage;
+                }
+#pragma unroll
+                for (int j = 0; j < Sh::SUB; ++j) {
+                    if (at.tile * KT + 16 * j >= len) break;
+                    const uint32_t ks = my_ring_s + stage * Sh::STAGE + j * 2 * Sh::SUBK, vs = ks + Sh::SUBK;
+                    // ---- S^T: rows are the 16 tokens, columns the query heads ----
+                    float s[NT][4], s2[NT][4];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
+                    const int krow = (lane & 7) + (lane & 8);
+#pragma unroll
+                    for (int k2 = 0; k2 < KS; ++k2) {           // 32 bytes of each of the 16 rows
+                        const int chunk = 2 * k2 + (lane >> 4);
+                        uint32_t r[4];
+                        ldsm4(ks + (chunk >> 3) * 2048 + krow * 128 + (((chunk & 7) ^ (krow & 7)) << 4), r);
+                        if constexpr (kF32) {
+                            uint32_t hi[4], lo[4];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) split_tf32(r[c], hi[c], lo[c]);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                uint32_t qh[2], ql[2];
+                                split_tf32(q[nt][k2][0], qh[0], ql[0]);
+                                split_tf32(q[nt][k2][1], qh[1], ql[1]);
+                                mma_tf32(s2[nt], lo, qh[0], qh[1]);
+                                mma_tf32(s2[nt], hi, ql[0], ql[1]);
+                                mma_tf32(s[nt], hi, qh[0], qh[1]);
+                            }
+                        } else if constexpr (!kF8) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_bf16(k2 & 1 ? s2[nt] : s[nt], r, q[nt][k2][0], q[nt][k2][1]);
+                        } else {
+                            const uint32_t x[4] = {e4m3x2_to_f16x2(r[0]), e4m3x2_to_f16x2(r[1]), e4m3x2_to_f16x2(r[0] >> 16), e4m3x2_to_f16x2(r[1] >> 16)};
+                            const uint32_t y[4] = {e4m3x2_to_f16x2(r[2]), e4m3x2_to_f16x2(r[3]), e4m3x2_to_f16x2(r[2] >> 16), e4m3x2_to_f16x2(r[3] >> 16)};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(s[nt], x, q[nt][k2][0], q[nt][k2][1]);
+                                mma_f16(s2[nt], y, q[nt][k2][2], q[nt][k2][3]);
+                            }
+                        }
+                    }
+                    // ---- weights ----
+                    const bool gone0 = bias[j][0] == -INFINITY, gone1 = bias[j][1] == -INFINITY;
+                    const unsigned gone = __ballot_sync(~0u, gone0) | __ballot_sync(~0u, gone1);
+                    bool grew = false;
+                    float f[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float x = fmaf(s[nt][c] + s2[nt][c], qmul[nt][c & 1], bias[j][c >> 1]);
+                            s[nt][c] = (c >> 1 ? gone1 : gone0) ? -INFINITY : x;
+                        }
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            float x = fmaxf(s[nt][b], s[nt][b + 2]);
+                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                            x = fmaxf(x, m[nt][b]);
+                            const float mb = x == -INFINITY ? 0.f : x;
+                            f[nt][b] = exp2_fast((m[nt][b] - mb) * kLog2e);
+                            grew = grew || x > m[nt][b];
+                            m[nt][b] = x;
+                            s[nt][b] = exp2_fast((s[nt][b] - mb) * kLog2e);
+                            s[nt][b + 2] = exp2_fast((s[nt][b + 2] - mb) * kLog2e);
+                        }
+                    }
+                    if (__any_sync(~0u, grew)) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            l[nt][0] *= f[nt][0]; l[nt][1] *= f[nt][1];
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) o[mt][nt][c] *= f[nt][c & 1];
+                        }
+                    }
+                    uint32_t ph[NT][2], pl[NT][2];              // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
+                    float pf[NT][4];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        l[nt][0] += s[nt][0] + s[nt][2];
+                        l[nt][1] += s[nt][1] + s[nt][3];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float p0 = s[nt][2 * x], p1 = s[nt][2 * x + 1];
+                            if constexpr (kF32) {
+                                const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+                                const uint32_t up = movm(__byte_perm(u0, u1, 0x7632)), down = movm(__byte_perm(u0, u1, 0x5410));
+                                pf[nt][2 * x] = __uint_as_float(__byte_perm(down, up, 0x5410));
+                                pf[nt][2 * x + 1] = __uint_as_float(__byte_perm(down, up, 0x7632));
+                            } else if constexpr (!kF8) {
+                                const __nv_bfloat162 hi = __floats2bfloat162_rn(p0, p1);
+                                const __nv_bfloat162 lo = __floats2bfloat162_rn(p0 - __low2float(hi), p1 - __high2float(hi));
+                                ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
+                                pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
+                            } else {
+                                const __half2 hi = __floats2half2_rn(p0, p1);
+                                const __half2 lo = __floats2half2_rn(p0 - __low2float(hi), p1 - __high2float(hi));
+                                ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
+                                pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
+                            }
+                        }
+                    }
+                    // ---- O^T += V^T P^T; rows of V that are masked may hold anything and are replaced by zeros ----
+                    // gone: bit 4 i (+ any lane of the quad) for token i or i + 8; a lane needs tokens 2 t4, 2 t4 + 1, + 8
+                    uint32_t keep0 = ~0u, keep1 = ~0u;          // 16-bit halves of a register: tokens 2 t4, 2 t4 + 1 (+ 8)
+                    if (gone) {
+                        const unsigned g0 = __ballot_sync(~0u, gone0), g1 = __ballot_sync(~0u, gone1);
+                        keep0 = ((g0 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g0 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
+                        keep1 = ((g1 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g1 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
+                    }
+                    if constexpr (kF32) {
+                        // step x: tokens 8 x .. 8 x + 7; k = t4 is token 2 t4, k = t4 + 4 is token 2 t4 + 1 (bank-conflict free)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const uint32_t keep = x ? keep1 : keep0;
+                            const bool drop0 = !(keep & 0xffffu), drop1 = !(keep >> 16);
+                            uint32_t bh[NT][2], bl[NT][2];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                split_tf32(__float_as_uint(pf[nt][2 * x]), bh[nt][0], bl[nt][0]);
+                                split_tf32(__float_as_uint(pf[nt][2 * x + 1]), bh[nt][1], bl[nt][1]);
+                            }
+                            const int row0 = 8 * x + 2 * t4, row1 = row0 + 1;
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt) {
+                                uint32_t hi[4], lo[4];
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    const int d = 16 * mt + 8 * (c & 1) + g, row = c >> 1 ? row1 : row0;
+                                    uint32_t u;
+                                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u)
+                                                 : "r"(vs + (d >> 5) * 2048 + row * 128 + ((((d & 31) >> 2) ^ (row & 7)) << 4) + (d & 3) * 4) : "memory");
+                                    if (c >> 1 ? drop1 : drop0) u = 0u;
+                                    split_tf32(u, hi[c], lo[c]);
+                                }
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma_tf32(o[mt][nt], lo, bh[nt][0], bh[nt][1]);
+                                    mma_tf32(o[mt][nt], hi, bl[nt][0], bl[nt][1]);
+                                    mma_tf32(o[mt][nt], hi, bh[nt][0], bh[nt][1]);
+                                }
+                            }
+                        }
+                    } else if constexpr (!kF8) {
+                        const int vrow = (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const int chunk = 2 * mt + ((lane >> 3) & 1);
+                            uint32_t r[4];
+                            ldsm4_trans(vs + (chunk >> 3) * 2048 + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4), r);
+                            if (gone) { r[0] &= keep0; r[1] &= keep0; r[2] &= keep1; r[3] &= keep1; }
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_bf16(o[mt][nt], r, pl[nt][0], pl[nt][1]);
+                                mma_bf16(o[mt][nt], r, ph[nt][0], ph[nt][1]);
+                            }
+                        }
+                    } else {
+                        // a transposed 8 x 8 matrix of byte pairs: tokens 2 t4 and 2 t4 + 1 of columns 2 g and 2 g + 1
+                        const int vrow = (lane & 7) + (lane & 8);
+#pragma unroll
+                        for (int m2 = 0; m2 < MT / 2; ++m2) {   // two 16-byte pieces
+                            const int chunk = 2 * m2 + (lane >> 4);
+                            uint32_t r[4];
+                            ldsm4_trans(vs + (chunk >> 3) * 2048 + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4), r);
+                            if (gone) { r[0] &= keep0; r[2] &= keep0; r[1] &= keep1; r[3] &= keep1; }
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const uint32_t u = __byte_perm(r[2 * x], 0u, 0x3120), w = __byte_perm(r[2 * x + 1], 0u, 0x3120);
+                                const uint32_t v[4] = {e4m3x2_to_f16x2(u), e4m3x2_to_f16x2(u >> 16), e4m3x2_to_f16x2(w), e4m3x2_to_f16x2(w >> 16)};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma_f16(o[2 * m2 + x][nt], v, pl[nt][0], pl[nt][1]);
+                                    mma_f16(o[2 * m2 + x][nt], v, ph[nt][0], ph[nt][1]);
+                                }
+                            }
+                        }
+                    }
+                }
+                __syncwarp();
+                if (k < count - 1 && to_load > 0) {             // the stage has been read
+                    load(stage);
+                    order |= (unsigned)stage << (4 * filled);
+                    ++filled;
+                }
+            }
+            if (dead) break;
+            left -= count;
+
+            // ---- the result, through the stage that was read last ----
+            float* const os = reinterpret_cast<float*>(my_ring + stage * Sh::STAGE);
+            const int which = at.tile > count ? 0 : 1;          // 0: it began in the part of the warp before
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float x = l[nt][b];
+                    x += __shfl_xor_sync(~0u, x, 4);
+                    x += __shfl_xor_sync(~0u, x, 8);
+                    x += __shfl_xor_sync(~0u, x, 16);
+                    if (g == 0) ml_of[warp][which][nt * 8 + 2 * t4 + b] = make_float2(m[nt][b], x);
+                }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int d = 16 * mt + (kF8 ? 2 * g + (c >> 1) : g + 8 * (c >> 1));
+                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = o[mt][nt][c];
+                    }
+            __syncwarp();
+            if (whole) {
+                join<TQ, ROWS, DP>(a, at.seq, at.seg, 1, [&](int) { return os; }, [&](int, int r) { return ml_of[warp][1][r]; },
+                                   [&](int r, int d) { return o_index(r, d, DP); }, true, nullptr, lane, 32);
+                fence_proxy_async();                            // the stage was written by this warp; TMA writes it next
+                __syncwarp();
+                if (to_load > 0) {
+                    load(stage);
+                    order |= (unsigned)stage << (4 * filled);
+                    ++filled;
+                }
+            } else if (lane == 0) {
+                piece[warp][which].seq = at.seq;
+                piece[warp][which].seg = at.seg;
+                piece[warp][which].off = (warp * S + stage) * Sh::STAGE;
+            }
+            if (left > 0) {                                     // the next (sequence, head)
+                at.tile = 0;
+                if (++at.seg == segs) {
+                    at.seg = 0;
+                    do { ++at.seq; } while (prefix[at.seq + 1] == prefix[at.seq]);
+                    at.tiles = prefix[at.seq + 1] - prefix[at.seq];
+                }
+            }
+        }
+        if (dead) {                                             // let the copies in flight land, then report
+            while (filled-- > 0) {
+                const int stage = order & 15;
+                order >>= 4;
+                for (int probes = 0; !mbar_try_wait(my_bar + 8 * stage, (phases >> stage) & 1) && probes < kWaitProbes; ++probes) {}
+            }
+            if (lane == 0) *p.status = LUVC_ERR_TIMEOUT;
+        }
+    }
     __syncthreads();
-    float mt = -INFINITY, st = 0.f;
-    for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, part_m[w]);
-    const float base = mt == -INFINITY ? 0.f : mt;
-    for (int w = 0; w < kWarps; ++w) st += part_s[w] * expf(part_m[w] - base);
-    for (int d = threadIdx.x; d < D; d += kThreads) {
-        float x = 0.f;
-        for (int w = 0; w < kWarps; ++w) x += part[w][d] * expf(part_m[w] - base);
-        put(static_cast<TQ*>(a.out) + ((long long)i * a.q_heads + hq) * D + d, st == 0.f ? 0.f : x * vs / st);
+
+    // ---- joins: first the parts of this CTA's warps ----
+    int cross_seq[2], cross_seg[2], crosses = 0;                // parts of a (sequence, head) that other CTAs share
+    for (int w = 0; w < NW; ++w) {
+        for (int which = w == 0 ? 0 : 1; which < 2; ++which) {  // a part 0 of a later warp belongs to a chain that began before
+            if (piece[w][which].off < 0) continue;
+            const int seq = piece[w][which].seq, seg = piece[w][which].seg;
+            const int tiles = prefix[seq + 1] - prefix[seq];
+            const long long s0 = (long long)prefix[seq] * segs + (long long)seg * tiles, s1 = s0 + tiles;
+            int last = w;
+            while (last + 1 < NW && min(cta_a + (last + 1) * each, cta_b) < s1 && piece[last + 1][0].off >= 0) ++last;
+            const bool emit = s0 >= cta_a && s1 <= cta_b;
+            const int slot = s0 >= cta_a ? 1 : 0;
+            float* const part = a.parts + ((size_t)blockIdx.x * 2 + slot) * (kPartBytes / sizeof(float));
+            join<TQ, ROWS, DP>(
+                a, seq, seg, last - w + 1,
+                [&](int k) { return reinterpret_cast<const float*>(ring + piece[w + k][k ? 0 : which].off); },
+                [&](int k, int r) { return ml_of[w + k][k ? 0 : which][r]; }, [&](int r, int d) { return o_index(r, d, DP); }, emit, part,
+                tid, NTHR);
+            if (!emit && crosses < 2) { cross_seq[crosses] = seq; cross_seg[crosses] = seg; ++crosses; }
+        }
     }
-    if (a.lse && threadIdx.x == 0) a.lse[(long long)i * a.q_heads + hq] = st == 0.f ? -INFINITY : base + logf(st);
+    // ---- then those of several CTAs, by the one that arrives last ----
+    for (int x = 0; x < crosses; ++x) {
+        const int seq = cross_seq[x], seg = cross_seg[x], tiles = prefix[seq + 1] - prefix[seq];
+        const long long s0 = (long long)prefix[seq] * segs + (long long)seg * tiles, s1 = s0 + tiles;
+        const int c0 = (int)((s0 + tol) / per), c1 = (int)((s1 - tol - 1) / per);
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) last_flag = atomicInc(&a.counters[c0], (unsigned)(c1 - c0)) == (unsigned)(c1 - c0);
+        __syncthreads();
+        if (!last_flag) continue;
+        __threadfence();
+        auto part_of = [&](int k) { return a.parts + ((size_t)(c0 + k) * 2 + (k ? 0 : 1)) * (kPartBytes / sizeof(float)); };
+        join<TQ, ROWS, DP>(a, seq, seg, c1 - c0 + 1, part_of,
+                           [&](int k, int r) { return *reinterpret_cast<const float2*>(part_of(k) + kMaxPartRows * kMaxPartCols + 2 * r); },
+                           [&](int r, int d) { return r * DP + d; }, true, nullptr, tid, NTHR);
+    }
+}
+
+// ---- launch -----------------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_tiled_fn() {
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    }
+    return fn;
+}
+
+int sm_count() {
+    static int sms = 0;
+    if (!sms) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        if (sms > kMaxCtas) sms = kMaxCtas;
+    }
+    return sms;
+}
+
+// The rows of one layer as a matrix [rows_total][D], fetched in boxes of 16 rows by 128 bytes.
+template <typename TC>
+bool layer_map(CUtensorMap* map, const luvc_kv_cache& c, void* pool, int layer, int rows_total) {
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)c.D, (cuuint64_t)rows_total}, strides[1] = {(cuuint64_t)c.D * sizeof(TC)};
+    const cuuint32_t box[2] = {128u / (cuuint32_t)sizeof(TC), 16u}, ones[2] = {1u, 1u};
+    void* base = static_cast<unsigned char*>(pool) + (size_t)layer * rows_total * c.D * sizeof(TC);
+    const CUtensorMapDataType type = sizeof(TC) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : sizeof(TC) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    return encode(map, type, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename TQ, typename TC, int DPB, int NT>
+int launch(const AttnProblem& p) {
+    using Sh = Shape<TC, DPB, NT>;
+    Args a;
+    a.p = p;
+    a.group = p.q_heads / p.c.heads;
+    a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
+    a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
+    a.counters = static_cast<unsigned*>(p.workspace);
+    a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kMaxCtas * sizeof(unsigned));
+    CUtensorMap kmap, vmap;
+    if (!layer_map<TC>(&kmap, p.c, p.c.k, p.layer, a.rows_total) || !layer_map<TC>(&vmap, p.c, p.c.v, p.layer, a.rows_total))
+        return LUVC_ERR_CUDA;
+    const size_t smem = 1024 + (size_t)Sh::NW * Sh::S * Sh::STAGE + (size_t)(p.n + 1) * sizeof(int);
+    static std::atomic<unsigned long long> set{0};              // devices on which the kernel may use this much
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return LUVC_ERR_CUDA;
+    if (dev > 63 || !((set.load(std::memory_order_relaxed) >> dev) & 1)) {
+        if (cudaFuncSetAttribute(attn_decode_kernel<TQ, TC, DPB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 1024 + Sh::NW * Sh::S * Sh::STAGE + (kKvMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess)
+            return LUVC_ERR_CUDA;
+        if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    const int sms = sm_count();
+    if (!sms) return LUVC_ERR_CUDA;
+    attn_decode_kernel<TQ, TC, DPB, NT><<<sms, 32 * Sh::NW, smem, p.stream>>>(kmap, vmap, a);
+    count_launch();
+    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+}
+
+template <typename TQ, typename TC, int DPB>
+int launch_heads(const AttnProblem& p) {
+    return p.q_heads / p.c.heads <= 8 ? launch<TQ, TC, DPB, 1>(p) : launch<TQ, TC, DPB, 2>(p);
 }
 
 }  // namespace
 
-size_t attn_workspace_bytes() { return 256; }
+size_t attn_workspace_bytes() { return align_up(kMaxCtas * sizeof(unsigned)) + (size_t)kMaxCtas * 2 * kPartBytes; }
 
 int attn_decode(const AttnProblem& p) {
-    const dim3 grid(p.q_heads, p.n);
-    if (p.c.dtype == LUVC_F32) attn_decode_kernel<float, float><<<grid, kThreads, 0, p.stream>>>(p);
-    else if (p.c.dtype == LUVC_BF16) attn_decode_kernel<__nv_bfloat16, __nv_bfloat16><<<grid, kThreads, 0, p.stream>>>(p);
-    else attn_decode_kernel<__nv_bfloat16, __nv_fp8_e4m3><<<grid, kThreads, 0, p.stream>>>(p);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
+    if (p.c.dtype == LUVC_F32)
+        return bytes <= 256 ? launch_heads<float, float, 256>(p) : bytes <= 512 ? launch_heads<float, float, 512>(p) : launch<float, float, 1024, 1>(p);
+    if (p.c.dtype == LUVC_BF16)
+        return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256>(p)
+                                                                                               : launch_heads<__nv_bfloat16, __nv_bfloat16, 512>(p);
+    return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 128>(p) : launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 256>(p);
 }
 
 }  // namespace luvc

@@ -212,7 +212,9 @@ def test_layers_slots_strides_and_streams(luvc, dtype):
     bad = seqs.clone()
     bad[1] = 4                                                    # no such slot: empty, and reported
     got = luvc.attn_decode(q, c, layer=2, seqs=bad)
-    assert luvc.check_status() == 2 and not got[1].any() and torch.equal(got[2], out[2])
+    assert luvc.check_status() == 2 and not got[1].any()
+    rest = torch.tensor([0, 2, 3, 4], device="cuda")              # the others are right (the split of the work may differ)
+    check(luvc, c, q[rest], got[rest], None, layer=2, seqs=seqs[rest].tolist())
 
 
 def test_results_repeat_bit_for_bit(luvc):
