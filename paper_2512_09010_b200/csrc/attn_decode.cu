@@ -92,10 +92,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// the part of a float that a tf32 operand holds, and (exactly) the rest
+// x as a sum of two tf32 operands, each the nearest: 11 bits, and 11 of the 12 that are left
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
-    hi = x & 0xffffe000u;
-    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) & 0xffffe000u;
+    hi = (x + 0x1000u) & 0xffffe000u;
+    lo = (__float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u) & 0xffffe000u;
 }
 
 // ---- shapes ---------------------------------------------------------------------------------------------
@@ -125,12 +125,6 @@ struct Args {
     float* parts;               // [kMaxCtas][2] of kPartBytes
 };
 
-// Results of a warp that are not final: its part of the list begins (0) or ends (1) inside a (sequence, head).
-struct Piece {
-    int off;                    // byte offset of O in the ring; -1: none
-    int seq, seg;
-};
-
 // Place of float d of row r of O in a stage: rows 2 t and 2 t + 1 of a lane quad start 8 banks apart.
 __device__ __forceinline__ int o_index(int r, int d, int dp) { return r * dp + (d ^ (((r >> 1) & 3) << 3)); }
 
@@ -141,42 +135,60 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// Joins `count` partial results, given by get_o(k) (rows of floats), get_ml(k, row) and index(row, d), over nthr threads.
-// With `emit` the result is final and goes to out / lse, else to `part` (O rows of DP floats, then (m, l) pairs).
-template <typename TQ, int ROWS, int DP, typename GetO, typename GetMl, typename Index>
-__device__ __forceinline__ void join(const Args& a, int seq, int seg, int count, GetO get_o, GetMl get_ml, Index index, bool emit,
-                                     float* part, int tid, int nthr) {
-    const AttnProblem& p = a.p;
-    const int h = seg / a.groups, r0 = (seg % a.groups) * ROWS;
-    const int rows = min(ROWS, a.group - r0), quads = p.c.D / 4;
-    const long long head0 = (long long)seq * p.q_heads + (long long)h * a.group + r0;
-    const float vs = p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
-    for (int e = tid; e < rows * quads; e += nthr) {
-        const int r = e / quads, d = (e - r * quads) * 4;
-        float m = -INFINITY;
-        for (int k = 0; k < count; ++k) m = fmaxf(m, get_ml(k, r).x);
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < count; ++k) {
-            const float2 ml = get_ml(k, r);
-            const float w = exp2_fast((ml.x - base) * kLog2e);
-            const float4 x = *reinterpret_cast<const float4*>(get_o(k) + index(r, d));
-            l += w * ml.y;
-            o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
+// One partial result: rows of O (o_index) and (m, l) of each row, in shared or global memory.
+struct Part {
+    const float* o;
+    const float2* ml;
+};
+
+// Joins `count` partial results for four columns of one row; part_of(k) is part k.  Up to eight parts are read at once, (m, l) along
+// with the columns, so a join costs one round trip to memory per eight parts.
+template <typename PartOf>
+__device__ __forceinline__ void join4(int count, PartOf part_of, int r, int at, float& m, float& l, float4& o) {
+    m = -INFINITY; l = 0.f; o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < count; k0 += 8) {
+        float4 x[8];
+        float2 ml[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                           // past the last part: the last one again, with weight 0
+            const Part q = part_of(min(k0 + k, count - 1));
+            ml[k] = q.ml[r];
+            x[k] = *reinterpret_cast<const float4*>(q.o + at);
         }
-        if (emit) {
-            const float f = l == 0.f ? 0.f : vs / l;
-            if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
-            o.x *= f; o.y *= f; o.z *= f; o.w *= f;
-            put4(static_cast<TQ*>(p.out) + (head0 + r) * p.c.D + d, o);
-            if (p.lse && d == 0) p.lse[head0 + r] = l == 0.f ? -INFINITY : base + logf(l);
-        } else {
-            *reinterpret_cast<float4*>(part + r * DP + d) = o;
-            if (d == 0) *reinterpret_cast<float2*>(part + kMaxPartRows * kMaxPartCols + 2 * r) = make_float2(m, l);
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+        const float base = top == -INFINITY ? 0.f : top, f = exp2_fast((m - base) * kLog2e);
+        m = top;
+        l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k0 + k >= count) continue;
+            const float w = exp2_fast((ml[k].x - base) * kLog2e);
+            l = fmaf(w, ml[k].y, l);
+            o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y);
+            o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
         }
     }
 }
+
+// Final values of four columns (of row `row` of out, all query heads of all sequences counted); no key left: zeros, -inf.
+template <typename TQ>
+__device__ __forceinline__ void emit4(const AttnProblem& p, long long row, int d, float vscale, float m, float l, float4 o) {
+    const float f = vscale / l;
+    put4(static_cast<TQ*>(p.out) + row * p.c.D + d,
+         l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + logf(l);
+}
+
+// What is joined in a CTA: the parts of warps first_warp .. first_warp + count - 1 of one (sequence, head).
+struct Chain {
+    int count;                  // 0: none
+    int from;                   // which of the first warp's two pieces
+    int rows, c0, c1, s0;       // c0 < c1: other CTAs have parts of it as well
+    float vscale;
+    long long row0;             // first row of out
+};
 
 template <typename TQ, typename TC, int DPB, int NT>
 __global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
@@ -187,8 +199,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[NW * S];
     __shared__ float2 ml_of[NW][2][ROWS];
-    __shared__ Piece piece[NW][2];
-    __shared__ int scan_warp[NW], last_flag;
+    // Results that are not final: of a (sequence, head) that a warp's part of the list begins in (0) or ends in (1).
+    __shared__ int piece_off[NW][2];                            // where O is in the ring
+    __shared__ Chain chains[NW + 1];                            // that begin with piece 1 of warp w; NW: with piece 0 of warp 0
+    __shared__ unsigned scan_warp[NW];
+    __shared__ int last_flag[2], out_chain;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
 
@@ -197,51 +212,69 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int g = lane >> 2, t4 = lane & 3;
 
     // ---- the list of tiles ----
-    if (tid < NW * S) {
-        mbar_init(smem_u32(&bars[tid]), 1);
+    if (lane < S) {
+        mbar_init(smem_u32(&bars[warp * S + lane]), 1);
         mbar_fence_init();
     }
-    if (tid < 2 * NW) piece[tid >> 1][tid & 1].off = -1;
-    if (tid == 0) prefix[0] = 0;
+    if (lane < 2) piece_off[warp][lane] = 0;
+    if (lane == 0) {
+        chains[warp].count = 0;
+        if (warp == 0) chains[NW].count = 0, out_chain = -1;
+    }
     auto slot_of = [&](int i) { return p.seqs ? p.seqs[i] : i; };
     auto length_of = [&](int slot) {
         return slot >= 0 && slot < p.c.slots ? max(0, min(p.c.lengths[slot], p.c.max_pages * ps)) : 0;
     };
-    bool fits = true;
-    int base = 0;
-    for (int i0 = 0; i0 < n; i0 += NTHR) {
-        const int i = i0 + tid;
-        int v = 0;
-        if (i < n) {
-            const int slot = slot_of(i);
-            v = (length_of(slot) + KT - 1) / KT;
-            if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
-        }
-        int x = v;
+    const int segs = p.c.heads * a.groups, limit = 2147483647 / segs;   // the list is numbered in 32 bits
+    bool fits;
+    int base;
+    auto tiles_of = [&](int i) {
+        const int slot = slot_of(i);
+        if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
+        return (length_of(slot) + KT - 1) / KT;
+    };
+    // at most 2^31 / 16 tiles in a sequence: no warp's sum overflows 32 bits
+    auto warp_scan = [&](unsigned x) {
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(~0u, x, d);
-            if (lane >= d) x = (int)min(2147483647ll, (long long)x + y);
+            const unsigned y = __shfl_up_sync(~0u, x, d);
+            if (lane >= d) x += y;
         }
-        if (lane == 31) scan_warp[warp] = x;
-        __syncthreads();
-        long long before = base, all = base;
+        return x;
+    };
+    if (n <= 32) {                                              // every warp for itself (the same values): no barrier
+        const unsigned x = warp_scan(lane < n ? tiles_of(lane) : 0u), all = __shfl_sync(~0u, x, 31);
+        fits = all <= (unsigned)limit;
+        base = (int)all;
+        if (lane == 0) prefix[0] = 0;
+        if (lane < n) prefix[lane + 1] = (int)x;
+        __syncwarp();
+    } else {
+        fits = true;
+        base = 0;
+        if (tid == 0) prefix[0] = 0;
+        for (int i0 = 0; i0 < n; i0 += NTHR) {
+            const int i = i0 + tid;
+            const unsigned x = warp_scan(i < n ? tiles_of(i) : 0u);
+            if (lane == 31) scan_warp[warp] = x;
+            __syncthreads();
+            long long before = base, all = base;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (w < warp) before += scan_warp[w];
-            all += scan_warp[w];
+            for (int w = 0; w < NW; ++w) {
+                if (w < warp) before += scan_warp[w];
+                all += scan_warp[w];
+            }
+            fits = fits && all <= limit;
+            base = fits ? (int)all : 0;
+            if (i < n) prefix[i + 1] = fits ? (int)(before + x) : 0;
+            __syncthreads();
         }
-        if (i < n) prefix[i + 1] = (int)min(2147483647ll, before + x);
-        fits = fits && all < 2147483647ll;
-        base = (int)min(2147483647ll, all);
-        __syncthreads();
     }
-    if (!fits) {                                                // 2^31 tiles: the list's numbers do not reach
+    if (!fits) {                                                // more than 2^31 tiles, a TB at least
         if (tid == 0) *p.status = LUVC_ERR_SHAPE;
         return;
     }
-    const int segs = p.c.heads * a.groups;
-    const long long total = (long long)base * segs;
+    const int total = base * segs;
 
     // sequences without tokens
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
@@ -253,37 +286,38 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     }
 
     // ---- this CTA's part of the list, this warp's part of that ----
-    struct Place { int seq, seg, tile, tiles; long long first; };   // a tile; its (sequence, head) starts at `first` in the list
-    auto place_of = [&](long long x) {
+    struct Place { int seq, seg, tile, tiles, first; };         // a tile; its (sequence, head) starts at `first` in the list
+    auto place_of = [&](int x) {
         int lo = 0, hi = n;                                     // prefix[lo] * segs <= x < prefix[hi] * segs
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((long long)prefix[mid] * segs <= x) lo = mid; else hi = mid;
+            if (prefix[mid] * segs <= x) lo = mid; else hi = mid;
         }
         Place q;
         q.seq = lo;
         q.tiles = prefix[lo + 1] - prefix[lo];
-        const long long in = x - (long long)prefix[lo] * segs;
-        q.seg = (int)(in / q.tiles);
-        q.tile = (int)(in - (long long)q.seg * q.tiles);
+        const int in = x - prefix[lo] * segs;
+        q.seg = in / q.tiles;
+        q.tile = in - q.seg * q.tiles;
         q.first = x - q.tile;
         return q;
     };
-    const long long per = max((total + gridDim.x - 1) / (long long)gridDim.x, (long long)NW * kMinTiles);
-    const int tol = (int)min(per / 4, 8ll);
-    auto bound_of = [&](long long c) {                          // start of CTA c's part, moved to a near (sequence, head) boundary
-        const long long x = c * per;
-        if (x <= 0) return 0ll;
-        if (x >= total) return total;
+    const int grid = gridDim.x, per = max(total / grid + (total % grid != 0), NW * kMinTiles), tol = min(per / 4, 8);
+    auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
+        if (c == 0) return 0;
+        if (c > (total - 1) / per) return total;                // c * per >= total
+        const int x = c * per;
         const Place q = place_of(x);
         if (q.tile <= tol) return q.first;
         if (q.tiles - q.tile <= tol) return q.first + q.tiles;
         return x;
     };
-    const long long cta_a = bound_of(blockIdx.x), cta_b = bound_of(blockIdx.x + 1ll);
+    const int bound = bound_of(blockIdx.x + (lane & 1));        // both in one go
+    const int cta_a = __shfl_sync(~0u, bound, 0), cta_b = __shfl_sync(~0u, bound, 1);
     if (cta_a >= cta_b) return;
-    const long long each = (cta_b - cta_a + NW - 1) / NW;
-    const long long wa = min(cta_a + warp * each, cta_b), wb = min(wa + each, cta_b);
+    const int each = (cta_b - cta_a) / NW, more = (cta_b - cta_a) % NW;     // the first `more` warps take one more
+    auto part_of_warp = [&](int w) { return cta_a + w * each + min(w, more); };
+    const int wa = part_of_warp(warp), wb = part_of_warp(warp + 1);
 
     unsigned char* const my_ring = ring + warp * S * Sh::STAGE;
     const uint32_t my_ring_s = smem_u32(my_ring), my_bar = smem_u32(&bars[warp * S]);
@@ -291,10 +325,17 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     if (wa < wb) {
         // what is to be loaded next
         Place ld = place_of(wa);
-        long long to_load = wb - wa;
+        int to_load = wb - wa;
         int ld_len = 0, ld_page = 0, ld_off = 0, pg_first = 0, pg = -1;
         const int32_t* ld_row = nullptr;
         auto load_start = [&](bool new_seq) {                   // at a new (sequence, head), or at the warp's first tile
+            {   // its queries are wanted soon
+                const int h = ld.seg / a.groups, r0 = (ld.seg - h * a.groups) * ROWS;
+                const char* const q0 = reinterpret_cast<const char*>(static_cast<const TQ*>(p.q) + ld.seq * p.q_stride +
+                                                                     ((long long)h * a.group + r0) * p.c.D);
+                const int bytes = min(ROWS, a.group - r0) * p.c.D * (int)sizeof(TQ);
+                for (int b = lane * 128; b < bytes; b += 32 * 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(q0 + b));
+            }
             if (new_seq) {
                 const int slot = slot_of(ld.seq);
                 ld_len = length_of(slot);
@@ -323,13 +364,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     }
                     const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
                     const int row = page >= 0 && page < p.c.pages ? (page * p.c.heads + h) * ps + ld_off : a.rows_total;
-                    if (lane == 0) {
-#pragma unroll
-                        for (int s = 0; s < Sh::SEGS; ++s) {
-                            tma_load_2d(dst + j * 2 * Sh::SUBK + s * 2048, &kmap, bar, s * (128 / Sh::ES), row);
-                            tma_load_2d(dst + j * 2 * Sh::SUBK + Sh::SUBK + s * 2048, &vmap, bar, s * (128 / Sh::ES), row);
-                        }
-                    }
+                    // one lane per box: 128 bytes of 16 rows of K (even lanes) or V
+                    if (lane < 2 * Sh::SEGS)
+                        tma_load_2d(dst + j * 2 * Sh::SUBK + (lane & 1) * Sh::SUBK + (lane >> 1) * 2048, lane & 1 ? &vmap : &kmap, bar,
+                                    (lane >> 1) * (128 / Sh::ES), row);
                     ld_off += 16;
                     if (ld_off == ps) { ld_off = 0; ++ld_page; }
                 }
@@ -355,12 +393,13 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             order |= (unsigned)filled << (4 * filled);
         }
 
-        long long left = wb - wa;
+        int left = wb - wa;
         bool dead = false;                                      // a wait gave up
         while (left > 0 && !dead) {
             const int h = at.seg / a.groups, r0 = (at.seg % a.groups) * ROWS;
             const int rows = min(ROWS, a.group - r0);
             const int len = length_of(slot_of(at.seq));
+            const float vscale = p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
             const float scale = p.scale * (p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
             // queries: B operand of S^T = K Q^T, head g of each group of 8
             const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
@@ -427,7 +466,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[mt][nt][c] = 0.f;
 
-            const int count = (int)min((long long)(at.tiles - at.tile), left);
+            const int count = min(at.tiles - at.tile, left);
             const bool whole = at.tile == 0 && count == at.tiles;
             int stage = 0;
             for (int k = 0; k < count; ++k, ++at.tile) {
@@ -460,6 +499,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
+                    float done[NT][4];                          // f32: finished sums of S
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) done[nt][c] = 0.f;
                     const int krow = (lane & 7) + (lane & 8);
 #pragma unroll
                     for (int k2 = 0; k2 < KS; ++k2) {           // 32 bytes of each of the 16 rows
@@ -477,7 +521,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                 split_tf32(q[nt][k2][1], qh[1], ql[1]);
                                 mma_tf32(s2[nt], lo, qh[0], qh[1]);
                                 mma_tf32(s2[nt], hi, ql[0], ql[1]);
-                                mma_tf32(s[nt], hi, qh[0], qh[1]);
+                                // tensor-core sums truncate: four steps at most in one, the rest rounded
+                                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_tf32(k2 % 4 ? s[nt] : part, hi, qh[0], qh[1]);
+                                if (k2 % 4 == 0)
+#pragma unroll
+                                    for (int c = 0; c < 4; ++c) { done[nt][c] += s[nt][c]; s[nt][c] = part[c]; }
                             }
                         } else if constexpr (!kF8) {
 #pragma unroll
@@ -501,7 +550,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const float x = fmaf(s[nt][c] + s2[nt][c], qmul[nt][c & 1], bias[j][c >> 1]);
+                            const float x = fmaf(done[nt][c] + s[nt][c] + s2[nt][c], qmul[nt][c & 1], bias[j][c >> 1]);
                             s[nt][c] = (c >> 1 ? gone1 : gone0) ? -INFINITY : x;
                         }
 #pragma unroll
@@ -591,9 +640,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                 }
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
-                                    mma_tf32(o[mt][nt], lo, bh[nt][0], bh[nt][1]);
-                                    mma_tf32(o[mt][nt], hi, bl[nt][0], bl[nt][1]);
-                                    mma_tf32(o[mt][nt], hi, bh[nt][0], bh[nt][1]);
+                                    float add[4] = {0.f, 0.f, 0.f, 0.f};    // a long sum is kept with rounded additions
+                                    mma_tf32(add, lo, bh[nt][0], bh[nt][1]);
+                                    mma_tf32(add, hi, bl[nt][0], bl[nt][1]);
+                                    mma_tf32(add, hi, bh[nt][0], bh[nt][1]);
+#pragma unroll
+                                    for (int c = 0; c < 4; ++c) o[mt][nt][c] += add[c];
                                 }
                             }
                         }
@@ -666,9 +718,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = o[mt][nt][c];
                     }
             __syncwarp();
+            const long long row0 = (long long)at.seq * p.q_heads + h * a.group + r0;
             if (whole) {
-                join<TQ, ROWS, DP>(a, at.seq, at.seg, 1, [&](int) { return os; }, [&](int, int r) { return ml_of[warp][1][r]; },
-                                   [&](int r, int d) { return o_index(r, d, DP); }, true, nullptr, lane, 32);
+                for (int e = lane; e < ROWS * (DP / 4); e += 32) {
+                    const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+                    if (r >= rows || d >= p.c.D) continue;
+                    const float2 ml = ml_of[warp][1][r];
+                    emit4<TQ>(p, row0 + r, d, vscale, ml.x, ml.y, *reinterpret_cast<const float4*>(os + o_index(r, d, DP)));
+                }
                 fence_proxy_async();                            // the stage was written by this warp; TMA writes it next
                 __syncwarp();
                 if (to_load > 0) {
@@ -677,9 +734,25 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     ++filled;
                 }
             } else if (lane == 0) {
-                piece[warp][which].seq = at.seq;
-                piece[warp][which].seg = at.seg;
-                piece[warp][which].off = (warp * S + stage) * Sh::STAGE;
+                piece_off[warp][which] = (warp * S + stage) * Sh::STAGE;
+                if (which == 1 || warp == 0) {                  // a chain begins here
+                    Chain& c = chains[which ? warp : NW];
+                    const int s0 = prefix[at.seq] * segs + at.seg * at.tiles, s1 = s0 + at.tiles;
+                    const int x = min(s1, cta_b) - 1 - cta_a, y = x - more * (each + 1);    // its last tile here, and whose that is
+                    const int last = y < 0 ? x / (each + 1) : more + y / each;
+                    c.count = last - warp + 1;
+                    c.from = which;
+                    c.rows = rows;
+                    c.vscale = vscale;
+                    c.row0 = row0;
+                    c.s0 = s0;
+                    c.c0 = c.c1 = 0;
+                    if (s0 < cta_a || s1 > cta_b) {
+                        c.c0 = (s0 + tol) / per;
+                        c.c1 = (s1 - tol - 1) / per;
+                        if (s0 >= cta_a) out_chain = warp;
+                    }
+                }
             }
             if (left > 0) {                                     // the next (sequence, head)
                 at.tile = 0;
@@ -701,42 +774,61 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     }
     __syncthreads();
 
-    // ---- joins: first the parts of this CTA's warps ----
-    int cross_seq[2], cross_seg[2], crosses = 0;                // parts of a (sequence, head) that other CTAs share
-    for (int w = 0; w < NW; ++w) {
-        for (int which = w == 0 ? 0 : 1; which < 2; ++which) {  // a part 0 of a later warp belongs to a chain that began before
-            if (piece[w][which].off < 0) continue;
-            const int seq = piece[w][which].seq, seg = piece[w][which].seg;
-            const int tiles = prefix[seq + 1] - prefix[seq];
-            const long long s0 = (long long)prefix[seq] * segs + (long long)seg * tiles, s1 = s0 + tiles;
-            int last = w;
-            while (last + 1 < NW && min(cta_a + (last + 1) * each, cta_b) < s1 && piece[last + 1][0].off >= 0) ++last;
-            const bool emit = s0 >= cta_a && s1 <= cta_b;
-            const int slot = s0 >= cta_a ? 1 : 0;
-            float* const part = a.parts + ((size_t)blockIdx.x * 2 + slot) * (kPartBytes / sizeof(float));
-            join<TQ, ROWS, DP>(
-                a, seq, seg, last - w + 1,
-                [&](int k) { return reinterpret_cast<const float*>(ring + piece[w + k][k ? 0 : which].off); },
-                [&](int k, int r) { return ml_of[w + k][k ? 0 : which][r]; }, [&](int r, int d) { return o_index(r, d, DP); }, emit, part,
-                tid, NTHR);
-            if (!emit && crosses < 2) { cross_seq[crosses] = seq; cross_seg[crosses] = seg; ++crosses; }
+    // ---- joins: the parts of this CTA's warps; then, of a (sequence, head) that other CTAs share, theirs, by the one that
+    //      arrives last ----
+    auto global_part = [&](int cta, int slot) {
+        float* const o = a.parts + ((size_t)cta * 2 + slot) * (kPartBytes / sizeof(float));
+        return Part{o, reinterpret_cast<const float2*>(o + kMaxPartRows * kMaxPartCols)};
+    };
+    unsigned some = 0;
+#pragma unroll
+    for (int c = 0; c <= NW; ++c) some |= (chains[c].count ? 1u : 0u) << c;
+#pragma unroll 1
+    for (; some; some &= some - 1) {
+        const int c = __ffs(some) - 1;
+        const Chain& ch = chains[c];
+        const int count = ch.count, w0 = c == NW ? 0 : c;
+        for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
+            const int r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
+            if (r >= ch.rows || d >= p.c.D) continue;
+            float m, l;
+            float4 o;
+            join4(count, [&](int k) {
+                const int from = k ? 0 : ch.from;
+                return Part{reinterpret_cast<const float*>(ring + piece_off[w0 + k][from]), ml_of[w0 + k][from]};
+            }, r, at, m, l, o);
+            if (ch.c0 == ch.c1) {
+                emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o);
+            } else {
+                const Part q = global_part(blockIdx.x, ch.s0 >= cta_a);
+                *reinterpret_cast<float4*>(const_cast<float*>(q.o) + at) = o;
+                if (d == 0) const_cast<float2*>(q.ml)[r] = make_float2(m, l);
+            }
         }
     }
-    // ---- then those of several CTAs, by the one that arrives last ----
-    for (int x = 0; x < crosses; ++x) {
-        const int seq = cross_seq[x], seg = cross_seg[x], tiles = prefix[seq + 1] - prefix[seq];
-        const long long s0 = (long long)prefix[seq] * segs + (long long)seg * tiles, s1 = s0 + tiles;
-        const int c0 = (int)((s0 + tol) / per), c1 = (int)((s1 - tol - 1) / per);
+    const bool in = chains[NW].count && chains[NW].c0 != chains[NW].c1;   // shared with the CTA before / with the next one only
+    if (!in && out_chain < 0) return;
+    __threadfence();
+    __syncthreads();
+    if (tid < 64 && lane == 0) {
+        const int c = warp == 0 ? (in ? NW : -1) : out_chain;
+        const unsigned wrap = c < 0 ? 0u : (unsigned)(chains[c].c1 - chains[c].c0);
+        last_flag[warp] = c >= 0 && atomicInc(&a.counters[chains[c].c0], wrap) == wrap;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int x = 0; x < 2; ++x) {
+        if (!last_flag[x]) continue;
         __threadfence();
-        __syncthreads();
-        if (tid == 0) last_flag = atomicInc(&a.counters[c0], (unsigned)(c1 - c0)) == (unsigned)(c1 - c0);
-        __syncthreads();
-        if (!last_flag) continue;
-        __threadfence();
-        auto part_of = [&](int k) { return a.parts + ((size_t)(c0 + k) * 2 + (k ? 0 : 1)) * (kPartBytes / sizeof(float)); };
-        join<TQ, ROWS, DP>(a, seq, seg, c1 - c0 + 1, part_of,
-                           [&](int k, int r) { return *reinterpret_cast<const float2*>(part_of(k) + kMaxPartRows * kMaxPartCols + 2 * r); },
-                           [&](int r, int d) { return r * DP + d; }, true, nullptr, tid, NTHR);
+        const Chain& ch = chains[x == 0 ? NW : out_chain];
+        for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
+            const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+            if (r >= ch.rows || d >= p.c.D) continue;
+            float m, l;
+            float4 o;
+            join4(ch.c1 - ch.c0 + 1, [&](int k) { return global_part(ch.c0 + k, k == 0); }, r, o_index(r, d, DP), m, l, o);
+            emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o);
+        }
     }
 }
 
