@@ -48,6 +48,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
 constexpr int kMaxPartRows = 16, kMaxPartCols = 256;
 constexpr size_t kPartBytes = (size_t)kMaxPartRows * (kMaxPartCols + 2) * sizeof(float);
+constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
 constexpr int kMinTiles = 2;                    // tiles a warp takes at least: fewer CTAs, not smaller parts, for little work
 constexpr int kWaitProbes = 1 << 22;            // probes before a wait for a copy gives up (seconds)
 
@@ -106,11 +107,11 @@ template <typename TC, int DPB_, int NT_>
 struct Shape {
     static constexpr int DPB = DPB_, NT = NT_, ES = sizeof(TC), DP = DPB / ES, SEGS = DPB / 128;
     static constexpr int SUBK = 16 * DPB;                       // bytes of 16 rows
-    // 16-token parts of a tile.  A stage of 8 KB or more; it also has room for a partial result (8 NT rows of DP floats).
-    static constexpr int SUB = (2 * SUBK < 8192 || NT > ES) ? 2 : 1;
+    // 16-token parts of a tile: one, or as many as make a stage large enough for a partial result (8 NT rows of DP floats).
+    static constexpr int SUB = NT > ES ? 2 : 1;
     static constexpr int KT = 16 * SUB, STAGE = SUB * 2 * SUBK;
-    // warps and stages: up to 196,608 bytes of ring, three stages or more each
-    static constexpr int NW = STAGE <= 8192 ? 8 : STAGE <= 16384 ? 4 : 2, S = 3;
+    // three stages for each warp, 196,608 bytes in all: the more warps the smaller a row is
+    static constexpr int S = 3, NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = 8 * NT;
     static_assert(ROWS * DP * 4 <= STAGE, "a partial result must fit a stage");
@@ -120,6 +121,7 @@ struct Shape {
 struct Args {
     AttnProblem p;
     int group, groups;          // query heads per key head; head groups of ROWS
+    int page_shift;             // log2 of the page size, -1 if it is no power of two
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
     unsigned* counters;         // [kMaxCtas]
     float* parts;               // [kMaxCtas][2] of kPartBytes
@@ -296,16 +298,19 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         Place q;
         q.seq = lo;
         q.tiles = prefix[lo + 1] - prefix[lo];
+        // quotient below segs <= 2^16: the float one is off by less than one
         const int in = x - prefix[lo] * segs;
-        q.seg = in / q.tiles;
+        q.seg = (int)__fdividef((float)in, (float)q.tiles);
         q.tile = in - q.seg * q.tiles;
+        if (q.tile < 0) { --q.seg; q.tile += q.tiles; }
+        if (q.tile >= q.tiles) { ++q.seg; q.tile -= q.tiles; }
         q.first = x - q.tile;
         return q;
     };
-    const int grid = gridDim.x, per = max(total / grid + (total % grid != 0), NW * kMinTiles), tol = min(per / 4, 8);
+    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW * kMinTiles), tol = min(per / 4, 8);
     auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
         if (c == 0) return 0;
-        if (c > (total - 1) / per) return total;                // c * per >= total
+        if ((long long)c * per >= total) return total;
         const int x = c * per;
         const Place q = place_of(x);
         if (q.tile <= tol) return q.first;
@@ -315,7 +320,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int bound = bound_of(blockIdx.x + (lane & 1));        // both in one go
     const int cta_a = __shfl_sync(~0u, bound, 0), cta_b = __shfl_sync(~0u, bound, 1);
     if (cta_a >= cta_b) return;
-    const int each = (cta_b - cta_a) / NW, more = (cta_b - cta_a) % NW;     // the first `more` warps take one more
+    const int each = (unsigned)(cta_b - cta_a) / NW, more = (unsigned)(cta_b - cta_a) % NW;     // the first `more` warps take one more
     auto part_of_warp = [&](int w) { return cta_a + w * each + min(w, more); };
     const int wa = part_of_warp(warp), wb = part_of_warp(warp + 1);
 
@@ -326,52 +331,51 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         // what is to be loaded next
         Place ld = place_of(wa);
         int to_load = wb - wa;
-        int ld_len = 0, ld_page = 0, ld_off = 0, pg_first = 0, pg = -1;
+        int ld_left = 0, ld_page = 0, ld_off = 0, ld_len = 0, ld_h = 0, pg_first = 0, pg = -1;
         const int32_t* ld_row = nullptr;
+        auto fetch_pages = [&] {
+            pg_first = ld_page;
+            pg = ld_page + lane < p.c.max_pages ? ld_row[ld_page + lane] : -1;
+        };
         auto load_start = [&](bool new_seq) {                   // at a new (sequence, head), or at the warp's first tile
-            {   // its queries are wanted soon
-                const int h = ld.seg / a.groups, r0 = (ld.seg - h * a.groups) * ROWS;
-                const char* const q0 = reinterpret_cast<const char*>(static_cast<const TQ*>(p.q) + ld.seq * p.q_stride +
-                                                                     ((long long)h * a.group + r0) * p.c.D);
-                const int bytes = min(ROWS, a.group - r0) * p.c.D * (int)sizeof(TQ);
-                for (int b = lane * 128; b < bytes; b += 32 * 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(q0 + b));
-            }
             if (new_seq) {
                 const int slot = slot_of(ld.seq);
                 ld_len = length_of(slot);
                 ld_row = p.c.table + (long long)slot * p.c.max_pages;
             }
             const int token = ld.tile * KT;
-            ld_page = token / ps;
+            ld_left = ld_len - token;
+            ld_page = a.page_shift >= 0 ? token >> a.page_shift : token / ps;
             ld_off = token - ld_page * ps;
-            if (new_seq || ld_page < pg_first || ld_page >= pg_first + 32) {
-                pg_first = ld_page;
-                pg = ld_page + lane < p.c.max_pages ? ld_row[ld_page + lane] : -1;
-            }
+            if (new_seq || ld_page < pg_first || ld_page >= pg_first + 32) fetch_pages();
+            ld_h = a.groups == 1 ? ld.seg : ld.seg / a.groups;
+            // its queries are wanted soon
+            const int r0 = (ld.seg - ld_h * a.groups) * ROWS;
+            const char* const q0 = reinterpret_cast<const char*>(static_cast<const TQ*>(p.q) + ld.seq * p.q_stride +
+                                                                 ((long long)ld_h * a.group + r0) * p.c.D);
+            const int bytes = min(ROWS, a.group - r0) * p.c.D * (int)sizeof(TQ);
+            for (int b = lane * 128; b < bytes; b += 32 * 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(q0 + b));
         };
+        const bool is_v = lane & 1;                             // one lane per box: 128 bytes of 16 rows of K (even lanes) or V
+        const CUtensorMap* const my_map = is_v ? &vmap : &kmap;
+        const uint32_t my_dst = my_ring_s + (is_v ? Sh::SUBK : 0) + (lane >> 1) * 2048;
         auto load = [&](int stage) {
-            const uint32_t bar = my_bar + 8 * stage, dst = my_ring_s + stage * Sh::STAGE;
-            const int h = ld.seg / a.groups;
-            const int left = ld_len - ld.tile * KT;
-            if (lane == 0) mbar_arrive_expect_tx(bar, min(Sh::SUB, (left + 15) / 16) * 2 * Sh::SUBK);
+            const uint32_t bar = my_bar + 8 * stage;
+            if (lane == 0) mbar_arrive_expect_tx(bar, Sh::SUB == 1 || ld_left > 16 ? Sh::STAGE : 2 * Sh::SUBK);
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < Sh::SUB; ++j) {
-                if (16 * j < left) {
-                    if (ld_page >= pg_first + 32) {
-                        pg_first = ld_page;
-                        pg = ld_page + lane < p.c.max_pages ? ld_row[ld_page + lane] : -1;
-                    }
+                if (j == 0 || 16 * j < ld_left) {
+                    if (ld_page >= pg_first + 32) fetch_pages();
                     const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
-                    const int row = page >= 0 && page < p.c.pages ? (page * p.c.heads + h) * ps + ld_off : a.rows_total;
-                    // one lane per box: 128 bytes of 16 rows of K (even lanes) or V
+                    const int row = (unsigned)page < (unsigned)p.c.pages ? (page * p.c.heads + ld_h) * ps + ld_off : a.rows_total;
                     if (lane < 2 * Sh::SEGS)
-                        tma_load_2d(dst + j * 2 * Sh::SUBK + (lane & 1) * Sh::SUBK + (lane >> 1) * 2048, lane & 1 ? &vmap : &kmap, bar,
-                                    (lane >> 1) * (128 / Sh::ES), row);
+                        tma_load_2d(my_dst + stage * Sh::STAGE + j * 2 * Sh::SUBK, my_map, bar, (lane >> 1) * (128 / Sh::ES), row);
                     ld_off += 16;
                     if (ld_off == ps) { ld_off = 0; ++ld_page; }
                 }
             }
+            ld_left -= KT;
             if (--to_load > 0 && ++ld.tile == ld.tiles) {       // the next (sequence, head)
                 ld.tile = 0;
                 bool new_seq = false;
@@ -393,10 +397,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             order |= (unsigned)filled << (4 * filled);
         }
 
+        // A lane's row address for ldmatrix: chunk c of row r of a box lies at r * 128 + 16 * (c ^ (r & 7)).  Matrices 0 .. 3 of
+        // K are (rows 0-7, c), (rows 8-15, c), (rows 0-7, c + 1), (rows 8-15, c + 1); of a 16-bit V the middle two change places.
+        // The next two chunks are at the address with 32 flipped in.
+        const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
+        const uint32_t k_lane = k_row * 128 + (((lane >> 4) ^ (k_row & 7)) << 4), v_lane = v_row * 128 + ((((lane >> 3) & 1) ^ (v_row & 7)) << 4);
         int left = wb - wa;
         bool dead = false;                                      // a wait gave up
         while (left > 0 && !dead) {
-            const int h = at.seg / a.groups, r0 = (at.seg % a.groups) * ROWS;
+            const int h = a.groups == 1 ? at.seg : at.seg / a.groups, r0 = (at.seg - h * a.groups) * ROWS;
             const int rows = min(ROWS, a.group - r0);
             const int len = length_of(slot_of(at.seq));
             const float vscale = p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
@@ -473,15 +482,22 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 stage = order & 15;
                 order >>= 4;
                 --filled;
+                // a tile with biases, or past the end (which is a bias of -inf)
+                const bool masked = p.bias_width > 0 || (at.tile + 1) * KT > len;
                 float bias[Sh::SUB][2];
 #pragma unroll
                 for (int j = 0; j < Sh::SUB; ++j)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int token = at.tile * KT + 16 * j + 8 * x + g;
-                        bias[j][x] = token < min(p.bias_width, len) ? p.bias[at.seq * p.bias_stride + token] : 0.f;
-                        if (token >= len) bias[j][x] = -INFINITY;
-                    }
+                    for (int x = 0; x < 2; ++x) bias[j][x] = 0.f;
+                if (masked)
+#pragma unroll
+                    for (int j = 0; j < Sh::SUB; ++j)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int token = at.tile * KT + 16 * j + 8 * x + g;
+                            if (token >= len) bias[j][x] = -INFINITY;
+                            else if (token < p.bias_width) bias[j][x] = p.bias[at.seq * p.bias_stride + token];
+                        }
                 {
                     const uint32_t bar = my_bar + 8 * stage;
                     int probes = 0;
@@ -491,7 +507,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 }
 #pragma unroll
                 for (int j = 0; j < Sh::SUB; ++j) {
-                    if (at.tile * KT + 16 * j >= len) break;
+                    if (j > 0 && at.tile * KT + 16 * j >= len) break;
                     const uint32_t ks = my_ring_s + stage * Sh::STAGE + j * 2 * Sh::SUBK, vs = ks + Sh::SUBK;
                     // ---- S^T: rows are the 16 tokens, columns the query heads ----
                     float s[NT][4], s2[NT][4];
@@ -504,12 +520,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) done[nt][c] = 0.f;
-                    const int krow = (lane & 7) + (lane & 8);
 #pragma unroll
                     for (int k2 = 0; k2 < KS; ++k2) {           // 32 bytes of each of the 16 rows
-                        const int chunk = 2 * k2 + (lane >> 4);
                         uint32_t r[4];
-                        ldsm4(ks + (chunk >> 3) * 2048 + krow * 128 + (((chunk & 7) ^ (krow & 7)) << 4), r);
+                        ldsm4(((ks + k_lane) ^ (32 * (k2 & 3))) + (k2 >> 2) * 2048, r);
                         if constexpr (kF32) {
                             uint32_t hi[4], lo[4];
 #pragma unroll
@@ -542,42 +556,54 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         }
                     }
                     // ---- weights ----
-                    const bool gone0 = bias[j][0] == -INFINITY, gone1 = bias[j][1] == -INFINITY;
-                    const unsigned gone = __ballot_sync(~0u, gone0) | __ballot_sync(~0u, gone1);
-                    bool grew = false;
-                    float f[NT][2];
+                    // Their reference m follows the maximum only when a score passes it by kSlack: weights stay below
+                    // e^kSlack, sums lose nothing, and most tiles need no maximum across the warp.
+                    bool over = false;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const float x = fmaf(done[nt][c] + s[nt][c] + s2[nt][c], qmul[nt][c & 1], bias[j][c >> 1]);
-                            s[nt][c] = (c >> 1 ? gone1 : gone0) ? -INFINITY : x;
+                            const float x = kF32 ? done[nt][c] + s[nt][c] + s2[nt][c] : s[nt][c] + s2[nt][c];
+                            s[nt][c] = fmaf(x, qmul[nt][c & 1], bias[j][c >> 1]);
                         }
+                    unsigned gone = 0;
+                    if (masked) {                               // whatever a masked row holds
+                        const bool gone0 = bias[j][0] == -INFINITY, gone1 = bias[j][1] == -INFINITY;
+                        gone = __ballot_sync(~0u, gone0 || gone1);
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            float x = fmaxf(s[nt][b], s[nt][b + 2]);
-                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-                            x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                            x = fmaxf(x, m[nt][b]);
-                            const float mb = x == -INFINITY ? 0.f : x;
-                            f[nt][b] = exp2_fast((m[nt][b] - mb) * kLog2e);
-                            grew = grew || x > m[nt][b];
-                            m[nt][b] = x;
-                            s[nt][b] = exp2_fast((s[nt][b] - mb) * kLog2e);
-                            s[nt][b + 2] = exp2_fast((s[nt][b + 2] - mb) * kLog2e);
-                        }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                if (c >> 1 ? gone1 : gone0) s[nt][c] = -INFINITY;
                     }
-                    if (__any_sync(~0u, grew)) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            l[nt][0] *= f[nt][0]; l[nt][1] *= f[nt][1];
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
+                        for (int c = 0; c < 4; ++c) over = over || s[nt][c] > m[nt][c & 1] + kSlack;
+                    if (__any_sync(~0u, over)) {
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) o[mt][nt][c] *= f[nt][c & 1];
-                        }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                float x = fmaxf(s[nt][b], s[nt][b + 2]);
+                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                                x = fmaxf(x, m[nt][b]);
+                                const float f = exp2_fast((m[nt][b] - (x == -INFINITY ? 0.f : x)) * kLog2e);
+                                m[nt][b] = x;
+                                l[nt][b] *= f;
+#pragma unroll
+                                for (int mt = 0; mt < MT; ++mt) { o[mt][nt][b] *= f; o[mt][nt][b + 2] *= f; }
+                            }
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float mb = m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1];
+                            s[nt][c] = exp2_fast((s[nt][c] - mb) * kLog2e);
+                        }
                     uint32_t ph[NT][2], pl[NT][2];              // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
                     float pf[NT][4];
 #pragma unroll
@@ -606,10 +632,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         }
                     }
                     // ---- O^T += V^T P^T; rows of V that are masked may hold anything and are replaced by zeros ----
-                    // gone: bit 4 i (+ any lane of the quad) for token i or i + 8; a lane needs tokens 2 t4, 2 t4 + 1, + 8
                     uint32_t keep0 = ~0u, keep1 = ~0u;          // 16-bit halves of a register: tokens 2 t4, 2 t4 + 1 (+ 8)
-                    if (gone) {
-                        const unsigned g0 = __ballot_sync(~0u, gone0), g1 = __ballot_sync(~0u, gone1);
+                    if (gone) {                                 // token g (+ 8) is that of lanes 4 g ..
+                        const unsigned g0 = __ballot_sync(~0u, bias[j][0] == -INFINITY), g1 = __ballot_sync(~0u, bias[j][1] == -INFINITY);
                         keep0 = ((g0 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g0 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
                         keep1 = ((g1 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g1 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
                     }
@@ -650,12 +675,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             }
                         }
                     } else if constexpr (!kF8) {
-                        const int vrow = (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
-                            const int chunk = 2 * mt + ((lane >> 3) & 1);
                             uint32_t r[4];
-                            ldsm4_trans(vs + (chunk >> 3) * 2048 + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4), r);
+                            ldsm4_trans(((vs + v_lane) ^ (32 * (mt & 3))) + (mt >> 2) * 2048, r);
                             if (gone) { r[0] &= keep0; r[1] &= keep0; r[2] &= keep1; r[3] &= keep1; }
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
@@ -665,12 +688,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         }
                     } else {
                         // a transposed 8 x 8 matrix of byte pairs: tokens 2 t4 and 2 t4 + 1 of columns 2 g and 2 g + 1
-                        const int vrow = (lane & 7) + (lane & 8);
 #pragma unroll
                         for (int m2 = 0; m2 < MT / 2; ++m2) {   // two 16-byte pieces
-                            const int chunk = 2 * m2 + (lane >> 4);
                             uint32_t r[4];
-                            ldsm4_trans(vs + (chunk >> 3) * 2048 + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4), r);
+                            ldsm4_trans(((vs + k_lane) ^ (32 * (m2 & 3))) + (m2 >> 2) * 2048, r);
                             if (gone) { r[0] &= keep0; r[2] &= keep0; r[1] &= keep1; r[3] &= keep1; }
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
@@ -884,6 +905,7 @@ int launch(const AttnProblem& p) {
     a.p = p;
     a.group = p.q_heads / p.c.heads;
     a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
+    a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
     a.counters = static_cast<unsigned*>(p.workspace);
     a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kMaxCtas * sizeof(unsigned));
