@@ -432,10 +432,11 @@ class KvCache:
         self.lengths = meta[:slots]
         self.refs = meta[slots:slots + pages]
         self.table = meta[slots + pages:].view(slots, max_pages)
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.index, self.dtype = k.device, k.get_device(), k.dtype
         self.layers, self.pages, self.heads, self.page_size, self.head_dim = layers, pages, heads, page_size, D
         self.slots, self.max_pages = slots, max_pages
-        self.io_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16    # of queries, new rows, outputs
+        # of queries, new rows and outputs
+        self.io_dtype, self.io_code = (torch.float32, F32) if k.dtype == torch.float32 else (torch.bfloat16, BF16)
         self.struct = KvCacheStruct(
             k.data_ptr(), v.data_ptr(), self.lengths.data_ptr(), self.refs.data_ptr(), self.table.data_ptr(),
             k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None,
@@ -445,22 +446,41 @@ class KvCache:
 _CACHE_DTYPES = {torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: E4M3}
 
 
-def _ints(t: torch.Tensor | None, cache: KvCache, shape, name: str):
-    """Address of a contiguous int32 tensor of the given shape on the cache's device (None: NULL)."""
+# A decode step makes many small calls, so what these bindings do per call is kept short: the stream's handle without a
+# torch.cuda.Stream object, no device context where the cache's device is current already, one comparison per rule.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_INT32 = torch.int32
+
+
+def _ints(t: torch.Tensor | None, cache: KvCache, count: int, name: str):
+    """Address of a contiguous int32 tensor [count] on the cache's device (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or t.device != cache.device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of shape %s on %s" % (name, tuple(shape), cache.device))
+    if t.dtype is not _INT32 or t.dim() != 1 or t.numel() != count or not t.is_cuda or t.get_device() != cache.index \
+            or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of %d entries on %s" % (name, count, cache.device))
     return t.data_ptr()
 
 
 def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
-    o = KvOpts(stream=_stream_ptr(cache.device))
+    o = KvOpts(_raw_stream(cache.index))
     if workspace is not None:
         o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if device_status is not None:
         o.device_status = device_status.data_ptr()
     return o
+
+
+def _kv_call(where: str, cache: KvCache, *args) -> None:
+    """lib.<where>(*args) with the cache's device current."""
+    fn = getattr(lib, where)
+    if torch.cuda.current_device() == cache.index:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(cache.index):
+            status = fn(*args)
+    if status != 0:
+        raise LuvcError(status, where)
 
 
 def kv_workspace_bytes(cache: KvCache, n: int) -> int:
@@ -475,21 +495,21 @@ def kv_reserve(cache: KvCache, counts: torch.Tensor, *, seqs: torch.Tensor | Non
                device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_reserve: room for counts[i] further tokens of each sequence (int32 [n]); seqs: slots (None: 0 .. n-1)."""
     n = counts.numel()
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_kv_reserve(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _ints(counts, cache, (n,), "counts"),
-                                   _kv_opts(cache, None, device_status)), "luvc_kv_reserve")
+    _kv_call("luvc_kv_reserve", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(counts, cache, n, "counts"),
+             _kv_opts(cache, None, device_status))
 
 
 def _token_stride(t: torch.Tensor, cache: KvCache, heads: int, name: str) -> int:
     """Elements from one token to the next of a [tokens, heads, D] tensor whose tokens are contiguous."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.head_dim or t.device != cache.device:
-        raise ValueError("%s must be [tokens, %d, %d] on %s" % (name, heads, cache.head_dim, cache.device))
-    if t.dtype != cache.io_dtype:
+    D = cache.head_dim
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or not t.is_cuda or t.get_device() != cache.index:
+        raise ValueError("%s must be [tokens, %d, %d] on %s" % (name, heads, D, cache.device))
+    if t.dtype is not cache.io_dtype:
         raise TypeError("%s must be %s for a %s cache, got %s" % (name, cache.io_dtype, cache.dtype, t.dtype))
     s0, s1, s2 = t.stride()
-    if s2 != 1 or (heads > 1 and s1 != cache.head_dim):
+    if s2 != 1 or (s1 != D and heads > 1):
         raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
-    return s0 if t.shape[0] > 1 else max(s0, heads * cache.head_dim)
+    return s0 if t.shape[0] > 1 else max(s0, heads * D)
 
 
 def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0, starts: torch.Tensor | None = None,
@@ -500,31 +520,26 @@ def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0
     [tokens], the values are written as v + log(size) (Eq. 2).  k and v may be parts of a wider tensor."""
     tokens = k.shape[0]
     n = tokens if starts is None else starts.numel() - 1
-    if v.shape != k.shape:
+    ks, vs = _token_stride(k, cache, cache.heads, "k"), _token_stride(v, cache, cache.heads, "v")
+    if v.shape[0] != tokens:
         raise ValueError("k and v must have one shape")
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_kv_write(cache.struct, layer, _ints(seqs, cache, (n,), "seqs"), n, k.data_ptr(), v.data_ptr(),
-                                 _token_stride(k, cache, cache.heads, "k"), _token_stride(v, cache, cache.heads, "v"), tokens,
-                                 _ints(starts, cache, (n + 1,), "starts"), _ints(sizes, cache, (tokens,), "sizes"),
-                                 F32 if k.dtype == torch.float32 else BF16, _kv_opts(cache, None, device_status)),
-               "luvc_kv_write")
+    _kv_call("luvc_kv_write", cache, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, k.data_ptr(), v.data_ptr(), ks, vs,
+             tokens, _ints(starts, cache, n + 1, "starts"), _ints(sizes, cache, tokens, "sizes"), cache.io_code,
+             _kv_opts(cache, None, device_status))
 
 
 def kv_fork(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, *, workspace: torch.Tensor | None = None,
             device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_fork: the empty slots dst (int32 [n]) become copies of the sequences src (int32 [n]); full pages are shared."""
     n = dst.numel()
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_kv_fork(cache.struct, _ints(src, cache, (n,), "src"), _ints(dst, cache, (n,), "dst"), n,
-                                _kv_opts(cache, workspace, device_status)), "luvc_kv_fork")
+    _kv_call("luvc_kv_fork", cache, cache.struct, _ints(src, cache, n, "src"), _ints(dst, cache, n, "dst"), n,
+             _kv_opts(cache, workspace, device_status))
 
 
 def kv_free(cache: KvCache, seqs: torch.Tensor, *, device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_free: empties the slots seqs (int32 [n]); pages nobody holds any more are free again."""
     n = seqs.numel()
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_kv_free(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _kv_opts(cache, None, device_status)),
-               "luvc_kv_free")
+    _kv_call("luvc_kv_free", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _kv_opts(cache, None, device_status))
 
 
 def kv_compact(cache: KvCache, first: torch.Tensor, span: torch.Tensor, idx: torch.Tensor, *,
@@ -533,11 +548,9 @@ def kv_compact(cache: KvCache, first: torch.Tensor, span: torch.Tensor, idx: tor
     """luvc_kv_compact: of the block of span[i] tokens from first[i] on, sequence i keeps the tokens idx[i] (int32
     [n, keep], relative to the block, ascending: the out_idx of spu_prune) and everything outside the block."""
     n, keep = idx.shape
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_kv_compact(cache.struct, _ints(seqs, cache, (n,), "seqs"), n, _ints(first, cache, (n,), "first"),
-                                   _ints(span, cache, (n,), "span"), _ints(idx, cache, (n, keep), "idx") if keep else None, keep,
-                                   _ints(counts, cache, (n,), "counts"), _kv_opts(cache, workspace, device_status)),
-               "luvc_kv_compact")
+    _kv_call("luvc_kv_compact", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(first, cache, n, "first"),
+             _ints(span, cache, n, "span"), _ints(idx.view(-1), cache, n * keep, "idx") if keep else None, keep,
+             _ints(counts, cache, n, "counts"), _kv_opts(cache, workspace, device_status))
 
 
 def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.Tensor | None = None, scale: float = 0.0,
@@ -549,24 +562,26 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     n, q_heads = q.shape[0], q.shape[1]
     stride = _token_stride(q, cache, q_heads, "q")
     if out is None:
-        out = torch.empty((n, q_heads, cache.head_dim), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or out.device != q.device:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_contiguous() or out.device != q.device:
         raise ValueError("out must be a contiguous tensor of q's shape and type")
-    lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device) if want_lse else None
-    o = AttnOpts(stream=_stream_ptr(cache.device), scale=scale)
+    o = AttnOpts(_raw_stream(cache.index))
+    if scale:
+        o.scale = scale
     if workspace is not None:
         o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if device_status is not None:
         o.device_status = device_status.data_ptr()
     if key_bias is not None:
-        if key_bias.dtype != torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n or key_bias.device != cache.device \
-                or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):
+        if key_bias.dtype is not torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n or not key_bias.is_cuda \
+                or key_bias.get_device() != cache.index or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):
             raise ValueError("key_bias must be a float32 [n, width] tensor on the cache's device, its rows contiguous")
         o.key_bias, o.bias_width = key_bias.data_ptr(), key_bias.shape[1]
         o.bias_stride = key_bias.stride(0) if n > 1 else max(key_bias.stride(0), key_bias.shape[1])
-    if lse is not None:
+    lse = None
+    if want_lse:
+        lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
         o.lse = lse.data_ptr()
-    with torch.cuda.device(cache.device):
-        _check(lib.luvc_attn_decode(q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, (n,), "seqs"), n, q_heads,
-                                    F32 if q.dtype == torch.float32 else BF16, out.data_ptr(), o), "luvc_attn_decode")
+    _kv_call("luvc_attn_decode", cache, q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, q_heads,
+             cache.io_code, out.data_ptr(), o)
     return (out, lse) if want_lse else out
