@@ -223,6 +223,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         chains[warp].count = 0;
         if (warp == 0) chains[NW].count = 0, out_chain = -1;
     }
+    if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &vmap : &kmap) : "memory");
+    pdl_trigger();
+    pdl_wait();
     auto slot_of = [&](int i) { return p.seqs ? p.seqs[i] : i; };
     auto length_of = [&](int slot) {
         return slot >= 0 && slot < p.c.slots ? max(0, min(p.c.lengths[slot], p.c.max_pages * ps)) : 0;
@@ -924,9 +927,7 @@ int launch(const AttnProblem& p) {
     }
     const int sms = sm_count();
     if (!sms) return LUVC_ERR_CUDA;
-    attn_decode_kernel<TQ, TC, DPB, NT><<<sms, 32 * Sh::NW, smem, p.stream>>>(kmap, vmap, a);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    return launch_overlapped(attn_decode_kernel<TQ, TC, DPB, NT>, sms, 32 * Sh::NW, smem, p.stream, kmap, vmap, a);
 }
 
 template <typename TQ, typename TC, int DPB>

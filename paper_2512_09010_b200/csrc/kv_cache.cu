@@ -4,10 +4,12 @@
 // sequences that hold a page, 0 is free, and a call takes the free pages with the lowest numbers, in the order
 // of its sequences; so the books after a call follow from those before it, whatever the timing.  A call that
 // takes pages first runs one CTA over the books (kv_plan_kernel): it works out what each sequence needs, finds
-// the free pages by an ordered scan of refs, and either commits everything or leaves the books as they were and
-// reports in the status word.  Rows are then copied by a second, wide kernel (kv_move_kernel).  Nothing is ever
-// copied in place: a compacted sequence gets new pages, so no row is overwritten while it is still to be read,
-// every row can move at the same time, and a page that other sequences share is never written.
+// the free pages by an ordered scan of refs, and either commits or leaves the books as they were and reports in
+// the status word.  What is left then is wide and has no order (kv_move_kernel): rows to copy, pages to share
+// or to give back.  Nothing is ever copied in place: a compacted sequence gets new pages, so no row is
+// overwritten while it is still to be read, every row can move at the same time, and a page that other sequences share is
+// never written.  The kernels are launched with overlap (programmatic dependent launch): the books are so little
+// work that the gaps between launches would be as long as the kernels.
 //
 // Layout.  A page holds, per layer and head, page_size consecutive rows of D elements ([layer][page][head][slot][D]):
 // the attention kernel reads a head's part of a page as one contiguous piece.
@@ -16,33 +18,39 @@
 #include <cuda_fp8.h>
 
 #include "luvc_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace luvc {
 namespace {
 
+using namespace ptx;
+
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
-constexpr int kPerThread = 16;                              // pages a thread looks at per sweep over refs
-constexpr int kSweep = kPlanThreads * kPerThread;
-constexpr int kCounts = kPerThread * kPlanWarps;            // one count of free pages per ballot
+constexpr int kPerLane = 8;                                 // pages a lane looks at per sweep over refs
+constexpr int kWarpPages = 32 * kPerLane, kSweep = kPlanWarps * kWarpPages;
 constexpr int kClaimed = -1;                                // lengths[] of a slot that the running call has claimed
 
 __device__ __forceinline__ bool stopped(const int* status) { return *reinterpret_cast<const volatile int*>(status) != 0; }
 
-__device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((long long)a + b - 1) / b); }
+__device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 // The plan's result for kv_move_kernel, in the call's workspace.
 struct MoveList {
-    int* total;      // pages to fill
-    int2* items;     // [total] (sequence of the call, page index within it)
-    int* old;        // [n, max_pages] compact: the sequences' pages before the call
+    int* head;       // [0]: pages to fill; [1]: 1 if the plan was committed
+    int2* items;     // [pages to fill] (sequence of the call, page index within it)
+    int* len;        // [n] tokens before the call
+    int* from;       // [n] first page that is not as before
+    int* old;        // [n, max_pages] compact: the sequences' pages before the call, from `from` on
 };
 
 MoveList move_list(void* ws, const luvc_kv_cache& c, int n) {
     unsigned char* p = static_cast<unsigned char*>(ws);
     MoveList m;
-    m.total = reinterpret_cast<int*>(p);
-    m.items = reinterpret_cast<int2*>(p + 256);
-    m.old = reinterpret_cast<int*>(p + 256 + align_up((size_t)n * c.max_pages * sizeof(int2)));
+    m.head = reinterpret_cast<int*>(p);
+    m.len = reinterpret_cast<int*>(p += 256);
+    m.from = reinterpret_cast<int*>(p += align_up((size_t)n * sizeof(int)));
+    m.items = reinterpret_cast<int2*>(p += align_up((size_t)n * sizeof(int)));
+    m.old = reinterpret_cast<int*>(p + align_up((size_t)n * c.max_pages * sizeof(int2)));
     return m;
 }
 
@@ -59,124 +67,118 @@ struct PlanArgs {
     int* status;
 };
 
-// Shared memory of the plan; start / from / len have n + 1, n and n entries.
+// Shared memory of the plan; the arrays have n + 1, n, n and n entries.
 struct PlanShared {
-    int error;               // highest luvc_status found
-    int total;               // pages to take
-    unsigned long long wide_total;
-    int warp_sum[kPlanWarps];
-    int count[kCounts];
-    int* start;              // exclusive sums of the pages the sequences need
-    int* from;               // first page index of each sequence that is to be taken
-    int* len;                // length before the call; kClaimed where the slot was not obtained
+    int error;                              // highest luvc_status found
+    int page_count[2][kPlanWarps];          // free pages each warp saw in a sweep (two sweeps alternate)
+    unsigned long long need_sum[kPlanWarps];
+    int* start;                             // pages the sequences need; then their exclusive sums
+    int* from;                              // first page index of each sequence that is to be taken
+    int* len;                               // length before the call; kClaimed where the slot was not obtained
+    int* slot;
 };
 
-// Exclusive scan over the block of one value per thread; the total goes to every thread.
-__device__ int block_scan(int v, int* warp_sum, int* total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int x = v;
+template <typename T>
+__device__ __forceinline__ T warp_inclusive(T x, int lane) {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(~0u, x, d);
+        const T y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
     }
-    __syncthreads();                                        // warp_sum of an earlier scan has been read
-    if (lane == 31) warp_sum[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        int s = warp_sum[lane];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(~0u, s, d);
-            if (lane >= d) s += y;
-        }
-        warp_sum[lane] = s;
-    }
-    __syncthreads();
-    *total = warp_sum[kPlanWarps - 1];
-    return x - v + (warp ? warp_sum[warp - 1] : 0);
+    return x;
 }
 
-// start[i] holds the pages sequence i needs; afterwards start[] is their exclusive sum, start[n] the total.
-// More than the pool has is an error; the sum is checked in 64 bits first, so that the scan cannot overflow.
-__device__ void scan_needs(PlanShared& s, int n, int pages) {
-    unsigned long long mine = 0;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) mine += (unsigned)s.start[i];
-    if (mine) atomicAdd(&s.wide_total, mine);
-    __syncthreads();
-    const bool fits = s.wide_total <= (unsigned long long)pages;
-    int base = 0;
+// start[i] holds the pages sequence i needs; afterwards start[] is their exclusive sum, start[n] the total, which is
+// returned (-1: more than the pool has; sums are formed in 64 bits, and only a total that fits is used).
+__device__ int scan_needs(PlanShared& s, int n, int pages) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long base = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + threadIdx.x;
-        int sum;
-        const int before = block_scan(fits && i < n ? s.start[i] : 0, s.warp_sum, &sum);
-        if (i < n) s.start[i] = base + before;
-        base += sum;
+        const unsigned long long v = i < n ? s.start[i] : 0;
+        const unsigned long long x = warp_inclusive(v, lane);
+        if (lane == 31) s.need_sum[warp] = x;
+        __syncthreads();
+        const unsigned long long all = warp_inclusive(s.need_sum[lane], lane);
+        const unsigned long long before = warp ? __shfl_sync(~0u, all, warp - 1) : (__shfl_sync(~0u, all, 31), 0ull);
+        if (i < n) s.start[i] = (int)(base + before + x - v);
+        base += __shfl_sync(~0u, all, 31);
+        if (n > kPlanThreads) __syncthreads();              // need_sum is written again
     }
-    if (threadIdx.x == 0) {
-        s.start[n] = base; s.total = base;
-        if (!fits) atomicMax(&s.error, (int)LUVC_ERR_PAGES);
-    }
+    if (threadIdx.x == 0) s.start[n] = (int)base;
     __syncthreads();
+    return base > (unsigned long long)pages ? -1 : (int)base;
 }
 
-// Hands the `total` lowest free pages to the sequences: give(i, page index, page).  False (nothing given) if
-// there are too few.  All threads call it.
+// One sweep over kSweep pages from c0 on: every warp looks at kWarpPages consecutive ones.
+struct Sweep {
+    unsigned mask[kPerLane];                // free pages, one ballot per 32
+    int first;                              // free pages of the sweep before this warp's
+    int sum;
+};
+
+__device__ __forceinline__ void sweep_load(const int32_t* refs, int pages, int c0, int (&r)[kPerLane]) {
+    const int at = c0 + (threadIdx.x >> 5) * kWarpPages + (threadIdx.x & 31);
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) r[k] = at + 32 * k < pages ? refs[at + 32 * k] : 1;
+}
+
+__device__ __forceinline__ void sweep_count(PlanShared& s, const int (&r)[kPerLane], int turn, Sweep& w) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+        w.mask[k] = __ballot_sync(~0u, r[k] == 0);
+        mine += __popc(w.mask[k]);
+    }
+    if (lane == 0) s.page_count[turn & 1][warp] = mine;
+    __syncthreads();
+    const int all = warp_inclusive(s.page_count[turn & 1][lane], lane);
+    w.sum = __shfl_sync(~0u, all, 31);
+    w.first = __shfl_sync(~0u, all, warp) - mine;
+}
+
+// Hands the `total` lowest free pages to the sequences: give(i, page index, rank, page).  False (nothing given) if there are too
+// few.  r: the first sweep's counts, loaded ahead.  All threads call it.
 template <typename F>
-__device__ bool take_pages(PlanShared& s, int* refs, int pages, int n, F give) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, total = s.total;
-    unsigned free_mask[kPerThread];                         // ballot of this warp, per sweep row
-    int sum = 0;
-    auto sweep = [&](int c0) {                              // count[] = exclusive sums in page order
+__device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pages, int n, int total, int (&r)[kPerLane], F give) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto hand_out = [&](const Sweep& w, int c0, int base) {
+        int rank0 = base + w.first;
 #pragma unroll
-        for (int k = 0; k < kPerThread; ++k) {
-            const int page = c0 + k * kPlanThreads + threadIdx.x;
-            const bool is_free = page < pages && refs[page] == 0;
-            free_mask[k] = __ballot_sync(~0u, is_free);
-        }
-        __syncthreads();                                    // count[] of the sweep before has been used
-        if (lane == 0)
-#pragma unroll
-            for (int k = 0; k < kPerThread; ++k) s.count[k * kPlanWarps + warp] = __popc(free_mask[k]);
-        __syncthreads();
-        const int mine = threadIdx.x < kCounts ? s.count[threadIdx.x] : 0;
-        const int before = block_scan(mine, s.warp_sum, &sum);
-        if (threadIdx.x < kCounts) s.count[threadIdx.x] = before;
-        __syncthreads();
-    };
-    auto hand_out = [&](int c0, int base) {
-#pragma unroll
-        for (int k = 0; k < kPerThread; ++k) {
-            if (!((free_mask[k] >> lane) & 1u)) continue;
-            const int rank = base + s.count[k * kPlanWarps + warp] + __popc(free_mask[k] & ((1u << lane) - 1u));
-            if (rank >= total) continue;
+        for (int k = 0; k < kPerLane; ++k) {
+            const int rank = rank0 + __popc(w.mask[k] & ((1u << lane) - 1u));
+            rank0 += __popc(w.mask[k]);
+            if (!((w.mask[k] >> lane) & 1u) || rank >= total) continue;
             int lo = 0, hi = n;                             // start[lo] <= rank < start[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (s.start[mid] <= rank) lo = mid; else hi = mid;
             }
-            const int page = c0 + k * kPlanThreads + threadIdx.x;
+            const int page = c0 + warp * kWarpPages + 32 * k + lane;
             refs[page] = 1;
             give(lo, s.from[lo] + rank - s.start[lo], rank, page);
         }
     };
     if (total == 0) return true;
-    int found = 0, c0 = 0;
-    for (; c0 < pages; c0 += kSweep) {
-        sweep(c0);
-        found += sum;
-        if (found >= total) break;
+    Sweep w;
+    sweep_count(s, r, 0, w);
+    if (w.sum >= total) {                                   // one sweep saw them all
+        hand_out(w, 0, 0);
+        return true;
+    }
+    int found = w.sum, end = kSweep, turn = 1;
+    for (; found < total && end < pages; end += kSweep, ++turn) {
+        sweep_load(refs, pages, end, r);
+        sweep_count(s, r, turn, w);
+        found += w.sum;
     }
     if (found < total) return false;
-    if (c0 == 0) {
-        hand_out(0, 0);                                     // one sweep saw them all
-    } else {
-        int base = 0;
-        for (int c = 0; c <= c0; c += kSweep) {
-            sweep(c);
-            hand_out(c, base);
-            base += sum;
-        }
+    for (int c0 = 0, base = 0; c0 < end; c0 += kSweep, ++turn) {
+        sweep_load(refs, pages, c0, r);
+        sweep_count(s, r, turn, w);
+        hand_out(w, c0, base);
+        base += w.sum;
     }
     return true;
 }
@@ -212,28 +214,32 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
     const luvc_kv_cache& c = a.c;
     const int n = a.n, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        s.error = 0; s.wide_total = 0;
-        s.start = dyn; s.from = dyn + n + 1; s.len = dyn + 2 * n + 1;
-        if (KIND != kReserve) *a.move.total = 0;
+        s.error = 0;
+        s.start = dyn; s.from = dyn + n + 1; s.len = dyn + 2 * n + 1; s.slot = dyn + 3 * n + 1;
     }
+    pdl_trigger();
+    pdl_wait();
+    int r[kPerLane];                                        // looked at last, but independent of everything before
+    sweep_load(c.refs, c.pages, 0, r);
+    if (KIND != kReserve && tid == 0) a.move.head[1] = 0;
     if (__syncthreads_or(stopped(a.status))) return;
     const long long most = (long long)c.max_pages * c.page_size;
-    auto slot_of = [&](int i) { return a.seqs ? a.seqs[i] : i; };
 
     // what each sequence needs; its slot is claimed, so that one named twice is noticed
     if (KIND == kFork) {
         for (int i = tid; i < n; i += kPlanThreads) {
-            const int src = a.src[i];
+            const int src = a.src[i], dst = a.seqs[i];
             int len = -1;
             if (src >= 0 && src < c.slots) len = c.lengths[src];
             if (len < 0 || len > most) { atomicMax(&s.error, (int)LUVC_ERR_SHAPE); len = 0; }
             s.from[i] = len / c.page_size;
             s.start[i] = len % c.page_size ? 1 : 0;
             s.len[i] = len;
+            s.slot[i] = dst;
         }
         __syncthreads();                                    // a source that is also a destination has been read
         for (int i = tid; i < n; i += kPlanThreads) {
-            const int dst = slot_of(i);
+            const int dst = s.slot[i];
             const int was = dst >= 0 && dst < c.slots ? atomicCAS(&c.lengths[dst], 0, kClaimed) : kClaimed;
             if (was != 0) {
                 atomicMax(&s.error, was == kClaimed ? (int)LUVC_ERR_SHAPE : (int)LUVC_ERR_TARGET);
@@ -242,10 +248,9 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
         }
     } else if (KIND == kReserve) {
         for (int i = tid; i < n; i += kPlanThreads) {
-            const int slot = slot_of(i), add = a.counts[i];
+            const int slot = a.seqs ? a.seqs[i] : i, add = a.counts[i];
             int len = kClaimed;
             if (slot >= 0 && slot < c.slots) len = a.seqs ? atomicExch(&c.lengths[slot], kClaimed) : c.lengths[slot];
-            s.len[i] = len;
             int need = 0, have = 0;
             if (len < 0 || add < 0) {
                 atomicMax(&s.error, (int)LUVC_ERR_SHAPE);
@@ -255,12 +260,11 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
                 have = ceil_div(len, c.page_size);
                 need = ceil_div(len + add, c.page_size) - have;
             }
-            s.from[i] = have;
-            s.start[i] = need;
+            s.len[i] = len; s.from[i] = have; s.start[i] = need; s.slot[i] = slot;
         }
     } else {
         for (int i = warp; i < n; i += kPlanWarps) {
-            const int slot = slot_of(i);
+            const int slot = a.seqs ? a.seqs[i] : i;
             int len = kClaimed;
             if (lane == 0 && slot >= 0 && slot < c.slots)
                 len = a.seqs ? atomicExch(&c.lengths[slot], kClaimed) : c.lengths[slot];
@@ -280,60 +284,34 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             }
             if (lane == 0) {
                 if (bad) atomicMax(&s.error, bad);
-                s.len[i] = len; s.from[i] = still; s.start[i] = need;
+                s.len[i] = len; s.from[i] = still; s.start[i] = need; s.slot[i] = slot;
+                a.move.len[i] = len; a.move.from[i] = still;
             }
         }
     }
     __syncthreads();
-    scan_needs(s, n, c.pages);
-    bool ok = s.error == 0;
-    if (ok) {
-        ok = take_pages(s, c.refs, c.pages, n, [&](int i, int index, int rank, int page) {
-            c.table[(long long)slot_of(i) * c.max_pages + index] = page;
+    const int total = scan_needs(s, n, c.pages);
+    int error = s.error;
+    if (total < 0 && error < LUVC_ERR_PAGES) error = LUVC_ERR_PAGES;
+    if (!error && !take_pages(s, c.refs, c.pages, n, total, r, [&](int i, int index, int rank, int page) {
+            c.table[(long long)s.slot[i] * c.max_pages + index] = page;
             if (KIND != kReserve) a.move.items[rank] = make_int2(i, index);
-        });
-        if (!ok && tid == 0) s.error = LUVC_ERR_PAGES;
-        __syncthreads();
-    }
-    if (!ok) {                                              // give the claimed slots back
-        for (int i = tid; i < n; i += kPlanThreads) {
-            if (s.len[i] == kClaimed) continue;
-            if (KIND == kFork) c.lengths[slot_of(i)] = 0;
-            else if (a.seqs) c.lengths[slot_of(i)] = s.len[i];
-        }
-        if (tid == 0) *a.status = s.error;
-        return;
-    }
-    // commit: lengths, and the pages that were shared or given up (several warps per sequence when there are few)
-    for (int i = tid; i < n; i += kPlanThreads) {
+        }))
+        error = LUVC_ERR_PAGES;
+    for (int i = tid; i < n; i += kPlanThreads) {           // lengths: committed, or the claimed slots given back
         int now = s.len[i];
-        if (KIND == kReserve) now += a.counts[i];
-        if (KIND == kCompact) now += (a.counts ? a.counts[i] : a.keep) - a.span[i];
-        c.lengths[slot_of(i)] = now;
-    }
-    if (KIND == kReserve) return;
-    if (tid == 0) *a.move.total = s.total;
-    int team = 1;
-    while (team < kPlanWarps && 2 * team * n <= kPlanWarps) team *= 2;
-    for (int i = warp / team; i < n; i += kPlanWarps / team) {
-        int32_t* row = c.table + (long long)slot_of(i) * c.max_pages;
-        const int lane0 = (warp % team) * 32 + lane;
-        if (KIND == kFork) {
-            const int32_t* from = c.table + (long long)a.src[i] * c.max_pages;
-            for (int p = lane0; p < s.from[i]; p += team * 32) {
-                const int page = from[p];
-                row[p] = page;
-                if (page >= 0 && page < c.pages) atomicAdd(&c.refs[page], 1);
-            }
+        if (error) {
+            if (now == kClaimed || !a.seqs) continue;
+            if (KIND == kFork) now = 0;
         } else {
-            const int before = ceil_div(s.len[i], c.page_size);
-            const int now = s.from[i] + s.start[i + 1] - s.start[i];
-            for (int p = s.from[i] + lane0; p < before; p += team * 32) {
-                const int page = a.move.old[(long long)i * c.max_pages + p];
-                if (page >= 0 && page < c.pages) atomicSub(&c.refs[page], 1);
-                if (p >= now) row[p] = -1;
-            }
+            if (KIND == kReserve) now += a.counts[i];
+            if (KIND == kCompact) now += (a.counts ? a.counts[i] : a.keep) - a.span[i];
         }
+        c.lengths[s.slot[i]] = now;
+    }
+    if (tid == 0) {
+        if (error) *a.status = error;
+        else if (KIND != kReserve) { a.move.head[0] = total; a.move.head[1] = 1; }
     }
 }
 
@@ -342,71 +320,121 @@ struct MoveArgs {
     const int32_t* seqs;     // fork: the destinations
     const int32_t* src;      // fork: the sources; null: compact
     const int32_t *first, *span, *idx, *counts;
-    int keep;
+    int n, keep;
     int es;                  // bytes of an element
     MoveList move;
     int* status;
 };
 
-// Fills the pages of the plan's list.  A work item is one page for up to kLanes (layer, K or V, head) triples; a thread
-// copies 16 bytes of a row for all of them, so a row's place is looked up once for kLanes copies and as many loads
-// are in flight per thread.
-constexpr int kMoveLanes = 8, kMoveThreads = 256;
+// Fills the pages of the plan's list, and settles the pages that change hands.  A work item is up to kMoveRows rows of one
+// page for kMoveLanes (layer, K or V, head) triples.  Where its rows come from is worked out once, while the item before is
+// being copied, and kept in shared memory; a thread then copies 16 bytes of a row for all triples, with as many loads in flight.
+constexpr int kMoveLanes = 8, kMoveRows = 64, kMoveThreads = 256;
 
 template <bool FORK>
 __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const __grid_constant__ MoveArgs a) {
+    __shared__ long long src_row[2][kMoveRows];             // row of head 0 of a layer's pool; -1: none
     const luvc_kv_cache& c = a.c;
-    const int triples = c.layers * 2 * c.heads, groups = (triples + kMoveLanes - 1) / kMoveLanes;
-    const long long work = (long long)*a.move.total * groups;
-    const int ps = c.page_size, units = c.D * a.es / 16;
-    const size_t head_bytes = (size_t)ps * c.D * a.es, layer_bytes = (size_t)c.pages * c.heads * head_bytes;
-    for (long long w = blockIdx.x; w < work; w += gridDim.x) {
-        const int2 item = a.move.items[w / groups];
-        const int g = (int)(w % groups) * kMoveLanes;
-        const int i = item.x, p = item.y;
+    const int tid = threadIdx.x, lane = tid & 31, ps = c.page_size;
+    pdl_trigger();
+    pdl_wait();
+    if (!a.move.head[1]) return;
+
+    // pages that change hands, a sequence per warp
+    for (int i = blockIdx.x * (kMoveThreads / 32) + (tid >> 5); i < a.n; i += gridDim.x * (kMoveThreads / 32)) {
         const int slot = a.seqs ? a.seqs[i] : i;
-        const int rows = min(ps, c.lengths[slot] - p * ps);
-        const int to_page = c.table[(long long)slot * c.max_pages + p];
-        unsigned char* base[kMoveLanes];
-#pragma unroll
-        for (int k = 0; k < kMoveLanes; ++k) {
-            const int t = min(g + k, triples - 1), layer = t / (2 * c.heads), rest = t % (2 * c.heads);
-            base[k] = static_cast<unsigned char*>(rest >= c.heads ? c.v : c.k) + layer * layer_bytes +
-                      (rest % c.heads) * head_bytes;
+        int32_t* const row = c.table + (long long)slot * c.max_pages;
+        if (FORK) {
+            const int32_t* const from = c.table + (long long)a.src[i] * c.max_pages;
+            const int full = c.lengths[slot] / ps;
+            for (int p = lane; p < full; p += 32) {
+                const int page = from[p];
+                row[p] = page;
+                if (page >= 0 && page < c.pages) atomicAdd(&c.refs[page], 1);
+            }
+        } else {
+            const int before = ceil_div(a.move.len[i], ps), now = ceil_div(c.lengths[slot], ps);
+            for (int p = a.move.from[i] + lane; p < before; p += 32) {
+                const int page = a.move.old[(long long)i * c.max_pages + p];
+                if (page >= 0 && page < c.pages) atomicSub(&c.refs[page], 1);
+                if (p >= now) row[p] = -1;
+            }
         }
-        for (int u = threadIdx.x; u < rows * units; u += kMoveThreads) {
-            const int r = u / units, off = (u - r * units) * 16;
-            int from = p * ps + r;                          // token of the old sequence that becomes row r of this page
-            int from_page;
+    }
+
+    const int triples = c.layers * 2 * c.heads, groups = (triples + kMoveLanes - 1) / kMoveLanes;
+    const int chunks = (ps + kMoveRows - 1) / kMoveRows, per_page = groups * chunks;
+    const long long work = (long long)a.move.head[0] * per_page;
+    const int units = c.D * a.es / 16;
+    const size_t row_bytes = (size_t)c.D * a.es, head_bytes = ps * row_bytes, layer_bytes = (size_t)c.pages * c.heads * head_bytes;
+
+    struct Item { int group, rows; long long dst; };        // dst: first row, as src_row
+    // Where item w's rows come from and go to; the first kMoveRows threads look up a row each.
+    auto look_up = [&](long long w, int buf) {
+        const int2 it = a.move.items[w / per_page];
+        const int rest = (int)(w % per_page), chunk = rest / groups;
+        const int i = it.x, p = it.y, slot = a.seqs ? a.seqs[i] : i;
+        Item q;
+        q.group = rest - chunk * groups;
+        q.rows = min(kMoveRows, min(ps, c.lengths[slot] - p * ps) - chunk * kMoveRows);
+        const int to = c.table[(long long)slot * c.max_pages + p];
+        q.dst = (long long)to * c.heads * ps + chunk * kMoveRows;
+        if (to < 0 || to >= c.pages) q.rows = 0;
+        if (tid < q.rows) {
+            int from = p * ps + chunk * kMoveRows + tid, page;  // token of the old sequence that becomes this row
             if (FORK) {
-                from_page = c.table[(long long)a.src[i] * c.max_pages + p];
+                page = c.table[(long long)a.src[i] * c.max_pages + p];
             } else {
                 const int first = a.first[i], span = a.span[i], count = a.counts ? a.counts[i] : a.keep;
                 if (from >= first + count) {
                     from += span - count;
                 } else if (from >= first) {
-                    const int e = a.idx[(long long)i * a.keep + from - first];
-                    const int in = min(max(e, 0), span - 1);
+                    const int e = a.idx[(long long)i * a.keep + from - first], in = min(max(e, 0), span - 1);
                     if (in != e) *a.status = LUVC_ERR_KEEP;
                     from = first + in;
                 }
-                from_page = a.move.old[(long long)i * c.max_pages + from / ps];
+                page = a.move.old[(long long)i * c.max_pages + from / ps];
             }
-            if (from_page < 0 || from_page >= c.pages || to_page < 0 || to_page >= c.pages) continue;
-            const size_t src = (size_t)from_page * c.heads * head_bytes + (size_t)(from % ps) * c.D * a.es + off;
-            const size_t dst = (size_t)to_page * c.heads * head_bytes + (size_t)r * c.D * a.es + off;
+            src_row[buf][tid] = page >= 0 && page < c.pages ? (long long)page * c.heads * ps + from % ps : -1;
+        }
+        return q;
+    };
+
+    long long w = blockIdx.x;
+    if (w >= work) return;
+    Item q = look_up(w, 0);
+    for (int buf = 0; w < work; w += gridDim.x, buf ^= 1) {
+        __syncthreads();                                    // src_row[buf] is there, src_row[buf ^ 1] has been used
+        Item next = q;
+        if (w + gridDim.x < work) next = look_up(w + gridDim.x, buf ^ 1);
+        unsigned char* base[kMoveLanes];
+#pragma unroll
+        for (int k = 0; k < kMoveLanes; ++k) {
+            const int t = min(q.group * kMoveLanes + k, triples - 1), layer = t / (2 * c.heads), rest = t - layer * 2 * c.heads;
+            base[k] = static_cast<unsigned char*>(rest >= c.heads ? c.v : c.k) + layer * layer_bytes +
+                      (rest >= c.heads ? rest - c.heads : rest) * head_bytes;
+        }
+        const int live = min(kMoveLanes, triples - q.group * kMoveLanes);
+        for (int u = tid; u < q.rows * units; u += kMoveThreads) {
+            const int r = u / units, off = (u - r * units) * 16;
+            const long long from = src_row[buf][r];
+            if (from < 0) continue;
+            const size_t src = from * row_bytes + off, dst = (q.dst + r) * row_bytes + off;
             uint4 v[kMoveLanes];
 #pragma unroll
-            for (int k = 0; k < kMoveLanes; ++k) v[k] = __ldg(reinterpret_cast<const uint4*>(base[k] + src));
+            for (int k = 0; k < kMoveLanes; ++k) v[k] = __ldcs(reinterpret_cast<const uint4*>(base[k] + src));
 #pragma unroll
             for (int k = 0; k < kMoveLanes; ++k)
-                if (g + k < triples) *reinterpret_cast<uint4*>(base[k] + dst) = v[k];
+                if (k < live) __stcs(reinterpret_cast<uint4*>(base[k] + dst), v[k]);
         }
+        q = next;
     }
 }
 
-__global__ void __launch_bounds__(128) kv_free_kernel(luvc_kv_cache c, const int32_t* seqs, int* status) {
+__global__ void __launch_bounds__(128) kv_free_kernel(const __grid_constant__ luvc_kv_cache c, const int32_t* seqs, int* status) {
     __shared__ int len;
+    pdl_trigger();
+    pdl_wait();
     if (__syncthreads_or(stopped(status))) return;
     const int slot = seqs ? seqs[blockIdx.x] : (int)blockIdx.x;
     if (slot < 0 || slot >= c.slots) {
@@ -436,15 +464,13 @@ struct WriteArgs {
 template <typename T> struct Vec;                           // the elements of 16 input bytes, as floats
 template <> struct Vec<float> {
     static constexpr int N = 4;
-    static __device__ void load(const float* p, float (&f)[8]) {
-        const float4 x = *reinterpret_cast<const float4*>(p);
-        f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+    static __device__ void unpack(uint4 x, float (&f)[8]) {
+        f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
     }
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
-    static __device__ void load(const __nv_bfloat16* p, float (&f)[8]) {
-        const uint4 x = *reinterpret_cast<const uint4*>(p);
+    static __device__ void unpack(uint4 x, float (&f)[8]) {
         const unsigned w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -454,10 +480,10 @@ template <> struct Vec<__nv_bfloat16> {
     }
 };
 
-__device__ __forceinline__ void store_row(float* p, const float (&f)[8], float) {
+__device__ __forceinline__ void store_row(float* p, const float (&f)[8], float2) {
     *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
 }
-__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8], float) {
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8], float2) {
     unsigned r[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -466,18 +492,41 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8],
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(r[0], r[1], r[2], r[3]);
 }
-// x / scale, saturated, to nearest even: a true division, so that the stored value is the nearest one to the quotient
-__device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8], float scale) {
-    unsigned r[2] = {0, 0};
+// x / scale, saturated, to nearest even.  The quotient is the correctly rounded one, so that the stored value is what a
+// division gives, at a third of its instructions: Markstein's method (q = x r, then q + r (x - q scale), fused), with r the
+// correctly rounded reciprocal.  Quotients that saturate anyway, infinities and NaN keep q.
+__device__ __forceinline__ float divided(float x, float scale, float r) {
+    const float q = x * r;
+    return fabsf(q) < 1024.f ? fmaf(fmaf(-q, scale, x), r, q) : q;
+}
+__device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8], float2 scale) {
+    unsigned w[2] = {0, 0};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const float2 x = make_float2(f[2 * q] / scale, f[2 * q + 1] / scale);
-        r[q >> 1] |= (unsigned)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * (q & 1));
+        float2 x;
+        if (isinf(scale.y)) x = make_float2(f[2 * q] / scale.x, f[2 * q + 1] / scale.x);     // scale below 2^-128
+        else x = make_float2(divided(f[2 * q], scale.x, scale.y), divided(f[2 * q + 1], scale.x, scale.y));
+        w[q >> 1] |= (unsigned)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * (q & 1));
     }
-    *reinterpret_cast<uint2*>(p) = make_uint2(r[0], r[1]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
 
-constexpr int kWriteTokens = 16, kWriteThreads = 256;
+// Last entry of ascending starts[0 .. n] (starts[0] = 0) that is <= t, below n: 32 probes at a time (one warp, one t).
+__device__ __forceinline__ int owner_of(const int32_t* starts, int n, int t, int lane) {
+    int lo = 0, size = n;                                   // the answer is in [lo, lo + size)
+    while (size > 1) {
+        const int step = (size + 31) / 32, at = lo + lane * step;
+        const unsigned m = __ballot_sync(~0u, lane * step < size && starts[at] <= t);
+        const int k = m ? 31 - __clz(m) : 0;
+        lo += k * step;
+        size = min(step, size - k * step);
+    }
+    return lo;
+}
+
+// A CTA writes kWriteTokens tokens.  A thread keeps its place in a token's row (16 bytes of K and of V) and takes every
+// `step`-th token; the first rows are on their way while the warps find out where the tokens go.
+constexpr int kWriteTokens = 16, kWriteThreads = 256, kWriteBatch = 4;
 
 template <typename TI, typename TC>
 __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_constant__ WriteArgs a) {
@@ -485,22 +534,33 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_co
     __shared__ long long row_of[kWriteTokens];              // row of head 0 in the layer's pool, -1: not written
     __shared__ float bias_of[kWriteTokens];
     const luvc_kv_cache& c = a.c;
+    const int t0 = blockIdx.x * kWriteTokens, ps = c.page_size, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per_row = c.D / V, per_token = c.heads * per_row, cols = min(per_token, kWriteThreads), step = kWriteThreads / cols;
+    const int mine = threadIdx.x / cols, tokens = min(kWriteTokens, a.tokens - t0);
+    pdl_trigger();
+    pdl_wait();
     if (__syncthreads_or(stopped(a.status))) return;
-    const int t0 = blockIdx.x * kWriteTokens, ps = c.page_size;
-    if (threadIdx.x < kWriteTokens) {
-        const int t = t0 + threadIdx.x;
-        long long row = -1;
-        if (t < a.tokens) {
-            int i = t, behind = 1;                          // tokens of the sequence from this one to its end
-            if (a.starts) {
-                int lo = 0, hi = a.n;                       // starts[lo] <= t < starts[hi]
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (a.starts[mid] <= t) lo = mid; else hi = mid;
-                }
-                i = lo;
-                behind = a.starts[lo + 1] - t;
+    uint4 kx[kWriteBatch], vx[kWriteBatch];
+    auto fetch = [&](int col, int t) {
+#pragma unroll
+        for (int b = 0; b < kWriteBatch; ++b)
+            if (t + b * step < tokens) {
+                const long long at = t0 + t + b * step;
+                kx[b] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const TI*>(a.k) + at * a.k_stride + col * V));
+                vx[b] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const TI*>(a.v) + at * a.v_stride + col * V));
             }
+    };
+    const int col0 = threadIdx.x - mine * cols;
+    if (mine < step) fetch(col0, mine);
+    for (int j = warp; j < tokens; j += kWriteThreads / 32) {
+        const int t = t0 + j;
+        int i = t, behind = 1;                              // tokens of the sequence from this one to its end
+        if (a.starts) {
+            i = owner_of(a.starts, a.n, t, lane);
+            behind = a.starts[i + 1] - t;
+        }
+        if (lane == 0) {
+            long long row = -1;
             const int slot = a.seqs ? a.seqs[i] : i;
             const int pos = slot >= 0 && slot < c.slots ? c.lengths[slot] - behind : -1;
             if (behind >= 1 && pos >= 0 && pos / ps < c.max_pages) {
@@ -508,31 +568,40 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_co
                 if (page >= 0 && page < c.pages) row = (long long)page * c.heads * ps + pos % ps;
             }
             if (row < 0) *a.status = LUVC_ERR_SHAPE;
-            bias_of[threadIdx.x] = a.sizes ? logf((float)a.sizes[t]) : 0.f;
+            bias_of[j] = a.sizes ? logf((float)a.sizes[t]) : 0.f;
+            row_of[j] = row;
         }
-        row_of[threadIdx.x] = row;
     }
     __syncthreads();
-    const int per_row = c.D / V, per_token = c.heads * per_row;
+    if (mine >= step) return;
     const long long layer_row = (long long)a.layer * c.pages * c.heads * ps;
-    TC* const kd = static_cast<TC*>(c.k);
-    TC* const vd = static_cast<TC*>(c.v);
-    for (int e = threadIdx.x; e < kWriteTokens * per_token; e += kWriteThreads) {
-        const int t = e / per_token, in = e - t * per_token, h = in / per_row;
-        const long long row = row_of[t];
-        if (row < 0) continue;
-        const long long dst = (layer_row + row + (long long)h * ps) * c.D + (long long)(in - h * per_row) * V;
-        float k[8], v[8];
-        Vec<TI>::load(static_cast<const TI*>(a.k) + (t0 + t) * a.k_stride + (long long)in * V, k);
-        Vec<TI>::load(static_cast<const TI*>(a.v) + (t0 + t) * a.v_stride + (long long)in * V, v);
-        const float b = bias_of[t];
-        if (a.sizes)
+    for (int col = col0; col < per_token; col += cols) {
+        const int h = col / per_row;
+        const long long in = (long long)h * ps * c.D + (long long)(col - h * per_row) * V;
+        TC* const kd = static_cast<TC*>(c.k) + in;
+        TC* const vd = static_cast<TC*>(c.v) + in;
+        float2 ks = make_float2(1.f, 1.f), vs = ks;         // scale and reciprocal
+        if (c.k_scale) {
+            ks.x = c.k_scale[a.layer * c.heads + h]; ks.y = 1.f / ks.x;
+            vs.x = c.v_scale[a.layer * c.heads + h]; vs.y = 1.f / vs.x;
+        }
+        for (int t = mine; t < tokens; t += kWriteBatch * step) {
+            if (col != col0 || t != mine) fetch(col, t);
 #pragma unroll
-            for (int q = 0; q < V; ++q) v[q] += b;
-        const float ks = c.k_scale ? c.k_scale[a.layer * c.heads + h] : 1.f;
-        const float vs = c.v_scale ? c.v_scale[a.layer * c.heads + h] : 1.f;
-        store_row(kd + dst, k, ks);
-        store_row(vd + dst, v, vs);
+            for (int b = 0; b < kWriteBatch; ++b) {
+                const int j = t + b * step;
+                if (j >= tokens || row_of[j] < 0) continue;
+                const long long dst = (layer_row + row_of[j]) * c.D;
+                float f[8];
+                Vec<TI>::unpack(kx[b], f);
+                store_row(kd + dst, f, ks);
+                Vec<TI>::unpack(vx[b], f);
+                if (a.sizes)
+#pragma unroll
+                    for (int x = 0; x < V; ++x) f[x] += bias_of[j];
+                store_row(vd + dst, f, vs);
+            }
+        }
     }
 }
 
@@ -548,18 +617,15 @@ int sm_count() {
 
 template <PlanKind KIND>
 int launch_plan(const PlanArgs& a, cudaStream_t stream) {
-    const size_t smem = (size_t)(3 * a.n + 1) * sizeof(int);
-    if (smem > 40 * 1024) cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    kv_plan_kernel<KIND><<<1, kPlanThreads, smem, stream>>>(a);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    const size_t smem = (size_t)(4 * a.n + 1) * sizeof(int);
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return LUVC_ERR_CUDA;
+    return launch_overlapped(kv_plan_kernel<KIND>, 1, kPlanThreads, smem, stream, a);
 }
 
 template <bool FORK>
 int launch_move(const MoveArgs& a, cudaStream_t stream) {
-    kv_move_kernel<FORK><<<4 * sm_count(), kMoveThreads, 0, stream>>>(a);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    return launch_overlapped(kv_move_kernel<FORK>, 4 * sm_count(), kMoveThreads, 0, stream, a);
 }
 
 }  // namespace
@@ -567,7 +633,8 @@ int launch_move(const MoveArgs& a, cudaStream_t stream) {
 size_t kv_elem_size(int dtype) { return dtype == LUVC_F32 ? 4 : dtype == LUVC_BF16 ? 2 : 1; }
 
 size_t kv_workspace_bytes(const luvc_kv_cache& c, int n) {
-    return 256 + align_up((size_t)n * c.max_pages * sizeof(int2)) + align_up((size_t)n * c.max_pages * sizeof(int));
+    return 256 + 2 * align_up((size_t)n * sizeof(int)) + align_up((size_t)n * c.max_pages * sizeof(int2)) +
+           align_up((size_t)n * c.max_pages * sizeof(int));
 }
 
 int kv_reserve(const luvc_kv_cache& c, const int32_t* seqs, int n, const int32_t* counts, int* status, cudaStream_t stream) {
@@ -582,7 +649,7 @@ int kv_fork(const luvc_kv_cache& c, const int32_t* src, const int32_t* dst, int 
     const int rc = launch_plan<kFork>(a, stream);
     if (rc) return rc;
     MoveArgs m = {};
-    m.c = c; m.seqs = dst; m.src = src; m.es = (int)kv_elem_size(c.dtype); m.move = a.move; m.status = status;
+    m.c = c; m.seqs = dst; m.src = src; m.n = n; m.es = (int)kv_elem_size(c.dtype); m.move = a.move; m.status = status;
     return launch_move<true>(m, stream);
 }
 
@@ -594,15 +661,13 @@ int kv_compact(const luvc_kv_cache& c, const int32_t* seqs, int n, const int32_t
     const int rc = launch_plan<kCompact>(a, stream);
     if (rc) return rc;
     MoveArgs m = {};
-    m.c = c; m.seqs = seqs; m.first = first; m.span = span; m.idx = idx; m.counts = counts; m.keep = keep;
+    m.c = c; m.seqs = seqs; m.first = first; m.span = span; m.idx = idx; m.counts = counts; m.n = n; m.keep = keep;
     m.es = (int)kv_elem_size(c.dtype); m.move = a.move; m.status = status;
     return launch_move<false>(m, stream);
 }
 
 int kv_free(const luvc_kv_cache& c, const int32_t* seqs, int n, int* status, cudaStream_t stream) {
-    kv_free_kernel<<<n, 128, 0, stream>>>(c, seqs, status);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    return launch_overlapped(kv_free_kernel, n, 128, 0, stream, c, seqs, status);
 }
 
 int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, const void* k, const void* v, long long k_stride,
@@ -611,11 +676,9 @@ int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, cons
     a.c = c; a.layer = layer; a.n = n; a.tokens = tokens; a.seqs = seqs; a.starts = starts; a.sizes = sizes;
     a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.status = status;
     const int grid = (tokens + kWriteTokens - 1) / kWriteTokens;
-    if (c.dtype == LUVC_F32) kv_write_kernel<float, float><<<grid, kWriteThreads, 0, stream>>>(a);
-    else if (c.dtype == LUVC_BF16) kv_write_kernel<__nv_bfloat16, __nv_bfloat16><<<grid, kWriteThreads, 0, stream>>>(a);
-    else kv_write_kernel<__nv_bfloat16, __nv_fp8_e4m3><<<grid, kWriteThreads, 0, stream>>>(a);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    if (c.dtype == LUVC_F32) return launch_overlapped(kv_write_kernel<float, float>, grid, kWriteThreads, 0, stream, a);
+    if (c.dtype == LUVC_BF16) return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_bfloat16>, grid, kWriteThreads, 0, stream, a);
+    return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_fp8_e4m3>, grid, kWriteThreads, 0, stream, a);
 }
 
 }  // namespace luvc

@@ -17,6 +17,21 @@ void count_launch(int n = 1);
 void phase_begin(int phase, cudaStream_t stream);
 void phase_end(int phase, cudaStream_t stream);
 
+// Launches a kernel that begins with ptx::pdl_wait (programmatic dependent launch: its start overlaps the end of the kernel
+// before it in the stream), and counts it.
+template <typename... P, typename... A>
+int launch_overlapped(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    count_launch();
+    return rc == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+}
+
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
 // ---- OIM -------------------------------------------------------------------

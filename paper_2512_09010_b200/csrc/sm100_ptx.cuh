@@ -97,6 +97,12 @@ __device__ __forceinline__ unsigned long long global_timer() {
     return t;
 }
 
+// Programmatic dependent launch.  A kernel launched with the attribute may start while the kernel before it in the stream
+// still runs; pdl_wait returns when that one has finished and its writes are visible, and comes before the first access
+// to memory that another kernel may write.  pdl_trigger lets the next such kernel start (it then waits in turn).
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // True in exactly one lane of a converged warp.  Code that only this lane runs (TMA and MMA issue)
 // sits inside warp-uniform control flow, so that the compiler keeps its operands in uniform registers.
 __device__ __forceinline__ bool elect_one() {
