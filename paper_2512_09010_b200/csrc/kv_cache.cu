@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(128) kv_free_kernel(const __grid_constant__ lu
 
 struct WriteArgs {
     luvc_kv_cache c;
-    int layer, n, tokens;
+    int layer, n, tokens, per;                              // per: tokens of a CTA
     const int32_t *seqs, *starts, *sizes;
     const void *k, *v;
     long long k_stride, v_stride;
@@ -480,10 +480,15 @@ template <> struct Vec<__nv_bfloat16> {
     }
 };
 
-__device__ __forceinline__ void store_row(float* p, const float (&f)[8], float2) {
+// What an e4m3 row is divided by: the scale, its reciprocal, and the largest quotient the short way is taken for.
+struct Scale {
+    float s, r, most;
+    __device__ explicit Scale(float scale) : s(scale), r(1.f / scale), most(isinf(1.f / scale) ? -1.f : 1024.f) {}
+};
+__device__ __forceinline__ void store_row(float* p, const float (&f)[8], const Scale&) {
     *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
 }
-__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8], float2) {
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8], const Scale&) {
     unsigned r[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -494,20 +499,26 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&f)[8],
 }
 // x / scale, saturated, to nearest even.  The quotient is the correctly rounded one, so that the stored value is what a
 // division gives, at a third of its instructions: Markstein's method (q = x r, then q + r (x - q scale), fused), with r the
-// correctly rounded reciprocal.  Quotients that saturate anyway, infinities and NaN keep q.
-__device__ __forceinline__ float divided(float x, float scale, float r) {
-    const float q = x * r;
-    return fabsf(q) < 1024.f ? fmaf(fmaf(-q, scale, x), r, q) : q;
-}
-__device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8], float2 scale) {
-    unsigned w[2] = {0, 0};
+// correctly rounded reciprocal.  Quotients far beyond 448, which include infinities, and scales below 2^-128 are divided.
+__device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8], const Scale& scale) {
+    float q[8], big = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float2 x;
-        if (isinf(scale.y)) x = make_float2(f[2 * q] / scale.x, f[2 * q + 1] / scale.x);     // scale below 2^-128
-        else x = make_float2(divided(f[2 * q], scale.x, scale.y), divided(f[2 * q + 1], scale.x, scale.y));
-        w[q >> 1] |= (unsigned)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * (q & 1));
+    for (int x = 0; x < 8; ++x) {
+        q[x] = f[x] * scale.r;
+        big = fmaxf(big, fabsf(q[x]));
     }
+    if (big < scale.most) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) q[x] = fmaf(fmaf(-q[x], scale.s, f[x]), scale.r, q[x]);
+    } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) q[x] = f[x] / scale.s;
+    }
+    unsigned w[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        w[x] = (unsigned)__nv_cvt_float2_to_fp8x2(make_float2(q[4 * x], q[4 * x + 1]), __NV_SATFINITE, __NV_E4M3) |
+               (unsigned)__nv_cvt_float2_to_fp8x2(make_float2(q[4 * x + 2], q[4 * x + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
     *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
 
@@ -524,19 +535,19 @@ __device__ __forceinline__ int owner_of(const int32_t* starts, int n, int t, int
     return lo;
 }
 
-// A CTA writes kWriteTokens tokens.  A thread keeps its place in a token's row (16 bytes of K and of V) and takes every
+// A CTA writes up to kWriteTokens tokens.  A thread keeps its place in a token's row (16 bytes of K and of V) and takes every
 // `step`-th token; the first rows are on their way while the warps find out where the tokens go.
-constexpr int kWriteTokens = 16, kWriteThreads = 256, kWriteBatch = 4;
+constexpr int kWriteTokens = 32, kWriteThreads = 256, kWriteBatch = 4;
 
 template <typename TI, typename TC>
-__global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWriteThreads, 4) kv_write_kernel(const __grid_constant__ WriteArgs a) {
     constexpr int V = Vec<TI>::N;
     __shared__ long long row_of[kWriteTokens];              // row of head 0 in the layer's pool, -1: not written
     __shared__ float bias_of[kWriteTokens];
     const luvc_kv_cache& c = a.c;
-    const int t0 = blockIdx.x * kWriteTokens, ps = c.page_size, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int t0 = blockIdx.x * a.per, ps = c.page_size, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_row = c.D / V, per_token = c.heads * per_row, cols = min(per_token, kWriteThreads), step = kWriteThreads / cols;
-    const int mine = threadIdx.x / cols, tokens = min(kWriteTokens, a.tokens - t0);
+    const int mine = threadIdx.x / cols, tokens = min(a.per, a.tokens - t0);
     pdl_trigger();
     pdl_wait();
     if (__syncthreads_or(stopped(a.status))) return;
@@ -552,14 +563,16 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_co
     };
     const int col0 = threadIdx.x - mine * cols;
     if (mine < step) fetch(col0, mine);
-    for (int j = warp; j < tokens; j += kWriteThreads / 32) {
-        const int t = t0 + j;
-        int i = t, behind = 1;                              // tokens of the sequence from this one to its end
-        if (a.starts) {
-            i = owner_of(a.starts, a.n, t, lane);
-            behind = a.starts[i + 1] - t;
-        }
-        if (lane == 0) {
+    if (warp == 0) {                                        // a token per lane, from the owner of the first one on
+        int i = a.starts ? owner_of(a.starts, a.n, t0, lane) : t0 + lane;
+        if (lane < tokens) {
+            const int t = t0 + lane;
+            int behind = 1;                                 // tokens of the sequence from this one to its end
+            if (a.starts) {
+                int end = a.starts[i + 1];
+                while (end <= t && i + 1 < a.n) end = a.starts[++i + 1];
+                behind = end - t;
+            }
             long long row = -1;
             const int slot = a.seqs ? a.seqs[i] : i;
             const int pos = slot >= 0 && slot < c.slots ? c.lengths[slot] - behind : -1;
@@ -568,8 +581,8 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_co
                 if (page >= 0 && page < c.pages) row = (long long)page * c.heads * ps + pos % ps;
             }
             if (row < 0) *a.status = LUVC_ERR_SHAPE;
-            bias_of[j] = a.sizes ? logf((float)a.sizes[t]) : 0.f;
-            row_of[j] = row;
+            bias_of[lane] = a.sizes ? logf((float)a.sizes[t]) : 0.f;
+            row_of[lane] = row;
         }
     }
     __syncthreads();
@@ -580,11 +593,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const __grid_co
         const long long in = (long long)h * ps * c.D + (long long)(col - h * per_row) * V;
         TC* const kd = static_cast<TC*>(c.k) + in;
         TC* const vd = static_cast<TC*>(c.v) + in;
-        float2 ks = make_float2(1.f, 1.f), vs = ks;         // scale and reciprocal
-        if (c.k_scale) {
-            ks.x = c.k_scale[a.layer * c.heads + h]; ks.y = 1.f / ks.x;
-            vs.x = c.v_scale[a.layer * c.heads + h]; vs.y = 1.f / vs.x;
-        }
+        const Scale ks(c.k_scale ? c.k_scale[a.layer * c.heads + h] : 1.f), vs(c.v_scale ? c.v_scale[a.layer * c.heads + h] : 1.f);
         for (int t = mine; t < tokens; t += kWriteBatch * step) {
             if (col != col0 || t != mine) fetch(col, t);
 #pragma unroll
@@ -675,7 +684,10 @@ int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, cons
     WriteArgs a;
     a.c = c; a.layer = layer; a.n = n; a.tokens = tokens; a.seqs = seqs; a.starts = starts; a.sizes = sizes;
     a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.status = status;
-    const int grid = (tokens + kWriteTokens - 1) / kWriteTokens;
+    // four CTAs per SM while there are few tokens (what counts then is the time of one), at least 4 tokens each
+    const int even = (int)(((long long)tokens + 4 * sm_count() - 1) / (4 * sm_count()));
+    a.per = even < 4 ? 4 : even > kWriteTokens ? kWriteTokens : even;
+    const int grid = (tokens + a.per - 1) / a.per;
     if (c.dtype == LUVC_F32) return launch_overlapped(kv_write_kernel<float, float>, grid, kWriteThreads, 0, stream, a);
     if (c.dtype == LUVC_BF16) return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_bfloat16>, grid, kWriteThreads, 0, stream, a);
     return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_fp8_e4m3>, grid, kWriteThreads, 0, stream, a);
