@@ -46,11 +46,9 @@ using namespace ptx;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
-constexpr int kMaxPartRows = 16, kMaxPartCols = 256;
-constexpr size_t kPartBytes = (size_t)kMaxPartRows * (kMaxPartCols + 2) * sizeof(float);
+constexpr int kMaxPartBytes = 16 * (256 + 2) * 4;   // of a partial result: 16 rows of 256 sums, and their (m, l)
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
-constexpr int kMinTiles = 2;                    // tiles a warp takes at least: fewer CTAs, not smaller parts, for little work
-constexpr int kWaitProbes = 1 << 22;            // probes before a wait for a copy gives up (seconds)
+constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 
 // ---- the instructions of this file -----------------------------------------------------------------
 
@@ -114,6 +112,8 @@ struct Shape {
     static constexpr int S = 3, NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = 8 * NT;
+    static constexpr int PART = ROWS * (DP + 2);                // floats of a partial result in the workspace: O, then (m, l) of each row
+    static_assert(PART * 4 <= kMaxPartBytes, "the workspace has room for less");
     static_assert(ROWS * DP * 4 <= STAGE, "a partial result must fit a stage");
     static_assert(NW * S * STAGE <= 196608, "ring too large");
 };
@@ -124,7 +124,7 @@ struct Args {
     int page_shift;             // log2 of the page size, -1 if it is no power of two
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
     unsigned* counters;         // [kMaxCtas]
-    float* parts;               // [kMaxCtas][2] of kPartBytes
+    float* parts;               // [kMaxCtas][2] of PART floats
 };
 
 // Place of float d of row r of O in a stage: rows 2 t and 2 t + 1 of a lane quad start 8 banks apart.
@@ -310,7 +310,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         q.first = x - q.tile;
         return q;
     };
-    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW * kMinTiles), tol = min(per / 4, 8);
+    // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.7 us, with two tiles
+    // 9.3, with three 11.8: even then a join across CTAs costs less than a warp's second tile).
+    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW), tol = min(per / 2, 8);
     auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
         if (c == 0) return 0;
         if ((long long)c * per >= total) return total;
@@ -416,7 +418,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             // queries: B operand of S^T = K Q^T, head g of each group of 8
             const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
             constexpr int KS = DPB / 32;                        // steps of 32 bytes of a row
-            uint32_t q[NT][KS][2 * (kF8 ? 2 : 1)];
+            uint32_t q[NT][KS][kF8 ? 4 : 2];
             float qmul[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -801,8 +803,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // ---- joins: the parts of this CTA's warps; then, of a (sequence, head) that other CTAs share, theirs, by the one that
     //      arrives last ----
     auto global_part = [&](int cta, int slot) {
-        float* const o = a.parts + ((size_t)cta * 2 + slot) * (kPartBytes / sizeof(float));
-        return Part{o, reinterpret_cast<const float2*>(o + kMaxPartRows * kMaxPartCols)};
+        float* const o = a.parts + ((size_t)cta * 2 + slot) * Sh::PART;
+        return Part{o, reinterpret_cast<const float2*>(o + ROWS * DP)};
     };
     unsigned some = 0;
 #pragma unroll
@@ -937,7 +939,7 @@ int launch_heads(const AttnProblem& p) {
 
 }  // namespace
 
-size_t attn_workspace_bytes() { return align_up(kMaxCtas * sizeof(unsigned)) + (size_t)kMaxCtas * 2 * kPartBytes; }
+size_t attn_workspace_bytes() { return align_up(kMaxCtas * sizeof(unsigned)) + (size_t)kMaxCtas * 2 * kMaxPartBytes; }
 
 int attn_decode(const AttnProblem& p) {
     const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
