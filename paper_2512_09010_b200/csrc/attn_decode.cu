@@ -47,6 +47,9 @@ using namespace ptx;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
 constexpr int kMaxPartBytes = 16 * (256 + 2) * 4;   // of a partial result: 16 rows of 256 sums, and their (m, l)
+constexpr int kSnap = 12;                       // tiles by which a part may move its ends to those of a (sequence, head): a join across CTAs
+                                                // costs about as much (one sequence of 16000 tokens: 13.1 us, with 8 tiles 13.9, with 6 15.9)
+constexpr size_t kCounterBytes = 3 * kMaxCtas * sizeof(unsigned);
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 
@@ -113,6 +116,7 @@ struct Shape {
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = 8 * NT;
     static constexpr int PART = ROWS * (DP + 2);                // floats of a partial result in the workspace: O, then (m, l) of each row
+    static constexpr int CAP = NW * S * STAGE / (PART * 4);     // partial results the ring has room for
     static_assert(PART * 4 <= kMaxPartBytes, "the workspace has room for less");
     static_assert(ROWS * DP * 4 <= STAGE, "a partial result must fit a stage");
     static_assert(NW * S * STAGE <= 196608, "ring too large");
@@ -123,8 +127,8 @@ struct Args {
     int group, groups;          // query heads per key head; head groups of ROWS
     int page_shift;             // log2 of the page size, -1 if it is no power of two
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
-    unsigned* counters;         // [kMaxCtas]
-    float* parts;               // [kMaxCtas][2] of PART floats
+    unsigned* counters;         // [3][kMaxCtas]: arrivals of (sequence, head)s, of their first groups, of the other groups
+    float* parts;               // [2][kMaxCtas][2] of PART floats: of CTAs, of groups of CTAs
 };
 
 // Place of float d of row r of O in a stage: rows 2 t and 2 t + 1 of a lane quad start 8 banks apart.
@@ -137,25 +141,24 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// One partial result: rows of O (o_index) and (m, l) of each row, in shared or global memory.
+// One partial result in the workspace: rows of O (o_index) and (m, l) of each row.
 struct Part {
-    const float* o;
-    const float2* ml;
+    float* o;
+    float2* ml;
 };
 
-// Joins `count` partial results for four columns of one row; part_of(k) is part k.  Up to eight parts are read at once, (m, l) along
-// with the columns, so a join costs one round trip to memory per eight parts.
-template <typename PartOf>
-__device__ __forceinline__ void join4(int count, PartOf part_of, int r, int at, float& m, float& l, float4& o) {
-    m = -INFINITY; l = 0.f; o = make_float4(0.f, 0.f, 0.f, 0.f);
+// A join of partial results in one step, where a thread has four columns of one row only: (m, l) are read along with the columns,
+// eight parts at a time, and what (m, l, o) hold is joined with them.
+template <typename GetMl, typename Columns>
+__device__ __forceinline__ void join1(int count, GetMl get_ml, Columns columns, float& m, float& l, float4& o) {
     for (int k0 = 0; k0 < count; k0 += 8) {
         float4 x[8];
         float2 ml[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {                           // past the last part: the last one again, with weight 0
-            const Part q = part_of(min(k0 + k, count - 1));
-            ml[k] = q.ml[r];
-            x[k] = *reinterpret_cast<const float4*>(q.o + at);
+            const int at = min(k0 + k, count - 1);
+            ml[k] = get_ml(at);
+            x[k] = *columns(at);
         }
         float top = m;
 #pragma unroll
@@ -173,14 +176,61 @@ __device__ __forceinline__ void join4(int count, PartOf part_of, int r, int at, 
         }
     }
 }
+// Where a thread has several columns, in two steps.  The first, by one warp for a row: the factor of every part,
+// exp(m_k - max m), which put(k, factor) gets, times vscale / l where the result is final; returns (m, l) of the whole.
+template <typename GetMl, typename Put>
+__device__ __forceinline__ float2 join_factors(int count, GetMl get_ml, Put put, bool final, float vscale, int lane) {
+    float2 ml[2] = {make_float2(-INFINITY, 0.f), make_float2(-INFINITY, 0.f)};      // of parts lane and lane + 32
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 32 * x < count) ml[x] = get_ml(lane + 32 * x);
+    float m = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    const float base = m == -INFINITY ? 0.f : m;
+    float f[2], l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        f[x] = exp2_fast((ml[x].x - base) * kLog2e);
+        l = fmaf(f[x], ml[x].y, l);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+    const float all = !final ? 1.f : l == 0.f ? 0.f : vscale / l;           // no key left: zeros
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 32 * x < count) put(lane + 32 * x, f[x] * all);
+    return make_float2(m, l);
+}
+// The second, by a thread for four columns of a row: adds the parts times their factors to o, eight at a time.
+template <typename Factor, typename Columns>
+__device__ __forceinline__ void join4(int count, Factor factor, Columns columns, float4& o) {
+    for (int k0 = 0; k0 < count; k0 += 8) {
+        float4 x[8];
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                           // past the last part: the last one again, with factor 0
+            const int at = min(k0 + k, count - 1);
+            w[k] = k0 + k < count ? factor(at) : 0.f;
+            x[k] = *columns(at);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k0 + k >= count) continue;
+            o.x = fmaf(w[k], x[k].x, o.x); o.y = fmaf(w[k], x[k].y, o.y);
+            o.z = fmaf(w[k], x[k].z, o.z); o.w = fmaf(w[k], x[k].w, o.w);
+        }
+    }
+}
+__device__ __forceinline__ float lse_of(float2 ml) { return ml.y == 0.f ? -INFINITY : (ml.x == -INFINITY ? 0.f : ml.x) + logf(ml.y); }
 
-// Final values of four columns (of row `row` of out, all query heads of all sequences counted); no key left: zeros, -inf.
+// Final values of four columns of a row of out; no key left: zeros, -inf.
 template <typename TQ>
 __device__ __forceinline__ void emit4(const AttnProblem& p, long long row, int d, float vscale, float m, float l, float4 o) {
     const float f = vscale / l;
     put4(static_cast<TQ*>(p.out) + row * p.c.D + d,
          l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-    if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + logf(l);
+    if (p.lse && d == 0) p.lse[row] = lse_of(make_float2(m, l));
 }
 
 // What is joined in a CTA: the parts of warps first_warp .. first_warp + count - 1 of one (sequence, head).
@@ -205,7 +255,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ int piece_off[NW][2];                            // where O is in the ring
     __shared__ Chain chains[NW + 1];                            // that begin with piece 1 of warp w; NW: with piece 0 of warp 0
     __shared__ unsigned scan_warp[NW];
-    __shared__ int last_flag[2], out_chain;
+    __shared__ float factors[ROWS * (DP / 4) > NTHR ? 64 : 1][ROWS];
+    __shared__ int last_flag[2], all_flag, out_chain;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
 
@@ -226,6 +277,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &vmap : &kmap) : "memory");
     pdl_trigger();
     pdl_wait();
+    auto out_row = [&](long long row) { return static_cast<TQ*>(p.out) + row * p.c.D; };
     auto slot_of = [&](int i) { return p.seqs ? p.seqs[i] : i; };
     auto length_of = [&](int slot) {
         return slot >= 0 && slot < p.c.slots ? max(0, min(p.c.lengths[slot], p.c.max_pages * ps)) : 0;
@@ -312,7 +364,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     };
     // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.7 us, with two tiles
     // 9.3, with three 11.8: even then a join across CTAs costs less than a warp's second tile).
-    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW), tol = min(per / 2, 8);
+    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW), tol = min(per / 2, kSnap);
     auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
         if (c == 0) return 0;
         if ((long long)c * per >= total) return total;
@@ -746,11 +798,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             __syncwarp();
             const long long row0 = (long long)at.seq * p.q_heads + h * a.group + r0;
             if (whole) {
+                if (lane < rows) {                              // the factor takes the maximum's place
+                    const float2 ml = ml_of[warp][1][lane];
+                    if (p.lse) p.lse[row0 + lane] = lse_of(ml);
+                    ml_of[warp][1][lane].x = ml.y == 0.f ? 0.f : vscale / ml.y;
+                }
+                __syncwarp();
                 for (int e = lane; e < ROWS * (DP / 4); e += 32) {
                     const int r = e / (DP / 4), d = e % (DP / 4) * 4;
                     if (r >= rows || d >= p.c.D) continue;
-                    const float2 ml = ml_of[warp][1][r];
-                    emit4<TQ>(p, row0 + r, d, vscale, ml.x, ml.y, *reinterpret_cast<const float4*>(os + o_index(r, d, DP)));
+                    const float4 x = *reinterpret_cast<const float4*>(os + o_index(r, d, DP));
+                    const float f = ml_of[warp][1][r].x;
+                    put4(out_row(row0 + r) + d, f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
                 }
                 fence_proxy_async();                            // the stage was written by this warp; TMA writes it next
                 __syncwarp();
@@ -804,57 +863,156 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     //      arrives last ----
     auto global_part = [&](int cta, int slot) {
         float* const o = a.parts + ((size_t)cta * 2 + slot) * Sh::PART;
-        return Part{o, reinterpret_cast<const float2*>(o + ROWS * DP)};
+        return Part{o, reinterpret_cast<float2*>(o + ROWS * DP)};
     };
     unsigned some = 0;
 #pragma unroll
     for (int c = 0; c <= NW; ++c) some |= (chains[c].count ? 1u : 0u) << c;
+    constexpr int E = (ROWS * (DP / 4) + NTHR - 1) / NTHR;      // four columns each, of a thread
+    if constexpr (E == 1) {
+        const int r = tid / (DP / 4), d = tid % (DP / 4) * 4, at = o_index(r, d, DP);
 #pragma unroll 1
-    for (; some; some &= some - 1) {
-        const int c = __ffs(some) - 1;
-        const Chain& ch = chains[c];
-        const int count = ch.count, w0 = c == NW ? 0 : c;
-        for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
-            const int r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
+        for (unsigned left = some; left; left &= left - 1) {
+            const int c = __ffs(left) - 1, w0 = c == NW ? 0 : c;
+            const Chain& ch = chains[c];
             if (r >= ch.rows || d >= p.c.D) continue;
-            float m, l;
-            float4 o;
-            join4(count, [&](int k) {
-                const int from = k ? 0 : ch.from;
-                return Part{reinterpret_cast<const float*>(ring + piece_off[w0 + k][from]), ml_of[w0 + k][from]};
-            }, r, at, m, l, o);
+            float m = -INFINITY, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            join1(ch.count, [&](int k) { return ml_of[w0 + k][k ? 0 : ch.from][r]; },
+                  [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) + at); },
+                  m, l, o);
             if (ch.c0 == ch.c1) {
                 emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o);
             } else {
                 const Part q = global_part(blockIdx.x, ch.s0 >= cta_a);
-                *reinterpret_cast<float4*>(const_cast<float*>(q.o) + at) = o;
-                if (d == 0) const_cast<float2*>(q.ml)[r] = make_float2(m, l);
+                *reinterpret_cast<float4*>(q.o + at) = o;
+                if (d == 0) q.ml[r] = make_float2(m, l);
+            }
+        }
+    } else {
+        for (unsigned left = some; left; left &= left - 1) {
+            const int c = __ffs(left) - 1, w0 = c == NW ? 0 : c;
+            const Chain& ch = chains[c];
+            const bool final = ch.c0 == ch.c1;
+            for (int r = warp; r < ch.rows; r += NW) {              // the factors take the places of the maxima
+                auto ml = [&](int k) -> float2& { return ml_of[w0 + k][k ? 0 : ch.from][r]; };
+                const float2 all = join_factors(ch.count, ml, [&](int k, float f) { ml(k).x = f; }, final, ch.vscale, lane);
+                if (lane == 0) {
+                    if (!final) global_part(blockIdx.x, ch.s0 >= cta_a).ml[r] = all;
+                    else if (p.lse) p.lse[ch.row0 + r] = lse_of(all);
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (unsigned left = some; left; left &= left - 1) {
+            const int c = __ffs(left) - 1, w0 = c == NW ? 0 : c;
+            const Chain& ch = chains[c];
+#pragma unroll 2
+            for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
+                const int r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
+                if (r >= ch.rows || d >= p.c.D) continue;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                join4(ch.count, [&](int k) { return ml_of[w0 + k][k ? 0 : ch.from][r].x; },
+                      [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) + at); }, o);
+                if (ch.c0 == ch.c1) put4(out_row(ch.row0 + r) + d, o);
+                else *reinterpret_cast<float4*>(global_part(blockIdx.x, ch.s0 >= cta_a).o + at) = o;
             }
         }
     }
     const bool in = chains[NW].count && chains[NW].c0 != chains[NW].c1;   // shared with the CTA before / with the next one only
     if (!in && out_chain < 0) return;
+    // Up to kDirect parts are joined at once.  More (few long sequences with few heads) are joined in groups of kGroup, by the last
+    // to arrive of each group, and the groups by the last of these: 148 parts take two short joins instead of one long one.
+    constexpr int kDirect = Sh::CAP < 48 ? Sh::CAP : 48, kGroup = 12;
     __threadfence();
     __syncthreads();
     if (tid < 64 && lane == 0) {
-        const int c = warp == 0 ? (in ? NW : -1) : out_chain;
-        const unsigned wrap = c < 0 ? 0u : (unsigned)(chains[c].c1 - chains[c].c0);
-        last_flag[warp] = c >= 0 && atomicInc(&a.counters[chains[c].c0], wrap) == wrap;
+        bool last = false;
+        if (warp == 0 ? in : out_chain >= 0) {
+            const Chain& ch = chains[warp == 0 ? NW : out_chain];
+            const int count = ch.c1 - ch.c0 + 1, first = (blockIdx.x - ch.c0) / kGroup * kGroup;    // of this CTA's group
+            const unsigned wrap = (count <= kDirect ? count : min(kGroup, count - first)) - 1;
+            // a CTA can be the first of a group of the (sequence, head) it begins in, and the beginning of another one
+            unsigned* const counter = a.counters + (count <= kDirect ? ch.c0 : first == 0 ? kMaxCtas + ch.c0 : 2 * kMaxCtas + ch.c0 + first);
+            last = atomicInc(counter, wrap) == wrap;
+        }
+        last_flag[warp] = last;
     }
     __syncthreads();
+
+    // Joins `count` parts (at most 64), copied to shared memory as many as fit at a time.
+    auto gather = [&](const Chain& ch, int count, auto part_of, bool final, Part to) {
+        float m = -INFINITY, l = 0.f;
+        float4 o[E];
+#pragma unroll
+        for (int x = 0; x < E; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < count; k0 += Sh::CAP) {
+            const int now = min(Sh::CAP, count - k0);
+            __syncthreads();                                    // the ring has been read
+            for (int k = warp; k < now; k += NW) {
+                const float* const src = part_of(k0 + k).o;
+                const uint32_t dst = smem_u32(ring) + k * (Sh::PART * 4);
+#pragma unroll
+                for (int x = lane; x < Sh::PART / 4; x += 32) cp_async16(dst + x * 16, src + x * 4, true);
+            }
+            cp_async_commit();
+            if (E > 1 && k0 == 0)                               // meanwhile the factors of all parts
+                for (int r = warp; r < ch.rows; r += NW) {
+                    const float2 all = join_factors(count, [&](int k) { return __ldcg(&part_of(k).ml[r]); },
+                                                    [&](int k, float f) { factors[k][r] = f; }, final, ch.vscale, lane);
+                    if (lane == 0) {
+                        if (!final) to.ml[r] = all;
+                        else if (p.lse) p.lse[ch.row0 + r] = lse_of(all);
+                    }
+                }
+            cp_async_wait<0>();
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                const int e = tid + x * NTHR, r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
+                if (r >= ch.rows || d >= p.c.D) continue;
+                auto columns = [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring) + k * Sh::PART + at); };
+                if constexpr (E == 1)
+                    join1(now, [&](int k) { return reinterpret_cast<const float2*>(reinterpret_cast<const float*>(ring) + k * Sh::PART + ROWS * DP)[r]; },
+                          columns, m, l, o[x]);
+                else
+                    join4(now, [&](int k) { return factors[k0 + k][r]; }, columns, o[x]);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < E; ++x) {
+            const int e = tid + x * NTHR, r = e / (DP / 4), d = e % (DP / 4) * 4;
+            if (r >= ch.rows || d >= p.c.D) continue;
+            if (final) {
+                if constexpr (E == 1) emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o[x]);
+                else put4(out_row(ch.row0 + r) + d, o[x]);
+            } else {
+                *reinterpret_cast<float4*>(to.o + o_index(r, d, DP)) = o[x];
+                if (E == 1 && d == 0) to.ml[r] = make_float2(m, l);
+            }
+        }
+    };
 #pragma unroll 1
     for (int x = 0; x < 2; ++x) {
         if (!last_flag[x]) continue;
         __threadfence();
         const Chain& ch = chains[x == 0 ? NW : out_chain];
-        for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
-            const int r = e / (DP / 4), d = e % (DP / 4) * 4;
-            if (r >= ch.rows || d >= p.c.D) continue;
-            float m, l;
-            float4 o;
-            join4(ch.c1 - ch.c0 + 1, [&](int k) { return global_part(ch.c0 + k, k == 0); }, r, o_index(r, d, DP), m, l, o);
-            emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o);
-        }
+        const int c0 = ch.c0, count = ch.c1 - c0 + 1;
+        const bool grouped = count > kDirect;
+        const int first = grouped ? (blockIdx.x - c0) / kGroup * kGroup : 0, members = grouped ? min(kGroup, count - first) : count;
+        // a group's result lies as far behind its first part as there are parts
+        auto group_part = [&](int k) { return global_part(kMaxCtas + c0 + k * kGroup, k == 0); };
+        gather(ch, members, [&](int k) { return global_part(c0 + first + k, first + k == 0); }, !grouped, group_part(first / kGroup));
+        if (!grouped) continue;
+        const int groups = (count + kGroup - 1) / kGroup;
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) all_flag = atomicInc(&a.counters[c0], (unsigned)(groups - 1)) == (unsigned)(groups - 1);
+        __syncthreads();
+        if (!all_flag) continue;
+        __threadfence();
+        gather(ch, groups, group_part, true, Part{});
     }
 }
 
@@ -913,7 +1071,7 @@ int launch(const AttnProblem& p) {
     a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
     a.counters = static_cast<unsigned*>(p.workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kMaxCtas * sizeof(unsigned));
+    a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kCounterBytes);
     CUtensorMap kmap, vmap;
     if (!layer_map<TC>(&kmap, p.c, p.c.k, p.layer, a.rows_total) || !layer_map<TC>(&vmap, p.c, p.c.v, p.layer, a.rows_total))
         return LUVC_ERR_CUDA;
@@ -939,7 +1097,7 @@ int launch_heads(const AttnProblem& p) {
 
 }  // namespace
 
-size_t attn_workspace_bytes() { return align_up(kMaxCtas * sizeof(unsigned)) + (size_t)kMaxCtas * 2 * kMaxPartBytes; }
+size_t attn_workspace_bytes() { return kCounterBytes + (size_t)2 * kMaxCtas * 2 * kMaxPartBytes; }
 
 int attn_decode(const AttnProblem& p) {
     const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
