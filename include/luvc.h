@@ -443,7 +443,8 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
  * sizes       optional DEVICE [tokens] int32, the out_sizes of luvc_oim_merge*: the values are written
  *             enhanced, V + log(size) (Eq. 2), formed in fp32 and rounded once
  * An E4M3 cache stores x / scale, saturated at +-448, rounded to nearest even.  Rows that would fall before
- * the start of their sequence are not written (LUVC_ERR_SHAPE in the status word).
+ * the start of their sequence are not written (LUVC_ERR_SHAPE in the status word).  Tokens that a fork shares are
+ * shared: writing them again writes them for every sequence that holds their page.
  */
 int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,
                   long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes,
@@ -475,7 +476,7 @@ int luvc_kv_compact(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
 
 /* ---- attention of one new token ------------------------------------------- */
 
-/* Bytes of workspace luvc_attn_decode needs on the current device, whatever the sequences; 0 on error. */
+/* Bytes of workspace luvc_attn_decode needs, whatever the sequences and heads (about 17 MB). */
 size_t luvc_attn_workspace_bytes(void);
 
 typedef struct {

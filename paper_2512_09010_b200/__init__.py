@@ -449,6 +449,7 @@ _CACHE_DTYPES = {torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: 
 # A decode step makes many small calls, so what these bindings do per call is kept short: the stream's handle without a
 # torch.cuda.Stream object, no device context where the cache's device is current already, one comparison per rule.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _INT32 = torch.int32
 
 
@@ -456,8 +457,7 @@ def _ints(t: torch.Tensor | None, cache: KvCache, count: int, name: str):
     """Address of a contiguous int32 tensor [count] on the cache's device (None: NULL)."""
     if t is None:
         return None
-    if t.dtype is not _INT32 or t.dim() != 1 or t.numel() != count or not t.is_cuda or t.get_device() != cache.index \
-            or not t.is_contiguous():
+    if t.dtype is not _INT32 or t.dim() != 1 or t.numel() != count or t.get_device() != cache.index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 tensor of %d entries on %s" % (name, count, cache.device))
     return t.data_ptr()
 
@@ -471,16 +471,15 @@ def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
     return o
 
 
-def _kv_call(where: str, cache: KvCache, *args) -> None:
-    """lib.<where>(*args) with the cache's device current."""
-    fn = getattr(lib, where)
-    if torch.cuda.current_device() == cache.index:
+def _kv_call(fn, cache: KvCache, *args) -> None:
+    """fn(*args) with the cache's device current; an error status raises."""
+    if _current_device() == cache.index:
         status = fn(*args)
     else:
         with torch.cuda.device(cache.index):
             status = fn(*args)
     if status != 0:
-        raise LuvcError(status, where)
+        raise LuvcError(status, fn.__name__)
 
 
 def kv_workspace_bytes(cache: KvCache, n: int) -> int:
@@ -495,21 +494,22 @@ def kv_reserve(cache: KvCache, counts: torch.Tensor, *, seqs: torch.Tensor | Non
                device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_reserve: room for counts[i] further tokens of each sequence (int32 [n]); seqs: slots (None: 0 .. n-1)."""
     n = counts.numel()
-    _kv_call("luvc_kv_reserve", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(counts, cache, n, "counts"),
+    _kv_call(lib.luvc_kv_reserve, cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(counts, cache, n, "counts"),
              _kv_opts(cache, None, device_status))
 
 
 def _token_stride(t: torch.Tensor, cache: KvCache, heads: int, name: str) -> int:
     """Elements from one token to the next of a [tokens, heads, D] tensor whose tokens are contiguous."""
     D = cache.head_dim
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or not t.is_cuda or t.get_device() != cache.index:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != D or t.get_device() != cache.index:
         raise ValueError("%s must be [tokens, %d, %d] on %s" % (name, heads, D, cache.device))
     if t.dtype is not cache.io_dtype:
         raise TypeError("%s must be %s for a %s cache, got %s" % (name, cache.io_dtype, cache.dtype, t.dtype))
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != D and heads > 1):
         raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
-    return s0 if t.shape[0] > 1 else max(s0, heads * D)
+    return s0 if shape[0] > 1 else max(s0, heads * D)
 
 
 def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0, starts: torch.Tensor | None = None,
@@ -523,7 +523,7 @@ def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0
     ks, vs = _token_stride(k, cache, cache.heads, "k"), _token_stride(v, cache, cache.heads, "v")
     if v.shape[0] != tokens:
         raise ValueError("k and v must have one shape")
-    _kv_call("luvc_kv_write", cache, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, k.data_ptr(), v.data_ptr(), ks, vs,
+    _kv_call(lib.luvc_kv_write, cache, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, k.data_ptr(), v.data_ptr(), ks, vs,
              tokens, _ints(starts, cache, n + 1, "starts"), _ints(sizes, cache, tokens, "sizes"), cache.io_code,
              _kv_opts(cache, None, device_status))
 
@@ -532,14 +532,14 @@ def kv_fork(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, *, workspace: 
             device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_fork: the empty slots dst (int32 [n]) become copies of the sequences src (int32 [n]); full pages are shared."""
     n = dst.numel()
-    _kv_call("luvc_kv_fork", cache, cache.struct, _ints(src, cache, n, "src"), _ints(dst, cache, n, "dst"), n,
+    _kv_call(lib.luvc_kv_fork, cache, cache.struct, _ints(src, cache, n, "src"), _ints(dst, cache, n, "dst"), n,
              _kv_opts(cache, workspace, device_status))
 
 
 def kv_free(cache: KvCache, seqs: torch.Tensor, *, device_status: torch.Tensor | None = None) -> None:
     """luvc_kv_free: empties the slots seqs (int32 [n]); pages nobody holds any more are free again."""
     n = seqs.numel()
-    _kv_call("luvc_kv_free", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _kv_opts(cache, None, device_status))
+    _kv_call(lib.luvc_kv_free, cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _kv_opts(cache, None, device_status))
 
 
 def kv_compact(cache: KvCache, first: torch.Tensor, span: torch.Tensor, idx: torch.Tensor, *,
@@ -548,7 +548,7 @@ def kv_compact(cache: KvCache, first: torch.Tensor, span: torch.Tensor, idx: tor
     """luvc_kv_compact: of the block of span[i] tokens from first[i] on, sequence i keeps the tokens idx[i] (int32
     [n, keep], relative to the block, ascending: the out_idx of spu_prune) and everything outside the block."""
     n, keep = idx.shape
-    _kv_call("luvc_kv_compact", cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(first, cache, n, "first"),
+    _kv_call(lib.luvc_kv_compact, cache, cache.struct, _ints(seqs, cache, n, "seqs"), n, _ints(first, cache, n, "first"),
              _ints(span, cache, n, "span"), _ints(idx.view(-1), cache, n * keep, "idx") if keep else None, keep,
              _ints(counts, cache, n, "counts"), _kv_opts(cache, workspace, device_status))
 
@@ -573,7 +573,7 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     if device_status is not None:
         o.device_status = device_status.data_ptr()
     if key_bias is not None:
-        if key_bias.dtype is not torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n or not key_bias.is_cuda \
+        if key_bias.dtype is not torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n \
                 or key_bias.get_device() != cache.index or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):
             raise ValueError("key_bias must be a float32 [n, width] tensor on the cache's device, its rows contiguous")
         o.key_bias, o.bias_width = key_bias.data_ptr(), key_bias.shape[1]
@@ -582,6 +582,6 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     if want_lse:
         lse = torch.empty((n, q_heads), dtype=torch.float32, device=q.device)
         o.lse = lse.data_ptr()
-    _kv_call("luvc_attn_decode", cache, q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, q_heads,
+    _kv_call(lib.luvc_attn_decode, cache, q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, q_heads,
              cache.io_code, out.data_ptr(), o)
     return (out, lse) if want_lse else out

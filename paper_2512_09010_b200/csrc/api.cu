@@ -80,17 +80,20 @@ int* status_word() {
     return static_cast<int*>(p);
 }
 
-// The current device's attention workspace: allocated and zeroed once (the kernel leaves it zeroed where it must be).
+// The current device's attention workspace: allocated and zeroed once (the kernel leaves it zeroed where it must be).  The lock
+// is held until the zeros are there: another thread's first call must not find the memory without them.
 void* attn_scratch() {
+    static std::mutex first_use;
     const int dev = current_device();
     if (dev < 0) return nullptr;
+    std::lock_guard<std::mutex> lock(first_use);
     {
-        std::lock_guard<std::mutex> lock(g_mutex);
+        std::lock_guard<std::mutex> inner(g_mutex);
         if (g_scratch[dev][kAttnWs].ptr) return g_scratch[dev][kAttnWs].ptr;
     }
     const size_t bytes = attn_workspace_bytes();
-    void* p = bytes ? scratch(kAttnWs, bytes) : nullptr;
-    if (p && cudaMemset(p, 0, bytes) != cudaSuccess) return nullptr;
+    void* p = scratch(kAttnWs, bytes);
+    if (p && (cudaMemset(p, 0, bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess)) return nullptr;
     return p;
 }
 
@@ -249,7 +252,8 @@ int luvc_check_status(void* cuda_stream) {
         const int dev = current_device();
         std::lock_guard<std::mutex> lock(g_mutex);
         const Scratch& sc = g_scratch[dev < 0 ? 0 : dev][kAttnWs];
-        if (dev >= 0 && sc.ptr && cudaMemset(sc.ptr, 0, sc.bytes) != cudaSuccess) return LUVC_ERR_CUDA;
+        if (dev >= 0 && sc.ptr && (cudaMemset(sc.ptr, 0, sc.bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess))
+            return LUVC_ERR_CUDA;
     }
     return status;
 }

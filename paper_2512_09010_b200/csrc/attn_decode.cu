@@ -26,7 +26,8 @@
 // that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
 // largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats (16 bits at least), because one
 // 16-bit float would cost as much again as the output's own rounding; tensor time is not the bound.  f32 caches use
-// tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 21 bits).  Sums, maxima and O are fp32.
+// tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 23 bits), or, where few heads share a row, fp32 on the CUDA cores.
+// Sums, maxima and O are fp32.
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -89,6 +90,16 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
     asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(d) : "r"(two));
     return d;
 }
+__device__ __forceinline__ float4 lds4(uint32_t addr) {
+    float4 x;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ float2 lds2(uint32_t addr) {
+    float2 x;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(addr) : "memory");
+    return x;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -103,18 +114,19 @@ __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& l
 // ---- shapes ---------------------------------------------------------------------------------------------
 
 // TC: element of the cache; DPB: bytes of a row in shared memory, a multiple of 128 (columns past D are filled with zeros by
-// TMA); NT: groups of 8 query heads per key head that one tile is multiplied with.
+// TMA); NT: groups of 8 query heads per key head that one tile is multiplied with, or, f32 only, -NT query heads on the CUDA cores.
 template <typename TC, int DPB_, int NT_>
 struct Shape {
     static constexpr int DPB = DPB_, NT = NT_, ES = sizeof(TC), DP = DPB / ES, SEGS = DPB / 128;
     static constexpr int SUBK = 16 * DPB;                       // bytes of 16 rows
     // 16-token parts of a tile: one, or as many as make a stage large enough for a partial result (8 NT rows of DP floats).
     static constexpr int SUB = NT > ES ? 2 : 1;
+    static constexpr bool CORES = NT < 0;
     static constexpr int KT = 16 * SUB, STAGE = SUB * 2 * SUBK;
     // three stages for each warp, 196,608 bytes in all: the more warps the smaller a row is
     static constexpr int S = 3, NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
-    static constexpr int ROWS = 8 * NT;
+    static constexpr int ROWS = CORES ? 4 : 8 * NT;
     static constexpr int PART = ROWS * (DP + 2);                // floats of a partial result in the workspace: O, then (m, l) of each row
     static constexpr int CAP = NW * S * STAGE / (PART * 4);     // partial results the ring has room for
     static_assert(PART * 4 <= kMaxPartBytes, "the workspace has room for less");
@@ -242,12 +254,99 @@ struct Chain {
     long long row0;             // first row of out
 };
 
+// A tile of 16 tokens of an f32 cache on the CUDA cores, for NH query heads: where few heads share a key head, splitting rows for the
+// tensor cores costs more than the products (one head of 64: 130 instead of 620 instructions).  Scores: two lanes per token, half a
+// row each; weighted values: DP / 32 columns per lane.  qs: [NH][DP], ps: [NH][16] of this warp.  bias: of token lane & 15; gone:
+// one bit for each masked token.
+template <int DP, int NH>
+__device__ __forceinline__ void f32_tile(uint32_t ks, uint32_t vs, const float* qs, float* ps, float scale, float bias, unsigned gone,
+                                         float (&m)[NH], float (&l)[NH], float (&o)[NH][DP / 32], int lane) {
+    const int key = lane & 15, half = lane >> 4;
+    float s[NH][2];
+#pragma unroll
+    for (int h = 0; h < NH; ++h) s[h][0] = s[h][1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+        const int c = half * (DP / 8) + i;
+        const float4 k = lds4(ks + (c >> 3) * 2048 + key * 128 + (((c & 7) ^ (key & 7)) << 4));
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const float4 q = *reinterpret_cast<const float4*>(qs + h * DP + c * 4);
+            s[h][0] = fmaf(q.x, k.x, s[h][0]); s[h][1] = fmaf(q.y, k.y, s[h][1]);
+            s[h][0] = fmaf(q.z, k.z, s[h][0]); s[h][1] = fmaf(q.w, k.w, s[h][1]);
+        }
+    }
+    bool over = false;
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+        float x = s[h][0] + s[h][1];
+        x += __shfl_xor_sync(~0u, x, 16);
+        x = (gone >> key) & 1u ? -INFINITY : fmaf(x, scale, bias);
+        s[h][0] = x;
+        over = over || x > m[h] + kSlack;
+    }
+    if (__any_sync(~0u, over)) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            float x = s[h][0];
+#pragma unroll
+            for (int d = 8; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+            x = fmaxf(x, m[h]);
+            const float f = exp2_fast((m[h] - (x == -INFINITY ? 0.f : x)) * kLog2e);
+            m[h] = x;
+            l[h] *= f;
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) o[h][j] *= f;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+        const float p = exp2_fast((s[h][0] - (m[h] == -INFINITY ? 0.f : m[h])) * kLog2e);
+        l[h] += p;
+        if (half == 0) ps[h * 16 + key] = p;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k4 = 0; k4 < 4; ++k4) {
+        float4 p[NH];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) p[h] = *reinterpret_cast<const float4*>(ps + h * 16 + 4 * k4);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int row = 4 * k4 + x;
+            if ((gone >> row) & 1u) continue;                   // a masked row may hold anything
+            float v[DP / 32];
+            if constexpr (DP == 64) {
+                const float2 y = lds2(vs + (lane >> 4) * 2048 + row * 128 + ((((lane & 15) >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8);
+                v[0] = y.x; v[1] = y.y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < DP / 128; ++i) {
+                    const float4 y = lds4(vs + (4 * i + (lane >> 3)) * 2048 + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                    v[4 * i] = y.x; v[4 * i + 1] = y.y; v[4 * i + 2] = y.z; v[4 * i + 3] = y.w;
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+                const float w = x == 0 ? p[h].x : x == 1 ? p[h].y : x == 2 ? p[h].z : p[h].w;
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) o[h][j] = fmaf(w, v[j], o[h][j]);
+            }
+        }
+    }
+    __syncwarp();                                               // ps is written again
+}
+// Column of a lane's element j in the form above.
+template <int DP>
+__device__ __forceinline__ int f32_column(int lane, int j) { return DP == 64 ? 2 * lane + j : 128 * (j >> 2) + 4 * lane + (j & 3); }
+
 template <typename TQ, typename TC, int DPB, int NT>
 __global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ Args a) {
     using Sh = Shape<TC, DPB, NT>;
     constexpr int NW = Sh::NW, S = Sh::S, MT = Sh::MT, DP = Sh::DP, ROWS = Sh::ROWS, KT = Sh::KT, NTHR = 32 * NW;
-    constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1;
+    constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1, kCores = Sh::CORES;
+    constexpr int NTX = kCores ? 1 : NT, NH = kCores ? -NT : 1; // sizes of arrays that are not used otherwise
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[NW * S];
     __shared__ float2 ml_of[NW][2][ROWS];
@@ -255,6 +354,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ int piece_off[NW][2];                            // where O is in the ring
     __shared__ Chain chains[NW + 1];                            // that begin with piece 1 of warp w; NW: with piece 0 of warp 0
     __shared__ unsigned scan_warp[NW];
+    __shared__ __align__(16) float core_q[kCores ? NW : 1][kCores ? NH * DP : 4], core_p[kCores ? NW : 1][NH * 16];
     __shared__ float factors[ROWS * (DP / 4) > NTHR ? 64 : 1][ROWS];
     __shared__ int last_flag[2], all_flag, out_chain;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -470,8 +570,16 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             // queries: B operand of S^T = K Q^T, head g of each group of 8
             const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
             constexpr int KS = DPB / 32;                        // steps of 32 bytes of a row
-            uint32_t q[NT][KS][kF8 ? 4 : 2];
-            float qmul[NT][2];
+            uint32_t q[NTX][KS][kF8 ? 4 : 2];
+            float qmul[NTX][2];
+            if constexpr (kCores) {
+                __syncwarp();                                   // the queries before have been used
+                for (int x = lane; x < NH * DP; x += 32) {
+                    const int r = x / DP, d = x % DP;
+                    core_q[warp][x] = r < rows && d < p.c.D ? reinterpret_cast<const float*>(qrow)[r * p.c.D + d] : 0.f;
+                }
+                __syncwarp();
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const TQ* const qh = qrow + (long long)(nt * 8 + g) * p.c.D;
@@ -522,7 +630,16 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 }
             }
 
-            float m[NT][2], l[NT][2], o[MT][NT][4];
+            float core_m[NH], core_l[NH], core_o[NH][DP / 32];
+            if constexpr (kCores)
+#pragma unroll
+                for (int h2 = 0; h2 < NH; ++h2) {
+                    core_m[h2] = -INFINITY;
+                    core_l[h2] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < DP / 32; ++j) core_o[h2][j] = 0.f;
+                }
+            float m[NTX][2], l[NTX][2], o[MT][NTX][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY, l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
@@ -551,7 +668,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     for (int j = 0; j < Sh::SUB; ++j)
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            const int token = at.tile * KT + 16 * j + 8 * x + g;
+                            const int token = at.tile * KT + 16 * j + (kCores ? lane & 15 : 8 * x + g);
                             if (token >= len) bias[j][x] = -INFINITY;
                             else if (token < p.bias_width) bias[j][x] = p.bias[at.seq * p.bias_stride + token];
                         }
@@ -566,13 +683,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 for (int j = 0; j < Sh::SUB; ++j) {
                     if (j > 0 && at.tile * KT + 16 * j >= len) break;
                     const uint32_t ks = my_ring_s + stage * Sh::STAGE + j * 2 * Sh::SUBK, vs = ks + Sh::SUBK;
+                    if constexpr (kCores) {
+                        const unsigned gone = masked ? __ballot_sync(~0u, bias[j][0] == -INFINITY) & 0xffffu : 0u;
+                        f32_tile<DP, NH>(ks, vs, core_q[warp], core_p[warp], scale, bias[j][0], gone, core_m, core_l, core_o, lane);
+                        continue;
+                    }
                     // ---- S^T: rows are the 16 tokens, columns the query heads ----
-                    float s[NT][4], s2[NT][4];
+                    float s[NTX][4], s2[NTX][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
-                    float done[NT][4];                          // f32: finished sums of S
+                    float done[NTX][4];                         // f32: finished sums of S
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -661,8 +783,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             const float mb = m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1];
                             s[nt][c] = exp2_fast((s[nt][c] - mb) * kLog2e);
                         }
-                    uint32_t ph[NT][2], pl[NT][2];              // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
-                    float pf[NT][4];
+                    uint32_t ph[NTX][2], pl[NTX][2];            // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
+                    float pf[NTX][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         l[nt][0] += s[nt][0] + s[nt][2];
@@ -701,7 +823,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         for (int x = 0; x < 2; ++x) {
                             const uint32_t keep = x ? keep1 : keep0;
                             const bool drop0 = !(keep & 0xffffu), drop1 = !(keep >> 16);
-                            uint32_t bh[NT][2], bl[NT][2];
+                            uint32_t bh[NTX][2], bl[NTX][2];
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 split_tf32(__float_as_uint(pf[nt][2 * x]), bh[nt][0], bl[nt][0]);
@@ -776,6 +898,17 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             // ---- the result, through the stage that was read last ----
             float* const os = reinterpret_cast<float*>(my_ring + stage * Sh::STAGE);
             const int which = at.tile > count ? 0 : 1;          // 0: it began in the part of the warp before
+            if constexpr (kCores) {
+#pragma unroll
+                for (int r = 0; r < NH; ++r) {
+                    float x = core_l[r];
+#pragma unroll
+                    for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+                    if (lane == 0) ml_of[warp][which][r] = make_float2(core_m[r], x);
+#pragma unroll
+                    for (int j = 0; j < DP / 32; ++j) os[o_index(r, f32_column<DP>(lane, j), DP)] = core_o[r][j];
+                }
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -1081,8 +1214,10 @@ int launch(const AttnProblem& p) {
     if (cudaGetDevice(&dev) != cudaSuccess) return LUVC_ERR_CUDA;
     if (dev > 63 || !((set.load(std::memory_order_relaxed) >> dev) & 1)) {
         if (cudaFuncSetAttribute(attn_decode_kernel<TQ, TC, DPB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 1024 + Sh::NW * Sh::S * Sh::STAGE + (kKvMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess)
+                                 1024 + Sh::NW * Sh::S * Sh::STAGE + (kKvMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess) {
+            cudaGetLastError();
             return LUVC_ERR_CUDA;
+        }
         if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     const int sms = sm_count();
@@ -1095,12 +1230,22 @@ int launch_heads(const AttnProblem& p) {
     return p.q_heads / p.c.heads <= 8 ? launch<TQ, TC, DPB, 1>(p) : launch<TQ, TC, DPB, 2>(p);
 }
 
+// f32 caches with up to four query heads per key head run on the CUDA cores (measured, against the tensor cores: 32 / 32 heads of
+// 128, 812 MB, 141 and 200 us; 16 / 16 of 64, 131 MB, 30.0 and 32.7; 32 / 8 of 128, 203 MB, 54 and 64; 8 / 8 of 256, 406 MB, 94 and
+// 226).  The queries of more heads would not fit shared memory beside the ring.
+template <int DPB>
+int launch_cores(const AttnProblem& p) {
+    return p.q_heads == p.c.heads ? launch<float, float, DPB, -1>(p) : launch<float, float, DPB, -4>(p);
+}
+
 }  // namespace
 
 size_t attn_workspace_bytes() { return kCounterBytes + (size_t)2 * kMaxCtas * 2 * kMaxPartBytes; }
 
 int attn_decode(const AttnProblem& p) {
     const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
+    if (p.c.dtype == LUVC_F32 && p.q_heads <= 4 * p.c.heads)
+        return bytes <= 256 ? launch_cores<256>(p) : bytes <= 512 ? launch_cores<512>(p) : launch_cores<1024>(p);
     if (p.c.dtype == LUVC_F32)
         return bytes <= 256 ? launch_heads<float, float, 256>(p) : bytes <= 512 ? launch_heads<float, float, 512>(p) : launch<float, float, 1024, 1>(p);
     if (p.c.dtype == LUVC_BF16)

@@ -632,8 +632,10 @@ int sm_count() {
 template <PlanKind KIND>
 int launch_plan(const PlanArgs& a, cudaStream_t stream) {
     const size_t smem = (size_t)(4 * a.n + 1) * sizeof(int);
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
         return LUVC_ERR_CUDA;
+    }
     return launch_overlapped(kv_plan_kernel<KIND>, 1, kPlanThreads, smem, stream, a);
 }
 

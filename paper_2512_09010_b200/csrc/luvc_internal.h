@@ -28,8 +28,12 @@ int launch_overlapped(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, 
     cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
     cfg.attrs = &attr; cfg.numAttrs = 1;
     const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    if (rc != cudaSuccess) {
+        cudaGetLastError();     // reported here, not by the next call
+        return LUVC_ERR_CUDA;
+    }
     count_launch();
-    return rc == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+    return LUVC_OK;
 }
 
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
@@ -219,7 +223,7 @@ struct AttnProblem {
     int* status;
     cudaStream_t stream;
 };
-size_t attn_workspace_bytes();      // 0: no device
+size_t attn_workspace_bytes();
 int attn_decode(const AttnProblem& p);
 
 }  // namespace luvc

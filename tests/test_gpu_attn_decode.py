@@ -118,6 +118,7 @@ SHAPES = [  # type, query heads, key heads, D, page
     ("bf16", 17, 1, 8, 16), ("bf16", 10, 2, 104, 16), ("bf16", 32, 1, 192, 16), ("bf16", 66, 2, 64, 16),
     ("e4m3", 28, 4, 128, 16), ("e4m3", 8, 8, 64, 32), ("e4m3", 12, 1, 256, 64), ("e4m3", 6, 3, 80, 16), ("e4m3", 40, 2, 48, 16),
     ("e4m3", 3, 1, 144, 16),
+    ("f32", 3, 1, 128, 16), ("f32", 12, 3, 256, 16), ("f32", 2, 2, 256, 32), ("f32", 5, 5, 100, 16), ("f32", 8, 2, 64, 64),
     ("f32", 16, 16, 64, 16), ("f32", 28, 4, 128, 48), ("f32", 4, 2, 20, 16), ("f32", 9, 1, 256, 16), ("f32", 34, 2, 68, 32),
 ]
 LENGTHS = [[1], [0, 1, 15, 16, 17, 0], [31, 32, 33, 100, 2, 5, 64, 63], [700, 1, 0, 1297], [4100]]
@@ -134,7 +135,7 @@ def test_ragged_sequences(luvc, shape, lengths):
     check(luvc, c, q, out, lse)
 
 
-@pytest.mark.parametrize("dtype,heads,D", [("bf16", 8, 128), ("e4m3", 4, 128), ("f32", 2, 64), ("bf16", 1, 64)])
+@pytest.mark.parametrize("dtype,heads,D", [("bf16", 8, 128), ("e4m3", 4, 128), ("f32", 2, 64), ("bf16", 1, 64), ("f32", 1, 256)])
 def test_long_and_many(luvc, dtype, heads, D):
     lengths = [16451, 3, 9000, 1] if heads > 1 else [40000]
     c = build(luvc, dtype, lengths, heads, D, 64, seed=5, nan=True)
@@ -144,6 +145,17 @@ def test_long_and_many(luvc, dtype, heads, D):
     c = build(luvc, dtype, lengths, heads, D, 16, seed=6)
     q = torch.randn((600, 4 * heads, D), generator=torch.Generator().manual_seed(2)).to(c.io_dtype).cuda()
     check(luvc, c, q, *luvc.attn_decode(q, c, want_lse=True))
+
+
+@pytest.mark.parametrize("dtype,q_heads,heads,D,tokens", [("bf16", 12, 1, 256, 30000), ("bf16", 32, 1, 128, 50000), ("e4m3", 8, 1, 128, 60000),
+                                                          ("f32", 7, 1, 256, 9000), ("bf16", 2, 2, 8, 40000)])
+def test_one_long_sequence_is_joined_across_all_ctas(luvc, dtype, q_heads, heads, D, tokens):
+    c = build(luvc, dtype, [tokens], heads, D, 32, seed=D)
+    q = torch.randn((1, q_heads, D), generator=torch.Generator().manual_seed(D)).to(c.io_dtype).cuda()
+    out, lse = luvc.attn_decode(q, c, want_lse=True)
+    check(luvc, c, q, out, lse)
+    for _ in range(4):
+        assert torch.equal(luvc.attn_decode(q, c), out)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3", "f32"])
