@@ -5,23 +5,26 @@
 // in one pass: a running maximum m, the sum l of the weights so far and their weighted sum O of value rows; when m grows,
 // l and O are scaled by exp(m_old - m_new).  Partial results of parts of a sequence join by the same rule.
 //
-// Bound.  Every cached row is read once, for all query heads that share it: 4 * G flops per element of K and V with G query
-// heads per key head, so HBM bounds it up to the largest G in use; what matters is to keep enough bytes in flight on every
-// SM, whatever the lengths.
+// Bound.  Every cached row is read once, for all query heads that share it: 2 G flops per cached element with G query heads
+// per key head, so HBM bounds long sequences up to the largest G in use, and latency short ones; what matters is to keep enough
+// bytes in flight on every SM, whatever the lengths.  Measured: 334 MB (eight sequences of 4173 to 16451 tokens, 8 key heads of 128,
+// bf16) in 62.7 us, 5.3 TB/s; while all SMs stream it is 7.2 TB/s, but SMs differ by a tenth in the bandwidth they get, and
+// the last 9 us belong to the slow ones.  The smallest call (one sequence of 97 tokens) takes 4.8 us.
 //
 // Split.  The work is the list of all tiles (KT tokens of one sequence and key head), sequence after sequence.  Each CTA (one per
 // SM) takes an equal part of that list, each of its warps an equal part of the CTA's, so no length leaves an SM idle and a
 // lone long sequence uses the whole GPU.  A warp works alone: it has a ring of stages in shared memory that TMA fills
-// (lane 0 issues; the page numbers of the next 32 pages are held one per lane), and it emits every
+// (a lane per box issues; the page numbers of the next 32 pages are held one per lane), and it emits every
 // (sequence, head) that lies wholly in its part.  Of the others a warp has at most two, at the ends of its part; their
 // partial results stay in the ring stage that was read last (that stage is not filled again) and are joined by the CTA
 // when its warps are done, then, where a sequence crosses CTAs, through the workspace by the CTA that comes last (a counter that
 // wraps to zero; the parts are added in the order of the list, so results do not depend on which that is).
 //
-// Matrix instructions.  With one query token the product of a tile has up to 16 columns (the query heads of a key head), too few
-// rows for tcgen05 (its M is 64 at least, over rows that would have to be loaded for one token); at 4 G flops per element the
-// warp-level mma.sync, keys as the M of m16n8k16 and query heads as its N, is far from being the bound.  S^T = K Q^T with K from
-// ldmatrix, then O^T += V^T P^T with V from ldmatrix.trans and P^T from the scores' registers by movmatrix.
+// Matrix instructions.  The products are narrow, 8 or 16 columns (the query heads of a key head): mma.sync m16n8k16 with tokens, or
+// columns of V, as M and query heads as N.  S^T = K Q^T with K from ldmatrix, then O^T += V^T P^T with V from
+// ldmatrix.trans and P^T from the scores' registers by movmatrix.  tcgen05 would want 128 tokens at a time and four warps in
+// step for each read of tensor memory; warps that work alone on 16 tokens suit short and ragged sequences, and the tensor
+// pipe is not the bound (18 % busy with an e4m3 cache).
 // Roundings: Q and K are used as they are (an e4m3 cache goes to f16, which is exact; the query, scaled by a power of two so
 // that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
 // largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats (16 bits at least), because one
@@ -686,200 +689,200 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     if constexpr (kCores) {
                         const unsigned gone = masked ? __ballot_sync(~0u, bias[j][0] == -INFINITY) & 0xffffu : 0u;
                         f32_tile<DP, NH>(ks, vs, core_q[warp], core_p[warp], scale, bias[j][0], gone, core_m, core_l, core_o, lane);
-                        continue;
-                    }
-                    // ---- S^T: rows are the 16 tokens, columns the query heads ----
-                    float s[NTX][4], s2[NTX][4];
+                    } else {
+                        // ---- S^T: rows are the 16 tokens, columns the query heads ----
+                        float s[NTX][4], s2[NTX][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
-                    float done[NTX][4];                         // f32: finished sums of S
+                            for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
+                        float done[NTX][4];                         // f32: finished sums of S
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) done[nt][c] = 0.f;
+                            for (int c = 0; c < 4; ++c) done[nt][c] = 0.f;
 #pragma unroll
-                    for (int k2 = 0; k2 < KS; ++k2) {           // 32 bytes of each of the 16 rows
-                        uint32_t r[4];
-                        ldsm4(((ks + k_lane) ^ (32 * (k2 & 3))) + (k2 >> 2) * 2048, r);
+                        for (int k2 = 0; k2 < KS; ++k2) {           // 32 bytes of each of the 16 rows
+                            uint32_t r[4];
+                            ldsm4(((ks + k_lane) ^ (32 * (k2 & 3))) + (k2 >> 2) * 2048, r);
+                            if constexpr (kF32) {
+                                uint32_t hi[4], lo[4];
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) split_tf32(r[c], hi[c], lo[c]);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    uint32_t qh[2], ql[2];
+                                    split_tf32(q[nt][k2][0], qh[0], ql[0]);
+                                    split_tf32(q[nt][k2][1], qh[1], ql[1]);
+                                    mma_tf32(s2[nt], lo, qh[0], qh[1]);
+                                    mma_tf32(s2[nt], hi, ql[0], ql[1]);
+                                    // tensor-core sums truncate: four steps at most in one, the rest rounded
+                                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                                    mma_tf32(k2 % 4 ? s[nt] : part, hi, qh[0], qh[1]);
+                                    if (k2 % 4 == 0)
+#pragma unroll
+                                        for (int c = 0; c < 4; ++c) { done[nt][c] += s[nt][c]; s[nt][c] = part[c]; }
+                                }
+                            } else if constexpr (!kF8) {
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma_bf16(k2 & 1 ? s2[nt] : s[nt], r, q[nt][k2][0], q[nt][k2][1]);
+                            } else {
+                                const uint32_t x[4] = {e4m3x2_to_f16x2(r[0]), e4m3x2_to_f16x2(r[1]), e4m3x2_to_f16x2(r[0] >> 16), e4m3x2_to_f16x2(r[1] >> 16)};
+                                const uint32_t y[4] = {e4m3x2_to_f16x2(r[2]), e4m3x2_to_f16x2(r[3]), e4m3x2_to_f16x2(r[2] >> 16), e4m3x2_to_f16x2(r[3] >> 16)};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma_f16(s[nt], x, q[nt][k2][0], q[nt][k2][1]);
+                                    mma_f16(s2[nt], y, q[nt][k2][2], q[nt][k2][3]);
+                                }
+                            }
+                        }
+                        // ---- weights ----
+                        // Their reference m follows the maximum only when a score passes it by kSlack: weights stay below
+                        // e^kSlack, sums lose nothing, and most tiles need no maximum across the warp.
+                        bool over = false;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const float x = kF32 ? done[nt][c] + s[nt][c] + s2[nt][c] : s[nt][c] + s2[nt][c];
+                                s[nt][c] = fmaf(x, qmul[nt][c & 1], bias[j][c >> 1]);
+                            }
+                        unsigned gone = 0;
+                        if (masked) {                               // whatever a masked row holds
+                            const bool gone0 = bias[j][0] == -INFINITY, gone1 = bias[j][1] == -INFINITY;
+                            gone = __ballot_sync(~0u, gone0 || gone1);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c)
+                                    if (c >> 1 ? gone1 : gone0) s[nt][c] = -INFINITY;
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) over = over || s[nt][c] > m[nt][c & 1] + kSlack;
+                        if (__any_sync(~0u, over)) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int b = 0; b < 2; ++b) {
+                                    float x = fmaxf(s[nt][b], s[nt][b + 2]);
+                                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                                    x = fmaxf(x, m[nt][b]);
+                                    const float f = exp2_fast((m[nt][b] - (x == -INFINITY ? 0.f : x)) * kLog2e);
+                                    m[nt][b] = x;
+                                    l[nt][b] *= f;
+#pragma unroll
+                                    for (int mt = 0; mt < MT; ++mt) { o[mt][nt][b] *= f; o[mt][nt][b + 2] *= f; }
+                                }
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const float mb = m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1];
+                                s[nt][c] = exp2_fast((s[nt][c] - mb) * kLog2e);
+                            }
+                        uint32_t ph[NTX][2], pl[NTX][2];            // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
+                        float pf[NTX][4];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            l[nt][0] += s[nt][0] + s[nt][2];
+                            l[nt][1] += s[nt][1] + s[nt][3];
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const float p0 = s[nt][2 * x], p1 = s[nt][2 * x + 1];
+                                if constexpr (kF32) {
+                                    const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+                                    const uint32_t up = movm(__byte_perm(u0, u1, 0x7632)), down = movm(__byte_perm(u0, u1, 0x5410));
+                                    pf[nt][2 * x] = __uint_as_float(__byte_perm(down, up, 0x5410));
+                                    pf[nt][2 * x + 1] = __uint_as_float(__byte_perm(down, up, 0x7632));
+                                } else if constexpr (!kF8) {
+                                    const __nv_bfloat162 hi = __floats2bfloat162_rn(p0, p1);
+                                    const __nv_bfloat162 lo = __floats2bfloat162_rn(p0 - __low2float(hi), p1 - __high2float(hi));
+                                    ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
+                                    pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
+                                } else {
+                                    const __half2 hi = __floats2half2_rn(p0, p1);
+                                    const __half2 lo = __floats2half2_rn(p0 - __low2float(hi), p1 - __high2float(hi));
+                                    ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
+                                    pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
+                                }
+                            }
+                        }
+                        // ---- O^T += V^T P^T; rows of V that are masked may hold anything and are replaced by zeros ----
+                        uint32_t keep0 = ~0u, keep1 = ~0u;          // 16-bit halves of a register: tokens 2 t4, 2 t4 + 1 (+ 8)
+                        if (gone) {                                 // token g (+ 8) is that of lanes 4 g ..
+                            const unsigned g0 = __ballot_sync(~0u, bias[j][0] == -INFINITY), g1 = __ballot_sync(~0u, bias[j][1] == -INFINITY);
+                            keep0 = ((g0 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g0 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
+                            keep1 = ((g1 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g1 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
+                        }
                         if constexpr (kF32) {
-                            uint32_t hi[4], lo[4];
+                            // step x: tokens 8 x .. 8 x + 7; k = t4 is token 2 t4, k = t4 + 4 is token 2 t4 + 1 (bank-conflict free)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) split_tf32(r[c], hi[c], lo[c]);
+                            for (int x = 0; x < 2; ++x) {
+                                const uint32_t keep = x ? keep1 : keep0;
+                                const bool drop0 = !(keep & 0xffffu), drop1 = !(keep >> 16);
+                                uint32_t bh[NTX][2], bl[NTX][2];
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                uint32_t qh[2], ql[2];
-                                split_tf32(q[nt][k2][0], qh[0], ql[0]);
-                                split_tf32(q[nt][k2][1], qh[1], ql[1]);
-                                mma_tf32(s2[nt], lo, qh[0], qh[1]);
-                                mma_tf32(s2[nt], hi, ql[0], ql[1]);
-                                // tensor-core sums truncate: four steps at most in one, the rest rounded
-                                float part[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma_tf32(k2 % 4 ? s[nt] : part, hi, qh[0], qh[1]);
-                                if (k2 % 4 == 0)
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    split_tf32(__float_as_uint(pf[nt][2 * x]), bh[nt][0], bl[nt][0]);
+                                    split_tf32(__float_as_uint(pf[nt][2 * x + 1]), bh[nt][1], bl[nt][1]);
+                                }
+                                const int row0 = 8 * x + 2 * t4, row1 = row0 + 1;
 #pragma unroll
-                                    for (int c = 0; c < 4; ++c) { done[nt][c] += s[nt][c]; s[nt][c] = part[c]; }
+                                for (int mt = 0; mt < MT; ++mt) {
+                                    uint32_t hi[4], lo[4];
+#pragma unroll
+                                    for (int c = 0; c < 4; ++c) {
+                                        const int d = 16 * mt + 8 * (c & 1) + g, row = c >> 1 ? row1 : row0;
+                                        uint32_t u;
+                                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u)
+                                                     : "r"(vs + (d >> 5) * 2048 + row * 128 + ((((d & 31) >> 2) ^ (row & 7)) << 4) + (d & 3) * 4) : "memory");
+                                        if (c >> 1 ? drop1 : drop0) u = 0u;
+                                        split_tf32(u, hi[c], lo[c]);
+                                    }
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        float add[4] = {0.f, 0.f, 0.f, 0.f};    // a long sum is kept with rounded additions
+                                        mma_tf32(add, lo, bh[nt][0], bh[nt][1]);
+                                        mma_tf32(add, hi, bl[nt][0], bl[nt][1]);
+                                        mma_tf32(add, hi, bh[nt][0], bh[nt][1]);
+#pragma unroll
+                                        for (int c = 0; c < 4; ++c) o[mt][nt][c] += add[c];
+                                    }
+                                }
                             }
                         } else if constexpr (!kF8) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma_bf16(k2 & 1 ? s2[nt] : s[nt], r, q[nt][k2][0], q[nt][k2][1]);
-                        } else {
-                            const uint32_t x[4] = {e4m3x2_to_f16x2(r[0]), e4m3x2_to_f16x2(r[1]), e4m3x2_to_f16x2(r[0] >> 16), e4m3x2_to_f16x2(r[1] >> 16)};
-                            const uint32_t y[4] = {e4m3x2_to_f16x2(r[2]), e4m3x2_to_f16x2(r[3]), e4m3x2_to_f16x2(r[2] >> 16), e4m3x2_to_f16x2(r[3] >> 16)};
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_f16(s[nt], x, q[nt][k2][0], q[nt][k2][1]);
-                                mma_f16(s2[nt], y, q[nt][k2][2], q[nt][k2][3]);
-                            }
-                        }
-                    }
-                    // ---- weights ----
-                    // Their reference m follows the maximum only when a score passes it by kSlack: weights stay below
-                    // e^kSlack, sums lose nothing, and most tiles need no maximum across the warp.
-                    bool over = false;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const float x = kF32 ? done[nt][c] + s[nt][c] + s2[nt][c] : s[nt][c] + s2[nt][c];
-                            s[nt][c] = fmaf(x, qmul[nt][c & 1], bias[j][c >> 1]);
-                        }
-                    unsigned gone = 0;
-                    if (masked) {                               // whatever a masked row holds
-                        const bool gone0 = bias[j][0] == -INFINITY, gone1 = bias[j][1] == -INFINITY;
-                        gone = __ballot_sync(~0u, gone0 || gone1);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c)
-                                if (c >> 1 ? gone1 : gone0) s[nt][c] = -INFINITY;
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) over = over || s[nt][c] > m[nt][c & 1] + kSlack;
-                    if (__any_sync(~0u, over)) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                float x = fmaxf(s[nt][b], s[nt][b + 2]);
-                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-                                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                                x = fmaxf(x, m[nt][b]);
-                                const float f = exp2_fast((m[nt][b] - (x == -INFINITY ? 0.f : x)) * kLog2e);
-                                m[nt][b] = x;
-                                l[nt][b] *= f;
-#pragma unroll
-                                for (int mt = 0; mt < MT; ++mt) { o[mt][nt][b] *= f; o[mt][nt][b + 2] *= f; }
-                            }
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const float mb = m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1];
-                            s[nt][c] = exp2_fast((s[nt][c] - mb) * kLog2e);
-                        }
-                    uint32_t ph[NTX][2], pl[NTX][2];            // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
-                    float pf[NTX][4];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        l[nt][0] += s[nt][0] + s[nt][2];
-                        l[nt][1] += s[nt][1] + s[nt][3];
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float p0 = s[nt][2 * x], p1 = s[nt][2 * x + 1];
-                            if constexpr (kF32) {
-                                const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-                                const uint32_t up = movm(__byte_perm(u0, u1, 0x7632)), down = movm(__byte_perm(u0, u1, 0x5410));
-                                pf[nt][2 * x] = __uint_as_float(__byte_perm(down, up, 0x5410));
-                                pf[nt][2 * x + 1] = __uint_as_float(__byte_perm(down, up, 0x7632));
-                            } else if constexpr (!kF8) {
-                                const __nv_bfloat162 hi = __floats2bfloat162_rn(p0, p1);
-                                const __nv_bfloat162 lo = __floats2bfloat162_rn(p0 - __low2float(hi), p1 - __high2float(hi));
-                                ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
-                                pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
-                            } else {
-                                const __half2 hi = __floats2half2_rn(p0, p1);
-                                const __half2 lo = __floats2half2_rn(p0 - __low2float(hi), p1 - __high2float(hi));
-                                ph[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&hi));
-                                pl[nt][x] = movm(*reinterpret_cast<const uint32_t*>(&lo));
-                            }
-                        }
-                    }
-                    // ---- O^T += V^T P^T; rows of V that are masked may hold anything and are replaced by zeros ----
-                    uint32_t keep0 = ~0u, keep1 = ~0u;          // 16-bit halves of a register: tokens 2 t4, 2 t4 + 1 (+ 8)
-                    if (gone) {                                 // token g (+ 8) is that of lanes 4 g ..
-                        const unsigned g0 = __ballot_sync(~0u, bias[j][0] == -INFINITY), g1 = __ballot_sync(~0u, bias[j][1] == -INFINITY);
-                        keep0 = ((g0 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g0 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
-                        keep1 = ((g1 >> (8 * t4)) & 1u ? 0u : 0xffffu) | ((g1 >> (8 * t4 + 4)) & 1u ? 0u : 0xffff0000u);
-                    }
-                    if constexpr (kF32) {
-                        // step x: tokens 8 x .. 8 x + 7; k = t4 is token 2 t4, k = t4 + 4 is token 2 t4 + 1 (bank-conflict free)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const uint32_t keep = x ? keep1 : keep0;
-                            const bool drop0 = !(keep & 0xffffu), drop1 = !(keep >> 16);
-                            uint32_t bh[NTX][2], bl[NTX][2];
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                split_tf32(__float_as_uint(pf[nt][2 * x]), bh[nt][0], bl[nt][0]);
-                                split_tf32(__float_as_uint(pf[nt][2 * x + 1]), bh[nt][1], bl[nt][1]);
-                            }
-                            const int row0 = 8 * x + 2 * t4, row1 = row0 + 1;
-#pragma unroll
                             for (int mt = 0; mt < MT; ++mt) {
-                                uint32_t hi[4], lo[4];
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const int d = 16 * mt + 8 * (c & 1) + g, row = c >> 1 ? row1 : row0;
-                                    uint32_t u;
-                                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u)
-                                                 : "r"(vs + (d >> 5) * 2048 + row * 128 + ((((d & 31) >> 2) ^ (row & 7)) << 4) + (d & 3) * 4) : "memory");
-                                    if (c >> 1 ? drop1 : drop0) u = 0u;
-                                    split_tf32(u, hi[c], lo[c]);
-                                }
+                                uint32_t r[4];
+                                ldsm4_trans(((vs + v_lane) ^ (32 * (mt & 3))) + (mt >> 2) * 2048, r);
+                                if (gone) { r[0] &= keep0; r[1] &= keep0; r[2] &= keep1; r[3] &= keep1; }
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
-                                    float add[4] = {0.f, 0.f, 0.f, 0.f};    // a long sum is kept with rounded additions
-                                    mma_tf32(add, lo, bh[nt][0], bh[nt][1]);
-                                    mma_tf32(add, hi, bl[nt][0], bl[nt][1]);
-                                    mma_tf32(add, hi, bh[nt][0], bh[nt][1]);
-#pragma unroll
-                                    for (int c = 0; c < 4; ++c) o[mt][nt][c] += add[c];
+                                    mma_bf16(o[mt][nt], r, pl[nt][0], pl[nt][1]);
+                                    mma_bf16(o[mt][nt], r, ph[nt][0], ph[nt][1]);
                                 }
                             }
-                        }
-                    } else if constexpr (!kF8) {
+                        } else {
+                            // a transposed 8 x 8 matrix of byte pairs: tokens 2 t4 and 2 t4 + 1 of columns 2 g and 2 g + 1
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            uint32_t r[4];
-                            ldsm4_trans(((vs + v_lane) ^ (32 * (mt & 3))) + (mt >> 2) * 2048, r);
-                            if (gone) { r[0] &= keep0; r[1] &= keep0; r[2] &= keep1; r[3] &= keep1; }
+                            for (int m2 = 0; m2 < MT / 2; ++m2) {   // two 16-byte pieces
+                                uint32_t r[4];
+                                ldsm4_trans(((vs + k_lane) ^ (32 * (m2 & 3))) + (m2 >> 2) * 2048, r);
+                                if (gone) { r[0] &= keep0; r[2] &= keep0; r[1] &= keep1; r[3] &= keep1; }
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_bf16(o[mt][nt], r, pl[nt][0], pl[nt][1]);
-                                mma_bf16(o[mt][nt], r, ph[nt][0], ph[nt][1]);
-                            }
-                        }
-                    } else {
-                        // a transposed 8 x 8 matrix of byte pairs: tokens 2 t4 and 2 t4 + 1 of columns 2 g and 2 g + 1
+                                for (int x = 0; x < 2; ++x) {
+                                    const uint32_t u = __byte_perm(r[2 * x], 0u, 0x3120), w = __byte_perm(r[2 * x + 1], 0u, 0x3120);
+                                    const uint32_t v[4] = {e4m3x2_to_f16x2(u), e4m3x2_to_f16x2(u >> 16), e4m3x2_to_f16x2(w), e4m3x2_to_f16x2(w >> 16)};
 #pragma unroll
-                        for (int m2 = 0; m2 < MT / 2; ++m2) {   // two 16-byte pieces
-                            uint32_t r[4];
-                            ldsm4_trans(((vs + k_lane) ^ (32 * (m2 & 3))) + (m2 >> 2) * 2048, r);
-                            if (gone) { r[0] &= keep0; r[2] &= keep0; r[1] &= keep1; r[3] &= keep1; }
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                const uint32_t u = __byte_perm(r[2 * x], 0u, 0x3120), w = __byte_perm(r[2 * x + 1], 0u, 0x3120);
-                                const uint32_t v[4] = {e4m3x2_to_f16x2(u), e4m3x2_to_f16x2(u >> 16), e4m3x2_to_f16x2(w), e4m3x2_to_f16x2(w >> 16)};
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    mma_f16(o[2 * m2 + x][nt], v, pl[nt][0], pl[nt][1]);
-                                    mma_f16(o[2 * m2 + x][nt], v, ph[nt][0], ph[nt][1]);
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        mma_f16(o[2 * m2 + x][nt], v, pl[nt][0], pl[nt][1]);
+                                        mma_f16(o[2 * m2 + x][nt], v, ph[nt][0], ph[nt][1]);
+                                    }
                                 }
                             }
                         }

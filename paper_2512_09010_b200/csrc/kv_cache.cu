@@ -485,6 +485,12 @@ template <> struct Vec<__nv_bfloat16> {
     }
 };
 
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d)
+        : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)), "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&d);
+}
 // What an e4m3 row is divided by: the scale, its reciprocal, and the largest quotient the short way is taken for.
 struct Scale {
     float s, r, most;
@@ -514,7 +520,12 @@ __device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8],
     }
     if (big < scale.most) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) q[x] = fmaf(fmaf(-q[x], scale.s, f[x]), scale.r, q[x]);
+        for (int x = 0; x < 8; x += 2) {                    // two at a time
+            float2 a = make_float2(q[x], q[x + 1]);
+            const float2 rest = fma2(make_float2(-a.x, -a.y), make_float2(scale.s, scale.s), make_float2(f[x], f[x + 1]));
+            a = fma2(rest, make_float2(scale.r, scale.r), a);
+            q[x] = a.x; q[x + 1] = a.y;
+        }
     } else {
 #pragma unroll
         for (int x = 0; x < 8; ++x) q[x] = f[x] / scale.s;
