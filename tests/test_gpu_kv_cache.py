@@ -289,6 +289,27 @@ def test_written_rows_are_enhanced_and_rounded_once(luvc, dtype, heads, D):
         assert ((got[1].double() - want[1]).abs() <= u * want[1].abs() + 4 * 2.0 ** -24 * (v.double().abs() + 3)).all()
 
 
+def test_every_bf16_value_is_divided_as_a_division_does(luvc):
+    """All 65536 bf16 patterns (subnormals, infinities and NaN among them) over scales that give ties, quotients that saturate, and
+    reciprocals that overflow: the stored byte is that of the nearest 8-bit value to the fp32 quotient."""
+    scales = [1.0, 0.75, 1.5, 3.0, 7.0, 0.1, 0.013, 1 / 3, 2.0 ** -20, 2.0 ** -126, 2.0 ** -130, 2.0 ** -149, 2.0 ** 100, 3e38, 1e-5, 448.0]
+    heads, D, tokens = len(scales), 64, 1024
+    x = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16).view(torch.bfloat16).view(tokens, 1, D)
+    x = x.expand(tokens, heads, D).contiguous()
+    s = torch.tensor([scales], device="cuda")
+    pool = torch.zeros((1, tokens // 64, heads, 64, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    cache = luvc.KvCache(pool, pool.clone(), 1, tokens // 64, k_scale=s, v_scale=s.flip(1))
+    count = torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    luvc.kv_reserve(cache, count)
+    luvc.kv_write(cache, x, x, starts=torch.tensor([0, tokens], dtype=torch.int32, device="cuda"))
+    assert luvc.check_status() == 0
+    for got, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        want = (x.float() / scale[0][:, None]).clamp(-448, 448).to(torch.float8_e4m3fn).float()
+        have = got.float()[0].transpose(1, 2).reshape(tokens, heads, D)
+        same = (have == want) | (have.isnan() & want.isnan())
+        assert bool(same.all()), (x[~same][:5], have[~same][:5], want[~same][:5])
+
+
 def test_a_step_can_be_captured_and_replayed(luvc):
     """A decode step (room, rows, attention) in a CUDA graph: page numbers are worked out on the device at every replay."""
     r = Rig(luvc, "bf16", pages=16, page=16, slots=2, max_pages=5, layers=1)
