@@ -141,6 +141,8 @@ struct Args {
     AttnProblem p;
     int group, groups;          // query heads per key head; head groups of ROWS
     int page_shift;             // log2 of the page size, -1 if it is no power of two
+    int limit;                  // tiles of all sequences up to which the list can be numbered in 32 bits
+    float one_grid;             // 1 / CTAs
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
     unsigned* counters;         // [3][kMaxCtas]: arrivals of (sequence, head)s, of their first groups, of the other groups
     float* parts;               // [2][kMaxCtas][2] of PART floats: of CTAs, of groups of CTAs
@@ -385,9 +387,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     auto length_of = [&](int slot) {
         return slot >= 0 && slot < p.c.slots ? max(0, min(p.c.lengths[slot], p.c.max_pages * ps)) : 0;
     };
-    const int segs = p.c.heads * a.groups, limit = 2147483647 / segs;   // the list is numbered in 32 bits
+    const int segs = p.c.heads * a.groups;
     bool fits;
-    int base;
+    int base, lane_tiles = 0, lane_first = 0;                   // tiles of all sequences; up to 32 of them: those of lane, and before it
     auto tiles_of = [&](int i) {
         const int slot = slot_of(i);
         if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
@@ -403,8 +405,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         return x;
     };
     if (n <= 32) {                                              // every warp for itself (the same values): no barrier
-        const unsigned x = warp_scan(lane < n ? tiles_of(lane) : 0u), all = __shfl_sync(~0u, x, 31);
-        fits = all <= (unsigned)limit;
+        lane_tiles = lane < n ? tiles_of(lane) : 0;
+        const unsigned x = warp_scan(lane_tiles), all = __shfl_sync(~0u, x, 31);
+        lane_first = (int)x - lane_tiles;
+        fits = all <= (unsigned)a.limit;
         base = (int)all;
         if (lane == 0) prefix[0] = 0;
         if (lane < n) prefix[lane + 1] = (int)x;
@@ -424,7 +428,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 if (w < warp) before += scan_warp[w];
                 all += scan_warp[w];
             }
-            fits = fits && all <= limit;
+            fits = fits && all <= a.limit;
             base = fits ? (int)all : 0;
             if (i < n) prefix[i + 1] = fits ? (int)(before + x) : 0;
             __syncthreads();
@@ -447,17 +451,25 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
     // ---- this CTA's part of the list, this warp's part of that ----
     struct Place { int seq, seg, tile, tiles, first; };         // a tile; its (sequence, head) starts at `first` in the list
-    auto place_of = [&](int x) {
-        int lo = 0, hi = n;                                     // prefix[lo] * segs <= x < prefix[hi] * segs
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (prefix[mid] * segs <= x) lo = mid; else hi = mid;
-        }
+    auto place_of = [&](int x) {                                // x < total, the same in all lanes
         Place q;
-        q.seq = lo;
-        q.tiles = prefix[lo + 1] - prefix[lo];
+        int first;
+        if (n <= 32) {                                          // the last lane that begins at or before x (it has tiles)
+            q.seq = 31 - __clz(__ballot_sync(~0u, lane < n && lane_first * segs <= x));
+            q.tiles = __shfl_sync(~0u, lane_tiles, q.seq);
+            first = __shfl_sync(~0u, lane_first, q.seq);
+        } else {
+            int lo = 0, hi = n;                                 // prefix[lo] * segs <= x < prefix[hi] * segs
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (prefix[mid] * segs <= x) lo = mid; else hi = mid;
+            }
+            q.seq = lo;
+            first = prefix[lo];
+            q.tiles = prefix[lo + 1] - first;
+        }
         // quotient below segs <= 2^16: the float one is off by less than one
-        const int in = x - prefix[lo] * segs;
+        const int in = x - first * segs;
         q.seg = (int)__fdividef((float)in, (float)q.tiles);
         q.tile = in - q.seg * q.tiles;
         if (q.tile < 0) { --q.seg; q.tile += q.tiles; }
@@ -467,7 +479,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     };
     // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.7 us, with two tiles
     // 9.3, with three 11.8: even then a join across CTAs costs less than a warp's second tile).
-    const int grid = gridDim.x, per = max((int)(((unsigned)total + grid - 1) / grid), NW), tol = min(per / 2, kSnap);
+    int per = max((int)((float)total * a.one_grid) - 1, 0);     // total / grid, rounded up
+    per -= per >> 20;
+    while ((long long)per * (int)gridDim.x < total) ++per;
+    per = max(per, NW);
+    const int tol = min(per / 2, kSnap);
     auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
         if (c == 0) return 0;
         if ((long long)c * per >= total) return total;
@@ -477,8 +493,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (q.tiles - q.tile <= tol) return q.first + q.tiles;
         return x;
     };
-    const int bound = bound_of(blockIdx.x + (lane & 1));        // both in one go
-    const int cta_a = __shfl_sync(~0u, bound, 0), cta_b = __shfl_sync(~0u, bound, 1);
+    const int cta_a = bound_of(blockIdx.x), cta_b = bound_of(blockIdx.x + 1);
     if (cta_a >= cta_b) return;
     const int each = (unsigned)(cta_b - cta_a) / NW, more = (unsigned)(cta_b - cta_a) % NW;     // the first `more` warps take one more
     auto part_of_warp = [&](int w) { return cta_a + w * each + min(w, more); };
@@ -1204,6 +1219,10 @@ int launch(const AttnProblem& p) {
     a.p = p;
     a.group = p.q_heads / p.c.heads;
     a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
+    const int sms = sm_count();
+    if (!sms) return LUVC_ERR_CUDA;
+    a.limit = 2147483647 / (p.c.heads * a.groups);
+    a.one_grid = 1.f / sms;
     a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
     a.counters = static_cast<unsigned*>(p.workspace);
@@ -1223,8 +1242,6 @@ int launch(const AttnProblem& p) {
         }
         if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    const int sms = sm_count();
-    if (!sms) return LUVC_ERR_CUDA;
     return launch_overlapped(attn_decode_kernel<TQ, TC, DPB, NT>, sms, 32 * Sh::NW, smem, p.stream, kmap, vmap, a);
 }
 
