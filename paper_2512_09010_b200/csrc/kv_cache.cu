@@ -28,6 +28,7 @@ using namespace ptx;
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
 constexpr int kPerLane = 8;                                 // pages a lane looks at per sweep over refs
 constexpr int kWarpPages = 32 * kPerLane, kSweep = kPlanWarps * kWarpPages;
+constexpr int kMaxNeed = 1 << 26;                           // pages one call takes for one sequence (2^30 tokens at least)
 constexpr int kClaimed = -1;                                // lengths[] of a slot that the running call has claimed
 
 __device__ __forceinline__ bool stopped(const int* status) { return *reinterpret_cast<const volatile int*>(status) != 0; }
@@ -71,7 +72,8 @@ struct PlanArgs {
 struct PlanShared {
     int error;                              // highest luvc_status found
     int page_count[2][kPlanWarps];          // free pages each warp saw in a sweep (two sweeps alternate)
-    unsigned long long need_sum[kPlanWarps];
+    unsigned need_sum[kPlanWarps];
+    int list[kSweep];                       // free pages of a sweep, in order
     int* start;                             // pages the sequences need; then their exclusive sums
     int* from;                              // first page index of each sequence that is to be taken
     int* len;                               // length before the call; kClaimed where the slot was not obtained
@@ -88,25 +90,31 @@ __device__ __forceinline__ T warp_inclusive(T x, int lane) {
     return x;
 }
 
-// start[i] holds the pages sequence i needs; afterwards start[] is their exclusive sum, start[n] the total, which is
-// returned (-1: more than the pool has; sums are formed in 64 bits, and only a total that fits is used).
+// start[i] holds the pages sequence i needs (at most kMaxNeed each); afterwards start[] is their exclusive sum, start[n] the
+// total, which is returned (-1: more than the pool has; the sum over warps is formed in 64 bits, and only one that fits is
+// used).  take_pages has a barrier before it reads start[].
 __device__ int scan_needs(PlanShared& s, int n, int pages) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (n <= 32) {                                          // every warp for itself; the first one writes
+        const unsigned v = lane < n ? s.start[lane] : 0, x = warp_inclusive(v, lane), all = __shfl_sync(~0u, x, 31);
+        __syncthreads();                                    // all have read the needs
+        if (warp == 0 && lane < n) s.start[lane] = (int)(x - v);
+        if (threadIdx.x == 0) s.start[n] = (int)all;
+        return all > (unsigned)pages ? -1 : (int)all;
+    }
     unsigned long long base = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + threadIdx.x;
-        const unsigned long long v = i < n ? s.start[i] : 0;
-        const unsigned long long x = warp_inclusive(v, lane);
+        const unsigned v = i < n ? s.start[i] : 0, x = warp_inclusive(v, lane);
         if (lane == 31) s.need_sum[warp] = x;
         __syncthreads();
-        const unsigned long long all = warp_inclusive(s.need_sum[lane], lane);
-        const unsigned long long before = warp ? __shfl_sync(~0u, all, warp - 1) : (__shfl_sync(~0u, all, 31), 0ull);
-        if (i < n) s.start[i] = (int)(base + before + x - v);
+        const unsigned long long all = warp_inclusive((unsigned long long)s.need_sum[lane], lane);
+        const unsigned long long before = __shfl_sync(~0u, all, (warp + 31) & 31);
+        if (i < n) s.start[i] = (int)(base + (warp ? before : 0) + x - v);
         base += __shfl_sync(~0u, all, 31);
         if (n > kPlanThreads) __syncthreads();              // need_sum is written again
     }
     if (threadIdx.x == 0) s.start[n] = (int)base;
-    __syncthreads();
     return base > (unsigned long long)pages ? -1 : (int)base;
 }
 
@@ -143,19 +151,22 @@ __device__ __forceinline__ void sweep_count(PlanShared& s, const int (&r)[kPerLa
 template <typename F>
 __device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pages, int n, int total, int (&r)[kPerLane], F give) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // first the sweep's free pages in order, then a page per thread: which sequence it goes to is searched for once, not per ballot
     auto hand_out = [&](const Sweep& w, int c0, int base) {
-        int rank0 = base + w.first;
+        int rank0 = w.first;
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) {
-            const int rank = rank0 + __popc(w.mask[k] & ((1u << lane) - 1u));
+            if ((w.mask[k] >> lane) & 1u) s.list[rank0 + __popc(w.mask[k] & ((1u << lane) - 1u))] = c0 + warp * kWarpPages + 32 * k + lane;
             rank0 += __popc(w.mask[k]);
-            if (!((w.mask[k] >> lane) & 1u) || rank >= total) continue;
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < min(w.sum, total - base); j += kPlanThreads) {
+            const int page = s.list[j], rank = base + j;
             int lo = 0, hi = n;                             // start[lo] <= rank < start[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (s.start[mid] <= rank) lo = mid; else hi = mid;
             }
-            const int page = c0 + warp * kWarpPages + 32 * k + lane;
             refs[page] = 1;
             give(lo, s.from[lo] + rank - s.start[lo], rank, page);
         }
@@ -179,6 +190,7 @@ __device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pag
         sweep_count(s, r, turn, w);
         hand_out(w, c0, base);
         base += w.sum;
+        __syncthreads();                                    // the list has been read
     }
     return true;
 }
@@ -260,6 +272,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
                 have = ceil_div(len, c.page_size);
                 need = ceil_div(len + add, c.page_size) - have;
             }
+            if (need > kMaxNeed) atomicMax(&s.error, (int)LUVC_ERR_PAGES), need = 0;
             s.len[i] = len; s.from[i] = have; s.start[i] = need; s.slot[i] = slot;
         }
     } else {
@@ -279,6 +292,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
                 const int same = count == span ? now : first + identity_prefix(a.idx + (long long)i * a.keep, count, lane);
                 still = same / c.page_size;
                 need = ceil_div(now, c.page_size) - still;
+                if (need > kMaxNeed) bad = LUVC_ERR_PAGES, need = 0;
                 for (int p = still + lane; p < ceil_div(len, c.page_size); p += 32)
                     a.move.old[(long long)i * c.max_pages + p] = c.table[(long long)slot * c.max_pages + p];
             }
@@ -374,6 +388,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
     if (w0 >= w1) return;
     const int units = c.D * a.es / 16;
     const size_t row_bytes = (size_t)c.D * a.es, head_bytes = ps * row_bytes, layer_bytes = (size_t)c.pages * c.heads * head_bytes;
+    const int row0 = tid / units, off0 = (tid - row0 * units) * 16;     // a thread's first 16 bytes of a piece
     const unsigned first_piece = w0 / groups, last_piece = (w1 - 1) / groups;
 
     for (unsigned piece0 = first_piece; piece0 <= last_piece; piece0 += batch) {
@@ -382,15 +397,15 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
         const unsigned piece = piece0 + k;
         if (k < batch && piece <= last_piece) {
             const int2 it = a.move.items[piece / chunks];
-            const int i = it.x, p = it.y, row0 = (int)(piece % (unsigned)chunks) * kMoveRows, slot = a.seqs ? a.seqs[i] : i;
+            const int i = it.x, p = it.y, skip = (int)(piece % (unsigned)chunks) * kMoveRows, slot = a.seqs ? a.seqs[i] : i;
             const int to = c.table[(long long)slot * c.max_pages + p];
-            const int rows = to >= 0 && to < c.pages ? min(cap, min(ps, c.lengths[slot] - p * ps) - row0) : 0;
+            const int rows = to >= 0 && to < c.pages ? min(cap, min(ps, c.lengths[slot] - p * ps) - skip) : 0;
             if (r == 0) {
-                dst_row[k] = (long long)to * c.heads * ps + row0;
+                dst_row[k] = (long long)to * c.heads * ps + skip;
                 rows_of[k] = rows;
             }
             if (r < rows) {
-                int from = p * ps + row0 + r, page;         // token of the old sequence that becomes this row
+                int from = p * ps + skip + r, page;         // token of the old sequence that becomes this row
                 if (FORK) {
                     page = c.table[(long long)a.src[i] * c.max_pages + p];
                 } else {
@@ -410,17 +425,23 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
         __syncthreads();
         const unsigned wa = max(w0, piece0 * groups), wb = min(w1, (piece0 + batch) * groups);
         int at = 0, group = wa - piece0 * groups;           // (only the first piece of the part may begin inside)
+        int layer = group * kMoveLanes / (2 * c.heads), rest = group * kMoveLanes - layer * 2 * c.heads;   // of the group's first triple
         for (unsigned w = wa; w < wb; ++w) {
+            const int live = min(kMoveLanes, triples - group * kMoveLanes);
             unsigned char* base[kMoveLanes];
 #pragma unroll
             for (int x = 0; x < kMoveLanes; ++x) {
-                const int t = min(group * kMoveLanes + x, triples - 1), layer = t / (2 * c.heads), rest = t - layer * 2 * c.heads;
-                base[x] = static_cast<unsigned char*>(rest >= c.heads ? c.v : c.k) + layer * layer_bytes +
-                          (rest >= c.heads ? rest - c.heads : rest) * head_bytes;
+                if (x < live) {
+                    base[x] = static_cast<unsigned char*>(rest >= c.heads ? c.v : c.k) + layer * layer_bytes +
+                              (rest >= c.heads ? rest - c.heads : rest) * head_bytes;
+                    if (++rest == 2 * c.heads) { rest = 0; ++layer; }
+                } else {
+                    base[x] = base[0];
+                }
             }
-            const int live = min(kMoveLanes, triples - group * kMoveLanes);
+            int row = row0, off = off0;
             for (int u = tid; u < rows_of[at] * units; u += kMoveThreads) {
-                const int row = u / units, off = (u - row * units) * 16;
+                if (u != tid) { row = u / units; off = (u - row * units) * 16; }
                 const long long from = src_row[at * cap + row];
                 if (from < 0) continue;
                 const size_t src = from * row_bytes + off, dst = (dst_row[at] + row) * row_bytes + off;
@@ -431,7 +452,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
                 for (int x = 0; x < kMoveLanes; ++x)
                     if (x < live) __stcs(reinterpret_cast<uint4*>(base[x] + dst), v[x]);
             }
-            if (++group == groups) { group = 0; ++at; }
+            if (++group == groups) { group = 0; layer = rest = 0; ++at; }
         }
     }
 }
@@ -643,7 +664,7 @@ int sm_count() {
 template <PlanKind KIND>
 int launch_plan(const PlanArgs& a, cudaStream_t stream) {
     const size_t smem = (size_t)(4 * a.n + 1) * sizeof(int);
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    if (smem > 12 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return LUVC_ERR_CUDA;
     }
