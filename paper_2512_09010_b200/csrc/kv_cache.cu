@@ -25,9 +25,8 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
 constexpr int kPerLane = 8;                                 // pages a lane looks at per sweep over refs
-constexpr int kWarpPages = 32 * kPerLane, kSweep = kPlanWarps * kWarpPages;
+constexpr int kWarpPages = 32 * kPerLane;
 constexpr int kMaxNeed = 1 << 26;                           // pages one call takes for one sequence (2^30 tokens at least)
 constexpr int kClaimed = -1;                                // lengths[] of a slot that the running call has claimed
 
@@ -68,12 +67,14 @@ struct PlanArgs {
     int* status;
 };
 
-// Shared memory of the plan; the arrays have n + 1, n, n and n entries.
+// Shared memory of the plan, run by THREADS threads; the arrays have n + 1, n, n and n entries.
+template <int THREADS>
 struct PlanShared {
+    static constexpr int WARPS = THREADS / 32, SWEEP = WARPS * kWarpPages;
     int error;                              // highest luvc_status found
-    int page_count[2][kPlanWarps];          // free pages each warp saw in a sweep (two sweeps alternate)
-    unsigned need_sum[kPlanWarps];
-    int list[kSweep];                       // free pages of a sweep, in order
+    int page_count[2][WARPS];               // free pages each warp saw in a sweep (two sweeps alternate)
+    unsigned need_sum[WARPS];
+    int list[SWEEP];                        // free pages of a sweep, in order
     int* start;                             // pages the sequences need; then their exclusive sums
     int* from;                              // first page index of each sequence that is to be taken
     int* len;                               // length before the call; kClaimed where the slot was not obtained
@@ -93,7 +94,9 @@ __device__ __forceinline__ T warp_inclusive(T x, int lane) {
 // start[i] holds the pages sequence i needs (at most kMaxNeed each); afterwards start[] is their exclusive sum, start[n] the
 // total, which is returned (-1: more than the pool has; the sum over warps is formed in 64 bits, and only one that fits is
 // used).  take_pages has a barrier before it reads start[].
-__device__ int scan_needs(PlanShared& s, int n, int pages) {
+template <int THREADS>
+__device__ int scan_needs(PlanShared<THREADS>& s, int n, int pages) {
+    constexpr int WARPS = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (n <= 32) {                                          // every warp for itself; the first one writes
         const unsigned v = lane < n ? s.start[lane] : 0, x = warp_inclusive(v, lane), all = __shfl_sync(~0u, x, 31);
@@ -103,22 +106,22 @@ __device__ int scan_needs(PlanShared& s, int n, int pages) {
         return all > (unsigned)pages ? -1 : (int)all;
     }
     unsigned long long base = 0;
-    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    for (int i0 = 0; i0 < n; i0 += THREADS) {
         const int i = i0 + threadIdx.x;
         const unsigned v = i < n ? s.start[i] : 0, x = warp_inclusive(v, lane);
         if (lane == 31) s.need_sum[warp] = x;
         __syncthreads();
-        const unsigned long long all = warp_inclusive((unsigned long long)s.need_sum[lane], lane);
+        const unsigned long long all = warp_inclusive(lane < WARPS ? (unsigned long long)s.need_sum[lane] : 0ull, lane);
         const unsigned long long before = __shfl_sync(~0u, all, (warp + 31) & 31);
         if (i < n) s.start[i] = (int)(base + (warp ? before : 0) + x - v);
         base += __shfl_sync(~0u, all, 31);
-        if (n > kPlanThreads) __syncthreads();              // need_sum is written again
+        if (n > THREADS) __syncthreads();              // need_sum is written again
     }
     if (threadIdx.x == 0) s.start[n] = (int)base;
     return base > (unsigned long long)pages ? -1 : (int)base;
 }
 
-// One sweep over kSweep pages from c0 on: every warp looks at kWarpPages consecutive ones.
+// One sweep over SWEEP pages from c0 on: every warp looks at kWarpPages consecutive ones.
 struct Sweep {
     unsigned mask[kPerLane];                // free pages, one ballot per 32
     int first;                              // free pages of the sweep before this warp's
@@ -131,7 +134,8 @@ __device__ __forceinline__ void sweep_load(const int32_t* refs, int pages, int c
     for (int k = 0; k < kPerLane; ++k) r[k] = at + 32 * k < pages ? refs[at + 32 * k] : 1;
 }
 
-__device__ __forceinline__ void sweep_count(PlanShared& s, const int (&r)[kPerLane], int turn, Sweep& w) {
+template <int THREADS>
+__device__ __forceinline__ void sweep_count(PlanShared<THREADS>& s, const int (&r)[kPerLane], int turn, Sweep& w) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int mine = 0;
 #pragma unroll
@@ -141,15 +145,15 @@ __device__ __forceinline__ void sweep_count(PlanShared& s, const int (&r)[kPerLa
     }
     if (lane == 0) s.page_count[turn & 1][warp] = mine;
     __syncthreads();
-    const int all = warp_inclusive(s.page_count[turn & 1][lane], lane);
+    const int all = warp_inclusive(lane < THREADS / 32 ? s.page_count[turn & 1][lane] : 0, lane);
     w.sum = __shfl_sync(~0u, all, 31);
     w.first = __shfl_sync(~0u, all, warp) - mine;
 }
 
 // Hands the `total` lowest free pages to the sequences: give(i, page index, rank, page).  False (nothing given) if there are too
 // few.  r: the first sweep's counts, loaded ahead.  All threads call it.
-template <typename F>
-__device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pages, int n, int total, int (&r)[kPerLane], F give) {
+template <int THREADS, typename F>
+__device__ __forceinline__ bool take_pages(PlanShared<THREADS>& s, int32_t* refs, int pages, int n, int total, int (&r)[kPerLane], F give) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // first the sweep's free pages in order, then a page per thread: which sequence it goes to is searched for once, not per ballot
     auto hand_out = [&](const Sweep& w, int c0, int base) {
@@ -160,7 +164,7 @@ __device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pag
             rank0 += __popc(w.mask[k]);
         }
         __syncthreads();
-        for (int j = threadIdx.x; j < min(w.sum, total - base); j += kPlanThreads) {
+        for (int j = threadIdx.x; j < min(w.sum, total - base); j += THREADS) {
             const int page = s.list[j], rank = base + j;
             int lo = 0, hi = n;                             // start[lo] <= rank < start[hi]
             while (hi - lo > 1) {
@@ -178,14 +182,14 @@ __device__ __forceinline__ bool take_pages(PlanShared& s, int32_t* refs, int pag
         hand_out(w, 0, 0);
         return true;
     }
-    int found = w.sum, end = kSweep, turn = 1;
-    for (; found < total && end < pages; end += kSweep, ++turn) {
+    int found = w.sum, end = PlanShared<THREADS>::SWEEP, turn = 1;
+    for (; found < total && end < pages; end += PlanShared<THREADS>::SWEEP, ++turn) {
         sweep_load(refs, pages, end, r);
         sweep_count(s, r, turn, w);
         found += w.sum;
     }
     if (found < total) return false;
-    for (int c0 = 0, base = 0; c0 < end; c0 += kSweep, ++turn) {
+    for (int c0 = 0, base = 0; c0 < end; c0 += PlanShared<THREADS>::SWEEP, ++turn) {
         sweep_load(refs, pages, c0, r);
         sweep_count(s, r, turn, w);
         hand_out(w, c0, base);
@@ -219,10 +223,10 @@ __device__ int identity_prefix(const int32_t* idx, int count, int lane) {
     return lo;
 }
 
-template <PlanKind KIND>
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_constant__ PlanArgs a) {
+template <PlanKind KIND, int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_plan_kernel(const __grid_constant__ PlanArgs a) {
     extern __shared__ int dyn[];
-    __shared__ PlanShared s;
+    __shared__ PlanShared<THREADS> s;
     const luvc_kv_cache& c = a.c;
     const int n = a.n, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -239,7 +243,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
 
     // what each sequence needs; its slot is claimed, so that one named twice is noticed
     if (KIND == kFork) {
-        for (int i = tid; i < n; i += kPlanThreads) {
+        for (int i = tid; i < n; i += THREADS) {
             const int src = a.src[i], dst = a.seqs[i];
             int len = -1;
             if (src >= 0 && src < c.slots) len = c.lengths[src];
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             s.slot[i] = dst;
         }
         __syncthreads();                                    // a source that is also a destination has been read
-        for (int i = tid; i < n; i += kPlanThreads) {
+        for (int i = tid; i < n; i += THREADS) {
             const int dst = s.slot[i];
             const int was = dst >= 0 && dst < c.slots ? atomicCAS(&c.lengths[dst], 0, kClaimed) : kClaimed;
             if (was != 0) {
@@ -259,7 +263,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             }
         }
     } else if (KIND == kReserve) {
-        for (int i = tid; i < n; i += kPlanThreads) {
+        for (int i = tid; i < n; i += THREADS) {
             const int slot = a.seqs ? a.seqs[i] : i, add = a.counts[i];
             int len = kClaimed;
             if (slot >= 0 && slot < c.slots) len = a.seqs ? atomicExch(&c.lengths[slot], kClaimed) : c.lengths[slot];
@@ -276,7 +280,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             s.len[i] = len; s.from[i] = have; s.start[i] = need; s.slot[i] = slot;
         }
     } else {
-        for (int i = warp; i < n; i += kPlanWarps) {
+        for (int i = warp; i < n; i += (THREADS / 32)) {
             const int slot = a.seqs ? a.seqs[i] : i;
             int len = kClaimed;
             if (lane == 0 && slot >= 0 && slot < c.slots)
@@ -312,7 +316,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             if (KIND != kReserve) a.move.items[rank] = make_int2(i, index);
         }))
         error = LUVC_ERR_PAGES;
-    for (int i = tid; i < n; i += kPlanThreads) {           // lengths: committed, or the claimed slots given back
+    for (int i = tid; i < n; i += THREADS) {           // lengths: committed, or the claimed slots given back
         int now = s.len[i];
         if (error) {
             if (now == kClaimed || !a.seqs) continue;
@@ -661,14 +665,22 @@ int sm_count() {
     return sms;
 }
 
-template <PlanKind KIND>
-int launch_plan(const PlanArgs& a, cudaStream_t stream) {
+template <PlanKind KIND, int THREADS>
+int launch_plan_as(const PlanArgs& a, cudaStream_t stream) {
     const size_t smem = (size_t)(4 * a.n + 1) * sizeof(int);
-    if (smem > 12 * 1024 && cudaFuncSetAttribute(kv_plan_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    if (sizeof(PlanShared<THREADS>) + smem > 48 * 1024 &&
+        cudaFuncSetAttribute(kv_plan_kernel<KIND, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return LUVC_ERR_CUDA;
     }
-    return launch_overlapped(kv_plan_kernel<KIND>, 1, kPlanThreads, smem, stream, a);
+    return launch_overlapped(kv_plan_kernel<KIND, THREADS>, 1, THREADS, smem, stream, a);
+}
+
+// A small CTA has shorter barriers (one token for 32 sequences: 3.8 us, with 1024 threads 4.9; 256 forks in all: 21.4, with 1024 22.4),
+// a large one gets through a large pool in fewer sweeps (about 0.6 us each).
+template <PlanKind KIND>
+int launch_plan(const PlanArgs& a, cudaStream_t stream) {
+    return a.n <= 256 && a.c.pages <= 4 * PlanShared<256>::SWEEP ? launch_plan_as<KIND, 256>(a, stream) : launch_plan_as<KIND, 1024>(a, stream);
 }
 
 // `pages`: about how many are filled.  Four CTAs per SM run at a time; up to four times as many are launched for long copies, so

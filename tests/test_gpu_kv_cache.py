@@ -168,16 +168,19 @@ def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
         r.check()
 
 
-def test_a_large_pool_and_many_sequences(luvc):
-    # more pages than one sweep of the scan covers (16384), more sequences than threads of its CTA, free pages far up
-    r = Rig(luvc, "bf16", pages=40000, page=16, slots=2100, max_pages=40, layers=1, heads=1, D=8)
-    r.append(list(range(500)), [16 * 40 - 3] * 500)
+@pytest.mark.parametrize("pages,slots,held", [(40000, 2100, 500), (8000, 420, 150)])
+def test_a_large_pool_and_many_sequences(luvc, pages, slots, held):
+    # more pages than one sweep of the scan covers, more sequences than threads of its CTA (first pool), free pages far up
+    r = Rig(luvc, "bf16", pages=pages, page=16, slots=slots, max_pages=40, layers=1, heads=1, D=8)
+    r.append(list(range(held)), [16 * 40 - 3] * held)
     r.check()
-    luvc.kv_free(r.cache, r.ints(list(range(0, 500, 7))))
-    for s in range(0, 500, 7):
+    luvc.kv_free(r.cache, r.ints(list(range(0, held, 7))))
+    for s in range(0, held, 7):
         r.model.free(s)
-    r.append(list(range(2099, 499, -1)), [(5 * s) % 37 for s in range(2099, 499, -1)])
-    r.append(list(range(0, 500, 7)), [16 * 20 + 1] * 72)
+    later = list(range(slots - 1, held - 1, -1))
+    for part in (later[:256], later[256:]) if slots < 1000 else (later,):
+        r.append(part, [(5 * s) % 37 for s in part])
+    r.append(list(range(0, held, 7)), [16 * 20 + 1] * len(range(0, held, 7)))
     r.check()
 
 
