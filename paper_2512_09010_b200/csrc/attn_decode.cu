@@ -219,23 +219,20 @@ __device__ __forceinline__ float2 join_factors(int count, GetMl get_ml, Put put,
         if (lane + 32 * x < count) put(lane + 32 * x, f[x] * all);
     return make_float2(m, l);
 }
-// The second, by a thread for four columns of a row: adds the parts times their factors to o, eight at a time.
-template <typename Factor, typename Columns>
-__device__ __forceinline__ void join4(int count, Factor factor, Columns columns, float4& o) {
-    for (int k0 = 0; k0 < count; k0 += 8) {
-        float4 x[8];
-        float w[8];
+// The second, by a thread for its E times four columns: adds the parts times their factors, part after part, so that the reads of
+// all columns are under way together.  factor(k, x) and columns(k, x) are of part k and the thread's columns x.
+template <int E, typename Factor, typename Columns>
+__device__ __forceinline__ void join4(int count, Factor factor, Columns columns, float4 (&o)[E]) {
+#pragma unroll 2
+    for (int k = 0; k < count; ++k) {
+        float4 v[E];
+        float w[E];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {                           // past the last part: the last one again, with factor 0
-            const int at = min(k0 + k, count - 1);
-            w[k] = k0 + k < count ? factor(at) : 0.f;
-            x[k] = *columns(at);
-        }
+        for (int x = 0; x < E; ++x) { w[x] = factor(k, x); v[x] = *columns(k, x); }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (k0 + k >= count) continue;
-            o.x = fmaf(w[k], x[k].x, o.x); o.y = fmaf(w[k], x[k].y, o.y);
-            o.z = fmaf(w[k], x[k].z, o.z); o.w = fmaf(w[k], x[k].w, o.w);
+        for (int x = 0; x < E; ++x) {
+            o[x].x = fmaf(w[x], v[x].x, o[x].x); o[x].y = fmaf(w[x], v[x].y, o[x].y);
+            o[x].z = fmaf(w[x], v[x].z, o[x].z); o[x].w = fmaf(w[x], v[x].w, o[x].w);
         }
     }
 }
@@ -1059,15 +1056,22 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         for (unsigned left = some; left; left &= left - 1) {
             const int c = __ffs(left) - 1, w0 = c == NW ? 0 : c;
             const Chain& ch = chains[c];
-#pragma unroll 2
-            for (int e = tid; e < ROWS * (DP / 4); e += NTHR) {
-                const int r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
+            float4 o[E];
+#pragma unroll
+            for (int x = 0; x < E; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+            // (rows past the last one hold sums of nothing: they are read, and not written)
+            join4<E>(ch.count, [&](int k, int x) { return ml_of[w0 + k][k ? 0 : ch.from][(tid + x * NTHR) / (DP / 4)].x; },
+                     [&](int k, int x) {
+                         const int e = tid + x * NTHR;
+                         return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) +
+                                                                o_index(e / (DP / 4), e % (DP / 4) * 4, DP));
+                     }, o);
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                const int e = tid + x * NTHR, r = e / (DP / 4), d = e % (DP / 4) * 4;
                 if (r >= ch.rows || d >= p.c.D) continue;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                join4(ch.count, [&](int k) { return ml_of[w0 + k][k ? 0 : ch.from][r].x; },
-                      [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) + at); }, o);
-                if (ch.c0 == ch.c1) put4(out_row(ch.row0 + r) + d, o);
-                else *reinterpret_cast<float4*>(global_part(blockIdx.x, ch.s0 >= cta_a).o + at) = o;
+                if (ch.c0 == ch.c1) put4(out_row(ch.row0 + r) + d, o[x]);
+                else *reinterpret_cast<float4*>(global_part(blockIdx.x, ch.s0 >= cta_a).o + o_index(r, d, DP)) = o[x];
             }
         }
     }
@@ -1119,16 +1123,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 }
             cp_async_wait<0>();
             __syncthreads();
-#pragma unroll
-            for (int x = 0; x < E; ++x) {
-                const int e = tid + x * NTHR, r = e / (DP / 4), d = e % (DP / 4) * 4, at = o_index(r, d, DP);
-                if (r >= ch.rows || d >= p.c.D) continue;
-                auto columns = [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring) + k * Sh::PART + at); };
-                if constexpr (E == 1)
-                    join1(now, [&](int k) { return reinterpret_cast<const float2*>(reinterpret_cast<const float*>(ring) + k * Sh::PART + ROWS * DP)[r]; },
-                          columns, m, l, o[x]);
-                else
-                    join4(now, [&](int k) { return factors[k0 + k][r]; }, columns, o[x]);
+            const float* const parts = reinterpret_cast<const float*>(ring);
+            auto columns = [&](int k, int x) {
+                const int e = tid + x * NTHR;
+                return reinterpret_cast<const float4*>(parts + k * Sh::PART + o_index(e / (DP / 4), e % (DP / 4) * 4, DP));
+            };
+            if constexpr (E == 1) {
+                const int r = tid / (DP / 4);
+                if (r < ch.rows)
+                    join1(now, [&](int k) { return reinterpret_cast<const float2*>(parts + k * Sh::PART + ROWS * DP)[r]; },
+                          [&](int k) { return columns(k, 0); }, m, l, o[0]);
+            } else {
+                join4<E>(now, [&](int k, int x) { return factors[k0 + k][(tid + x * NTHR) / (DP / 4)]; }, columns, o);
             }
         }
 #pragma unroll
