@@ -12,6 +12,9 @@
  *        visual token by the energy of the low-pass-filtered token sequence and
  *        keeps the highest-scoring tokens in their original order.
  *
+ * and what a decoder does with the tokens they leave: a paged key-value cache and the attention of one new
+ * token over it (luvc_kv_*, luvc_attn_decode).
+ *
  * General rules
  *   - Every function returns a luvc_status (int); 0 is success.  Nothing aborts
  *     or throws.  Argument errors are reported before any work is queued and
