@@ -483,10 +483,12 @@ def _kv_call(fn, cache: KvCache, *args) -> None:
 
 
 def kv_workspace_bytes(cache: KvCache, n: int) -> int:
+    """Bytes a caller's workspace for kv_fork or kv_compact of n sequences must have (256-byte aligned)."""
     return int(lib.luvc_kv_workspace_bytes(cache.struct, n))
 
 
 def attn_workspace_bytes() -> int:
+    """Bytes a caller's workspace for attn_decode must have (256-byte aligned, zeroed before its first use; one per stream)."""
     return int(lib.luvc_attn_workspace_bytes())
 
 
@@ -558,7 +560,8 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
                 workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None):
     """luvc_attn_decode: attention of the queries q [n, q_heads, D], one new token per sequence, over the cached tokens of
     `layer`.  key_bias: float32 [n, width], added to the scores of the first `width` tokens; scale 0: 1/sqrt(D).
-    Returns out [n, q_heads, D] and, with want_lse, the log-sum-exp of the scores [n, q_heads] float32."""
+    workspace: None, the library's own, which calls on other streams must not use at the same time, or attn_workspace_bytes()
+    zeroed bytes.  Returns out [n, q_heads, D] and, with want_lse, the log-sum-exp of the scores [n, q_heads] float32."""
     n, q_heads = q.shape[0], q.shape[1]
     stride = _token_stride(q, cache, q_heads, "q")
     if out is None:

@@ -122,8 +122,10 @@ def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
     rng = np.random.default_rng(1234 + page + D)
     r = Rig(luvc, dtype, pages=150, page=page, slots=12, max_pages=9, heads=heads, D=D)
     most = 9 * page
+    own = torch.full((luvc.kv_workspace_bytes(r.cache, 12),), 0xAB, dtype=torch.uint8, device="cuda")
     for step in range(40):
         m = r.model
+        ws = own if step % 2 else None                           # a caller's workspace needs no preparation
         used = [s for s in range(12) if m.ids[s]]
         empty = [s for s in range(12) if not m.ids[s]]
         what = rng.choice(["append", "fork", "compact", "free"], p=[0.4, 0.2, 0.3, 0.1])
@@ -134,7 +136,7 @@ def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
         elif what == "fork" and used and empty:
             n = int(rng.integers(1, len(empty) + 1))
             src, dst = rng.choice(used, n).tolist(), rng.permutation(empty)[:n].tolist()
-            luvc.kv_fork(r.cache, r.ints(src), r.ints(dst))
+            luvc.kv_fork(r.cache, r.ints(src), r.ints(dst), workspace=ws)
             for s, d in zip(src, dst):
                 m.fork(s, d)
             for d in dst:
@@ -156,7 +158,7 @@ def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
             table = torch.full((len(slots), width), 1 << 30, dtype=torch.int32)      # what is past counts[i] is not read
             for row, chosen in zip(table, idx):
                 row[:len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
-            luvc.kv_compact(r.cache, r.ints(first), r.ints(span), table.cuda(), counts=r.ints([len(x) for x in idx]), seqs=r.ints(slots))
+            luvc.kv_compact(r.cache, r.ints(first), r.ints(span), table.cuda(), counts=r.ints([len(x) for x in idx]), seqs=r.ints(slots), workspace=ws)
             old = [m.compact(s, f, sp, x) for s, f, sp, x in zip(slots, first, span, idx)]
             for pages in old:
                 m.drop(pages)
