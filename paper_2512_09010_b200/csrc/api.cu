@@ -87,13 +87,20 @@ void* attn_scratch() {
     const int dev = current_device();
     if (dev < 0) return nullptr;
     std::lock_guard<std::mutex> lock(first_use);
+    Scratch& sc = g_scratch[dev][kAttnWs];
     {
         std::lock_guard<std::mutex> inner(g_mutex);
-        if (g_scratch[dev][kAttnWs].ptr) return g_scratch[dev][kAttnWs].ptr;
+        if (sc.ptr) return sc.ptr;
     }
     const size_t bytes = attn_workspace_bytes();
-    void* p = scratch(kAttnWs, bytes);
-    if (p && (cudaMemset(p, 0, bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess)) return nullptr;
+    void* p = nullptr;
+    if (cudaMalloc(&p, bytes) != cudaSuccess || cudaMemset(p, 0, bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
+        cudaFree(p);                    // (during a capture, say) memory without the zeros is not kept
+        cudaGetLastError();
+        return nullptr;
+    }
+    std::lock_guard<std::mutex> inner(g_mutex);
+    sc.ptr = p; sc.bytes = bytes;
     return p;
 }
 
