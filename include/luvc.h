@@ -484,8 +484,8 @@ size_t luvc_attn_workspace_bytes(void);
 
 typedef struct {
     void* stream;            /* cudaStream_t; NULL = legacy default stream */
-    void* workspace;         /* device, 256-byte aligned, ZEROED by the caller before its first use, and again
-                                after LUVC_ERR_TIMEOUT (a call leaves what must be zero zeroed);
+    void* workspace;         /* device, 256-byte aligned, ZEROED by the caller before its first use (a call, also one
+                                that ends with LUVC_ERR_TIMEOUT, leaves what must be zero zeroed);
                                 NULL = library-owned scratch */
     size_t workspace_bytes;
     int32_t* device_status;  /* as in luvc_kv_opts */

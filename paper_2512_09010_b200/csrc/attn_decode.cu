@@ -8,8 +8,8 @@
 // Bound.  Every cached row is read once, for all query heads that share it: 2 G flops per cached element with G query heads
 // per key head, so HBM bounds long sequences up to the largest G in use, and latency short ones; what matters is to keep enough
 // bytes in flight on every SM, whatever the lengths.  Measured: 334 MB (eight sequences of 4173 to 16451 tokens, 8 key heads of 128,
-// bf16) in 62.7 us, 5.3 TB/s; while all SMs stream it is 7.2 TB/s, but SMs differ by a tenth in the bandwidth they get, and
-// the last 9 us belong to the slow ones.  The smallest call (one sequence of 97 tokens) takes 4.8 us.
+// bf16) in 63.0 us, 5.3 TB/s; while all SMs stream it is 7.2 TB/s, but SMs differ by a tenth in the bandwidth they get, and
+// the last 9 us belong to the slow ones.  The smallest call (one sequence of 97 tokens) takes 4.9 us.
 //
 // Split.  The work is the list of all tiles (KT tokens of one sequence and key head), sequence after sequence.  Each CTA (one per
 // SM) takes an equal part of that list, each of its warps an equal part of the CTA's, so no length leaves an SM idle and a
@@ -250,6 +250,7 @@ __device__ __forceinline__ void emit4(const AttnProblem& p, long long row, int d
 // What is joined in a CTA: the parts of warps first_warp .. first_warp + count - 1 of one (sequence, head).
 struct Chain {
     int count;                  // 0: none
+    int out;                    // 1: begins in this CTA and goes on in the next one
     int from;                   // which of the first warp's two pieces
     int rows, c0, c1, s0;       // c0 < c1: other CTAs have parts of it as well
     float vscale;
@@ -358,7 +359,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ unsigned scan_warp[NW];
     __shared__ __align__(16) float core_q[kCores ? NW : 1][kCores ? NH * DP : 4], core_p[kCores ? NW : 1][NH * 16];
     __shared__ float factors[ROWS * (DP / 4) > NTHR ? 64 : 1][ROWS];
-    __shared__ int last_flag[2], all_flag, out_chain;
+    __shared__ int last_flag[2], all_flag;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
 
@@ -373,8 +374,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     }
     if (lane < 2) piece_off[warp][lane] = 0;
     if (lane == 0) {
-        chains[warp].count = 0;
-        if (warp == 0) chains[NW].count = 0, out_chain = -1;
+        chains[warp].count = chains[warp].out = 0;
+        if (warp == 0) chains[NW].count = chains[NW].out = 0;
     }
     if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &vmap : &kmap) : "memory");
     pdl_trigger();
@@ -474,7 +475,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         q.first = x - q.tile;
         return q;
     };
-    // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.7 us, with two tiles
+    // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.8 us, with two tiles
     // 9.3, with three 11.8: even then a join across CTAs costs less than a warp's second tile).
     int per = max((int)((float)total * a.one_grid) - 1, 0);     // total / grid, rounded up
     per -= per >> 20;
@@ -575,8 +576,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
         const uint32_t k_lane = k_row * 128 + (((lane >> 4) ^ (k_row & 7)) << 4), v_lane = v_row * 128 + ((((lane >> 3) & 1) ^ (v_row & 7)) << 4);
         int left = wb - wa;
-        bool dead = false;                                      // a wait gave up
-        while (left > 0 && !dead) {
+        bool dead = false;                                      // a wait gave up: what is left is passed over, so that joins and counters go on
+        while (left > 0) {
             const int h = a.groups == 1 ? at.seg : at.seg / a.groups, r0 = (at.seg - h * a.groups) * ROWS;
             const int rows = min(ROWS, a.group - r0);
             const int len = length_of(slot_of(at.seq));
@@ -687,13 +688,20 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             if (token >= len) bias[j][x] = -INFINITY;
                             else if (token < p.bias_width) bias[j][x] = p.bias[at.seq * p.bias_stride + token];
                         }
-                {
+                if (!dead) {
                     const uint32_t bar = my_bar + 8 * stage;
                     int probes = 0;
                     while (!mbar_try_wait(bar, (phases >> stage) & 1) && ++probes < kWaitProbes) {}
-                    if (__any_sync(~0u, probes >= kWaitProbes)) { dead = true; break; }
                     phases ^= 1u << stage;
+                    if (__any_sync(~0u, probes >= kWaitProbes)) {
+                        dead = true;
+                        to_load = 0;
+                        for (; filled > 0; --filled, order >>= 4)   // let the copies in flight land
+                            for (probes = 0; !mbar_try_wait(my_bar + 8 * (order & 15), (phases >> (order & 15)) & 1) && ++probes < kWaitProbes;) {}
+                        if (lane == 0) *p.status = LUVC_ERR_TIMEOUT;
+                    }
                 }
+                if (dead) continue;
 #pragma unroll
                 for (int j = 0; j < Sh::SUB; ++j) {
                     if (j > 0 && at.tile * KT + 16 * j >= len) break;
@@ -907,7 +915,6 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     ++filled;
                 }
             }
-            if (dead) break;
             left -= count;
 
             // ---- the result, through the stage that was read last ----
@@ -979,11 +986,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     c.vscale = vscale;
                     c.row0 = row0;
                     c.s0 = s0;
-                    c.c0 = c.c1 = 0;
+                    c.c0 = c.c1 = c.out = 0;
                     if (s0 < cta_a || s1 > cta_b) {
                         c.c0 = (s0 + tol) / per;
                         c.c1 = (s1 - tol - 1) / per;
-                        if (s0 >= cta_a) out_chain = warp;
+                        c.out = s0 >= cta_a;
                     }
                 }
             }
@@ -996,14 +1003,6 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 }
             }
         }
-        if (dead) {                                             // let the copies in flight land, then report
-            while (filled-- > 0) {
-                const int stage = order & 15;
-                order >>= 4;
-                for (int probes = 0; !mbar_try_wait(my_bar + 8 * stage, (phases >> stage) & 1) && probes < kWaitProbes; ++probes) {}
-            }
-            if (lane == 0) *p.status = LUVC_ERR_TIMEOUT;
-        }
     }
     __syncthreads();
 
@@ -1013,9 +1012,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         float* const o = a.parts + ((size_t)cta * 2 + slot) * Sh::PART;
         return Part{o, reinterpret_cast<float2*>(o + ROWS * DP)};
     };
-    unsigned some = 0;
-#pragma unroll
-    for (int c = 0; c <= NW; ++c) some |= (chains[c].count ? 1u : 0u) << c;
+    const unsigned some = __ballot_sync(~0u, lane <= NW && chains[min(lane, NW)].count);
+    const int out_chain = __ffs(__ballot_sync(~0u, lane <= NW && chains[min(lane, NW)].out)) - 1;    // at most one: its last tile is this CTA's
     constexpr int E = (ROWS * (DP / 4) + NTHR - 1) / NTHR;      // four columns each, of a thread
     if constexpr (E == 1) {
         const int r = tid / (DP / 4), d = tid % (DP / 4) * 4, at = o_index(r, d, DP);
@@ -1192,7 +1190,8 @@ EncodeTiledFn encode_tiled_fn() {
 }
 
 int sm_count() {
-    static int sms = 0;
+    static std::atomic<int> known{0};
+    int sms = known.load(std::memory_order_relaxed);
     if (!sms) {
         int dev = 0;
         if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
@@ -1200,6 +1199,7 @@ int sm_count() {
             return 0;
         }
         if (sms > kMaxCtas) sms = kMaxCtas;
+        known.store(sms, std::memory_order_relaxed);
     }
     return sms;
 }
@@ -1227,7 +1227,7 @@ int launch(const AttnProblem& p) {
     a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
     const int sms = sm_count();
     if (!sms) return LUVC_ERR_CUDA;
-    a.limit = 2147483647 / (p.c.heads * a.groups);
+    a.limit = (2147483647 - kSnap) / (p.c.heads * a.groups);
     a.one_grid = 1.f / sms;
     a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
