@@ -347,8 +347,8 @@ struct MoveArgs {
 // Fills the pages of the plan's list, and settles the pages that change hands.  The work is the list of all (page, up to
 // kMoveRows of its rows, group of kMoveLanes (layer, K or V, head) triples); a CTA takes an equal, contiguous part of it.  Where rows
 // come from is looked up first, a row per thread, once for all the groups of the part; a thread then copies 16 bytes of a row for
-// all triples of a group, with as many loads in flight.  (Four triples and 64 registers let four CTAs share an SM: 196 us for
-// the 1.09 GB of a prune of eight videos, as with eight triples and two CTAs, and 11.6 instead of 12.3 us for one image.)
+// all triples of a group, with as many loads in flight.  (Four triples and 64 registers let four CTAs share an SM: 190 us for
+// the 1.09 GB of a prune of eight videos, 10.0 for one image; with eight triples and two CTAs 193 and 10.5.)
 constexpr int kMoveLanes = 4, kMoveRows = 64, kMoveThreads = 256;
 
 template <bool FORK>
@@ -683,13 +683,14 @@ int launch_plan(const PlanArgs& a, cudaStream_t stream) {
     return a.n <= 256 && a.c.pages <= 4 * PlanShared<256>::SWEEP ? launch_plan_as<KIND, 256>(a, stream) : launch_plan_as<KIND, 1024>(a, stream);
 }
 
-// `pages`: about how many are filled.  Four CTAs per SM run at a time; up to four times as many are launched for long copies, so
-// that SMs that get less bandwidth take fewer of them (1.09 GB: 196 us, with one wave 204).
+// `pages`: about how many are filled.  Four CTAs per SM run at a time; up to six times as many are launched for long copies, so
+// that SMs that get less bandwidth take fewer of them, as long as each has 128 KB to copy (1.09 GB: 189 us, with one wave of CTAs
+// 201, with four 191; last pages of 256 forks, 59 MB at most: one wave 20.8, two 21.7).
 template <bool FORK>
 int launch_move(const MoveArgs& a, long long pages, cudaStream_t stream) {
     const luvc_kv_cache& c = a.c;
-    const long long items = pages * ((c.page_size + kMoveRows - 1) / kMoveRows) * ((c.layers * 2 * c.heads + kMoveLanes - 1) / kMoveLanes);
-    const long long one = 4ll * sm_count(), grid = items / 4 < one ? one : items / 4 > 4 * one ? 4 * one : items / 4;
+    const long long one = 4ll * sm_count(), bytes = pages * c.page_size * c.layers * 2 * c.heads * c.D * a.es;
+    const long long waves = bytes / (one * (128 << 10)), grid = one * (waves < 1 ? 1 : waves > 6 ? 6 : waves);
     return launch_overlapped(kv_move_kernel<FORK>, (unsigned)grid, kMoveThreads, 0, stream, a);
 }
 
