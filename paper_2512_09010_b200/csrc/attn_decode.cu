@@ -29,7 +29,7 @@
 // that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
 // largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats (16 bits at least), because one
 // 16-bit float would cost as much again as the output's own rounding; tensor time is not the bound.  f32 caches use
-// tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 23 bits), or, where few heads share a row, fp32 on the CUDA cores.
+// tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 23 bits), or, where few heads share a row or it is long, fp32 on the CUDA cores.
 // Sums, maxima and O are fp32.
 
 #include <cuda.h>
@@ -126,8 +126,11 @@ struct Shape {
     static constexpr int SUB = NT > ES ? 2 : 1;
     static constexpr bool CORES = NT < 0;
     static constexpr int KT = 16 * SUB, STAGE = SUB * 2 * SUBK;
-    // three stages for each warp, 196,608 bytes in all: the more warps the smaller a row is
-    static constexpr int S = 3, NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
+    // Three stages for each warp, 196,608 bytes in all: the more warps the smaller a row is.  Two where an f32 row is long and
+    // its products, not HBM, are the bound, for half as many warps again (28 / 4 heads of 128, 159 MB: 50 instead of 57 us;
+    // 32 / 8, 318 MB: 70 and 76; 8 / 8 of 256, 50 MB: 18 and 24), but not for one head of 128 (32 / 32, 903 MB: 158 and 151).
+    static constexpr int S = ES == 4 && DPB >= 512 && !(NT == -1 && DPB == 512) ? 2 : 3;
+    static constexpr int NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = CORES ? 4 : 8 * NT;
     static constexpr int PART = ROWS * (DP + 2);                // floats of a partial result in the workspace: O, then (m, l) of each row
@@ -711,11 +714,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         f32_tile<DP, NH>(ks, vs, core_q[warp], core_p[warp], scale, bias[j][0], gone, core_m, core_l, core_o, lane);
                     } else {
                         // ---- S^T: rows are the 16 tokens, columns the query heads ----
-                        float s[NTX][4], s2[NTX][4];
+                        float s[NTX][4], s2[NTX][4], s3[NTX][4];    // sums that do not wait for one another
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.f;
+                            for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = s3[nt][c] = 0.f;
                         float done[NTX][4];                         // f32: finished sums of S
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
@@ -735,7 +738,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                     split_tf32(q[nt][k2][0], qh[0], ql[0]);
                                     split_tf32(q[nt][k2][1], qh[1], ql[1]);
                                     mma_tf32(s2[nt], lo, qh[0], qh[1]);
-                                    mma_tf32(s2[nt], hi, ql[0], ql[1]);
+                                    mma_tf32(NT == 1 ? s3[nt] : s2[nt], hi, ql[0], ql[1]);
                                     // tensor-core sums truncate: four steps at most in one, the rest rounded
                                     float part[4] = {0.f, 0.f, 0.f, 0.f};
                                     mma_tf32(k2 % 4 ? s[nt] : part, hi, qh[0], qh[1]);
@@ -764,7 +767,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
-                                const float x = kF32 ? done[nt][c] + s[nt][c] + s2[nt][c] : s[nt][c] + s2[nt][c];
+                                const float x = kF32 ? done[nt][c] + s[nt][c] + (s2[nt][c] + s3[nt][c]) : s[nt][c] + s2[nt][c];
                                 s[nt][c] = fmaf(x, qmul[nt][c & 1], bias[j][c >> 1]);
                             }
                         unsigned gone = 0;
@@ -853,26 +856,43 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                 }
                                 const int row0 = 8 * x + 2 * t4, row1 = row0 + 1;
 #pragma unroll
-                                for (int mt = 0; mt < MT; ++mt) {
-                                    uint32_t hi[4], lo[4];
+                                constexpr int MB = NT == 1 ? 4 : 1;             // 16-column groups at a time: products that do not wait for one another
+                                for (int m0 = 0; m0 < MT; m0 += MB) {
+                                    uint32_t hi[MB][4], lo[MB][4];
 #pragma unroll
-                                    for (int c = 0; c < 4; ++c) {
-                                        const int d = 16 * mt + 8 * (c & 1) + g, row = c >> 1 ? row1 : row0;
-                                        uint32_t u;
-                                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u)
-                                                     : "r"(vs + (d >> 5) * 2048 + row * 128 + ((((d & 31) >> 2) ^ (row & 7)) << 4) + (d & 3) * 4) : "memory");
-                                        if (c >> 1 ? drop1 : drop0) u = 0u;
-                                        split_tf32(u, hi[c], lo[c]);
-                                    }
+                                    for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                                    for (int nt = 0; nt < NT; ++nt) {
-                                        float add[4] = {0.f, 0.f, 0.f, 0.f};    // a long sum is kept with rounded additions
-                                        mma_tf32(add, lo, bh[nt][0], bh[nt][1]);
-                                        mma_tf32(add, hi, bl[nt][0], bl[nt][1]);
-                                        mma_tf32(add, hi, bh[nt][0], bh[nt][1]);
+                                        for (int c = 0; c < 4; ++c) {
+                                            const int d = 16 * (m0 + mb) + 8 * (c & 1) + g, row = c >> 1 ? row1 : row0;
+                                            uint32_t u;
+                                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u)
+                                                         : "r"(vs + (d >> 5) * 2048 + row * 128 + ((((d & 31) >> 2) ^ (row & 7)) << 4) + (d & 3) * 4) : "memory");
+                                            if (c >> 1 ? drop1 : drop0) u = 0u;
+                                            split_tf32(u, hi[mb][c], lo[mb][c]);
+                                        }
+                                    float add[MB][NTX][4];                      // a long sum is kept with rounded additions
 #pragma unroll
-                                        for (int c = 0; c < 4; ++c) o[mt][nt][c] += add[c];
-                                    }
+                                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                                        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                                            for (int c = 0; c < 4; ++c) add[mb][nt][c] = 0.f;
+                                            mma_tf32(add[mb][nt], lo[mb], bh[nt][0], bh[nt][1]);
+                                        }
+#pragma unroll
+                                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                                        for (int nt = 0; nt < NT; ++nt) mma_tf32(add[mb][nt], hi[mb], bl[nt][0], bl[nt][1]);
+#pragma unroll
+                                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                                        for (int nt = 0; nt < NT; ++nt) mma_tf32(add[mb][nt], hi[mb], bh[nt][0], bh[nt][1]);
+#pragma unroll
+                                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                            for (int c = 0; c < 4; ++c) o[m0 + mb][nt][c] += add[mb][nt][c];
                                 }
                             }
                         } else if constexpr (!kF8) {
@@ -1258,7 +1278,8 @@ int launch_heads(const AttnProblem& p) {
 
 // f32 caches with up to four query heads per key head run on the CUDA cores (measured, against the tensor cores: 32 / 32 heads of
 // 128, 812 MB, 141 and 200 us; 16 / 16 of 64, 131 MB, 30.0 and 32.7; 32 / 8 of 128, 203 MB, 54 and 64; 8 / 8 of 256, 406 MB, 94 and
-// 226).  The queries of more heads would not fit shared memory beside the ring.
+// 226), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 66 and 77 us, 8 / 1 52 and 53).  The
+// others do not: 28 / 4 of 128, 159 MB, 63 us in this form, 47 on the tensor cores; 16 / 2 of 64, 39 MB, 22 and 16.
 template <int DPB>
 int launch_cores(const AttnProblem& p) {
     return p.q_heads == p.c.heads ? launch<float, float, DPB, -1>(p) : launch<float, float, DPB, -4>(p);
@@ -1270,10 +1291,10 @@ size_t attn_workspace_bytes() { return kCounterBytes + (size_t)2 * kMaxCtas * 2 
 
 int attn_decode(const AttnProblem& p) {
     const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
-    if (p.c.dtype == LUVC_F32 && p.q_heads <= 4 * p.c.heads)
+    if (p.c.dtype == LUVC_F32 && (p.q_heads <= 4 * p.c.heads || bytes > 512))
         return bytes <= 256 ? launch_cores<256>(p) : bytes <= 512 ? launch_cores<512>(p) : launch_cores<1024>(p);
     if (p.c.dtype == LUVC_F32)
-        return bytes <= 256 ? launch_heads<float, float, 256>(p) : bytes <= 512 ? launch_heads<float, float, 512>(p) : launch<float, float, 1024, 1>(p);
+        return bytes <= 256 ? launch_heads<float, float, 256>(p) : launch_heads<float, float, 512>(p);
     if (p.c.dtype == LUVC_BF16)
         return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256>(p)
                                                                                                : launch_heads<__nv_bfloat16, __nv_bfloat16, 512>(p);
