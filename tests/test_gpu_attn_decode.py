@@ -158,6 +158,19 @@ def test_one_long_sequence_is_joined_across_all_ctas(luvc, dtype, q_heads, heads
         assert torch.equal(luvc.attn_decode(q, c), out)
 
 
+@pytest.mark.parametrize("dtype,q_heads,heads,D", [("e4m3", 5, 5, 16), ("e4m3", 10, 2, 48), ("e4m3", 16, 1, 64), ("e4m3", 40, 2, 64), ("e4m3", 16, 16, 64),
+                                                   ("f32", 12, 1, 256), ("f32", 18, 2, 200), ("f32", 5, 1, 132), ("f32", 14, 2, 112), ("f32", 20, 1, 128)])
+def test_short_and_long_rows(luvc, dtype, q_heads, heads, D):
+    for lengths, page in (([1, 0, 700, 63, 16, 17, 333], 48), ([3300], 16), ([95] * 40, 32)):
+        c = build(luvc, dtype, lengths, heads, D, page, seed=q_heads + len(lengths), nan=True)
+        q = torch.randn((len(lengths), q_heads, D), generator=torch.Generator().manual_seed(D)).to(c.io_dtype).cuda()
+        check(luvc, c, q, *luvc.attn_decode(q, c, want_lse=True))
+    bias = torch.randn((40, 80), generator=torch.Generator().manual_seed(4)).cuda()
+    bias[3] = -float("inf")
+    bias[5, 7:50] = torch.finfo(torch.float32).min
+    check(luvc, c, q, *luvc.attn_decode(q, c, key_bias=bias, want_lse=True), bias=bias)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3", "f32"])
 def test_biases_and_masks(luvc, dtype):
     lengths = [200, 33, 16, 70, 40]
