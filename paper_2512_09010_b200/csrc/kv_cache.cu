@@ -342,16 +342,21 @@ struct MoveArgs {
     int es;                  // bytes of an element
     MoveList move;
     int* status;
+    // of the launch: (layer, K or V, head) triples and groups of them; rows of a piece at most, pieces of a page, pieces looked up at a
+    // time; 16-byte parts of a row; teams, and threads of one
+    int triples, groups, cap, chunks, batch, units, teams, size;
 };
 
 // Fills the pages of the plan's list, and settles the pages that change hands.  The work is the list of all (page, up to
 // kMoveRows of its rows, group of kMoveLanes (layer, K or V, head) triples); a CTA takes an equal, contiguous part of it.  Where rows
 // come from is looked up first, a row per thread, once for all the groups of the part; a thread then copies 16 bytes of a row for
 // all triples of a group, with as many loads in flight.  (Four triples and 64 registers let four CTAs share an SM: 190 us for
-// the 1.09 GB of a prune of eight videos, 10.0 for one image; with eight triples and two CTAs 193 and 10.5.)
+// the 1.09 GB of a prune of eight videos, 10.0 for one image; with eight triples and two CTAs 193 and 10.5.)  Where a piece of
+// a page has no more 16-byte parts than half the threads, the CTA works in TEAMS, each on a group of its own (16 heads of 64 in
+// 8 bits, pages of 16, 620 MB: 140 us, without 211; a fork of 16 such sequences 15.1 and 21.5).
 constexpr int kMoveLanes = 4, kMoveRows = 64, kMoveThreads = 256;
 
-template <bool FORK>
+template <bool FORK, bool TEAMS>
 __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_constant__ MoveArgs a) {
     __shared__ long long src_row[kMoveThreads];             // row of head 0 of a layer's pool; -1: none
     __shared__ long long dst_row[kMoveThreads / 16];        // first row of a piece (a page's rows, at most kMoveRows)
@@ -384,15 +389,13 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
         }
     }
 
-    const int triples = c.layers * 2 * c.heads, groups = (triples + kMoveLanes - 1) / kMoveLanes;
-    const int cap = min(ps, kMoveRows), chunks = (ps + kMoveRows - 1) / kMoveRows, batch = kMoveThreads / cap;   // page sizes: 16 and up
+    const int triples = a.triples, groups = a.groups, cap = a.cap, chunks = a.chunks, batch = a.batch, units = a.units, teams = TEAMS ? a.teams : 1;
     // below 2^31: each item is 256 bytes of a pool at least
     const unsigned work = (unsigned)(a.move.head[0] * chunks * groups), share = work / gridDim.x, more = work % gridDim.x;
     const unsigned w0 = share * blockIdx.x + min(blockIdx.x, more), w1 = w0 + share + (blockIdx.x < more);
     if (w0 >= w1) return;
-    const int units = c.D * a.es / 16;
     const size_t row_bytes = (size_t)c.D * a.es, head_bytes = ps * row_bytes, layer_bytes = (size_t)c.pages * c.heads * head_bytes;
-    const int row0 = tid / units, off0 = (tid - row0 * units) * 16;     // a thread's first 16 bytes of a piece
+    const int size = TEAMS ? a.size : kMoveThreads, team = TEAMS ? tid / size : 0, unit0 = tid - team * size, row0 = unit0 / units, off0 = (unit0 - row0 * units) * 16;      // a thread's first 16 bytes of a piece
     const unsigned first_piece = w0 / groups, last_piece = (w1 - 1) / groups;
 
     for (unsigned piece0 = first_piece; piece0 <= last_piece; piece0 += batch) {
@@ -430,7 +433,13 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
         const unsigned wa = max(w0, piece0 * groups), wb = min(w1, (piece0 + batch) * groups);
         int at = 0, group = wa - piece0 * groups;           // (only the first piece of the part may begin inside)
         int layer = group * kMoveLanes / (2 * c.heads), rest = group * kMoveLanes - layer * 2 * c.heads;   // of the group's first triple
-        for (unsigned w = wa; w < wb; ++w) {
+        for (unsigned w = team < teams ? wa + team : wb; w < wb; w += teams) {
+            if (TEAMS) {
+                at = w / groups - piece0;
+                group = w % groups;
+                layer = group * kMoveLanes / (2 * c.heads);
+                rest = group * kMoveLanes - layer * 2 * c.heads;
+            }
             const int live = min(kMoveLanes, triples - group * kMoveLanes);
             unsigned char* base[kMoveLanes];
 #pragma unroll
@@ -444,8 +453,8 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
                 }
             }
             int row = row0, off = off0;
-            for (int u = tid; u < rows_of[at] * units; u += kMoveThreads) {
-                if (u != tid) { row = u / units; off = (u - row * units) * 16; }
+            for (int u = unit0; u < rows_of[at] * units; u += size) {
+                if (u != unit0) { row = u / units; off = (u - row * units) * 16; }
                 const long long from = src_row[at * cap + row];
                 if (from < 0) continue;
                 const size_t src = from * row_bytes + off, dst = (dst_row[at] + row) * row_bytes + off;
@@ -687,11 +696,20 @@ int launch_plan(const PlanArgs& a, cudaStream_t stream) {
 // that SMs that get less bandwidth take fewer of them, as long as each has 128 KB to copy (1.09 GB: 189 us, with one wave of CTAs
 // 201, with four 191; last pages of 256 forks, 59 MB at most: one wave 20.8, two 21.7).
 template <bool FORK>
-int launch_move(const MoveArgs& a, long long pages, cudaStream_t stream) {
+int launch_move(MoveArgs& a, long long pages, cudaStream_t stream) {
     const luvc_kv_cache& c = a.c;
+    a.triples = c.layers * 2 * c.heads;
+    a.groups = (a.triples + kMoveLanes - 1) / kMoveLanes;
+    a.cap = c.page_size < kMoveRows ? c.page_size : kMoveRows;          // page sizes: 16 and up
+    a.chunks = (c.page_size + kMoveRows - 1) / kMoveRows;
+    a.batch = kMoveThreads / a.cap;
+    a.units = c.D * a.es / 16;
+    a.teams = 2 * a.cap * a.units <= kMoveThreads ? kMoveThreads / (a.cap * a.units) : 1;
+    a.size = a.teams > 1 ? a.cap * a.units : kMoveThreads;
     const long long one = 4ll * sm_count(), bytes = pages * c.page_size * c.layers * 2 * c.heads * c.D * a.es;
     const long long waves = bytes / (one * (128 << 10)), grid = one * (waves < 1 ? 1 : waves > 6 ? 6 : waves);
-    return launch_overlapped(kv_move_kernel<FORK>, (unsigned)grid, kMoveThreads, 0, stream, a);
+    return a.teams > 1 ? launch_overlapped(kv_move_kernel<FORK, true>, (unsigned)grid, kMoveThreads, 0, stream, a)
+                       : launch_overlapped(kv_move_kernel<FORK, false>, (unsigned)grid, kMoveThreads, 0, stream, a);
 }
 
 }  // namespace

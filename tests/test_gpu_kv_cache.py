@@ -170,6 +170,30 @@ def test_a_life_of_appends_forks_prunes_and_frees(luvc, dtype, page, D, heads):
         r.check()
 
 
+@pytest.mark.parametrize("dtype,page,D,heads,layers", [("e4m3", 16, 16, 37, 3), ("e4m3", 16, 48, 32, 2), ("e4m3", 16, 128, 9, 3), ("bf16", 32, 24, 21, 2),
+                                                       ("f32", 16, 28, 16, 3), ("f32", 48, 256, 5, 2)])
+def test_short_rows_are_moved_by_teams(luvc, dtype, page, D, heads, layers):
+    r = Rig(luvc, dtype, pages=900, page=page, slots=12, max_pages=4000 // page, layers=layers, heads=heads, D=D)
+    m = r.model
+    r.append([0, 1, 2, 3], [3501, 2000, 31, 1777])
+    first, span, keep = [3, 500, 0, 0], [3400, 1490, 31, 1777], [1700, 1489, 30, 888]
+    rng = np.random.default_rng(D)
+    idx = [np.sort(rng.permutation(n)[:k]).tolist() for n, k in zip(span, keep)]
+    table = torch.zeros((4, max(keep)), dtype=torch.int32)
+    for row, chosen in zip(table, idx):
+        row[:len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
+    luvc.kv_compact(r.cache, r.ints(first), r.ints(span), table.cuda(), counts=r.ints(keep), seqs=r.ints([0, 1, 2, 3]))
+    for pages in [m.compact(s, f, n, x) for s, f, n, x in zip(range(4), first, span, idx)]:
+        m.drop(pages)
+    r.check()
+    luvc.kv_fork(r.cache, r.ints([0, 0, 1, 2, 3, 3]), r.ints([4, 5, 6, 7, 8, 9]))
+    for s, d in zip([0, 0, 1, 2, 3, 3], [4, 5, 6, 7, 8, 9]):
+        m.fork(s, d)
+    for d in range(4, 10):
+        m.share(d)
+    r.check()
+
+
 @pytest.mark.parametrize("pages,slots,held", [(40000, 2100, 500), (8000, 420, 150)])
 def test_a_large_pool_and_many_sequences(luvc, pages, slots, held):
     # more pages than one sweep of the scan covers, more sequences than threads of its CTA (first pool), free pages far up
