@@ -51,8 +51,6 @@ using namespace ptx;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
 constexpr int kMaxPartBytes = 16 * (256 + 2) * 4;   // of a partial result: 16 rows of 256 sums, and their (m, l)
-constexpr int kSnap = 12;                       // tiles by which a part may move its ends to those of a (sequence, head): a join across CTAs
-                                                // costs about as much (one sequence of 16000 tokens: 13.1 us, with 8 tiles 13.9, with 6 15.9)
 constexpr size_t kCounterBytes = 3 * kMaxCtas * sizeof(unsigned);
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
@@ -132,6 +130,12 @@ struct Shape {
     // 32 / 8, 318 MB: 70 and 76; 8 / 8 of 256, 50 MB: 18 and 24), but not for one head of 128 (32 / 32, 903 MB: 158 and 151).
     static constexpr int S = ES == 4 && DPB >= 512 && !(NT == -1 && DPB == 512) ? 2 : 3;
     static constexpr int NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
+    // Tiles by which a part may move its ends to those of a (sequence, head).  A join across CTAs costs about as much as two tiles of
+    // every warp: 24 sequences of 886 to 1395 tokens, 28 / 4 heads of 128 in 8 bits (16 warps): 14.0 us, with 12 tiles 15.8; six of
+    // 5625 to 6957 in bf16 (8 warps): 18.0, with 6 tiles 18.8, with 24 17.9; 12 of 600 to 2500, 12 / 1 heads of 256 in f32 (3
+    // warps): 39, with 9 tiles 42, with 12 46.  (Parts of unequal length can cost more than the joins: 32 / 8 heads, 24 sequences in
+    // 8 bits 20.3, with 12 tiles 19.6.)
+    static constexpr int SNAP = 2 * NW;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = CORES ? 4 : 8 * NT;
     static constexpr int PART = ROWS * (DP + 2);                // floats of a partial result in the workspace: O, then (m, l) of each row
@@ -485,7 +489,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     per -= per >> 20;
     while ((long long)per * (int)gridDim.x < total) ++per;
     per = max(per, NW);
-    const int tol = min(per / 2, kSnap);
+    const int tol = min(per / 2, Sh::SNAP);
     auto bound_of = [&](int c) {                                // start of CTA c's part, moved to a near (sequence, head) boundary
         if (c == 0) return 0;
         if ((long long)c * per >= total) return total;
@@ -858,8 +862,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                     split_tf32(__float_as_uint(pf[nt][2 * x + 1]), bh[nt][1], bl[nt][1]);
                                 }
                                 const int row0 = 8 * x + 2 * t4, row1 = row0 + 1;
-#pragma unroll
                                 constexpr int MB = NT == 1 ? 4 : 1;             // 16-column groups at a time: products that do not wait for one another
+#pragma unroll
                                 for (int m0 = 0; m0 < MT; m0 += MB) {
                                     uint32_t hi[MB][4], lo[MB][4];
 #pragma unroll
@@ -1250,7 +1254,7 @@ int launch(const AttnProblem& p) {
     a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
     const int sms = sm_count();
     if (!sms) return LUVC_ERR_CUDA;
-    a.limit = (2147483647 - kSnap) / (p.c.heads * a.groups);
+    a.limit = (2147483647 - Sh::SNAP) / (p.c.heads * a.groups);
     a.one_grid = 1.f / sms;
     a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;
@@ -1282,7 +1286,7 @@ int launch_heads(const AttnProblem& p) {
 
 // f32 caches with up to four query heads per key head run on the CUDA cores (measured, against the tensor cores: 32 / 32 heads of
 // 128, 812 MB, 141 and 200 us; 16 / 16 of 64, 131 MB, 30.0 and 32.7; 32 / 8 of 128, 203 MB, 54 and 64; 8 / 8 of 256, 406 MB, 94 and
-// 226), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 66 and 77 us, 8 / 1 52 and 53).  The
+// 226), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 63 and 77 us, 8 / 1 52 and 53).  The
 // others do not: 28 / 4 of 128, 159 MB, 63 us in this form, 47 on the tensor cores; 16 / 2 of 64, 39 MB, 22 and 16.
 template <int DPB>
 int launch_cores(const AttnProblem& p) {
