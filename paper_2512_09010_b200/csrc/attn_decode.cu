@@ -228,15 +228,20 @@ __device__ __forceinline__ float2 join_factors(int count, GetMl get_ml, Put put,
     return make_float2(m, l);
 }
 // The second, by a thread for its E times four columns: adds the parts times their factors, part after part, so that the reads of
-// all columns are under way together.  factor(k, x) and columns(k, x) are of part k and the thread's columns x.
+// all columns are under way together.  factor(k, x) and columns(k, x) are of part k and the thread's columns x; `last`: whether the
+// thread has the last of its E (where E times the threads are more than a part's columns, some do not: nothing is read for them).
 template <int E, typename Factor, typename Columns>
-__device__ __forceinline__ void join4(int count, Factor factor, Columns columns, float4 (&o)[E]) {
+__device__ __forceinline__ void join4(int count, bool last, Factor factor, Columns columns, float4 (&o)[E]) {
 #pragma unroll 2
     for (int k = 0; k < count; ++k) {
         float4 v[E];
         float w[E];
 #pragma unroll
-        for (int x = 0; x < E; ++x) { w[x] = factor(k, x); v[x] = *columns(k, x); }
+        for (int x = 0; x < E; ++x) {
+            w[x] = 0.f;
+            v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (x < E - 1 || last) { w[x] = factor(k, x); v[x] = *columns(k, x); }
+        }
 #pragma unroll
         for (int x = 0; x < E; ++x) {
             o[x].x = fmaf(w[x], v[x].x, o[x].x); o[x].y = fmaf(w[x], v[x].y, o[x].y);
@@ -1042,6 +1047,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const unsigned some = __ballot_sync(~0u, lane <= NW && chains[min(lane, NW)].count);
     const int out_chain = __ffs(__ballot_sync(~0u, lane <= NW && chains[min(lane, NW)].out)) - 1;    // at most one: its last tile is this CTA's
     constexpr int E = (ROWS * (DP / 4) + NTHR - 1) / NTHR;      // four columns each, of a thread
+    const bool all_columns = E * NTHR == ROWS * (DP / 4) || tid + (E - 1) * NTHR < ROWS * (DP / 4);     // the last E included
     if constexpr (E == 1) {
         const int r = tid / (DP / 4), d = tid % (DP / 4) * 4, at = o_index(r, d, DP);
 #pragma unroll 1
@@ -1084,8 +1090,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             float4 o[E];
 #pragma unroll
             for (int x = 0; x < E; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-            // (rows past the last one hold sums of nothing: they are read, and not written)
-            join4<E>(ch.count, [&](int k, int x) { return ml_of[w0 + k][k ? 0 : ch.from][(tid + x * NTHR) / (DP / 4)].x; },
+            // (rows of a part past the last head's hold sums of nothing: they are read, and not written)
+            join4<E>(ch.count, all_columns, [&](int k, int x) { return ml_of[w0 + k][k ? 0 : ch.from][(tid + x * NTHR) / (DP / 4)].x; },
                      [&](int k, int x) {
                          const int e = tid + x * NTHR;
                          return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) +
@@ -1159,7 +1165,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     join1(now, [&](int k) { return reinterpret_cast<const float2*>(parts + k * Sh::PART + ROWS * DP)[r]; },
                           [&](int k) { return columns(k, 0); }, m, l, o[0]);
             } else {
-                join4<E>(now, [&](int k, int x) { return factors[k0 + k][(tid + x * NTHR) / (DP / 4)]; }, columns, o);
+                join4<E>(now, all_columns, [&](int k, int x) { return factors[k0 + k][(tid + x * NTHR) / (DP / 4)]; }, columns, o);
             }
         }
 #pragma unroll

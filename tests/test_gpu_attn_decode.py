@@ -242,6 +242,18 @@ def test_layers_slots_strides_and_streams(luvc, dtype):
     check(luvc, c, q[rest], got[rest], None, layer=2, seqs=seqs[rest].tolist())
 
 
+@pytest.mark.parametrize("q_heads,heads,D", [(7, 1, 128), (16, 2, 80), (5, 1, 68), (12, 1, 128), (12, 1, 256), (18, 3, 100)])
+def test_every_number_of_parts_around_a_full_ring(luvc, q_heads, heads, D):
+    # Parts of one (sequence, head) that are joined at once fill shared memory up to the last one that fits (47 of 8 rows of 128
+    # floats; 23 of 16).  One sequence of T tiles of 16 tokens has about T / 6 parts (six warps to a CTA, a tile for each), with
+    # three or four warps more.
+    for tokens in list(range(2100, 2500, 56)) + list(range(4300, 4760, 32)) + [4465, 4500, 4560]:
+        c = build(luvc, "f32", [tokens], heads, D, 32, seed=tokens, nan=True)
+        q = torch.randn((1, q_heads, D), generator=torch.Generator().manual_seed(D)).cuda()
+        check(luvc, c, q, *luvc.attn_decode(q, c, want_lse=True))
+    assert luvc.check_status() == 0
+
+
 def test_results_repeat_bit_for_bit(luvc):
     c = build(luvc, "bf16", [9000, 100, 2500], 4, 128, 16, seed=14)
     q = torch.randn((3, 28, 128), generator=torch.Generator().manual_seed(6)).bfloat16().cuda()
