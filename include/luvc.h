@@ -388,7 +388,8 @@ int luvc_spu_static_status(void* cuda_stream);
  * itself is host memory and is read during the call only.  The books of a new cache are lengths = 0,
  * refs = 0, table = -1; only the functions below write them, entirely on the device, so that a call's
  * page numbers need no host round trip and the calls can be captured in a CUDA graph (after a warm-up
- * call has grown the library's scratch, or with a workspace of the caller's).
+ * call has grown the library's scratch, or with a workspace of the caller's).  Scratch that a graph was
+ * captured with stays allocated until luvc_shutdown, also when a later call needs more.
  */
 typedef struct {
     void* k;                 /* [layers, pages, heads, page_size, D] of element type dtype */

@@ -47,6 +47,11 @@ constexpr int kMaxDevices = 64;
 struct Scratch { void* ptr = nullptr; size_t bytes = 0; };
 Scratch g_scratch[kMaxDevices][kSlots];
 std::mutex g_mutex;
+// Buffers of kKvWs that a larger one has replaced: a captured graph may still use them, so they stay allocated until luvc_shutdown.
+// Each is at least twice the one before (while memory lasts), so together they are smaller than the one in use.
+constexpr int kMaxReplaced = 64;
+void* g_replaced[kMaxDevices][kMaxReplaced];
+int g_replaced_count[kMaxDevices];
 
 int current_device() {
     int dev = 0;
@@ -60,9 +65,17 @@ void* scratch(Slot s, size_t bytes) {
     std::lock_guard<std::mutex> lock(g_mutex);
     Scratch& sc = g_scratch[dev][s];
     if (sc.bytes >= bytes && sc.ptr) return sc.ptr;
-    if (sc.ptr) { cudaDeviceSynchronize(); cudaFree(sc.ptr); sc.ptr = nullptr; sc.bytes = 0; }
     void* p = nullptr;
-    if (cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return nullptr; }
+    if (s == kKvWs && sc.ptr) {
+        if (g_replaced_count[dev] == kMaxReplaced) return nullptr;
+        const size_t twice = 2 * sc.bytes;
+        if (twice > bytes && cudaMalloc(&p, twice) == cudaSuccess) bytes = twice;
+        else cudaGetLastError();
+    } else if (sc.ptr) {
+        cudaDeviceSynchronize(); cudaFree(sc.ptr); sc.ptr = nullptr; sc.bytes = 0;
+    }
+    if (!p && cudaMalloc(&p, bytes) != cudaSuccess) { cudaGetLastError(); return nullptr; }
+    if (sc.ptr) g_replaced[dev][g_replaced_count[dev]++] = sc.ptr;
     sc.ptr = p; sc.bytes = bytes;
     return p;
 }
@@ -248,6 +261,7 @@ int luvc_shutdown(void) {
         if (sc.ptr) cudaFree(sc.ptr);
         sc.ptr = nullptr; sc.bytes = 0;
     }
+    while (g_replaced_count[dev] > 0) cudaFree(g_replaced[dev][--g_replaced_count[dev]]);
     return LUVC_OK;
 }
 

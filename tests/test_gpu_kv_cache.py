@@ -386,6 +386,48 @@ def test_a_step_can_be_captured_and_replayed(luvc):
     r.check()
 
 
+def test_a_captured_fork_keeps_its_scratch(luvc):
+    """The library's scratch grows for a call that needs more; a graph captured before goes on with the memory it was captured with."""
+    luvc.shutdown()                                                        # scratch starts small
+    r = Rig(luvc, "bf16", pages=40, page=16, slots=6, max_pages=5)
+    r.append([0, 1], [40, 21])
+    src, dst = r.ints([0, 1, 0]), r.ints([2, 3, 4])
+
+    def step():
+        luvc.kv_fork(r.cache, src, dst)
+        luvc.kv_compact(r.cache, zero, span, idx, seqs=dst)
+        luvc.kv_free(r.cache, dst)
+
+    zero, span, idx = r.ints([0] * 3), r.ints([17] * 3), r.ints([[1, 4, 16]] * 3)
+    step()                                                                 # grows the scratch, loads the kernels
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    big = Rig(luvc, "bf16", pages=4000, page=16, slots=400, max_pages=5000, layers=1, heads=1, D=8)
+    big.append([0], [77])
+    luvc.kv_fork(big.cache, big.ints([0] * 399), big.ints(list(range(1, 400))))
+    for d in range(1, 400):
+        big.model.fork(0, d)
+    for d in range(1, 400):
+        big.model.share(d)
+    big.check()
+    # what a freed scratch would be given to: its contents are looked at after the replays
+    fill = [torch.full((1 << 16,), 0x5a5a5a5a, dtype=torch.int32, device="cuda") for _ in range(64)]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    r.check()
+    big.check()
+    assert all(bool((f == 0x5a5a5a5a).all()) for f in fill)
+    luvc.kv_fork(r.cache, src, dst)
+    for s, d in ((0, 2), (1, 3), (0, 4)):
+        r.model.fork(s, d)
+    for d in (2, 3, 4):
+        r.model.share(d)
+    r.check()
+
+
 def test_python_refusals(luvc):
     pool = torch.zeros((1, 4, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(TypeError):
