@@ -462,12 +462,22 @@ def _ints(t: torch.Tensor | None, cache: KvCache, count: int, name: str):
     return t.data_ptr()
 
 
-def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
-    o = KvOpts(_raw_stream(cache.index))
+def _buffers(o, cache: KvCache, workspace, device_status) -> None:
+    """Enters a caller's workspace and status block (None: the library's) into the options."""
     if workspace is not None:
+        if workspace.get_device() != cache.index or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on %s" % cache.device)
         o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if device_status is not None:
+        if device_status.dtype is not _INT32 or device_status.numel() < 4 or device_status.get_device() != cache.index \
+                or not device_status.is_contiguous():
+            raise ValueError("device_status must be a contiguous int32 tensor of 4 entries at least on %s" % cache.device)
         o.device_status = device_status.data_ptr()
+
+
+def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
+    o = KvOpts(_raw_stream(cache.index))
+    _buffers(o, cache, workspace, device_status)
     return o
 
 
@@ -571,10 +581,7 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     o = AttnOpts(_raw_stream(cache.index))
     if scale:
         o.scale = scale
-    if workspace is not None:
-        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    if device_status is not None:
-        o.device_status = device_status.data_ptr()
+    _buffers(o, cache, workspace, device_status)
     if key_bias is not None:
         if key_bias.dtype is not torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n \
                 or key_bias.get_device() != cache.index or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):

@@ -462,3 +462,28 @@ def test_python_refusals(luvc):
     with pytest.raises(luvc.LuvcError) as e:
         luvc.attn_decode(torch.zeros((2, 3, 64), dtype=torch.bfloat16, device="cuda"), c)
     assert e.value.status == 2
+
+
+def test_workspaces_and_status_blocks_elsewhere_are_refused(luvc):
+    """Memory that the kernels cannot reach, or that is shorter than they take it for, is refused before anything is queued."""
+    pool = torch.zeros((1, 4, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+    c = luvc.KvCache(pool, pool.clone(), 2, 2)
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    row = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    calls = (lambda **o: luvc.kv_fork(c, one - 1, one, **o), lambda **o: luvc.kv_compact(c, one - 1, one - 1, one[None] - 1, **o),
+             lambda **o: luvc.attn_decode(row, c, **o))
+    size = luvc.attn_workspace_bytes()
+    for call in calls:
+        for bad in (torch.zeros(size, dtype=torch.uint8), torch.zeros((size // 256, 512), dtype=torch.uint8, device="cuda")[:, :256]):
+            with pytest.raises(ValueError):
+                call(workspace=bad)
+        with pytest.raises(luvc.LuvcError) as e:
+            call(workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+        assert e.value.status == 8
+    calls += (lambda **o: luvc.kv_reserve(c, one, **o), lambda **o: luvc.kv_write(c, row, row, **o), lambda **o: luvc.kv_free(c, one, **o))
+    for call in calls:
+        for bad in (torch.zeros(4, dtype=torch.int32), torch.zeros(4, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"),
+                    torch.zeros(8, dtype=torch.int32, device="cuda")[::2]):
+            with pytest.raises(ValueError):
+                call(device_status=bad)
+    assert luvc.check_status() == 0 and not c.meta[:6].any()
