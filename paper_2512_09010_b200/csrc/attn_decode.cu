@@ -106,10 +106,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// x as a sum of two tf32 operands, each the nearest: 11 bits, and 11 of the 12 that are left
+// x as a sum of two tf32 operands: the nearest with 11 bits, and what is left, 12 bits, of which the product's operand keeps 11.  (The
+// bit that may be dropped is a tie, so rounding it would not be closer.)  What is not finite shows as a NaN in lo, if not in hi:
+// the sum that rounds hi makes 0 of the NaN 0x7fffffff, and infinity of the largest floats.
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
     hi = (x + 0x1000u) & 0xffffe000u;
-    lo = (__float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u) & 0xffffe000u;
+    lo = __float_as_uint(__fsub_rn(__uint_as_float(x), __uint_as_float(hi)));
 }
 
 // ---- shapes ---------------------------------------------------------------------------------------------
@@ -355,6 +357,60 @@ __device__ __forceinline__ void f32_tile(uint32_t ks, uint32_t vs, const float* 
 // Column of a lane's element j in the form above.
 template <int DP>
 __device__ __forceinline__ int f32_column(int lane, int j) { return DP == 64 ? 2 * lane + j : 128 * (j >> 2) + 4 * lane + (j & 3); }
+
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// The partial result of tokens t0 .. t1 - 1 of a (sequence, head group) once more, by a warp, product by product as the formula has
+// them, into a stage (O) and ml.  The tensor-core forms split weights, and rows of 32 bits, into parts whose products an infinity or
+// a value near the end of the range turns into NaN (inf times the lower part of a weight, which may be 0 or negative; inf - inf), so a
+// result that is not finite is worked out again.  It is rare, and need not be fast.
+template <typename T, int DP>
+__device__ __noinline__ void plain_piece(const Args& a, int seq, int h, int r0, int rows, int t0, int t1, float scale, float* os, float2* ml) {
+    const AttnProblem& p = a.p;
+    const int lane = threadIdx.x & 31, ps = p.c.page_size, D = p.c.D;
+    const int32_t* const table = p.c.table + (long long)(p.seqs ? p.seqs[seq] : seq) * p.c.max_pages;
+    const T* const q0 = static_cast<const T*>(p.q) + seq * p.q_stride + ((long long)h * a.group + r0) * D;
+    const size_t layer = (size_t)p.layer * a.rows_total;
+    for (int r = 0; r < rows; ++r) {
+        float q[DP / 32], o[DP / 32], m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) {
+            q[j] = lane + 32 * j < D ? as_float(q0[r * D + lane + 32 * j]) : 0.f;
+            o[j] = 0.f;
+        }
+        for (int t = t0; t < t1; ++t) {
+            const float bias = t < p.bias_width ? p.bias[seq * p.bias_stride + t] : 0.f;
+            const int page = table[t / ps];
+            if (bias == -INFINITY) continue;
+            const bool held = (unsigned)page < (unsigned)p.c.pages;         // as in the tiles: rows of no page are zeros
+            const size_t at = (layer + (held ? (page * p.c.heads + h) * ps + t % ps : 0)) * D;
+            float s = 0.f, v[DP / 32];
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) {
+                const int d = lane + 32 * j;
+                v[j] = 0.f;
+                if (held && d < D) {
+                    s = fmaf(q[j], as_float(static_cast<const T*>(p.c.k)[at + d]), s);
+                    v[j] = as_float(static_cast<const T*>(p.c.v)[at + d]);
+                }
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+            s = fmaf(s, scale, bias);
+            const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+            const float f = exp2_fast((m - base) * kLog2e), w = exp2_fast((s - base) * kLog2e);
+            m = top;
+            l = fmaf(l, f, w);
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) o[j] = lane + 32 * j < D ? fmaf(o[j], f, w * v[j]) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) os[o_index(r, lane + 32 * j, DP)] = o[j];
+        if (lane == 0) ml[r] = make_float2(m, l);
+    }
+    __syncwarp();
+}
 
 template <typename TQ, typename TC, int DPB, int NT>
 __global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
@@ -983,6 +1039,19 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = o[mt][nt][c];
                     }
             __syncwarp();
+            if constexpr (!kCores && !kF8) {                    // (an e4m3 cache has no infinities, and its rows are not split)
+                float z[4] = {0.f, 0.f, 0.f, 0.f};              // 0, or NaN
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        z[c] = fmaf(l[nt][c & 1], 0.f, z[c]);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) z[c] = fmaf(o[mt][nt][c], 0.f, z[c]);
+                    }
+                if (__any_sync(~0u, z[0] + z[1] + (z[2] + z[3]) != 0.f) && !dead)
+                    plain_piece<TC, DP>(a, at.seq, h, r0, rows, (at.tile - count) * KT, min(at.tile * KT, len), scale, os, ml_of[warp][which]);
+            }
             const long long row0 = (long long)at.seq * p.q_heads + h * a.group + r0;
             if (whole) {
                 if (lane < rows) {                              // the factor takes the maximum's place

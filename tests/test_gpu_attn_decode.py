@@ -218,6 +218,70 @@ def test_a_nan_in_a_row_that_counts_is_seen(luvc):
     assert bool(luvc.attn_decode(q, c).isnan().all())
 
 
+@pytest.mark.parametrize("dtype,q_heads,heads,D", [("bf16", 28, 4, 128), ("bf16", 12, 1, 64), ("bf16", 6, 2, 200), ("f32", 28, 4, 128), ("f32", 16, 2, 60),
+                                                   ("f32", 12, 1, 128), ("f32", 34, 2, 64), ("f32", 4, 4, 128), ("f32", 12, 1, 256)])
+@pytest.mark.parametrize("what", ["v inf", "v both", "v nan", "v large", "k inf", "k -inf", "k nan", "k large", "q large"])
+def test_what_is_not_finite_counts_as_the_formula_says(luvc, dtype, q_heads, heads, D, what):
+    """Infinities, NaN (also the one arithmetic gives) and values near the ends of the range, in rows that count: an infinite value makes
+    its column infinite and leaves the others; a score of -inf has weight zero; NaN goes through; large finite values stay finite."""
+    lengths = [300, 2000]
+    c = build(luvc, dtype, lengths, heads, D, 16, seed=D + q_heads, nan=False)
+    q = torch.randn((2, q_heads, D), generator=torch.Generator().manual_seed(7)).to(c.io_dtype).cuda()
+    nan = torch.tensor(0x7fffffff, dtype=torch.int32).view(torch.float32).item() if dtype == "f32" else math.nan
+
+    def put(pool, slot, token, d, x):
+        cell = pool[0, int(c.table[slot, token // 16]), :, token % 16, d]
+        if dtype == "f32" and x != x:                             # the very bits
+            cell.view(torch.int32).fill_(0x7fffffff if token % 2 else -1)
+        else:
+            cell.fill_(x)
+
+    group = q_heads // heads
+    for slot, tokens in enumerate(([5, 131], [44, 1700, 1999])):
+        for t in tokens:
+            if what == "v inf":
+                put(c.v, slot, t, 3, math.inf), put(c.v, slot, t, D - 1, -math.inf)
+            elif what == "v both":
+                put(c.v, slot, t, 3, math.inf if t % 2 else -math.inf)
+            elif what == "v nan":
+                put(c.v, slot, t, 3, nan)
+            elif what == "v large":
+                put(c.v, slot, t, 3, 1e35), put(c.v, slot, t, 5, -1e35)
+            elif what in ("k inf", "k -inf"):                     # "k -inf": the same sign for every head, so that all scores of t are -inf
+                put(c.k, slot, t, 2, math.inf if what == "k inf" else -math.inf)
+            elif what == "k nan":
+                put(c.k, slot, t, 2, nan)
+            elif what == "k large":
+                put(c.k, slot, t, 2, 1e37)
+    if what == "k -inf":
+        q[:, :, 2] = q[:, :, 2].abs() + 0.25
+    if what == "k large":
+        q[:, :, 2] *= 1e-37
+    if what == "q large":
+        q[:, :, 2] *= 1e36
+        c.k[..., 2] *= 1e-36
+    out, lse = luvc.attn_decode(q, c, want_lse=True)
+    assert luvc.check_status() == 0
+    u = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+    for i, n in enumerate(lengths):
+        k, v = (x.repeat_interleave(group, 1) for x in rows(c, i, 0, n))
+        s = torch.einsum("hd,thd->ht", q[i].double(), k) * D ** -0.5
+        p = torch.exp(s - s.amax(1, keepdim=True))
+        p = p / p.sum(1, keepdim=True)
+        term = p.t()[:, :, None] * v
+        want = term.sum(0)
+        size = (q[i].double()[:, None].abs() * k.transpose(0, 1).abs()).sum(2) * D ** -0.5
+        off = torch.where(size.isfinite(), size, 0.0).amax(1, keepdim=True) * (D + 3) * 2.0 ** -23      # of scores, as above
+        bound = term.abs().sum(0) * (2 * off + 2 * 2.0 ** -17 * (dtype != "f32") + (n / 16 + D + 64) * 2.0 ** -23) * 1.01 + u * want.abs()
+        got = out[i].double()
+        assert torch.equal(got.isnan(), want.isnan()), (i, int(got.isnan().sum()), int(want.isnan().sum()))
+        assert torch.equal(got.isinf(), want.isinf()) and torch.equal(got[got.isinf()], want[want.isinf()])
+        fine = want.isfinite()
+        assert bool(((got - want).abs() <= bound)[fine].all())
+        assert torch.equal(lse[i].isnan(), s.isnan().any(1) | (s == math.inf).any(1))
+    assert what in ("k inf", "k nan") or bool(out.isfinite().any())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_layers_slots_strides_and_streams(luvc, dtype):
     c = build(luvc, dtype, [100, 0, 45, 300], 2, 64, 16, layers=3, seed=13)
