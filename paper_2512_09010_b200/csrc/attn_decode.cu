@@ -27,8 +27,10 @@
 // pipe is not the bound (18 % busy with an e4m3 cache).
 // Roundings: Q and K are used as they are (an e4m3 cache goes to f16, which is exact; the query, scaled by a power of two so
 // that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
-// largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats (16 bits at least), because one
-// 16-bit float would cost as much again as the output's own rounding; tensor time is not the bound.  f32 caches use
+// largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats, because one 16-bit float would cost as much
+// again as the output's own rounding; tensor time is not the bound.  bf16 keeps 16 bits of every weight.  f16, with an e4m3 cache,
+// keeps 22, but nothing below 2^-25: there the weights' reference also follows scores that stay far below it, so that a weight is
+// off by 2^-16 of the largest one of its 16 tokens at most (see kRise).  f32 caches use
 // tf32 products of hi + lo pairs (hi hi + hi lo + lo hi: 23 bits), or, where few heads share a row or it is long, fp32 on the CUDA cores.
 // Sums, maxima and O are fp32.
 
@@ -53,6 +55,11 @@ constexpr int kMaxCtas = 256;                   // CTAs the workspace has room f
 constexpr int kMaxPartBytes = 16 * (256 + 2) * 4;   // of a partial result: 16 rows of 256 sums, and their (m, l)
 constexpr size_t kCounterBytes = 3 * kMaxCtas * sizeof(unsigned);
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
+// With an e4m3 cache weights are f16: below 65504, in steps of 2^-24 of one.  The reference m is set kLead below the maximum of 16
+// scores when that is above m + kRise, or below m - kFall (a token far above all others, as at the start of a text, leaves only small
+// weights).  So the largest of 16 weights is between e^-kFall and e^kRise, and e^kLead at least where it is the largest so far.
+constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f;
+constexpr float kMostGain = 60.f;               // log2 of what a lane's sum of weights may become when m falls
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 
 // ---- the instructions of this file -----------------------------------------------------------------
@@ -828,8 +835,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             }
                         }
                         // ---- weights ----
-                        // Their reference m follows the maximum only when a score passes it by kSlack: weights stay below
-                        // e^kSlack, sums lose nothing, and most tiles need no maximum across the warp.
+                        // Their reference m follows the maximum only when a score passes it by kSlack (e4m3: kRise): weights stay
+                        // below e^kSlack, sums lose nothing, and most tiles need no maximum across the warp.
                         bool over = false;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
@@ -848,11 +855,44 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                 for (int c = 0; c < 4; ++c)
                                     if (c >> 1 ? gone1 : gone0) s[nt][c] = -INFINITY;
                         }
+                        if constexpr (kF8) {
+                            unsigned seen = 0;                      // a bit per head whose largest score is not too small; bit 16: one is too large
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int b = 0; b < 2; ++b) {
+                                    const float x = fmaxf(s[nt][b], s[nt][b + 2]);
+                                    if (x >= m[nt][b] - kFall) seen |= 1u << (8 * nt + b);
+                                    over = over || x > m[nt][b] + kRise;
+                                }
+                            if (__reduce_or_sync(~0u, seen << (2 * t4) | (over ? 1u << 16 : 0u)) != (1u << (8 * NTX)) - 1u) {
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int b = 0; b < 2; ++b) {
+                                        float x = fmaxf(s[nt][b], s[nt][b + 2]), most = l[nt][b];
+#pragma unroll
+                                        for (int d = 4; d <= 16; d *= 2) {
+                                            x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+                                            most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+                                        }
+                                        float to = m[nt][b];
+                                        if (x > to + kRise) to = x - kLead;
+                                        else if (x > -INFINITY && x < to - kFall)
+                                            to -= fminf(to - (x - kLead), fmaxf(kMostGain - __log2f(most), 0.f) / kLog2e);
+                                        const float f = exp2_fast((m[nt][b] - (to == -INFINITY ? 0.f : to)) * kLog2e);
+                                        m[nt][b] = to;
+                                        l[nt][b] *= f;
+#pragma unroll
+                                        for (int mt = 0; mt < MT; ++mt) { o[mt][nt][b] *= f; o[mt][nt][b + 2] *= f; }
+                                    }
+                            }
+                        } else
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) over = over || s[nt][c] > m[nt][c & 1] + kSlack;
-                        if (__any_sync(~0u, over)) {
+                        if (!kF8 && __any_sync(~0u, over)) {
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -202,6 +202,48 @@ def test_biases_and_masks(luvc, dtype):
     assert ((out[4].double() - last).abs() <= 2.0 ** -8 * last.abs() + 1e-6).all()
 
 
+@pytest.mark.parametrize("q_heads,heads,D", [(32, 8, 128), (5, 5, 64), (12, 1, 256), (28, 4, 80), (3, 1, 32)])
+@pytest.mark.parametrize("gap", [6, 10, 14, 18, 30])
+def test_small_weights_of_an_8_bit_cache(luvc, q_heads, heads, D, gap):
+    """A token whose score is far above all others and whose value row is zero (for every other head): what is left are the small weights.
+
+    They enter their product as the sum of two halves of 11 bits, in steps of 2^-24 of what 1 stands for; a rounding is off by 2^-25.
+    The largest weight of 16 tokens is at least e^-6 there, and e^8 where the largest weight of all is among them.  A warp's part of
+    the tokens begins anywhere, so every 16 tokens are given the larger bound of the tiles they can be in."""
+    lengths = [700, 1, 16, 40, 333, 2500]
+    c = build(luvc, "e4m3", lengths, heads, D, 16, seed=gap + D, nan=True)
+    q = 0.3 * torch.randn((len(lengths), q_heads, D), generator=torch.Generator().manual_seed(D))
+    q[:, :, 0] = 0.0
+    q[:, ::2, 0] = 80.0
+    q = q.bfloat16().cuda()
+    c.k.view(torch.uint8)[..., 0] = 0
+    for slot, t in enumerate([0, 0, 5, 39, 200, 1777]):
+        page, at = int(c.table[slot, t // 16]), t % 16
+        top = gap * D ** 0.5 / 80 / c.k_scale[0]
+        assert float(top.max()) < 448
+        c.k[0, page, :, at, 0] = top.to(torch.float8_e4m3fn)
+        c.v.view(torch.uint8)[0, page, :, at] = 0
+    out, lse = luvc.attn_decode(q, c, want_lse=True)
+    assert luvc.check_status() == 0
+    for i, n in enumerate(lengths):
+        k, v = (x.repeat_interleave(q_heads // heads, 1) for x in rows(c, i, 0, n))
+        s = torch.einsum("hd,thd->ht", q[i].double(), k) * D ** -0.5
+        size = torch.einsum("hd,thd->ht", q[i].double().abs(), k.abs()) * D ** -0.5
+        off = (size * (D + 3) * 2.0 ** -23 + D ** -0.5 * 2.0 ** -25 * q[i].double().abs().amax(1)[:, None] * k.abs().sum(2).t()).amax(1, keepdim=True)
+        top = s.amax(1, keepdim=True)
+        w = torch.exp(s - top)
+        total = w.sum(1, keepdim=True)
+        tiles = torch.nn.functional.pad(w, (0, -n % 16)).view(q_heads, -1, 16).amax(2)
+        floor = torch.where(tiles == 1.0, math.exp(-8), tiles * math.exp(6)).repeat_interleave(16, 1)[:, :n] * 2.0 ** -25
+        want = torch.einsum("ht,thd->hd", w / total, v)
+        spread = torch.einsum("ht,thd->hd", w / total, v.abs())
+        bound = (2.0 ** -8 * want.abs() + spread * (2 * off + 2 * 2.0 ** -17 + (n / 16 + D + 64) * 2.0 ** -23)
+                 + torch.einsum("ht,thd->hd", floor / total, v.abs())) * 1.01
+        diff = (out[i].double() - want).abs()
+        assert bool((diff <= bound).all()), (i, n, float((diff / bound).max()))
+        assert bool(((lse[i].double() - (top + total.log())[:, 0]).abs() <= off[:, 0] + (n / 16 + 64) * 2.0 ** -23 + top[:, 0].abs() * 2.0 ** -22).all())
+
+
 def test_large_scores_and_a_scale(luvc):
     c = build(luvc, "bf16", [500, 77], 2, 128, 16, seed=11)
     q = 20 * torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
