@@ -470,14 +470,19 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
     }
 }
 
+// A CTA per sequence.  Each looks at all slots of the call first: whether any of them is out of range, and then none is freed, must not
+// depend on which CTA comes first (the status word that one sets is read by the others).
 __global__ void __launch_bounds__(128) kv_free_kernel(const __grid_constant__ luvc_kv_cache c, const int32_t* seqs, int* status) {
     __shared__ int len;
     pdl_trigger();
     pdl_wait();
-    if (__syncthreads_or(stopped(status))) return;
     const int slot = seqs ? seqs[blockIdx.x] : (int)blockIdx.x;
-    if (slot < 0 || slot >= c.slots) {
-        if (threadIdx.x == 0) *status = LUVC_ERR_SHAPE;
+    const bool stop = stopped(status);
+    bool bad = false;
+    if (seqs)                                               // else slots 0 .. n - 1, which the host has checked
+        for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) bad = bad || (unsigned)seqs[i] >= (unsigned)c.slots;
+    if (__syncthreads_or(stop || bad)) {
+        if (!stop && threadIdx.x == 0 && blockIdx.x == 0) *status = LUVC_ERR_SHAPE;
         return;
     }
     if (threadIdx.x == 0) len = atomicExch(&c.lengths[slot], 0);

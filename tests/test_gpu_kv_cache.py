@@ -279,6 +279,25 @@ def test_rows_before_the_sequence_are_not_written(luvc):
     assert bool(r.cache.k[0, r.model.table[0][0], :, 3:].isnan().all())
 
 
+@pytest.mark.parametrize("bad", [0, 1777, 2999])
+@pytest.mark.parametrize("slot", [-1, 3000, 1 << 30])
+def test_a_slot_that_does_not_exist_frees_none_of_the_others(luvc, bad, slot):
+    r = Rig(luvc, "bf16", pages=3100, page=16, slots=3000, max_pages=2, layers=1, heads=1, D=8)
+    r.append(list(range(3000)), [1 + s % 16 for s in range(3000)])
+    before = r.cache.meta.clone()
+    seqs = list(range(3000))
+    seqs[bad] = slot
+    for _ in range(5):
+        luvc.kv_free(r.cache, r.ints(seqs))
+        assert luvc.check_status() == 2
+        assert torch.equal(r.cache.meta, before)
+    del seqs[bad]
+    luvc.kv_free(r.cache, r.ints(seqs))
+    for s in seqs:
+        r.model.free(s)
+    r.check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "e4m3"])
 @pytest.mark.parametrize("heads,D", [(4, 128), (3, 80), (1, 16)])
 def test_written_rows_are_enhanced_and_rounded_once(luvc, dtype, heads, D):
