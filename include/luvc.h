@@ -447,7 +447,9 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
  * sizes       optional DEVICE [tokens] int32, the out_sizes of luvc_oim_merge*: the values are written
  *             enhanced, V + log(size) (Eq. 2), formed in fp32 and rounded once
  * An E4M3 cache stores x / scale, saturated at +-448, rounded to nearest even.  Rows that would fall before
- * the start of their sequence are not written (LUVC_ERR_SHAPE in the status word).  Tokens that a fork shares are
+ * the start of their sequence, or whose slot is out of range, are not written (LUVC_ERR_SHAPE in the status
+ * word); all others are, also by the luvc_kv_write calls that follow, until another call finds the word.  (Until
+ * luvc_read_status it may hold the status in its low 8 bits.)  Tokens that a fork shares are
  * shared: writing them again writes them for every sequence that holds their page.
  */
 int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,

@@ -123,7 +123,7 @@ int read_status_block(int* block, cudaStream_t stream) {
     int host = 0;
     if (cudaMemcpy(&host, block, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return LUVC_ERR_CUDA;
     if (host != 0 && cudaMemset(block, 0, sizeof(int)) != cudaSuccess) return LUVC_ERR_CUDA;
-    return host;
+    return host & kStatusMask;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

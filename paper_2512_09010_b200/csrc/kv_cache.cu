@@ -30,7 +30,13 @@ constexpr int kWarpPages = 32 * kPerLane;
 constexpr int kMaxNeed = 1 << 26;                           // pages one call takes for one sequence (2^30 tokens at least)
 constexpr int kClaimed = -1;                                // lengths[] of a slot that the running call has claimed
 
-__device__ __forceinline__ bool stopped(const int* status) { return *reinterpret_cast<const volatile int*>(status) != 0; }
+__device__ __forceinline__ int status_of(int* status) { return *reinterpret_cast<volatile int*>(status); }
+
+// For a call that has found the status word set and does nothing: rows that a write has skipped become a plain status, at which further
+// writes stop too.
+__device__ __forceinline__ void stop_writes(int* status, int word) {
+    if (word == kRowsSkipped && threadIdx.x == 0) *status = word & kStatusMask;
+}
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
@@ -238,7 +244,11 @@ __global__ void __launch_bounds__(THREADS) kv_plan_kernel(const __grid_constant_
     int r[kPerLane];                                        // looked at last, but independent of everything before
     sweep_load(c.refs, c.pages, 0, r);
     if (KIND != kReserve && tid == 0) a.move.head[1] = 0;
-    if (__syncthreads_or(stopped(a.status))) return;
+    const int word = status_of(a.status);
+    if (__syncthreads_or(word)) {
+        stop_writes(a.status, word);
+        return;
+    }
     const long long most = (long long)c.max_pages * c.page_size;
 
     // what each sequence needs; its slot is claimed, so that one named twice is noticed
@@ -477,12 +487,13 @@ __global__ void __launch_bounds__(128) kv_free_kernel(const __grid_constant__ lu
     pdl_trigger();
     pdl_wait();
     const int slot = seqs ? seqs[blockIdx.x] : (int)blockIdx.x;
-    const bool stop = stopped(status);
+    const int word = status_of(status);
     bool bad = false;
     if (seqs)                                               // else slots 0 .. n - 1, which the host has checked
         for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) bad = bad || (unsigned)seqs[i] >= (unsigned)c.slots;
-    if (__syncthreads_or(stop || bad)) {
-        if (!stop && threadIdx.x == 0 && blockIdx.x == 0) *status = LUVC_ERR_SHAPE;
+    if (__syncthreads_or(word || bad)) {
+        if (!word && threadIdx.x == 0 && blockIdx.x == 0) *status = LUVC_ERR_SHAPE;
+        stop_writes(status, word);
         return;
     }
     if (threadIdx.x == 0) len = atomicExch(&c.lengths[slot], 0);
@@ -605,7 +616,8 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv_write_kernel(const __grid
     const int mine = threadIdx.x / cols, tokens = min(a.per, a.tokens - t0);
     pdl_trigger();
     pdl_wait();
-    if (__syncthreads_or(stopped(a.status))) return;
+    const int word = status_of(a.status);                   // this launch sets no other value than the one that does not stop it
+    if (__syncthreads_or(word != 0 && word != kRowsSkipped)) return;
     uint4 kx[kWriteBatch], vx[kWriteBatch];
     auto fetch = [&](int col, int t) {
 #pragma unroll
@@ -635,7 +647,7 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv_write_kernel(const __grid
                 const int page = c.table[(long long)slot * c.max_pages + pos / ps];
                 if (page >= 0 && page < c.pages) row = (long long)page * c.heads * ps + pos % ps;
             }
-            if (row < 0) *a.status = LUVC_ERR_SHAPE;
+            if (row < 0) *a.status = kRowsSkipped;
             bias_of[lane] = a.sizes ? logf((float)a.sizes[t]) : 0.f;
             row_of[lane] = row;
         }

@@ -69,6 +69,9 @@ struct OimProblem {
 // [1] > 0 replaces the probe limit of the chain's waits, [2] is subtracted from the first image's
 // count of finished lines of the first step, so that the waits on it can never be satisfied.
 enum { kStatusWord = 0, kStatusProbeLimit = 1, kStatusHoldBack = 2, kStatusWords = 4 };
+// What luvc_kv_write puts into word 0 when it skips rows: a LUVC_ERR_SHAPE that luvc_kv_write itself, whose CTAs read the word while
+// others may set it, does not stop at.  Any other cache call that finds it does nothing and makes it the plain status.
+constexpr int kStatusMask = 0xff, kRowsSkipped = 0x100 | LUVC_ERR_SHAPE;
 size_t oim_workspace_bytes(int B, int H, int W, int D, int dtype, int matching = 0);
 int oim_run(const OimProblem& p);
 int oim_value_enhance(const void* values, const int32_t* sizes, long long rows, int D, int dtype, void* out,

@@ -298,6 +298,38 @@ def test_a_slot_that_does_not_exist_frees_none_of_the_others(luvc, bad, slot):
     r.check()
 
 
+def test_rows_that_cannot_be_placed_leave_the_others_written(luvc):
+    n, each, layers = 50, 1000, 3                                        # more rows than run at a time
+    r = Rig(luvc, "bf16", pages=n * 63 + 2, page=16, slots=n, max_pages=64, layers=layers, heads=1, D=8)
+    slots = list(range(n))
+    luvc.kv_reserve(r.cache, r.ints([each] * n))
+    for s in slots:
+        r.model.reserve(s, range(1 + s * each, 1 + (s + 1) * each))
+    starts = r.ints([each * s for s in range(n + 1)])
+    ids = sum((r.model.ids[s] for s in slots), [])
+    rows = [[rows_for(ids, layer, 1, 8, kind, torch.bfloat16) for kind in (0, 1)] for layer in range(layers)]
+    for lost in (0, 7, 49):
+        for pool in (r.cache.k, r.cache.v):
+            pool.fill_(float("nan"))
+        wrong = r.ints(slots)
+        wrong[lost] = n
+        for layer in range(layers):                                       # a report of a write does not stop the writes of further layers
+            luvc.kv_write(r.cache, *rows[layer], layer=layer, starts=starts, seqs=wrong)
+        before = r.cache.meta.clone()
+        luvc.kv_reserve(r.cache, r.ints([1] * n))                         # but everything else,
+        luvc.kv_free(r.cache, r.ints(slots))
+        luvc.kv_write(r.cache, rows[0][0] + 1, rows[0][1], starts=starts)  # and then writes too
+        assert luvc.check_status() == 2
+        assert luvc.check_status() == 0
+        assert torch.equal(r.cache.meta, before)
+        pages = torch.tensor(r.model.table[lost], device="cuda")
+        for pool in (r.cache.k, r.cache.v):
+            assert bool(pool[:, pages].isnan().all())
+        for layer in range(layers):
+            luvc.kv_write(r.cache, *(x[lost * each:(lost + 1) * each] for x in rows[layer]), layer=layer, starts=r.ints([0, each]), seqs=r.ints([lost]))
+        r.check()                                                        # every other row was there
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "e4m3"])
 @pytest.mark.parametrize("heads,D", [(4, 128), (3, 80), (1, 16)])
 def test_written_rows_are_enhanced_and_rounded_once(luvc, dtype, heads, D):
