@@ -482,7 +482,8 @@ int luvc_kv_compact(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
 
 /* ---- attention of one new token ------------------------------------------- */
 
-/* Bytes of workspace luvc_attn_decode needs, whatever the sequences and heads (about 17 MB). */
+/* Bytes of workspace luvc_attn_decode needs, whatever the sequences and heads (about 17 MB).  Calls that share
+ * one must not overlap (their results are undefined if they do; calls after them are not affected). */
 size_t luvc_attn_workspace_bytes(void);
 
 typedef struct {

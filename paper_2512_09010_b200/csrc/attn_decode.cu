@@ -18,7 +18,7 @@
 // (sequence, head) that lies wholly in its part.  Of the others a warp has at most two, at the ends of its part; their
 // partial results stay in the ring stage that was read last (that stage is not filled again) and are joined by the CTA
 // when its warps are done, then, where a sequence crosses CTAs, through the workspace by the CTA that comes last (a counter that
-// wraps to zero; the parts are added in the order of the list, so results do not depend on which that is).
+// is zero again then; the parts are added in the order of the list, so results do not depend on which that is).
 //
 // Matrix instructions.  The products are narrow, 8 or 16 columns (the query heads of a key head): mma.sync m16n8k16 with tokens, or
 // columns of V, as M and query heads as N.  S^T = K Q^T with K from ldmatrix, then O^T += V^T P^T with V from
@@ -53,7 +53,7 @@ using namespace ptx;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCtas = 256;                   // CTAs the workspace has room for (one per SM)
 constexpr int kMaxPartBytes = 16 * (256 + 2) * 4;   // of a partial result: 16 rows of 256 sums, and their (m, l)
-constexpr size_t kCounterBytes = 3 * kMaxCtas * sizeof(unsigned);
+constexpr size_t kCounterBytes = 5 * kMaxCtas * sizeof(unsigned);
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
 // With an e4m3 cache weights are f16: below 65504, in steps of 2^-24 of one.  The reference m is set kLead below the maximum of 16
 // scores when that is above m + kRise, or below m - kFall (a token far above all others, as at the start of a text, leaves only small
@@ -161,7 +161,8 @@ struct Args {
     int limit;                  // tiles of all sequences up to which the list can be numbered in 32 bits
     float one_grid;             // 1 / CTAs
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
-    unsigned* counters;         // [3][kMaxCtas]: arrivals of (sequence, head)s, of their first groups, of the other groups
+    unsigned* counters;         // [5][kMaxCtas]: arrivals of (sequence, head)s, of their first groups, of the other groups; groups that
+                                // are done; CTAs that are done with these
     float* parts;               // [2][kMaxCtas][2] of PART floats: of CTAs, of groups of CTAs
 };
 
@@ -174,6 +175,15 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
     const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
+
+// Arrival number i of n at a counter that is zero before the first and after the last of them; true for the one that completes it.  The
+// summands are 1, and 1 - n for i = 0: their sum is zero whatever comes in between, so calls that overlap, and take each other's arrivals
+// for their own, leave zero behind all the same.
+__device__ __forceinline__ unsigned arrive_count(unsigned* counter, int i, int n) {
+    const unsigned x = i ? 1u : 1u - (unsigned)n;
+    return atomicAdd(counter, x) + x;
+}
+__device__ __forceinline__ bool arrive(unsigned* counter, int i, int n) { return arrive_count(counter, i, n) == 0u; }
 
 // One partial result in the workspace: rows of O (o_index) and (m, l) of each row.
 struct Part {
@@ -1220,17 +1230,26 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // Up to kDirect parts are joined at once.  More (few long sequences with few heads) are joined in groups of kGroup, by the last
     // to arrive of each group, and the groups by the last of these: 148 parts take two short joins instead of one long one.
     constexpr int kDirect = Sh::CAP < 48 ? Sh::CAP : 48, kGroup = 12;
+    // How often the groups' counter is counted up depends on who is last of each, and goes wrong where calls overlap: so the CTA that is
+    // the last of all to pass it sets it to zero (which it is, in calls that do not).
+    auto pass_groups = [&](const Chain& ch) { return arrive_count(a.counters + 4 * kMaxCtas + ch.c0, blockIdx.x - ch.c0, ch.c1 - ch.c0 + 1); };
+    auto groups_passed = [&](const Chain& ch, unsigned count) {
+        if (count == 0u) a.counters[3 * kMaxCtas + ch.c0] = 0u;
+    };
     __threadfence();
     __syncthreads();
     if (tid < 64 && lane == 0) {
         bool last = false;
         if (warp == 0 ? in : out_chain >= 0) {
             const Chain& ch = chains[warp == 0 ? NW : out_chain];
-            const int count = ch.c1 - ch.c0 + 1, first = (blockIdx.x - ch.c0) / kGroup * kGroup;    // of this CTA's group
-            const unsigned wrap = (count <= kDirect ? count : min(kGroup, count - first)) - 1;
-            // a CTA can be the first of a group of the (sequence, head) it begins in, and the beginning of another one
-            unsigned* const counter = a.counters + (count <= kDirect ? ch.c0 : first == 0 ? kMaxCtas + ch.c0 : 2 * kMaxCtas + ch.c0 + first);
-            last = atomicInc(counter, wrap) == wrap;
+            const int count = ch.c1 - ch.c0 + 1, i = blockIdx.x - ch.c0, first = i / kGroup * kGroup;       // of this CTA's group
+            if (count <= kDirect) {
+                last = arrive(a.counters + ch.c0, i, count);
+            } else {
+                // a CTA can be the first of a group of the (sequence, head) it begins in, and the beginning of another one
+                last = arrive(a.counters + (first == 0 ? kMaxCtas + ch.c0 : 2 * kMaxCtas + ch.c0 + first), i - first, min(kGroup, count - first));
+                if (!last) groups_passed(ch, pass_groups(ch));
+            }
         }
         last_flag[warp] = last;
     }
@@ -1305,11 +1324,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         const int groups = (count + kGroup - 1) / kGroup;
         __threadfence();
         __syncthreads();
-        if (tid == 0) all_flag = atomicInc(&a.counters[c0], (unsigned)(groups - 1)) == (unsigned)(groups - 1);
+        if (tid == 0) all_flag = arrive(a.counters + 3 * kMaxCtas + c0, first / kGroup, groups);
         __syncthreads();
-        if (!all_flag) continue;
         __threadfence();
-        gather(ch, groups, group_part, true, Part{});
+        const unsigned passed = tid == 0 ? pass_groups(ch) : 1u;     // the answer is looked at after the join
+        if (all_flag) gather(ch, groups, group_part, true, Part{});
+        groups_passed(ch, passed);
     }
 }
 

@@ -368,6 +368,35 @@ def test_results_repeat_bit_for_bit(luvc):
         assert torch.equal(luvc.attn_decode(q, c), first)
 
 
+@pytest.mark.parametrize("own", [False, True])
+def test_calls_after_calls_that_overlapped_are_right(luvc, own):
+    """Calls that share a workspace must not overlap, and what they give if they do is undefined; but when they have ended the workspace is
+    as it was: calls that are kept in order from then on are right."""
+    ws = torch.zeros(luvc.attn_workspace_bytes(), dtype=torch.uint8, device="cuda") if own else None
+    g = torch.Generator().manual_seed(3)
+    jobs = []
+    shapes = (([30000], 8, 1, 64), ([2000], 8, 1, 64), ([5000, 700], 8, 2, 64), ([16451, 4173, 9000], 32, 8, 128), ([20000, 20001], 16, 4, 128),
+              ([60000], 8, 2, 128), ([7000] * 7, 12, 3, 128))
+    for i, (lengths, q_heads, heads, D) in enumerate(shapes):
+        c = build(luvc, "bf16", lengths, heads, D, 16, seed=i, nan=False)
+        q = torch.randn((len(lengths), q_heads, D), generator=g).bfloat16().cuda()
+        jobs.append((c, q, luvc.attn_decode(q, c, workspace=ws)))
+        check(luvc, c, q, jobs[-1][2], None)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    for a in range(len(jobs)):
+        for b in range(len(jobs)):
+            torch.cuda.synchronize()
+            for k in range(12):
+                for s, j in zip(streams, (a, b, b, a)):
+                    with torch.cuda.stream(s):
+                        luvc.attn_decode(jobs[j][1], jobs[j][0], workspace=ws)
+            torch.cuda.synchronize()
+            for c, q, want in jobs:
+                for _ in range(2):
+                    assert torch.equal(luvc.attn_decode(q, c, workspace=ws), want), (a, b)
+    assert luvc.check_status() == 0
+
+
 def test_offsets_past_32_bits(luvc):
     # the last pages of a pool of more than 2^32 elements per tensor (8 GB of one byte each)
     heads, D, page = 8, 256, 64
