@@ -268,15 +268,7 @@ int luvc_shutdown(void) {
 int luvc_check_status(void* cuda_stream) {
     int* word = status_word();
     if (!word) return LUVC_ERR_CUDA;
-    const int status = read_status_block(word, static_cast<cudaStream_t>(cuda_stream));
-    if (status == LUVC_ERR_TIMEOUT) {   // an attention call that gave up may have left a counter of its workspace behind
-        const int dev = current_device();
-        std::lock_guard<std::mutex> lock(g_mutex);
-        const Scratch& sc = g_scratch[dev < 0 ? 0 : dev][kAttnWs];
-        if (dev >= 0 && sc.ptr && (cudaMemset(sc.ptr, 0, sc.bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess))
-            return LUVC_ERR_CUDA;
-    }
-    return status;
+    return read_status_block(word, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int luvc_read_status(int32_t* device_status, void* cuda_stream) {

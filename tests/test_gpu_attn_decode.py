@@ -397,6 +397,30 @@ def test_calls_after_calls_that_overlapped_are_right(luvc, own):
     assert luvc.check_status() == 0
 
 
+def test_reading_the_status_leaves_a_running_call_alone(luvc):
+    """Another operator's wait gives up (made to, by the knobs of its status block), and the word is read while attention runs on another
+    stream with the library's workspace."""
+    c = build(luvc, "f32", [16451, 9000, 30000], 1, 256, 64, seed=2, nan=False)    # leaves room on the SMs for what else would run
+    q = torch.randn((3, 12, 256), generator=torch.Generator().manual_seed(5)).cuda()
+    want = luvc.attn_decode(q, c)
+    x = torch.randn((3, 12, 12, 64), generator=torch.Generator().manual_seed(6)).cuda()
+    luvc.oim_merge(x, 36)
+    side, stream = torch.cuda.Stream(), torch.cuda.current_stream().cuda_stream
+    outs = [torch.empty_like(want) for _ in range(12)]
+    for _ in range(100):
+        assert luvc.lib.luvc_debug_wait_probes(4, 1000, None, stream) == 0
+        luvc.oim_merge(x, 36)                                     # gives up: the word is set
+        assert luvc.lib.luvc_debug_wait_probes(0, 0, None, stream) == 0
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for o in outs:
+                luvc.attn_decode(q, c, out=o)
+        assert luvc.check_status() == 10
+        torch.cuda.synchronize()
+        assert luvc.check_status() == 0
+        assert all(torch.equal(o, want) for o in outs)
+
+
 def test_offsets_past_32_bits(luvc):
     # the last pages of a pool of more than 2^32 elements per tensor (8 GB of one byte each)
     heads, D, page = 8, 256, 64
