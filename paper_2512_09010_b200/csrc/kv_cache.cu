@@ -17,6 +17,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "luvc_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -693,11 +695,23 @@ int sm_count() {
 
 template <PlanKind KIND, int THREADS>
 int launch_plan_as(const PlanArgs& a, cudaStream_t stream) {
+    // The attribute belongs to the kernel, not to the call, and other threads launch it too: the most that any call needs, once per device.
+    static std::atomic<unsigned long long> set{0};
     const size_t smem = (size_t)(4 * a.n + 1) * sizeof(int);
-    if (sizeof(PlanShared<THREADS>) + smem > 48 * 1024 &&
-        cudaFuncSetAttribute(kv_plan_kernel<KIND, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        cudaGetLastError();
-        return LUVC_ERR_CUDA;
+    if (sizeof(PlanShared<THREADS>) + smem > 48 * 1024) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) {
+            cudaGetLastError();
+            return LUVC_ERR_CUDA;
+        }
+        if (dev > 63 || !((set.load(std::memory_order_relaxed) >> dev) & 1)) {
+            if (cudaFuncSetAttribute(kv_plan_kernel<KIND, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (4 * kKvMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess) {
+                cudaGetLastError();
+                return LUVC_ERR_CUDA;
+            }
+            if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
     }
     return launch_overlapped(kv_plan_kernel<KIND, THREADS>, 1, THREADS, smem, stream, a);
 }

@@ -479,6 +479,34 @@ def test_a_captured_fork_keeps_its_scratch(luvc):
     r.check()
 
 
+def test_threads_with_few_and_many_sequences(luvc):
+    """Calls of different size from two host threads at once, each on its own cache, stream and status block (the plan's shared
+    memory depends on the number of sequences)."""
+    import threading
+
+    failed = []
+
+    def work(n):
+        try:
+            r = Rig(luvc, "bf16", pages=8, page=16, slots=n, max_pages=2, layers=1, heads=1, D=8)
+            word, zero, slots = torch.zeros(4, dtype=torch.int32, device="cuda"), r.ints([0] * n), r.ints(list(range(n)))
+            torch.cuda.synchronize()
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(3000):
+                    luvc.kv_reserve(r.cache, zero, seqs=slots, device_status=word)
+            torch.cuda.synchronize()
+            assert luvc.read_status(word) == 0
+        except Exception as e:                                            # noqa: BLE001
+            failed.append((n, e))
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in (1000, 4096, 1500, 3000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+
+
 def test_python_refusals(luvc):
     pool = torch.zeros((1, 4, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(TypeError):
