@@ -12,6 +12,20 @@ namespace luvc {
 static std::atomic<long long> g_launches{0};
 void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
+int sm_count() {
+    static std::atomic<int> known{0};
+    int sms = known.load(std::memory_order_relaxed);
+    if (!sms) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        known.store(sms, std::memory_order_relaxed);
+    }
+    return sms;
+}
+
 static std::atomic<int> g_profile{0};
 static cudaEvent_t g_ev[LUVC_PHASE_COUNT][2];
 static bool g_ev_made = false, g_ev_used[LUVC_PHASE_COUNT];

@@ -40,6 +40,7 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "luvc_internal.h"
@@ -1351,21 +1352,6 @@ EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-int sm_count() {
-    static std::atomic<int> known{0};
-    int sms = known.load(std::memory_order_relaxed);
-    if (!sms) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-            cudaGetLastError();
-            return 0;
-        }
-        if (sms > kMaxCtas) sms = kMaxCtas;
-        known.store(sms, std::memory_order_relaxed);
-    }
-    return sms;
-}
-
 // The rows of one layer as a matrix [rows_total][D], fetched in boxes of 16 rows by PITCH bytes.
 template <typename TC, int PITCH>
 bool layer_map(CUtensorMap* map, const luvc_kv_cache& c, void* pool, int layer, int rows_total) {
@@ -1387,7 +1373,7 @@ int launch(const AttnProblem& p) {
     a.p = p;
     a.group = p.q_heads / p.c.heads;
     a.groups = (a.group + Sh::ROWS - 1) / Sh::ROWS;
-    const int sms = sm_count();
+    const int sms = std::min(sm_count(), kMaxCtas);
     if (!sms) return LUVC_ERR_CUDA;
     a.limit = (2147483647 - Sh::SNAP) / (p.c.heads * a.groups);
     a.one_grid = 1.f / sms;

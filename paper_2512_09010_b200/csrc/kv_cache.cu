@@ -683,16 +683,6 @@ __global__ void __launch_bounds__(kWriteThreads, 4) kv_write_kernel(const __grid
     }
 }
 
-int sm_count() {
-    static int sms = 0;
-    if (!sms) {
-        int dev = 0;
-        cudaGetDevice(&dev);
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    }
-    return sms;
-}
-
 template <PlanKind KIND, int THREADS>
 int launch_plan_as(const PlanArgs& a, cudaStream_t stream) {
     // The attribute belongs to the kernel, not to the call, and other threads launch it too: the most that any call needs, once per device.
@@ -737,7 +727,9 @@ int launch_move(MoveArgs& a, long long pages, cudaStream_t stream) {
     a.units = c.D * a.es / 16;
     a.teams = 2 * a.cap * a.units <= kMoveThreads ? kMoveThreads / (a.cap * a.units) : 1;
     a.size = a.teams > 1 ? a.cap * a.units : kMoveThreads;
-    const long long one = 4ll * sm_count(), bytes = pages * c.page_size * c.layers * 2 * c.heads * c.D * a.es;
+    const int sms = sm_count();
+    if (!sms) return LUVC_ERR_CUDA;
+    const long long one = 4ll * sms, bytes = pages * c.page_size * c.layers * 2 * c.heads * c.D * a.es;
     const long long waves = bytes / (one * (128 << 10)), grid = one * (waves < 1 ? 1 : waves > 6 ? 6 : waves);
     return a.teams > 1 ? launch_overlapped(kv_move_kernel<FORK, true>, (unsigned)grid, kMoveThreads, 0, stream, a)
                        : launch_overlapped(kv_move_kernel<FORK, false>, (unsigned)grid, kMoveThreads, 0, stream, a);
@@ -791,7 +783,9 @@ int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, cons
     a.c = c; a.layer = layer; a.n = n; a.tokens = tokens; a.seqs = seqs; a.starts = starts; a.sizes = sizes;
     a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.status = status;
     // four CTAs per SM while there are few tokens (what counts then is the time of one), at least 4 tokens each
-    const int even = (int)(((long long)tokens + 4 * sm_count() - 1) / (4 * sm_count()));
+    const int sms = sm_count();
+    if (!sms) return LUVC_ERR_CUDA;
+    const int even = (int)(((long long)tokens + 4 * sms - 1) / (4 * sms));
     a.per = even < 4 ? 4 : even > kWriteTokens ? kWriteTokens : even;
     const int grid = (tokens + a.per - 1) / a.per;
     if (c.dtype == LUVC_F32) return launch_overlapped(kv_write_kernel<float, float>, grid, kWriteThreads, 0, stream, a);

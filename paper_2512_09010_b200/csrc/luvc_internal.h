@@ -201,6 +201,7 @@ int spu_inv2_run(const float* Y, float* part, int B, int N, int D, int sigma, in
 // ---- paged key-value cache (kv_cache.cu) and the attention over it (attn_decode.cu) ---------------
 
 constexpr int kKvMaxSeqs = 4096;    // sequences of one call
+int sm_count();                     // SMs of the GPU (of the first device asked about: all are of one kind); 0 if it cannot be found out
 size_t kv_elem_size(int dtype);
 size_t kv_workspace_bytes(const luvc_kv_cache& c, int n);
 int kv_reserve(const luvc_kv_cache& c, const int32_t* seqs, int n, const int32_t* counts, int* status, cudaStream_t stream);

@@ -1,6 +1,9 @@
 """Argument checks of the key-value cache's and the attention's entry points: they answer without touching a GPU
 (CPU only: no compute call is made here)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -91,3 +94,25 @@ def test_the_status_has_a_name(luvc):
     assert luvc.STATUS_NAMES[12] == "LUVC_ERR_PAGES"
     assert b"page" in luvc.lib.luvc_status_string(12)
     assert ctypes.sizeof(luvc.KvCacheStruct) == 7 * 8 + 8 * 4
+
+
+def test_without_a_gpu_a_call_answers_with_an_error():
+    """The number of SMs that launches are sized by cannot be asked of a device that is not there."""
+    code = """
+import paper_2512_09010_b200 as luvc
+A = 4096
+c = luvc.KvCacheStruct(A, A, A, A, A, None, None, 2, 64, 4, 16, 128, 8, 32, luvc.BF16)
+o = luvc.KvOpts(workspace=A, workspace_bytes=1 << 20, device_status=A)
+L = luvc.lib
+assert L.luvc_kv_write(c, 0, None, 4, A, A, 512, 512, 4, None, None, 0, o) == 9
+assert L.luvc_kv_reserve(c, None, 4, A, o) == 9
+assert L.luvc_kv_free(c, A, 4, o) == 9
+assert L.luvc_kv_fork(c, A, A, 4, o) == 9
+assert L.luvc_kv_compact(c, None, 4, A, A, A, 4, None, o) == 9
+a = luvc.AttnOpts(workspace=A, workspace_bytes=1 << 30, device_status=A)
+assert L.luvc_attn_decode(A, 3584, c, 0, None, 4, 28, 0, A, a) == 9
+print("answered")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, CUDA_VISIBLE_DEVICES=""), capture_output=True, text=True)
+    assert r.returncode == 0 and "answered" in r.stdout, (r.returncode, r.stderr[-500:])
