@@ -436,7 +436,10 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
                         if (in != e) *a.status = LUVC_ERR_KEEP;
                         from = first + in;
                     }
-                    page = a.move.old[(long long)i * c.max_pages + from / ps];
+                    // a token moves towards the start, so it comes from a page that is not as before; only an entry that was replaced
+                    // (or is out of order) can stand for one on a page that stays
+                    if (from < p * ps && from / ps < a.move.from[i]) page = c.table[(long long)slot * c.max_pages + from / ps];
+                    else page = a.move.old[(long long)i * c.max_pages + from / ps];
                 }
                 src_row[tid] = page >= 0 && page < c.pages ? (long long)page * c.heads * ps + from % ps : -1;
             }

@@ -269,6 +269,18 @@ def test_an_index_outside_its_block_is_replaced_and_reported(luvc):
     r.check()
 
 
+@pytest.mark.parametrize("tail", [[-5], [-5, 25], [25, 400, 401], [-1 << 31, (1 << 31) - 1]])
+def test_an_index_outside_its_block_after_pages_that_stay(luvc, tail):
+    # the nearest token inside may lie on a page that is not moved
+    r = Rig(luvc, "bf16", pages=12, page=16, slots=2, max_pages=5)
+    r.append([0, 1], [70, 5])
+    own = torch.full((luvc.kv_workspace_bytes(r.cache, 1),), 0xAB, dtype=torch.uint8, device="cuda")
+    luvc.kv_compact(r.cache, r.ints([3]), r.ints([60]), r.ints([list(range(20)) + tail]), workspace=own)
+    assert luvc.check_status() == 4
+    r.model.drop(r.model.compact(0, 3, 60, list(range(20)) + [min(max(e, 0), 59) for e in tail]))
+    r.check()
+
+
 def test_rows_before_the_sequence_are_not_written(luvc):
     r = Rig(luvc, "bf16", pages=4, page=16, slots=2, max_pages=2)
     r.append([0, 1], [3, 2])
