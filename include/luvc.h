@@ -106,6 +106,8 @@ int luvc_read_status(int32_t* device_status, void* cuda_stream);
  * `hold_back` > 0 starts the first image's count of finished lines of the first merge step that
  * far below zero, so that no wait on it can ever be satisfied and each gives up after `probes`
  * probes (microseconds).  The call that follows then ends with LUVC_ERR_TIMEOUT in the block.
+ * luvc_attn_decode takes them as the limit (4096 at least) of its waits for copies, and as one such wait
+ * that is never satisfied.
  * 0, 0 restores normal operation.  Synchronises the stream. */
 int luvc_debug_wait_probes(int probes, int hold_back, int32_t* device_status, void* cuda_stream);
 

@@ -62,12 +62,17 @@ constexpr float kSlack = 6.f;                   // the reference of the weights 
 constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f;
 constexpr float kMostGain = 60.f;               // log2 of what a lane's sum of weights may become when m falls
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
+constexpr int kLeastProbes = 1 << 12;           // and with a limit from the status block (a test's), so that copies which do come are waited for
 
 // ---- the instructions of this file -----------------------------------------------------------------
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int x, int row) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(row) : "memory");
+}
+// The barrier's phase waits for so many bytes more.
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -650,6 +655,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         };
         Place at = ld;
         load_start(true);
+        // a test's knob: the first wait of the first warp cannot end
+        if (blockIdx.x == 0 && tid == 0 && p.status[kStatusHoldBack] > 0) mbar_expect_tx(my_bar, 16);
+        __syncwarp();
         unsigned order = 0, phases = 0;                         // stages in the order they were filled (4 bits each); their phases
         int filled = 0;
         for (; filled < S && to_load > 0; ++filled) {
@@ -779,10 +787,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         }
                 if (!dead) {
                     const uint32_t bar = my_bar + 8 * stage;
-                    int probes = 0;
-                    while (!mbar_try_wait(bar, (phases >> stage) & 1) && ++probes < kWaitProbes) {}
+                    int probes = 0, limit = kWaitProbes;
+                    while (!mbar_try_wait(bar, (phases >> stage) & 1) && ++probes < limit)
+                        if (probes == kLeastProbes - 1) {
+                            const int knob = *reinterpret_cast<volatile int*>(p.status + kStatusProbeLimit);
+                            if (knob > 0) limit = max(kLeastProbes, knob);
+                        }
                     phases ^= 1u << stage;
-                    if (__any_sync(~0u, probes >= kWaitProbes)) {
+                    if (__any_sync(~0u, probes >= limit)) {
                         dead = true;
                         to_load = 0;
                         for (; filled > 0; --filled, order >>= 4)   // let the copies in flight land

@@ -421,6 +421,37 @@ def test_reading_the_status_leaves_a_running_call_alone(luvc):
         assert all(torch.equal(o, want) for o in outs)
 
 
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("dtype,q_heads,heads,D,lengths", [("bf16", 8, 1, 64, [40000]), ("bf16", 28, 4, 128, [97]), ("e4m3", 32, 8, 128, [3000, 20, 0, 900]),
+                                                           ("f32", 16, 2, 64, [5000]), ("f32", 3, 1, 256, [2000, 2000]), ("f32", 28, 4, 128, [9, 3000])])
+def test_a_wait_that_gives_up_is_reported_and_the_next_call_is_right(luvc, own, dtype, q_heads, heads, D, lengths):
+    """The knobs of the status block let the first wait of the first warp run out, after a few thousand probes; nothing hangs.  The
+    workspace is usable as it is afterwards."""
+    c = build(luvc, dtype, lengths, heads, D, 16, seed=1, nan=False)
+    q = torch.randn((len(lengths), q_heads, D), generator=torch.Generator().manual_seed(2)).to(c.io_dtype).cuda()
+    stream = torch.cuda.current_stream().cuda_stream
+    block = torch.zeros(4, dtype=torch.int32, device="cuda") if own else None
+    options = dict(device_status=block, workspace=torch.zeros(luvc.attn_workspace_bytes(), dtype=torch.uint8, device="cuda")) if own else {}
+
+    def read():
+        return luvc.read_status(block) if own else luvc.check_status()
+
+    want = luvc.attn_decode(q, c, **options)
+    assert read() == 0
+    check(luvc, c, q, want, None)
+    for _ in range(3):
+        assert luvc.lib.luvc_debug_wait_probes(5000, 1, block.data_ptr() if own else None, stream) == 0
+        luvc.attn_decode(q, c, **options)
+        torch.cuda.synchronize()
+        assert luvc.lib.luvc_debug_wait_probes(0, 0, block.data_ptr() if own else None, stream) == 0
+        assert torch.equal(luvc.attn_decode(q, c, **options), want)      # also while the word is set
+        assert read() == 10 and read() == 0
+        assert torch.equal(luvc.attn_decode(q, c, **options), want)
+    if own:
+        assert luvc.check_status() == 0
+        assert not options["workspace"][:5 * 256 * 4].any()
+
+
 def test_offsets_past_32_bits(luvc):
     # the last pages of a pool of more than 2^32 elements per tensor (8 GB of one byte each)
     heads, D, page = 8, 256, 64
