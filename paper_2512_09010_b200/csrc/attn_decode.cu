@@ -483,7 +483,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     auto tiles_of = [&](int i) {
         const int slot = slot_of(i);
         if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
-        return (length_of(slot) + KT - 1) / KT;
+        return (int)(((unsigned)length_of(slot) + (KT - 1u)) / (unsigned)KT);       // (up to 2^31 - 1 tokens)
     };
     // at most 2^31 / 16 tiles in a sequence: no warp's sum overflows 32 bits
     auto warp_scan = [&](unsigned x) {
@@ -770,7 +770,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 order >>= 4;
                 --filled;
                 // a tile with biases, or past the end (which is a bias of -inf)
-                const bool masked = p.bias_width > 0 || (at.tile + 1) * KT > len;
+                const bool masked = p.bias_width > 0 || len - at.tile * KT < KT;
                 float bias[Sh::SUB][2];
 #pragma unroll
                 for (int j = 0; j < Sh::SUB; ++j)

@@ -482,3 +482,37 @@ def test_offsets_past_32_bits(luvc):
     assert luvc.check_status() == 0 and c.lengths[0] == 8 * page and int(c.table[0, 0]) >= pages - 9
     moved = c.k[0][c.table[0, :8].long().tolist()[0]].float().transpose(0, 1)
     assert torch.equal(moved, k8[2 * n // 3:2 * n // 3 + page].float())
+
+
+def test_the_longest_sequence_of_an_8_bit_cache(luvc):
+    # 2^31 - 20 tokens of one key head of 16 (32 GB of keys, 32 GB of values): the last 32-token tile ends past 2^31 - 1
+    pages, page, D, n = (1 << 27) - 1, 16, 16, (1 << 31) - 20
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    k = torch.zeros((1, pages, 1, page, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    v = torch.zeros((1, pages, 1, page, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    one = torch.ones((1, 1), device="cuda")
+    c = luvc.KvCache(k, v, 1, pages, k_scale=one, v_scale=one)
+    c.table.copy_(torch.arange(pages, dtype=torch.int32, device="cuda")[None])
+    c.lengths.fill_(n)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    live = n - (pages - 1) * page                                 # tokens of the last page; what follows them is NaN
+    k.view(torch.uint8)[0, -1, 0, live:] = 0x7f
+    v.view(torch.uint8)[0, -1, 0, live:] = 0x7f
+    last = torch.randn((live, D), generator=g, device="cuda").to(torch.float8_e4m3fn)
+    v[0, -1, 0, :live] = last
+    k[0, -1, 0, :live, 0] = torch.full((live,), 8.0, device="cuda").to(torch.float8_e4m3fn)
+    q = torch.zeros((1, 10, D), dtype=torch.bfloat16, device="cuda")
+    q[0, :, 0] = torch.arange(10, device="cuda") + 8.0
+    out, lse = luvc.attn_decode(q, c, scale=0.5, want_lse=True)   # the last tokens' scores are 4 (8 .. 17) = 32 .. 68, all others' 0
+    assert luvc.check_status() == 0
+    top = 4 * q[0, :, :1].double()
+    total = live + (n - live) * torch.exp(-top)
+    want = last.double().sum(0) / total
+    # the weights of 4 equal keys and of the rest, summed in 32 bits in pieces of some 10^4 tiles (see check)
+    rel = 2 * 2.0 ** -17 + 2 * 68 * 18 * 2.0 ** -23 + (n / 16 / 148 / 16 + 200) * 2.0 ** -23 * (1 - live / total)
+    bound = 2.0 ** -8 * want.abs() + last.double().abs().sum(0) / total * (rel + 64 * 2.0 ** -23)
+    assert bool(((out[0].double() - want).abs() <= bound).all())
+    assert bool(((lse[0].double() - top[:, 0] - total[:, 0].log()).abs() <= rel[:, 0] + 68 * 2.0 ** -20).all())
+    del c, k, v
+    torch.cuda.empty_cache()
