@@ -521,7 +521,7 @@ def _token_stride(t: torch.Tensor, cache: KvCache, heads: int, name: str) -> int
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != D and heads > 1):
         raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
-    return s0 if shape[0] > 1 else max(s0, heads * D)
+    return s0 if shape[0] > 1 else heads * D            # the stride of a lone token is not used
 
 
 def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0, starts: torch.Tensor | None = None,

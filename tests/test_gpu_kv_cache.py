@@ -578,3 +578,18 @@ def test_workspaces_and_status_blocks_elsewhere_are_refused(luvc):
             with pytest.raises(ValueError):
                 call(device_status=bad)
     assert luvc.check_status() == 0 and not c.meta[:6].any()
+
+
+def test_a_lone_token_may_have_any_stride(luvc):
+    r = Rig(luvc, "bf16", pages=4, page=16, slots=1, max_pages=2, layers=1)
+    r.append([0], [20])
+    luvc.kv_reserve(r.cache, r.ints([1]))
+    r.model.reserve(0, [r.next_id])
+    rows = [torch.zeros((3, 129), dtype=torch.bfloat16, device="cuda")[:, :128].view(3, 2, 64)[:1] for _ in range(2)]   # 129 elements to the next row
+    for kind in (0, 1):
+        rows[kind].copy_(rows_for([r.next_id], 0, 2, 64, kind, torch.bfloat16))
+    assert rows[0].stride(0) == 129
+    luvc.kv_write(r.cache, *rows)
+    r.check()
+    q = torch.randn((2, 257), device="cuda").bfloat16()[:, :256].view(2, 4, 64)[:1]
+    assert q.stride(0) == 257 and torch.equal(luvc.attn_decode(q, r.cache), luvc.attn_decode(q.contiguous(), r.cache))
