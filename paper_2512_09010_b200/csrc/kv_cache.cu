@@ -790,7 +790,7 @@ int kv_write(const luvc_kv_cache& c, int layer, const int32_t* seqs, int n, cons
     if (!sms) return LUVC_ERR_CUDA;
     const int even = (int)(((long long)tokens + 4 * sms - 1) / (4 * sms));
     a.per = even < 4 ? 4 : even > kWriteTokens ? kWriteTokens : even;
-    const int grid = (tokens + a.per - 1) / a.per;
+    const int grid = (tokens - 1) / a.per + 1;             // tokens: 1 .. 2^31 - 1
     if (c.dtype == LUVC_F32) return launch_overlapped(kv_write_kernel<float, float>, grid, kWriteThreads, 0, stream, a);
     if (c.dtype == LUVC_BF16) return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_bfloat16>, grid, kWriteThreads, 0, stream, a);
     return launch_overlapped(kv_write_kernel<__nv_bfloat16, __nv_fp8_e4m3>, grid, kWriteThreads, 0, stream, a);

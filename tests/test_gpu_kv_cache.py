@@ -593,3 +593,25 @@ def test_a_lone_token_may_have_any_stride(luvc):
     r.check()
     q = torch.randn((2, 257), device="cuda").bfloat16()[:, :256].view(2, 4, 64)[:1]
     assert q.stride(0) == 257 and torch.equal(luvc.attn_decode(q, r.cache), luvc.attn_decode(q.contiguous(), r.cache))
+
+
+def test_the_largest_write(luvc):
+    # 2^31 - 16 tokens of one head of 8 (32 GB) in one call: the number of CTAs is counted without overflow
+    if torch.cuda.mem_get_info()[0] < 110 << 30:
+        pytest.skip("needs 110 GB")
+    pages, n = (1 << 27) - 1, (1 << 31) - 16
+    pool = torch.zeros((1, pages, 1, 16, 8), dtype=torch.bfloat16, device="cuda")
+    c = luvc.KvCache(pool, torch.zeros_like(pool), 1, pages)
+    rows = torch.empty((n, 1, 8), dtype=torch.bfloat16, device="cuda")
+    rows.view(torch.int32).random_(generator=torch.Generator(device="cuda").manual_seed(3)).bitwise_and_(-1077952577)     # 0xbfbfbfbf: finite
+    for count in (1 << 30, n - (1 << 30)):
+        luvc.kv_reserve(c, torch.tensor([count], dtype=torch.int32, device="cuda"))
+    luvc.kv_write(c, rows, rows, starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    assert luvc.check_status() == 0
+    assert int(c.lengths[0]) == n and c.table[0, :3].tolist() == [0, 1, 2] and int(c.table[0, -1]) == pages - 1
+    want = rows.view(-1).view(torch.int64)
+    for got in (c.k, c.v):                                        # the pages were handed out in order
+        for a, b in zip(got.view(-1).view(torch.int64).split(1 << 28), want.split(1 << 28)):
+            assert torch.equal(a, b)
+    del c, pool, rows, want, got, a, b
+    torch.cuda.empty_cache()
