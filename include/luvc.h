@@ -515,7 +515,7 @@ typedef struct {
  * A sequence without tokens, or whose keys are all masked by -inf, gives a row of zeros.  A key masked
  * by -inf contributes nothing, whatever its rows hold; rows past the length are never used.  Scores,
  * softmax and sums are fp32; a weight enters its product with V with 16 bits at least (LUVC_E4M3: off by
- * 2^-16 of the largest weight of its 16 tokens at most).  A call repeated gives the same bits; how the work is split, and with it the last bits,
+ * 2^-16 of the largest weight of its 16 tokens, or 2^-60 of the largest of all, at most).  A call repeated gives the same bits; how the work is split, and with it the last bits,
  * depends on all lengths of the call.  The call runs whatever the status word says.
  */
 int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,

@@ -58,9 +58,9 @@ constexpr size_t kCounterBytes = 5 * kMaxCtas * sizeof(unsigned);
 constexpr float kSlack = 6.f;                   // the reference of the weights may lag behind the maximum by this much
 // With an e4m3 cache weights are f16: below 65504, in steps of 2^-24 of one.  The reference m is set kLead below the maximum of 16
 // scores when that is above m + kRise, or below m - kFall (a token far above all others, as at the start of a text, leaves only small
-// weights).  So the largest of 16 weights is between e^-kFall and e^kRise, and e^kLead at least where it is the largest so far.
-constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f;
-constexpr float kMostGain = 60.f;               // log2 of what a lane's sum of weights may become when m falls
+// weights).  So the largest of 16 weights is between e^-kFall and e^kRise, and e^kLead at least where it is the largest so far.  m does
+// not follow scores below m - kGone (masks of a lowest value), and only as far as sums of weights stay below 2^kMostGain.
+constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f, kGone = 60.f, kMostGain = 60.f;
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;           // and with a limit from the status block (a test's), so that copies which do come are waited for
 
@@ -901,7 +901,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                         }
                                         float to = m[nt][b];
                                         if (x > to + kRise) to = x - kLead;
-                                        else if (x > -INFINITY && x < to - kFall)
+                                        else if (x < to - kFall && x > to - kGone)
                                             to -= fminf(to - (x - kLead), fmaxf(kMostGain - __log2f(most), 0.f) / kLog2e);
                                         const float f = exp2_fast((m[nt][b] - (to == -INFINITY ? 0.f : to)) * kLog2e);
                                         m[nt][b] = to;

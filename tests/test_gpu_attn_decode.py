@@ -324,6 +324,26 @@ def test_what_is_not_finite_counts_as_the_formula_says(luvc, dtype, q_heads, hea
     assert what in ("k inf", "k nan") or bool(out.isfinite().any())
 
 
+@pytest.mark.parametrize("dtype,q_heads,heads,D", [("e4m3", 4, 1, 64), ("e4m3", 12, 1, 128), ("bf16", 4, 1, 64), ("f32", 8, 1, 64), ("f32", 2, 1, 64)])
+def test_masks_of_the_lowest_value_in_turn_with_tokens_that_count(luvc, dtype, q_heads, heads, D):
+    """Every other 16 tokens carry the lowest bias, or one far below all others: the weights' reference does not follow them and back."""
+    n = 200000
+    c = build(luvc, dtype, [n, 333], heads, D, 16, seed=8, nan=False)
+    c.v.view(torch.uint8).zero_()
+    c.v.copy_((torch.ones(c.v.shape, device="cuda") * 1.75).to(c.v.dtype))            # equal values: the mean is exact but for the sums
+    q = torch.randn((2, q_heads, D), generator=torch.Generator().manual_seed(1)).to(c.io_dtype).cuda()
+    t = torch.arange(n, device="cuda") // 16 % 2
+    for low in (torch.finfo(torch.float32).min, -200.0, -90.0):
+        bias = torch.where(t == 1, low, 0.0).expand(2, n).contiguous()
+        out, lse = luvc.attn_decode(q, c, key_bias=bias, want_lse=True)
+        want = 1.75 * (c.v_scale[0] if c.v_scale is not None else torch.ones(1, device="cuda")).double()
+        u = 2.0 ** -8 if dtype != "f32" else 2.0 ** -24
+        # numerator and denominator are sums of the same weights: what is left is the rounding of 16-bit weights and of the sums
+        rel = 2 * 2.0 ** -17 * (dtype != "f32") + (n / 16 / 148 + 64) * 2.0 ** -23
+        assert bool(((out.double() - want).abs() <= (u + rel) * want).all()), (low, float((out.double() / want - 1).abs().max()))
+        check(luvc, c, q[1:], out[1:], lse[1:], seqs=[1], bias=bias[1:])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_layers_slots_strides_and_streams(luvc, dtype):
     c = build(luvc, dtype, [100, 0, 45, 300], 2, 64, 16, layers=3, seed=13)
