@@ -94,32 +94,23 @@ void* scratch(Slot s, size_t bytes) {
     return p;
 }
 
-// The current device's status block: 256 bytes allocated once and zeroed, kept until luvc_shutdown.
-int* status_word() {
+// The current device's buffer of one purpose that has to be zero at first, allocated and zeroed once and kept until luvc_shutdown.  The
+// lock is held until the zeros are there: neither another thread's first call nor this one's, on a stream that does not wait for
+// the legacy one, must find the memory without them.
+void* zeroed_scratch(Slot s, size_t bytes) {
+    static std::mutex first_use;
     const int dev = current_device();
     if (dev < 0) return nullptr;
     {
         std::lock_guard<std::mutex> lock(g_mutex);
-        if (g_scratch[dev][kStatus].ptr) return static_cast<int*>(g_scratch[dev][kStatus].ptr);
+        if (g_scratch[dev][s].ptr) return g_scratch[dev][s].ptr;
     }
-    void* p = scratch(kStatus, 256);
-    if (p && cudaMemset(p, 0, 256) != cudaSuccess) return nullptr;
-    return static_cast<int*>(p);
-}
-
-// The current device's attention workspace: allocated and zeroed once (the kernel leaves it zeroed where it must be).  The lock
-// is held until the zeros are there: another thread's first call must not find the memory without them.
-void* attn_scratch() {
-    static std::mutex first_use;
-    const int dev = current_device();
-    if (dev < 0) return nullptr;
     std::lock_guard<std::mutex> lock(first_use);
-    Scratch& sc = g_scratch[dev][kAttnWs];
+    Scratch& sc = g_scratch[dev][s];
     {
         std::lock_guard<std::mutex> inner(g_mutex);
         if (sc.ptr) return sc.ptr;
     }
-    const size_t bytes = attn_workspace_bytes();
     void* p = nullptr;
     if (cudaMalloc(&p, bytes) != cudaSuccess || cudaMemset(p, 0, bytes) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
         cudaFree(p);                    // (during a capture, say) memory without the zeros is not kept
@@ -130,6 +121,10 @@ void* attn_scratch() {
     sc.ptr = p; sc.bytes = bytes;
     return p;
 }
+
+// The current device's status block, and its attention workspace (which the kernel leaves zeroed where it must be).
+int* status_word() { return static_cast<int*>(zeroed_scratch(kStatus, 256)); }
+void* attn_scratch() { return zeroed_scratch(kAttnWs, attn_workspace_bytes()); }
 
 // Reads (after synchronising the stream) and clears the first word of a status block.
 int read_status_block(int* block, cudaStream_t stream) {

@@ -88,3 +88,39 @@ def test_spu_reports_into_a_caller_block_too(luvc):
     b = luvc.spu_prune(x, 40, 0.25)
     assert luvc.read_status(block) == 0 and luvc.check_status() == 0
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_first_calls_on_side_streams_find_a_clear_status_word(luvc):
+    """After a shutdown the library's block is made anew: by whichever thread and stream calls first, zeroed before anything reads it."""
+    import threading
+
+    x = torch.randn((2, 12, 12, 64), generator=torch.Generator().manual_seed(79)).cuda()
+    want = luvc.oim_merge(x, 36)[1]
+    assert luvc.check_status() == 0
+    stream = torch.cuda.current_stream().cuda_stream
+    for _ in range(20):
+        assert luvc.lib.luvc_debug_wait_probes(4, 1000, None, stream) == 0      # what the freed block leaves behind
+        luvc.shutdown()
+        got, failed = [], []
+
+        def first(k):
+            try:
+                block = torch.zeros((1, 4, 1, 16, 8), dtype=torch.bfloat16, device="cuda")
+                cache = luvc.KvCache(block, block.clone(), 2, 2)
+                one = torch.ones(2, dtype=torch.int32, device="cuda")
+                torch.cuda.synchronize()
+                with torch.cuda.stream(torch.cuda.Stream()):
+                    luvc.kv_reserve(cache, one)
+                torch.cuda.synchronize()
+                got.append(cache.lengths.tolist())
+            except Exception as e:                                                # noqa: BLE001
+                failed.append((k, e))
+
+        threads = [threading.Thread(target=first, args=(k,)) for k in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not failed and got == [[1, 1]] * 4
+        assert torch.equal(luvc.oim_merge(x, 36)[1], want)                        # no knob is left set
+        assert luvc.check_status() == 0
