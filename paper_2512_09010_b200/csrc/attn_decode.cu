@@ -386,8 +386,9 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 
 // The partial result of tokens t0 .. t1 - 1 of a (sequence, head group) once more, by a warp, product by product as the formula has
 // them, into a stage (O) and ml.  The tensor-core forms split weights, and rows of 32 bits, into parts whose products an infinity or
-// a value near the end of the range turns into NaN (inf times the lower part of a weight, which may be 0 or negative; inf - inf), so a
-// result that is not finite is worked out again.  It is rare, and need not be fast.
+// a value near the end of the range turns into NaN (inf times the lower part of a weight, which may be 0 or negative; inf - inf), and
+// weights above 1, while their reference lags behind, can take values beyond that end.  So a result that is not finite is worked out
+// again.  It is rare, and need not be fast.
 template <typename T, int DP>
 __device__ __noinline__ void plain_piece(const Args& a, int seq, int h, int r0, int rows, int t0, int t1, float scale, float* os, float2* ml) {
     const AttnProblem& p = a.p;
@@ -1102,7 +1103,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = o[mt][nt][c];
                     }
             __syncwarp();
-            if constexpr (!kCores && !kF8) {                    // (an e4m3 cache has no infinities, and its rows are not split)
+            if constexpr (!kF8) {                               // (an e4m3 cache has no infinities, and its rows are not split)
                 float z[4] = {0.f, 0.f, 0.f, 0.f};              // 0, or NaN
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -1112,6 +1113,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) z[c] = fmaf(o[mt][nt][c], 0.f, z[c]);
                     }
+                if constexpr (kCores)
+#pragma unroll
+                    for (int r = 0; r < NH; ++r)
+#pragma unroll
+                        for (int j = 0; j < DP / 32; ++j) z[j & 3] = fmaf(core_o[r][j], 0.f, z[j & 3]);
                 if (__any_sync(~0u, z[0] + z[1] + (z[2] + z[3]) != 0.f) && !dead)
                     plain_piece<TC, DP>(a, at.seq, h, r0, rows, (at.tile - count) * KT, min(at.tile * KT, len), scale, os, ml_of[warp][which]);
             }

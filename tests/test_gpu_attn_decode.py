@@ -344,6 +344,31 @@ def test_masks_of_the_lowest_value_in_turn_with_tokens_that_count(luvc, dtype, q
         check(luvc, c, q[1:], out[1:], lse[1:], seqs=[1], bias=bias[1:])
 
 
+@pytest.mark.parametrize("dtype,q_heads,heads,D", [("bf16", 28, 4, 128), ("bf16", 12, 1, 64), ("f32", 28, 4, 128), ("f32", 12, 1, 128), ("f32", 4, 4, 128),
+                                                   ("f32", 8, 2, 64), ("f32", 12, 1, 256)])
+def test_the_largest_values_do_not_overflow(luvc, dtype, q_heads, heads, D):
+    # a weight is at most 1 relative to the largest, so the weighted sum stays finite where the formula's does; a warp reads many tokens
+    # in turn, and one of them scores as much above those before it as their weights' reference may lag behind
+    n, group = 60000, q_heads // heads
+    c = build(luvc, dtype, [n], heads, D, 16, seed=D, nan=False)
+    c.k.zero_()
+    q = torch.ones((1, q_heads, D), dtype=c.io_dtype, device="cuda")
+    big = 3.0e38
+    for t, score, sign in ((3, 0.0, 1), (40, 5.5, 1), (45, 0.0, -1), (31000, 5.5, -1), (59999, 2.0, 1)):
+        page = int(c.table[0, t // 16])
+        c.k[0, page, :, t % 16, 0] = score * D ** 0.5
+        c.v[0, page, :, t % 16, 3] = big * sign
+    out = luvc.attn_decode(q, c)[0].double()
+    k, v = (x.repeat_interleave(group, 1) for x in rows(c, 0, 0, n))
+    s = torch.einsum("hd,thd->ht", q[0].double(), k) * D ** -0.5
+    p = torch.softmax(s, 1)
+    want, spread = torch.einsum("ht,thd->hd", p, v), torch.einsum("ht,thd->hd", p, v.abs())
+    off = 5.5 * (D + 3) * 2.0 ** -23
+    u = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+    bound = spread * (2 * off + 2 * 2.0 ** -17 * (dtype != "f32") + (n / 16 + D + 64) * 2.0 ** -23) * 1.01 + u * want.abs()
+    assert bool((want.abs() < 3.0e38).all()) and bool(((out - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_layers_slots_strides_and_streams(luvc, dtype):
     c = build(luvc, dtype, [100, 0, 45, 300], 2, 64, 16, layers=3, seed=13)
