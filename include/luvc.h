@@ -474,7 +474,8 @@ int luvc_kv_free(const luvc_kv_cache* cache, const int32_t* seqs, int n, const l
  * first, span DEVICE [n]; idx DEVICE [n, keep]; counts optional DEVICE [n], entries of idx that count
  *             (NULL: keep)
  * The kept tokens close up in order.  Leading full pages of which nothing moves stay where they are
- * (and stay shared); all other rows are copied to newly taken pages and the old pages are given back
+ * (and stay shared); all other rows are copied to newly taken pages (a partly filled last page also where
+ * nothing is dropped) and the old pages are given back
  * afterwards, so sequences that share pages with this one are not touched, and the pool needs the new pages
  * free at the call.  An idx entry outside the block is replaced by the nearest one inside
  * (LUVC_ERR_KEEP in the status word, after the fact).

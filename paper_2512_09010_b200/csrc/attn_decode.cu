@@ -5,11 +5,11 @@
 // in one pass: a running maximum m, the sum l of the weights so far and their weighted sum O of value rows; when m grows,
 // l and O are scaled by exp(m_old - m_new).  Partial results of parts of a sequence join by the same rule.
 //
-// Bound.  Every cached row is read once, for all query heads that share it: 2 G flops per cached element with G query heads
-// per key head, so HBM bounds long sequences up to the largest G in use, and latency short ones; what matters is to keep enough
+// Bound.  Every cached row is read once for up to 16 query heads that share it (four, where an f32 row is longer than 512 bytes; each
+// further group of so many reads it again): 2 G flops per cached element with G query heads per key head, so HBM bounds long sequences up to the largest G in use, and latency short ones; what matters is to keep enough
 // bytes in flight on every SM, whatever the lengths.  Measured: 334 MB (eight sequences of 4173 to 16451 tokens, 8 key heads of 128,
-// bf16) in 63.0 us, 5.3 TB/s; while all SMs stream it is 7.2 TB/s, but SMs differ by a tenth in the bandwidth they get, and
-// the last 9 us belong to the slow ones.  The smallest call (one sequence of 97 tokens) takes 4.9 us.
+// bf16) in 63.2 us, 5.3 TB/s; while all SMs stream it is 7.2 TB/s, but SMs differ by a tenth in the bandwidth they get, and
+// the last 9 us belong to the slow ones.  The smallest call (one sequence of 97 tokens) takes 5.0 us.
 //
 // Split.  The work is the list of all tiles (KT tokens of one sequence and key head), sequence after sequence.  Each CTA (one per
 // SM) takes an equal part of that list, each of its warps an equal part of the CTA's, so no length leaves an SM idle and a
@@ -24,7 +24,7 @@
 // columns of V, as M and query heads as N.  S^T = K Q^T with K from ldmatrix, then O^T += V^T P^T with V from
 // ldmatrix.trans and P^T from the scores' registers by movmatrix.  tcgen05 would want 128 tokens at a time and four warps in
 // step for each read of tensor memory; warps that work alone on 16 tokens suit short and ragged sequences, and the tensor
-// pipe is not the bound (18 % busy with an e4m3 cache).
+// pipe is not the bound (23 % busy with an e4m3 cache).
 // Roundings: Q and K are used as they are (an e4m3 cache goes to f16, which is exact; the query, scaled by a power of two so
 // that its largest element is below 2, is rounded to f16's 11 bits, exact unless an element is 2^14 times smaller than the
 // largest).  The weights p enter the second product as a pair hi + lo of 16-bit floats, because one 16-bit float would cost as much
@@ -141,15 +141,15 @@ struct Shape {
     static constexpr bool CORES = NT < 0;
     static constexpr int KT = 16 * SUB, STAGE = SUB * 2 * SUBK;
     // Three stages for each warp, 196,608 bytes in all: the more warps the smaller a row is.  Two where an f32 row is long and
-    // its products, not HBM, are the bound, for half as many warps again (28 / 4 heads of 128, 159 MB: 50 instead of 57 us;
-    // 32 / 8, 318 MB: 70 and 76; 8 / 8 of 256, 50 MB: 18 and 24), but not for one head of 128 (32 / 32, 903 MB: 158 and 151).
+    // its products, not HBM, are the bound, for half as many warps again (28 / 4 heads of 128, 158 MB: 46.3 us, with three
+    // 47.9; 32 / 8, 317 MB: 70 and 73; 12 / 1 of 256, 79 MB: 64 and 81; 8 / 8 of 256, 77 MB: 23 and 28, but 406 MB: 89 and 87), but
+    // not for one head of 128 (32 / 32, 903 MB: 158 with two and 151).
     static constexpr int S = ES == 4 && DPB >= 512 && !(NT == -1 && DPB == 512) ? 2 : 3;
     static constexpr int NW = 196608 / (S * STAGE) < 16 ? 196608 / (S * STAGE) : 16;
     // Tiles by which a part may move its ends to those of a (sequence, head).  A join across CTAs costs about as much as two tiles of
-    // every warp: 24 sequences of 886 to 1395 tokens, 28 / 4 heads of 128 in 8 bits (16 warps): 14.0 us, with 12 tiles 15.8; six of
-    // 5625 to 6957 in bf16 (8 warps): 18.0, with 6 tiles 18.8, with 24 17.9; 12 of 600 to 2500, 12 / 1 heads of 256 in f32 (3
-    // warps): 39, with 9 tiles 42, with 12 46.  (Parts of unequal length can cost more than the joins: 32 / 8 heads, 24 sequences in
-    // 8 bits 20.3, with 12 tiles 19.6.)
+    // every warp: 24 sequences of 886 to 1395 tokens, 28 / 4 heads of 128 in 8 bits (16 warps): 14.5 us, with 12 tiles 16.4; six of
+    // 5625 to 6957 in bf16 (8 warps): 18.3 with either; 12 of 600 to 2500, 12 / 1 heads of 256 in f32 (3 warps): 39.7, with 12 tiles
+    // 45.9.  (Parts of unequal length can cost more than the joins: 32 / 8 heads, 24 sequences in 8 bits 21.1, with 12 tiles 20.4.)
     static constexpr int SNAP = 2 * NW;
     static constexpr int MT = DP / 16;                          // 16-row groups of O^T
     static constexpr int ROWS = CORES ? 4 : 8 * NT;
@@ -568,8 +568,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         q.first = x - q.tile;
         return q;
     };
-    // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 8.8 us, with two tiles
-    // 9.3, with three 11.8: even then a join across CTAs costs less than a warp's second tile).
+    // Equal parts, of a tile for each warp at least (measured at eight sequences of 340 to 463 tokens: 9.0 us, with two tiles
+    // 9.6: even then a join across CTAs costs less than a warp's second tile).
     int per = max((int)((float)total * a.one_grid) - 1, 0);     // total / grid, rounded up
     per -= per >> 20;
     while ((long long)per * (int)gridDim.x < total) ++per;
@@ -1424,9 +1424,9 @@ int launch_heads(const AttnProblem& p) {
 }
 
 // f32 caches with up to four query heads per key head run on the CUDA cores (measured, against the tensor cores: 32 / 32 heads of
-// 128, 812 MB, 141 and 200 us; 16 / 16 of 64, 131 MB, 30.0 and 32.7; 32 / 8 of 128, 203 MB, 54 and 64; 8 / 8 of 256, 406 MB, 94 and
-// 226), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 63 and 77 us, 8 / 1 52 and 53).  The
-// others do not: 28 / 4 of 128, 159 MB, 63 us in this form, 47 on the tensor cores; 16 / 2 of 64, 39 MB, 22 and 16.
+// 128, 812 MB, 141 and 168 us; 16 / 16 of 64, 203 MB, 42.7 and 42.4, 38 MB 12.3 and 15.3; 32 / 8 of 128, 203 MB, 49 and 52; 8 / 8 of
+// 256, 406 MB, 89 and 141), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 64 and 68 us, 8 / 1
+// 50 and 53).  The others do not: 28 / 4 of 128, 158 MB, 63 us in this form, 46 on the tensor cores; 16 / 2 of 64, 40 MB, 24 and 16.
 template <int DPB>
 int launch_cores(const AttnProblem& p) {
     return p.q_heads == p.c.heads ? launch<float, float, DPB, -1>(p) : launch<float, float, DPB, -4>(p);
@@ -1445,7 +1445,7 @@ int attn_decode(const AttnProblem& p) {
     if (p.c.dtype == LUVC_BF16)
         return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256>(p)
                                                                                                : launch_heads<__nv_bfloat16, __nv_bfloat16, 512>(p);
-    // rows of 64 bytes halve the conversions and products (16 / 16 heads of 64, 79 MB: 26.7 us, as rows of 128 bytes 33.8)
+    // rows of 64 bytes halve the conversions and products (16 / 16 heads of 64, 79 MB: 28.0 us, as rows of 128 bytes 35.1)
     return bytes <= 64 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 64>(p) : bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 128>(p) : launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 256>(p);
 }
 
