@@ -377,6 +377,36 @@ int luvc_spu_prune_static(const void* hidden, int B, int N, int D, float cutoff,
  * (No counterpart in the paper.) */
 int luvc_spu_static_status(void* cuda_stream);
 
+/* ---- rotary positions ------------------------------------------------------ */
+
+typedef struct {
+    void* stream;            /* cudaStream_t; NULL = legacy default stream */
+    const int32_t* axis;     /* optional DEVICE [rotary / 2]: the row of `positions` that turns each pair (an entry outside
+                                0 .. axes-1 reads as the nearest one); NULL: row 0 */
+    int axes;                /* rows of `positions`: 1 to 64; 0 = 1 */
+    long long position_stride;   /* entries from one row of positions to the next; not read for one row */
+    int interleaved;         /* 0: pairs (i, i + rotary / 2); 1: pairs (2 i, 2 i + 1) */
+    int inverse;             /* 1: turns back, by minus the angle */
+    float factor;            /* of the result's turned elements; 0 = 1 */
+} luvc_rope_opts;
+
+/*
+ * Turns the first `rotary` elements of every head by the token's position, before the rows enter a cache or meet one:
+ *
+ *   out[a] = factor (x[a] cos t - x[b] sin t),  out[b] = factor (x[a] sin t + x[b] cos t),  t = positions[axis[i]][token] * freqs[i]
+ *
+ * for the pairs i < rotary / 2 at (a, b); the elements from `rotary` on are copied.  With several rows of positions (frame, row and
+ * column of a patch, say) each pair is turned by its own.  The gradient of x is the call with `inverse` on the gradient of out.
+ *
+ * x, out      [tokens, heads, D] of `dtype` (LUVC_BF16 or LUVC_F32); x_stride / out_stride: elements from one token to the next, a
+ *             token's heads * D elements are contiguous.  out may be x with the same stride (in place), and must not overlap it otherwise.
+ * positions   DEVICE [axes, tokens] int32, any value; freqs DEVICE [rotary / 2] fp32, radians per position
+ * Angles are formed in 64 bits (a far position keeps its angle), sines, cosines and products in fp32, results rounded once.
+ * rotary: even, 2 to D; D up to 1024; heads up to 65536.  tokens = 0 does nothing.
+ */
+int luvc_rope(const void* x, long long x_stride, const int32_t* positions, const float* freqs, int tokens, int heads, int D, int rotary,
+              int dtype, void* out, long long out_stride, const luvc_rope_opts* opts);
+
 /* ---- paged key-value cache ------------------------------------------------ */
 
 /*

@@ -8,6 +8,7 @@ library cannot be built or loaded, importing this package fails.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -32,7 +33,7 @@ EXPORTS = (
     "luvc_oim_merge_host", "luvc_oim_value_enhance", "luvc_spu_sigma", "luvc_spu_workspace_bytes", "luvc_spu_prune",
     "luvc_spu_prune_f32", "luvc_spu_prune_ex", "luvc_spu_prune_host", "luvc_spu_prune_static", "luvc_spu_static_status",
     "luvc_spu_cascade", "luvc_kv_workspace_bytes", "luvc_kv_reserve", "luvc_kv_write", "luvc_kv_fork", "luvc_kv_free",
-    "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode",
+    "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode", "luvc_rope",
 )
 
 
@@ -74,6 +75,13 @@ class KvOpts(ctypes.Structure):
     _fields_ = [
         ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
         ("device_status", ctypes.c_void_p),
+    ]
+
+
+class RopeOpts(ctypes.Structure):
+    _fields_ = [
+        ("stream", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("axes", ctypes.c_int), ("position_stride", ctypes.c_longlong),
+        ("interleaved", ctypes.c_int), ("inverse", ctypes.c_int), ("factor", ctypes.c_float),
     ]
 
 
@@ -137,6 +145,7 @@ def _load() -> ctypes.CDLL:
     L.luvc_attn_workspace_bytes.restype = sz
     L.luvc_attn_workspace_bytes.argtypes = []
     L.luvc_attn_decode.argtypes = [p, ll, cache, i, p, i, i, i, p, ctypes.POINTER(AttnOpts)]
+    L.luvc_rope.argtypes = [p, ll, p, p, i, i, i, i, i, p, ll, ctypes.POINTER(RopeOpts)]
     return L
 
 
@@ -481,15 +490,20 @@ def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
     return o
 
 
-def _kv_call(fn, cache: KvCache, *args) -> None:
-    """fn(*args) with the cache's device current; an error status raises."""
-    if _current_device() == cache.index:
+def _call_on(index: int, fn, *args) -> None:
+    """fn(*args) with device `index` current; an error status raises."""
+    if _current_device() == index:
         status = fn(*args)
     else:
-        with torch.cuda.device(cache.index):
+        with torch.cuda.device(index):
             status = fn(*args)
     if status != 0:
         raise LuvcError(status, fn.__name__)
+
+
+def _kv_call(fn, cache: KvCache, *args) -> None:
+    """fn(*args) with the cache's device current; an error status raises."""
+    _call_on(cache.index, fn, *args)
 
 
 def kv_workspace_bytes(cache: KvCache, n: int) -> int:
@@ -595,3 +609,76 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     _kv_call(lib.luvc_attn_decode, cache, q.data_ptr(), stride, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, q_heads,
              cache.io_code, out.data_ptr(), o)
     return (out, lse) if want_lse else out
+
+
+# ---- rotary positions ----------------------------------------------------------------------------
+
+
+def rope_frequencies(rotary: int, base: float = 10000.0, *, stretch: float = 1.0, method: str = "linear", context: int = 0,
+                     fast: float = 32.0, slow: float = 1.0, device=None):
+    """Frequencies (float32 [rotary / 2], radians per position) and the result's factor for rope: base^(-2 i / rotary), for a context
+    `stretch` times as long as the one the model was trained on (`context` positions).
+    "linear": all frequencies divided by the stretch (position interpolation); "base": the base raised so that the lowest frequency is
+    divided by the stretch and the highest stays (NTK-aware); "ramp": those that turn more than `fast` times in `context` stay, those
+    that turn less than `slow` times are divided, linearly in between by index, and the factor is 0.1 ln(stretch) + 1 (YaRN)."""
+    if rotary < 2 or rotary % 2 or not base > 0 or not stretch > 0:
+        raise ValueError("rotary must be even and at least 2, base and stretch positive")
+    index = torch.arange(0, rotary, 2, dtype=torch.float64)
+    factor = 1.0
+    if method == "base" and rotary > 2:
+        base = base * stretch ** (rotary / (rotary - 2))
+    freqs = float(base) ** (-index / rotary)
+    if method == "linear":
+        freqs = freqs / stretch
+    elif method == "ramp":
+        if context < 1 or not fast > slow > 0 or not base > 1:
+            raise ValueError("ramp needs the context the model was trained on, fast > slow > 0 and a base above 1")
+        # the index at which a pair turns so many times in the context
+        at = [rotary * math.log(context / (2 * math.pi * turns)) / (2 * math.log(base)) for turns in (fast, slow)]
+        low, high = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rotary - 1)
+        mix = ((index / 2 - low) / max(high - low, 1e-3)).clamp(0, 1)
+        freqs = freqs * (1 - mix) + freqs / stretch * mix
+        factor = 0.1 * math.log(stretch) + 1.0 if stretch > 1 else 1.0
+    elif method != "base":
+        raise ValueError("method must be linear, base or ramp, got %r" % (method,))
+    return freqs.float().to(device or "cpu"), factor
+
+
+def rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, *, axis: torch.Tensor | None = None, interleaved: bool = False,
+         inverse: bool = False, factor: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """luvc_rope: the first 2 * len(freqs) elements of each head of x [tokens, heads, D] (bfloat16 or float32; may be part of a wider
+    tensor whose tokens are contiguous) turned by positions * freqs.  positions: int32 [tokens], or [axes, tokens] with
+    axis (int32 [len(freqs)]) naming the row that turns each pair.  interleaved: pairs are neighbours, not halves apart;
+    inverse: turned back, which is also the gradient; factor: of the turned elements; out: x itself for in place."""
+    code = _dtype_code(x)
+    if x.dim() != 3 or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor [tokens, heads, D]")
+    tokens, heads, D = x.shape
+    index = x.get_device()
+
+    def stride(t, name):
+        s0, s1, s2 = t.stride()
+        if (s2 != 1 and D > 1) or (s1 != D and heads > 1):
+            raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
+        return s0 if tokens > 1 else heads * D          # the stride of a lone token is not used
+
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
+        raise ValueError("out must be a tensor of x's shape, type and device")
+    if freqs.dtype is not torch.float32 or freqs.dim() != 1 or freqs.get_device() != index or not freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous float32 tensor [rotary / 2] on x's device")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if positions.dtype is not _INT32 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or positions.get_device() != index \
+            or (tokens > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be an int32 tensor [tokens] or [axes, tokens] on x's device, its rows contiguous")
+    if (axis is not None or axes > 1) and (axis is None or axis.dtype is not _INT32 or axis.shape != freqs.shape
+                                           or axis.get_device() != index or not axis.is_contiguous()):
+        raise ValueError("several rows of positions go with axis, a contiguous int32 tensor of freqs' shape")
+    o = RopeOpts(_raw_stream(index), axis.data_ptr() if axis is not None else None, axes,
+                 positions.stride(0) if axes > 1 else 0, int(interleaved), int(inverse), factor)
+    if factor == 0:
+        raise ValueError("factor must not be 0")
+    _call_on(index, lib.luvc_rope, x.data_ptr(), stride(x, "x"), positions.data_ptr(), freqs.data_ptr(), tokens, heads, D,
+             2 * freqs.numel(), code, out.data_ptr(), stride(out, "out"), o)
+    return out

@@ -1,5 +1,5 @@
 // C ABI of the library: argument checks, stream and scratch handling, and the
-// host-buffer variants.  All arithmetic lives in oim.cu, spu.cu, kv_cache.cu and attn_decode.cu.
+// host-buffer variants.  All arithmetic lives in oim.cu, spu.cu, rope.cu, kv_cache.cu, attn_decode.cu and attn_cross.cu.
 
 #include <atomic>
 #include <cmath>
@@ -598,6 +598,32 @@ int luvc_spu_prune_host(const void* hidden, int B, int N, int D, float cutoff, i
     cudaMemcpyAsync(out_hidden, dout, (size_t)B * keep * D * es, cudaMemcpyDeviceToHost, st);
     cudaMemcpyAsync(out_idx, didx, (size_t)B * keep * 4, cudaMemcpyDeviceToHost, st);
     return cudaStreamSynchronize(st) == cudaSuccess ? LUVC_OK : LUVC_ERR_CUDA;
+}
+
+// ---- rotary positions ----------------------------------------------------------
+
+int luvc_rope(const void* x, long long x_stride, const int32_t* positions, const float* freqs, int tokens, int heads, int D, int rotary,
+              int dtype, void* out, long long out_stride, const luvc_rope_opts* opts) {
+    const luvc_rope_opts o = opts ? *opts : luvc_rope_opts{};
+    if (!freqs || ((!x || !positions || !out) && tokens > 0)) return LUVC_ERR_NULL;
+    if (dtype != LUVC_BF16 && dtype != LUVC_F32) return LUVC_ERR_DTYPE;
+    const int axes = o.axes ? o.axes : 1;
+    if (tokens < 0 || heads < 1 || heads > 65536 || D < 1 || D > 1024 || rotary < 2 || rotary > D || rotary % 2 ||
+        x_stride < (long long)heads * D || out_stride < (long long)heads * D || axes < 1 || axes > 64 ||
+        (axes > 1 && o.position_stride < 0) || (x == out && x_stride != out_stride) || !std::isfinite(o.factor))
+        return LUVC_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if ((D * es) % 16 || (x_stride * es) % 16 || (out_stride * es) % 16 || !aligned16(x) || !aligned16(out) || !aligned4(positions) ||
+        !aligned4(freqs) || !aligned4(o.axis))
+        return LUVC_ERR_ALIGN;
+    if (tokens == 0) return LUVC_OK;
+    RopeProblem p;
+    p.x = x; p.out = out; p.x_stride = x_stride; p.out_stride = out_stride; p.position_stride = axes > 1 ? o.position_stride : 0;
+    p.positions = positions; p.freqs = freqs; p.axis = axes > 1 ? o.axis : nullptr; p.axes = axes; p.tokens = tokens; p.heads = heads;
+    p.D = D; p.rotary = rotary; p.dtype = dtype; p.interleaved = o.interleaved; p.inverse = o.inverse;
+    p.factor = o.factor != 0.f ? o.factor : 1.f;
+    p.stream = static_cast<cudaStream_t>(o.stream);
+    return rope(p);
 }
 
 // ---- paged key-value cache -----------------------------------------------------

@@ -230,4 +230,19 @@ struct AttnProblem {
 size_t attn_workspace_bytes();
 int attn_decode(const AttnProblem& p);
 
+// ---- rotary positions (rope.cu) ---------------------------------------------------------------------
+
+struct RopeProblem {
+    const void* x;
+    void* out;
+    long long x_stride, out_stride, position_stride;
+    const int32_t* positions;
+    const float* freqs;
+    const int32_t* axis;
+    int axes, tokens, heads, D, rotary, dtype, interleaved, inverse;
+    float factor;
+    cudaStream_t stream;
+};
+int rope(const RopeProblem& p);
+
 }  // namespace luvc
