@@ -65,9 +65,9 @@ typedef enum {
     LUVC_ERR_PAGES = 12      /* not enough free pages, or table entries, in a key-value cache */
 } luvc_status;
 
-/* LUVC_E4M3 (8-bit floats, 4 exponent and 3 mantissa bits, no infinities) is a type of
- * key-value caches only. */
-typedef enum { LUVC_BF16 = 0, LUVC_F32 = 1, LUVC_E4M3 = 2 } luvc_dtype;
+/* LUVC_E4M3 (8-bit floats, 4 exponent and 3 mantissa bits, no infinities) and LUVC_E4M3_BLOCK (the
+ * same with a scale for each LUVC_KV_BLOCK tokens of a head) are types of key-value caches only. */
+typedef enum { LUVC_BF16 = 0, LUVC_F32 = 1, LUVC_E4M3 = 2, LUVC_E4M3_BLOCK = 4 } luvc_dtype;
 
 /* Cutoff used when the caller passes cutoff <= 0.  The paper never states the
  * value of its sigma_t; 1/8 of the band is this library's choice. */
@@ -429,14 +429,24 @@ typedef struct {
     int32_t* lengths;        /* [slots] tokens of each sequence; 0: the slot is empty */
     int32_t* refs;           /* [pages] sequences that hold the page; 0: the page is free */
     int32_t* table;          /* [slots, max_pages] page of each run of page_size tokens, -1 past the sequence */
-    const float* k_scale;    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; else NULL */
-    const float* v_scale;    /* the same for the values */
+    union {
+        const float* k_scale;    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; else NULL */
+        float* k_block_scale;    /* LUVC_E4M3_BLOCK: [layers, pages, heads, page_size / LUVC_KV_BLOCK], a stored key x stands for x
+                                    times the scale of its block; written along with the rows */
+    };
+    union {
+        const float* v_scale;    /* the same for the values */
+        float* v_block_scale;
+    };
     int layers, pages, heads, page_size, D, slots, max_pages;
-    int dtype;               /* LUVC_BF16, LUVC_F32 or LUVC_E4M3 */
+    int dtype;               /* LUVC_BF16, LUVC_F32, LUVC_E4M3 or LUVC_E4M3_BLOCK */
 } luvc_kv_cache;
 
+/* Consecutive tokens of a page that share the scales of a LUVC_E4M3_BLOCK cache. */
+#define LUVC_KV_BLOCK 16
+
 /*
- * Limits: page_size a multiple of 16; D a multiple of 8 (of 16 for LUVC_E4M3, of 4 for LUVC_F32) up to
+ * Limits: page_size a multiple of 16; D a multiple of 8 (of 16 for LUVC_E4M3 and LUVC_E4M3_BLOCK, of 4 for LUVC_F32) up to
  * 256; at most 4096 sequences per call; layers * heads <= 65536; at most 2^31 - 1 token rows
  * (pages * heads * page_size) per layer and 2^31 - 1 tokens per sequence.  Offsets into the pools are 64-bit.
  */
@@ -470,7 +480,7 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
 /*
  * Writes the key and value rows of the LAST tokens of n sequences into one layer.
  *
- * k, v        [tokens, heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or E4M3 cache, LUVC_F32 for
+ * k, v        [tokens, heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or 8-bit cache, LUVC_F32 for
  *             an f32 cache.  k_stride / v_stride: elements from one token to the next (rows of a fused
  *             projection need no copy); a token's heads * D elements are contiguous
  * starts      DEVICE [n + 1], ascending: sequence i owns rows starts[i] .. starts[i+1]-1, which are its
@@ -478,7 +488,10 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
  *             (tokens = n)
  * sizes       optional DEVICE [tokens] int32, the out_sizes of luvc_oim_merge*: the values are written
  *             enhanced, V + log(size) (Eq. 2), formed in fp32 and rounded once
- * An E4M3 cache stores x / scale, saturated at +-448, rounded to nearest even.  Rows that would fall before
+ * An 8-bit cache stores x / scale, saturated at +-448, rounded to nearest even.  The scales of a LUVC_E4M3_BLOCK cache follow from the
+ * rows: of the rows of a block that are written, the smallest power of two 2^e, -60 <= e <= 60, whose 448-fold no finite element exceeds; if the block has rows
+ * before them, the larger of that and its scale, and if that is not its scale the rows before are brought to it (exactly, but for
+ * magnitudes that fall below 2^-6 of the scale, which are rounded to steps of 2^-9).  Rows that would fall before
  * the start of their sequence, or whose slot is out of range, are not written (LUVC_ERR_SHAPE in the status
  * word); all others are, also by the luvc_kv_write calls that follow, until another call finds the word.  (Until
  * luvc_read_status it may hold the status in its low 8 bits.)  Tokens that a fork shares are
@@ -487,6 +500,20 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
 int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,
                   long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes,
                   int dtype, const luvc_kv_opts* opts);
+
+/*
+ * Reads rows of n sequences of one layer back: k, v (OUTPUTS, laid out and typed as luvc_kv_write's inputs) get the tokens
+ * first[i] .. first[i] + starts[i+1] - starts[i] - 1 of sequence i as rows starts[i] .. starts[i+1]-1, the values that an 8-bit cache's
+ * rows stand for rounded to bf16.
+ *
+ * first       DEVICE [n], NULL: from the first token on
+ * starts      DEVICE [n + 1], ascending, starts[0] = 0, starts[n] <= tokens; NULL: one token each (tokens = n).  Rows from starts[n] on are
+ *             left as they are
+ * A slot may be named several times.  Rows of tokens that a sequence does not have are zeros (LUVC_ERR_SHAPE in the status word).  The
+ * call runs whatever the status word says.
+ */
+int luvc_kv_read(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const int32_t* first, void* k, void* v,
+                 long long k_stride, long long v_stride, int tokens, const int32_t* starts, int dtype, const luvc_kv_opts* opts);
 
 /* Sequence dst[i] (DEVICE, n distinct empty slots) becomes a copy of sequence src[i] (DEVICE; the same
  * source may be named several times) in all layers.  Full pages are shared and counted in refs; the
@@ -508,7 +535,8 @@ int luvc_kv_free(const luvc_kv_cache* cache, const int32_t* seqs, int n, const l
  * nothing is dropped) and the old pages are given back
  * afterwards, so sequences that share pages with this one are not touched, and the pool needs the new pages
  * free at the call.  An idx entry outside the block is replaced by the nearest one inside
- * (LUVC_ERR_KEEP in the status word, after the fact).
+ * (LUVC_ERR_KEEP in the status word, after the fact).  The rows that a block of a LUVC_E4M3_BLOCK cache is made of get the largest of the
+ * scales they had.
  */
 int luvc_kv_compact(const luvc_kv_cache* cache, const int32_t* seqs, int n, const int32_t* first, const int32_t* span,
                     const int32_t* idx, int keep, const int32_t* counts, const luvc_kv_opts* opts);
@@ -538,7 +566,7 @@ typedef struct {
  * out[i, h, :] = sum_t p_t V[t] / sum_t p_t,  p_t = exp(scale * <q[i, h], K[t]> + key_bias[i, t]),
  * over the tokens t < lengths[seqs[i]] of one layer; query head h reads key head h / (q_heads / heads).
  *
- * q, out      [n, q_heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or E4M3 cache, LUVC_F32 for an
+ * q, out      [n, q_heads, D] of element type `dtype`: LUVC_BF16 for a bf16 or 8-bit cache, LUVC_F32 for an
  *             f32 cache; q_stride: elements from one sequence's queries to the next (a sequence's q_heads * D
  *             elements are contiguous); out is dense
  * seqs        DEVICE [n] slots, NULL = 0 .. n-1; a slot may be named several times.  A slot out of range
@@ -546,7 +574,8 @@ typedef struct {
  * A sequence without tokens, or whose keys are all masked by -inf, gives a row of zeros.  A key masked
  * by -inf contributes nothing, whatever its rows hold; rows past the length are never used.  Scores,
  * softmax and sums are fp32; a weight enters its product with V with 16 bits at least (LUVC_E4M3: off by
- * 2^-16 of the largest weight of its 16 tokens, or 2^-60 of the largest of all, at most).  A call repeated gives the same bits; how the work is split, and with it the last bits,
+ * 2^-16 of the largest weight of its 16 tokens, or 2^-60 of the largest of all, at most; LUVC_E4M3_BLOCK: 2^-14, and a block whose values' scale
+ * is below 2^-60 of another's counts as if it were that).  A call repeated gives the same bits; how the work is split, and with it the last bits,
  * depends on all lengths of the call.  The call runs whatever the status word says.
  */
 int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,

@@ -15,7 +15,8 @@ import torch
 
 from . import _build
 
-BF16, F32, E4M3 = 0, 1, 2
+BF16, F32, E4M3, E4M3_BLOCK = 0, 1, 2, 4
+KV_BLOCK = 16           # tokens that share a scale in an E4M3_BLOCK cache
 DEFAULT_CUTOFF = 0.125
 
 STATUS_NAMES = {
@@ -33,7 +34,7 @@ EXPORTS = (
     "luvc_oim_merge_host", "luvc_oim_value_enhance", "luvc_spu_sigma", "luvc_spu_workspace_bytes", "luvc_spu_prune",
     "luvc_spu_prune_f32", "luvc_spu_prune_ex", "luvc_spu_prune_host", "luvc_spu_prune_static", "luvc_spu_static_status",
     "luvc_spu_cascade", "luvc_kv_workspace_bytes", "luvc_kv_reserve", "luvc_kv_write", "luvc_kv_fork", "luvc_kv_free",
-    "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode", "luvc_rope",
+    "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode", "luvc_rope", "luvc_kv_read",
 )
 
 
@@ -139,6 +140,7 @@ def _load() -> ctypes.CDLL:
     L.luvc_kv_workspace_bytes.argtypes = [cache, i]
     L.luvc_kv_reserve.argtypes = [cache, p, i, p, kv]
     L.luvc_kv_write.argtypes = [cache, i, p, i, p, p, ll, ll, i, p, p, i, kv]
+    L.luvc_kv_read.argtypes = [cache, i, p, i, p, p, p, ll, ll, i, p, i, kv]
     L.luvc_kv_fork.argtypes = [cache, p, p, i, kv]
     L.luvc_kv_free.argtypes = [cache, p, i, kv]
     L.luvc_kv_compact.argtypes = [cache, p, i, p, p, p, i, p, kv]
@@ -411,7 +413,9 @@ class KvCache:
     """A paged key-value cache of a group of decoder layers that hold the same tokens (luvc_kv_cache).
 
     k, v: the caller's pools, CUDA tensors [layers, pages, heads, page_size, D] in bfloat16, float32 or
-    float8_e4m3fn (then with k_scale / v_scale, float32 [layers, heads]: a stored x stands for x * scale).
+    float8_e4m3fn (then with k_scale / v_scale, float32: a stored x stands for x * scale).  Scales [layers, heads] are the caller's and
+    stay as they are; scales [layers, pages, heads, page_size // KV_BLOCK], one for each KV_BLOCK tokens of a page and head, are
+    written along with the rows.
     slots: sequences; max_pages: pages a sequence may have.  meta: optional int32 tensor of
     slots + pages + slots * max_pages entries that holds the books (made empty if not given); `lengths`, `refs`
     and `table` are views of it, so that one copy of `meta` is a snapshot of all three."""
@@ -434,9 +438,10 @@ class KvCache:
         for s in (k_scale, v_scale):
             if (s is not None) != (k.dtype == torch.float8_e4m3fn):
                 raise ValueError("k_scale and v_scale go with float8_e4m3fn pools, and only with them")
-            if s is not None and (s.dtype != torch.float32 or s.shape != (layers, heads) or not s.is_contiguous()
-                                  or s.device != k.device):
-                raise ValueError("scales must be contiguous float32 [layers, heads] tensors on the pools' device")
+            if s is not None and (s.dtype != torch.float32 or s.shape not in ((layers, heads), (layers, pages, heads, page_size // KV_BLOCK))
+                                  or s.shape != k_scale.shape or not s.is_contiguous() or s.device != k.device):
+                raise ValueError("scales must be contiguous float32 [layers, heads] or [layers, pages, heads, page_size // %d] tensors on the "
+                                 "pools' device" % KV_BLOCK)
         self.k, self.v, self.meta, self.k_scale, self.v_scale = k, v, meta, k_scale, v_scale
         self.lengths = meta[:slots]
         self.refs = meta[slots:slots + pages]
@@ -444,12 +449,13 @@ class KvCache:
         self.device, self.index, self.dtype = k.device, k.get_device(), k.dtype
         self.layers, self.pages, self.heads, self.page_size, self.head_dim = layers, pages, heads, page_size, D
         self.slots, self.max_pages = slots, max_pages
+        self.blocks = k_scale is not None and k_scale.dim() == 4
         # of queries, new rows and outputs
         self.io_dtype, self.io_code = (torch.float32, F32) if k.dtype == torch.float32 else (torch.bfloat16, BF16)
         self.struct = KvCacheStruct(
             k.data_ptr(), v.data_ptr(), self.lengths.data_ptr(), self.refs.data_ptr(), self.table.data_ptr(),
             k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None,
-            layers, pages, heads, page_size, D, slots, max_pages, _CACHE_DTYPES[k.dtype])
+            layers, pages, heads, page_size, D, slots, max_pages, E4M3_BLOCK if self.blocks else _CACHE_DTYPES[k.dtype])
 
 
 _CACHE_DTYPES = {torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: E4M3}
@@ -552,6 +558,20 @@ def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0
     _kv_call(lib.luvc_kv_write, cache, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, k.data_ptr(), v.data_ptr(), ks, vs,
              tokens, _ints(starts, cache, n + 1, "starts"), _ints(sizes, cache, tokens, "sizes"), cache.io_code,
              _kv_opts(cache, None, device_status))
+
+
+def kv_read(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, layer: int = 0, starts: torch.Tensor | None = None,
+            first: torch.Tensor | None = None, seqs: torch.Tensor | None = None, device_status: torch.Tensor | None = None) -> None:
+    """luvc_kv_read: rows of the sequences in `layer` back into k, v [tokens, heads, D] (the queries' type; may be parts of a wider tensor).
+    starts: int32 [n+1], rows starts[i] .. starts[i+1]-1 get the tokens of sequence i from first[i] on (int32 [n], None: from 0); None:
+    one row each."""
+    tokens = k.shape[0]
+    n = tokens if starts is None else starts.numel() - 1
+    ks, vs = _token_stride(k, cache, cache.heads, "k"), _token_stride(v, cache, cache.heads, "v")
+    if v.shape[0] != tokens:
+        raise ValueError("k and v must have one shape")
+    _kv_call(lib.luvc_kv_read, cache, cache.struct, layer, _ints(seqs, cache, n, "seqs"), n, _ints(first, cache, n, "first"), k.data_ptr(),
+             v.data_ptr(), ks, vs, tokens, _ints(starts, cache, n + 1, "starts"), cache.io_code, _kv_opts(cache, None, device_status))
 
 
 def kv_fork(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, *, workspace: torch.Tensor | None = None,

@@ -192,8 +192,9 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 int check_cache(const luvc_kv_cache* c) {
     if (!c || !c->k || !c->v || !c->lengths || !c->refs || !c->table) return LUVC_ERR_NULL;
-    if (c->dtype != LUVC_BF16 && c->dtype != LUVC_F32 && c->dtype != LUVC_E4M3) return LUVC_ERR_DTYPE;
-    if ((c->dtype == LUVC_E4M3) != (c->k_scale != nullptr) || (c->dtype == LUVC_E4M3) != (c->v_scale != nullptr)) return LUVC_ERR_NULL;
+    if (c->dtype != LUVC_BF16 && c->dtype != LUVC_F32 && c->dtype != LUVC_E4M3 && c->dtype != LUVC_E4M3_BLOCK) return LUVC_ERR_DTYPE;
+    const bool scaled = c->dtype == LUVC_E4M3 || c->dtype == LUVC_E4M3_BLOCK;
+    if (scaled != (c->k_scale != nullptr) || scaled != (c->v_scale != nullptr)) return LUVC_ERR_NULL;
     if (c->layers < 1 || c->pages < 1 || c->heads < 1 || c->page_size < 1 || c->D < 1 || c->slots < 1 || c->max_pages < 1)
         return LUVC_ERR_SHAPE;
     if (c->page_size % 16 || c->D > 256 || (long long)c->layers * c->heads > 65536) return LUVC_ERR_SHAPE;
@@ -213,6 +214,20 @@ int check_kv_call(const luvc_kv_cache* c, const int32_t* seqs, int n, const int3
     if (rc) return rc;
     if (n < 1 || n > kKvMaxSeqs || (!seqs && n > c->slots)) return LUVC_ERR_SHAPE;
     if (!aligned4(seqs) || (device_status && !aligned16(device_status))) return LUVC_ERR_ALIGN;
+    return LUVC_OK;
+}
+
+// Rows that go into a layer or come out of it.  `ints`: a further optional array of the call.
+int check_kv_rows(const luvc_kv_cache* c, int layer, const int32_t* seqs, int n, const void* k, const void* v, long long k_stride,
+                  long long v_stride, int tokens, const int32_t* starts, const int32_t* ints, int dtype, const int32_t* device_status) {
+    const int rc = check_kv_call(c, seqs, n, device_status);
+    if (rc) return rc;
+    if ((!k || !v) && tokens > 0) return LUVC_ERR_NULL;
+    if (dtype != (c->dtype == LUVC_F32 ? LUVC_F32 : LUVC_BF16)) return LUVC_ERR_DTYPE;
+    const long long row = (long long)c->heads * c->D;
+    if (layer < 0 || layer >= c->layers || tokens < 0 || (!starts && tokens != n) || k_stride < row || v_stride < row) return LUVC_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if (!aligned16(k) || !aligned16(v) || (k_stride * es) % 16 || (v_stride * es) % 16 || !aligned4(starts) || !aligned4(ints)) return LUVC_ERR_ALIGN;
     return LUVC_OK;
 }
 
@@ -648,21 +663,24 @@ int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, in
                   long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes, int dtype,
                   const luvc_kv_opts* opts) {
     const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
-    const int rc = check_kv_call(cache, seqs, n, o.device_status);
+    const int rc = check_kv_rows(cache, layer, seqs, n, k, v, k_stride, v_stride, tokens, starts, sizes, dtype, o.device_status);
     if (rc) return rc;
-    if ((!k || !v) && tokens > 0) return LUVC_ERR_NULL;
-    if (dtype != (cache->dtype == LUVC_F32 ? LUVC_F32 : LUVC_BF16)) return LUVC_ERR_DTYPE;
-    const long long row = (long long)cache->heads * cache->D;
-    if (layer < 0 || layer >= cache->layers || tokens < 0 || (!starts && tokens != n) || k_stride < row || v_stride < row)
-        return LUVC_ERR_SHAPE;
-    const size_t es = elem_size(dtype);
-    if (!aligned16(k) || !aligned16(v) || (k_stride * es) % 16 || (v_stride * es) % 16 || !aligned4(starts) || !aligned4(sizes))
-        return LUVC_ERR_ALIGN;
     int* status = o.device_status ? o.device_status : status_word();
     if (!status) return LUVC_ERR_CUDA;
     if (tokens == 0) return LUVC_OK;
-    return kv_write(*cache, layer, seqs, n, k, v, k_stride, v_stride, tokens, starts, sizes, status,
-                    static_cast<cudaStream_t>(o.stream));
+    const auto write = cache->dtype == LUVC_E4M3_BLOCK ? kv_write_blocks : kv_write;
+    return write(*cache, layer, seqs, n, k, v, k_stride, v_stride, tokens, starts, sizes, status, static_cast<cudaStream_t>(o.stream));
+}
+
+int luvc_kv_read(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const int32_t* first, void* k, void* v,
+                 long long k_stride, long long v_stride, int tokens, const int32_t* starts, int dtype, const luvc_kv_opts* opts) {
+    const luvc_kv_opts o = opts ? *opts : luvc_kv_opts{};
+    const int rc = check_kv_rows(cache, layer, seqs, n, k, v, k_stride, v_stride, tokens, starts, first, dtype, o.device_status);
+    if (rc) return rc;
+    int* status = o.device_status ? o.device_status : status_word();
+    if (!status) return LUVC_ERR_CUDA;
+    if (tokens == 0) return LUVC_OK;
+    return kv_read(*cache, layer, seqs, n, first, k, v, k_stride, v_stride, tokens, starts, status, static_cast<cudaStream_t>(o.stream));
 }
 
 int luvc_kv_fork(const luvc_kv_cache* cache, const int32_t* src, const int32_t* dst, int n, const luvc_kv_opts* opts) {

@@ -42,6 +42,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "luvc_internal.h"
 #include "sm100_ptx.cuh"
@@ -61,6 +62,9 @@ constexpr float kSlack = 6.f;                   // the reference of the weights 
 // weights).  So the largest of 16 weights is between e^-kFall and e^kRise, and e^kLead at least where it is the largest so far.  m does
 // not follow scores below m - kGone (masks of a lowest value), and only as far as sums of weights stay below 2^kMostGain.
 constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f, kGone = 60.f, kMostGain = 60.f;
+// Blocks: a block's scale is at least this part of the unit of the sums O, or the unit becomes the block's scale (neighbours mostly differ
+// by a factor of two; the product with V keeps two bits less of a weight at most).
+constexpr float kLeastUnit = 0.25f;
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;           // and with a limit from the status block (a test's), so that copies which do come are waited for
 
@@ -73,6 +77,13 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint
 // The barrier's phase waits for so many bytes more.
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Four bytes into shared memory; and an arrival at the barrier when the copies of this thread have landed.
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -128,6 +139,11 @@ __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& l
 }
 
 // ---- shapes ---------------------------------------------------------------------------------------------
+
+// Elements of an e4m3 cache with scales for blocks of 16 tokens.
+struct E4m3Block {
+    unsigned char x;
+};
 
 // TC: element of the cache; DPB: bytes of a row in shared memory, 64 or a multiple of 128 (columns past D are filled with zeros by
 // TMA); NT: groups of 8 query heads per key head that one tile is multiplied with, or, f32 only, -NT query heads on the CUDA cores.
@@ -441,7 +457,7 @@ __global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ Args a) {
     using Sh = Shape<TC, DPB, NT>;
     constexpr int NW = Sh::NW, S = Sh::S, MT = Sh::MT, DP = Sh::DP, ROWS = Sh::ROWS, KT = Sh::KT, NTHR = 32 * NW;
-    constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1, kCores = Sh::CORES;
+    constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1, kCores = Sh::CORES, kBlocks = std::is_same<TC, E4m3Block>::value;
     constexpr int NTX = kCores ? 1 : NT, NH = kCores ? -NT : 1; // sizes of arrays that are not used otherwise
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[NW * S];
@@ -452,6 +468,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ unsigned scan_warp[NW];
     __shared__ __align__(16) float core_q[kCores ? NW : 1][kCores ? NH * DP : 4], core_p[kCores ? NW : 1][NH * 16];
     __shared__ float factors[ROWS * (DP / 4) > NTHR ? 64 : 1][ROWS];
+    __shared__ float block_scales[kBlocks ? NW * S : 1][2 * Sh::SUB];      // of a stage's 16-token parts: K, V
     __shared__ int last_flag[2], all_flag;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
@@ -462,7 +479,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
     // ---- the list of tiles ----
     if (lane < S) {
-        mbar_init(smem_u32(&bars[warp * S + lane]), 1);
+        mbar_init(smem_u32(&bars[warp * S + lane]), kBlocks ? 1 + 2 * Sh::SUB : 1);     // (and the lanes that bring scales)
         mbar_fence_init();
     }
     if (lane < 2) piece_off[warp][lane] = 0;
@@ -631,14 +648,26 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < Sh::SUB; ++j) {
+                bool scaled = false;
                 if (j == 0 || 16 * j < ld_left) {
                     if (ld_page >= pg_first + 32) fetch_pages();
                     const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
                     const int row = (unsigned)page < (unsigned)p.c.pages ? (page * p.c.heads + ld_h) * ps + ld_off : a.rows_total;
                     if (lane < 2 * Sh::SEGS)
                         tma_load_2d(my_dst + stage * Sh::STAGE + j * 2 * Sh::SUBK, my_map, bar, (lane >> 1) * (Sh::PITCH / Sh::ES), row);
+                    if (kBlocks && lane < 2) {                  // its scale arrives with the stage (of no page: 1)
+                        float* const to = &block_scales[warp * S + stage][2 * j + lane];
+                        const float* const from = (is_v ? p.c.v_block_scale : p.c.k_block_scale) + ((size_t)p.layer * a.rows_total + row) / kKvBlock;
+                        scaled = row < a.rows_total;
+                        if (scaled) cp_async4(smem_u32(to), from);
+                        else *to = 1.f;
+                    }
                     ld_off += 16;
                     if (ld_off == ps) { ld_off = 0; ++ld_page; }
+                }
+                if (kBlocks && lane < 2) {
+                    if (scaled) cp_async_arrive(bar);
+                    else mbar_arrive(bar);
                 }
             }
             ld_left -= KT;
@@ -679,8 +708,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             const int h = a.groups == 1 ? at.seg : at.seg / a.groups, r0 = (at.seg - h * a.groups) * ROWS;
             const int rows = min(ROWS, a.group - r0);
             const int len = length_of(slot_of(at.seq));
-            const float vscale = p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
-            const float scale = p.scale * (p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
+            const float vscale = !kBlocks && p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
+            const float scale = p.scale * (!kBlocks && p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
+            // blocks: the sums O are in units of v_unit, which follows the blocks' scales and is never far below the largest so far
+            float v_unit = 0x1p-126f, v_per_unit = 0x1p126f, v_top = 0.f;
             // queries: B operand of S^T = K Q^T, head g of each group of 8
             const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
             constexpr int KS = DPB / 32;                        // steps of 32 bytes of a row
@@ -867,7 +898,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 const float x = kF32 ? done[nt][c] + s[nt][c] + (s2[nt][c] + s3[nt][c]) : s[nt][c] + s2[nt][c];
-                                s[nt][c] = fmaf(x, qmul[nt][c & 1], bias[j][c >> 1]);
+                                s[nt][c] = fmaf(x, kBlocks ? qmul[nt][c & 1] * block_scales[warp * S + stage][2 * j] : qmul[nt][c & 1], bias[j][c >> 1]);
                             }
                         unsigned gone = 0;
                         if (masked) {                               // whatever a masked row holds
@@ -940,6 +971,24 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                 const float mb = m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1];
                                 s[nt][c] = exp2_fast((s[nt][c] - mb) * kLog2e);
                             }
+                        float w_scale = 1.f;                        // of the weights in their product with V
+                        if constexpr (kBlocks) {
+                            float now = block_scales[warp * S + stage][2 * j + 1];
+                            if (!(now <= v_unit && now >= kLeastUnit * v_unit)) {
+                                if (!(now > 0.f && now < INFINITY)) now = 0.f;
+                                v_top = fmaxf(v_top, now);
+                                const float unit = fmaxf(now, fmaxf(v_top * 0x1p-60f, 0x1p-126f)), f = v_unit / unit;
+                                v_unit = unit;
+                                v_per_unit = 1.f / unit;
+#pragma unroll
+                                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                        for (int c = 0; c < 4; ++c) o[mt][nt][c] *= f;
+                            }
+                            w_scale = now * v_per_unit;
+                        }
                         uint32_t ph[NTX][2], pl[NTX][2];            // P^T, B operand: tokens 2 t4, 2 t4 + 1 (and + 8) of head g
                         float pf[NTX][4];
 #pragma unroll
@@ -948,7 +997,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             l[nt][1] += s[nt][1] + s[nt][3];
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                const float p0 = s[nt][2 * x], p1 = s[nt][2 * x + 1];
+                                const float p0 = kBlocks ? s[nt][2 * x] * w_scale : s[nt][2 * x], p1 = kBlocks ? s[nt][2 * x + 1] * w_scale : s[nt][2 * x + 1];
                                 if constexpr (kF32) {
                                     const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
                                     const uint32_t up = movm(__byte_perm(u0, u1, 0x7632)), down = movm(__byte_perm(u0, u1, 0x5410));
@@ -1100,7 +1149,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int d = 16 * mt + (kF8 ? 2 * g + (c >> 1) : g + 8 * (c >> 1));
-                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = o[mt][nt][c];
+                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = kBlocks ? o[mt][nt][c] * v_unit : o[mt][nt][c];
                     }
             __syncwarp();
             if constexpr (!kF8) {                               // (an e4m3 cache has no infinities, and its rows are not split)
@@ -1445,6 +1494,9 @@ int attn_decode(const AttnProblem& p) {
     if (p.c.dtype == LUVC_BF16)
         return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256>(p)
                                                                                                : launch_heads<__nv_bfloat16, __nv_bfloat16, 512>(p);
+    if (p.c.dtype == LUVC_E4M3_BLOCK)
+        return bytes <= 64 ? launch_heads<__nv_bfloat16, E4m3Block, 64>(p) : bytes <= 128 ? launch_heads<__nv_bfloat16, E4m3Block, 128>(p)
+                                                                                          : launch_heads<__nv_bfloat16, E4m3Block, 256>(p);
     // rows of 64 bytes halve the conversions and products (16 / 16 heads of 64, 79 MB: 28.0 us, as rows of 128 bytes 35.1)
     return bytes <= 64 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 64>(p) : bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 128>(p) : launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 256>(p);
 }

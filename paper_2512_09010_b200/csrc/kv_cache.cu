@@ -19,6 +19,7 @@
 
 #include <atomic>
 
+#include "kv_common.cuh"
 #include "luvc_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -31,16 +32,6 @@ constexpr int kPerLane = 8;                                 // pages a lane look
 constexpr int kWarpPages = 32 * kPerLane;
 constexpr int kMaxNeed = 1 << 26;                           // pages one call takes for one sequence (2^30 tokens at least)
 constexpr int kClaimed = -1;                                // lengths[] of a slot that the running call has claimed
-
-__device__ __forceinline__ int status_of(int* status) { return *reinterpret_cast<volatile int*>(status); }
-
-// For a call that has found the status word set and does nothing: rows that a write has skipped become a plain status, at which further
-// writes stop too.
-__device__ __forceinline__ void stop_writes(int* status, int word) {
-    if (word == kRowsSkipped && threadIdx.x == 0) *status = word & kStatusMask;
-}
-
-__device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 // The plan's result for kv_move_kernel, in the call's workspace.
 struct MoveList {
@@ -359,27 +350,13 @@ struct MoveArgs {
     int triples, groups, cap, chunks, batch, units, teams, size;
 };
 
-// Fills the pages of the plan's list, and settles the pages that change hands.  The work is the list of all (page, up to
-// kMoveRows of its rows, group of kMoveLanes (layer, K or V, head) triples); a CTA takes an equal, contiguous part of it.  Where rows
-// come from is looked up first, a row per thread, once for all the groups of the part; a thread then copies 16 bytes of a row for
-// all triples of a group, with as many loads in flight.  (Four triples and 64 registers let four CTAs share an SM: 190 us for
-// the 1.09 GB of a prune of eight videos, 10.0 for one image; with eight triples and two CTAs 193 and 10.5.)  Where a piece of
-// a page has no more 16-byte parts than half the threads, the CTA works in TEAMS, each on a group of its own (16 heads of 64 in
-// 8 bits, pages of 16, 620 MB: 140 us, without 211; a fork of 16 such sequences 15.1 and 21.5).
 constexpr int kMoveLanes = 4, kMoveRows = 64, kMoveThreads = 256;
 
-template <bool FORK, bool TEAMS>
-__global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_constant__ MoveArgs a) {
-    __shared__ long long src_row[kMoveThreads];             // row of head 0 of a layer's pool; -1: none
-    __shared__ long long dst_row[kMoveThreads / 16];        // first row of a piece (a page's rows, at most kMoveRows)
-    __shared__ int rows_of[kMoveThreads / 16];
+// Pages that change hands, a sequence per warp of a grid of kMoveThreads threads each.
+template <bool FORK>
+__device__ __forceinline__ void settle_pages(const MoveArgs& a) {
     const luvc_kv_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, ps = c.page_size;
-    pdl_trigger();
-    pdl_wait();
-    if (!a.move.head[1]) return;
-
-    // pages that change hands, a sequence per warp
     for (int i = blockIdx.x * (kMoveThreads / 32) + (tid >> 5); i < a.n; i += gridDim.x * (kMoveThreads / 32)) {
         const int slot = a.seqs ? a.seqs[i] : i;
         int32_t* const row = c.table + (long long)slot * c.max_pages;
@@ -400,6 +377,52 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
             }
         }
     }
+}
+
+// Place in a layer's pool (row of head 0) of the token that becomes row r of the page index p of sequence i; -1: none.
+template <bool FORK>
+__device__ __forceinline__ long long source_row(const MoveArgs& a, int i, int p, int r) {
+    const luvc_kv_cache& c = a.c;
+    const int ps = c.page_size, slot = a.seqs ? a.seqs[i] : i;
+    int from = p * ps + r, page;         // token of the old sequence that becomes this row
+    if (FORK) {
+        page = c.table[(long long)a.src[i] * c.max_pages + p];
+    } else {
+        const int first = a.first[i], span = a.span[i], count = a.counts ? a.counts[i] : a.keep;
+        if (from >= first + count) {
+            from += span - count;
+        } else if (from >= first) {
+            const int e = a.idx[(long long)i * a.keep + from - first], in = min(max(e, 0), span - 1);
+            if (in != e) *a.status = LUVC_ERR_KEEP;
+            from = first + in;
+        }
+        // a token moves towards the start, so it comes from a page that is not as before; only an entry that was replaced
+        // (or is out of order) can stand for one on a page that stays
+        if (from < p * ps && from / ps < a.move.from[i]) page = c.table[(long long)slot * c.max_pages + from / ps];
+        else page = a.move.old[(long long)i * c.max_pages + from / ps];
+    }
+    return page >= 0 && page < c.pages ? (long long)page * c.heads * ps + from % ps : -1;
+}
+
+// Fills the pages of the plan's list, and settles the pages that change hands.  The work is the list of all (page, up to
+// kMoveRows of its rows, group of kMoveLanes (layer, K or V, head) triples); a CTA takes an equal, contiguous part of it.  Where rows
+// come from is looked up first, a row per thread, once for all the groups of the part; a thread then copies 16 bytes of a row for
+// all triples of a group, with as many loads in flight.  (Four triples and 64 registers let four CTAs share an SM: 190 us for
+// the 1.09 GB of a prune of eight videos, 10.0 for one image; with eight triples and two CTAs 193 and 10.5.)  Where a piece of
+// a page has no more 16-byte parts than half the threads, the CTA works in TEAMS, each on a group of its own (16 heads of 64 in
+// 8 bits, pages of 16, 620 MB: 140 us, without 211; a fork of 16 such sequences 15.1 and 21.5).
+template <bool FORK, bool TEAMS>
+__global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_constant__ MoveArgs a) {
+    __shared__ long long src_row[kMoveThreads];             // row of head 0 of a layer's pool; -1: none
+    __shared__ long long dst_row[kMoveThreads / 16];        // first row of a piece (a page's rows, at most kMoveRows)
+    __shared__ int rows_of[kMoveThreads / 16];
+    const luvc_kv_cache& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 31, ps = c.page_size;
+    pdl_trigger();
+    pdl_wait();
+    if (!a.move.head[1]) return;
+
+    settle_pages<FORK>(a);
 
     const int triples = a.triples, groups = a.groups, cap = a.cap, chunks = a.chunks, batch = a.batch, units = a.units, teams = TEAMS ? a.teams : 1;
     // below 2^31: each item is 256 bytes of a pool at least
@@ -423,26 +446,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
                 dst_row[k] = (long long)to * c.heads * ps + skip;
                 rows_of[k] = rows;
             }
-            if (r < rows) {
-                int from = p * ps + skip + r, page;         // token of the old sequence that becomes this row
-                if (FORK) {
-                    page = c.table[(long long)a.src[i] * c.max_pages + p];
-                } else {
-                    const int first = a.first[i], span = a.span[i], count = a.counts ? a.counts[i] : a.keep;
-                    if (from >= first + count) {
-                        from += span - count;
-                    } else if (from >= first) {
-                        const int e = a.idx[(long long)i * a.keep + from - first], in = min(max(e, 0), span - 1);
-                        if (in != e) *a.status = LUVC_ERR_KEEP;
-                        from = first + in;
-                    }
-                    // a token moves towards the start, so it comes from a page that is not as before; only an entry that was replaced
-                    // (or is out of order) can stand for one on a page that stays
-                    if (from < p * ps && from / ps < a.move.from[i]) page = c.table[(long long)slot * c.max_pages + from / ps];
-                    else page = a.move.old[(long long)i * c.max_pages + from / ps];
-                }
-                src_row[tid] = page >= 0 && page < c.pages ? (long long)page * c.heads * ps + from % ps : -1;
-            }
+            if (r < rows) src_row[tid] = source_row<FORK>(a, i, p, skip + r);
         }
         __syncthreads();
         const unsigned wa = max(w0, piece0 * groups), wb = min(w1, (piece0 + batch) * groups);
@@ -485,6 +489,71 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_move_kernel(const __grid_c
     }
 }
 
+// The same for a cache with scales for blocks: the rows of a new block get the largest of the scales they had, and rows of another one are brought
+// to it.  The work is the list of all (page, block of it, group of kMoveLanes triples); a warp takes an equal, contiguous part of it,
+// looks up where a block's rows come from, a row per lane, and takes one triple after the other.
+template <bool FORK>
+__global__ void __launch_bounds__(kMoveThreads, 4) kv_move_block_kernel(const __grid_constant__ MoveArgs a) {
+    const luvc_kv_cache& c = a.c;
+    const int lane = threadIdx.x & 31, ps = c.page_size;
+    pdl_trigger();
+    pdl_wait();
+    if (!a.move.head[1]) return;
+    settle_pages<FORK>(a);
+    const int blocks = ps / kKvBlock, units = c.D / 16;     // of a page; of a row
+    const unsigned warps = gridDim.x * (kMoveThreads / 32), me = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
+    const unsigned work = (unsigned)(a.move.head[0] * blocks * a.groups), share = work / warps, more = work % warps;
+    const unsigned w0 = share * me + min(me, more), w1 = w0 + share + (me < more);
+    const unsigned part = 65536 / units + 1;                // a unit's row: unit * part / 65536, exact for 384 units of rows of up to 16
+    const size_t rows_of_layer = (size_t)c.pages * c.heads * ps;
+    long long from = -1, to_row = -1;                       // of this lane's row; of the block's first one (head 0 of a layer's pool)
+    int rows = 0;
+    for (unsigned w = w0; w < w1; ++w) {
+        const unsigned group = w % a.groups;
+        if (w == w0 || group == 0) {
+            const unsigned block = w / a.groups;
+            const int2 it = a.move.items[block / blocks];
+            const int at = (int)(block % blocks) * kKvBlock, slot = a.seqs ? a.seqs[it.x] : it.x;
+            const int to = c.table[(long long)slot * c.max_pages + it.y];
+            rows = to >= 0 && to < c.pages ? min(kKvBlock, c.lengths[slot] - it.y * ps - at) : 0;
+            to_row = (long long)to * c.heads * ps + at;
+            from = lane < rows ? source_row<FORK>(a, it.x, it.y, at + lane) : -1;
+        }
+        if (rows <= 0) continue;
+        for (int triple = group * kMoveLanes; triple < min(a.triples, (int)(group + 1) * kMoveLanes); ++triple) {
+            const int layer = triple / (2 * c.heads), rest = triple - layer * 2 * c.heads, h = rest >= c.heads ? rest - c.heads : rest;
+            unsigned char* const pool = static_cast<unsigned char*>(rest >= c.heads ? c.v : c.k) + (layer * rows_of_layer + (size_t)h * ps) * c.D;
+            float* const scales = (rest >= c.heads ? c.v_block_scale : c.k_block_scale) + (layer * rows_of_layer + (size_t)h * ps) / kKvBlock;
+            const float had = from >= 0 ? scales[from / kKvBlock] : 0.f;
+            const float now = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(had)));
+            const float f = had == now ? 1.f : had / now;   // (powers of two: exact)
+            const bool same = __all_sync(~0u, from < 0 || f == 1.f);
+            if (lane == 0) scales[to_row / kKvBlock] = now;
+            for (int u0 = 0; u0 < 16 * units; u0 += 128) {      // four pieces of 16 bytes of a lane at a time
+                long long src[4];
+                float by[4];
+                uint4 x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int u = u0 + 32 * e + lane, row = (int)(u * part >> 16);
+                    src[e] = __shfl_sync(~0u, from, row & 15);
+                    by[e] = __shfl_sync(~0u, f, row & 15);
+                    if (row > 15) src[e] = -1;
+                    if (src[e] >= 0) x[e] = __ldcs(reinterpret_cast<const uint4*>(pool + src[e] * c.D) + (u - row * units));
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int u = u0 + 32 * e + lane;
+                    if (src[e] < 0) continue;
+                    if (!same && by[e] != 1.f)
+                        x[e] = make_uint4(scaled_e4m3x4(x[e].x, by[e]), scaled_e4m3x4(x[e].y, by[e]), scaled_e4m3x4(x[e].z, by[e]), scaled_e4m3x4(x[e].w, by[e]));
+                    __stcs(reinterpret_cast<uint4*>(pool + to_row * c.D) + u, x[e]);
+                }
+            }
+        }
+    }
+}
+
 // A CTA per sequence.  Each looks at all slots of the call first: whether any of them is out of range, and then none is freed, must not
 // depend on which CTA comes first (the status word that one sets is read by the others).
 __global__ void __launch_bounds__(128) kv_free_kernel(const __grid_constant__ luvc_kv_cache c, const int32_t* seqs, int* status) {
@@ -519,25 +588,6 @@ struct WriteArgs {
     const void *k, *v;
     long long k_stride, v_stride;
     int* status;
-};
-
-template <typename T> struct Vec;                           // the elements of 16 input bytes, as floats
-template <> struct Vec<float> {
-    static constexpr int N = 4;
-    static __device__ void unpack(uint4 x, float (&f)[8]) {
-        f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
-    }
-};
-template <> struct Vec<__nv_bfloat16> {
-    static constexpr int N = 8;
-    static __device__ void unpack(uint4 x, float (&f)[8]) {
-        const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            f[2 * q] = __uint_as_float(w[q] << 16);
-            f[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-        }
-    }
 };
 
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -591,19 +641,6 @@ __device__ __forceinline__ void store_row(__nv_fp8_e4m3* p, const float (&f)[8],
         w[x] = (unsigned)__nv_cvt_float2_to_fp8x2(make_float2(q[4 * x], q[4 * x + 1]), __NV_SATFINITE, __NV_E4M3) |
                (unsigned)__nv_cvt_float2_to_fp8x2(make_float2(q[4 * x + 2], q[4 * x + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
     *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-}
-
-// Last entry of ascending starts[0 .. n] (starts[0] = 0) that is <= t, below n: 32 probes at a time (one warp, one t).
-__device__ __forceinline__ int owner_of(const int32_t* starts, int n, int t, int lane) {
-    int lo = 0, size = n;                                   // the answer is in [lo, lo + size)
-    while (size > 1) {
-        const int step = (size + 31) / 32, at = lo + lane * step;
-        const unsigned m = __ballot_sync(~0u, lane * step < size && starts[at] <= t);
-        const int k = m ? 31 - __clz(m) : 0;
-        lo += k * step;
-        size = min(step, size - k * step);
-    }
-    return lo;
 }
 
 // A CTA writes up to kWriteTokens tokens.  A thread keeps its place in a token's row (16 bytes of K and of V) and takes every
@@ -724,6 +761,10 @@ int launch_move(MoveArgs& a, long long pages, cudaStream_t stream) {
     const luvc_kv_cache& c = a.c;
     a.triples = c.layers * 2 * c.heads;
     a.groups = (a.triples + kMoveLanes - 1) / kMoveLanes;
+    if (c.dtype == LUVC_E4M3_BLOCK) {
+        const int sms = sm_count();
+        return sms ? launch_overlapped(kv_move_block_kernel<FORK>, 4 * sms, kMoveThreads, 0, stream, a) : LUVC_ERR_CUDA;
+    }
     a.cap = c.page_size < kMoveRows ? c.page_size : kMoveRows;          // page sizes: 16 and up
     a.chunks = (c.page_size + kMoveRows - 1) / kMoveRows;
     a.batch = kMoveThreads / a.cap;
