@@ -12,8 +12,8 @@
  *        visual token by the energy of the low-pass-filtered token sequence and
  *        keeps the highest-scoring tokens in their original order.
  *
- * and what a decoder does with the tokens they leave: a paged key-value cache and the attention of one new
- * token over it (luvc_kv_*, luvc_attn_decode).
+ * and what a decoder does with the tokens they leave: rotary positions (luvc_rope), a paged key-value cache and the attention of one
+ * new token over it (luvc_kv_*, luvc_attn_decode), and the attention of a text to them as states of an encoder (luvc_attn_cross).
  *
  * General rules
  *   - Every function returns a luvc_status (int); 0 is success.  Nothing aborts
@@ -580,6 +580,45 @@ typedef struct {
  */
 int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n,
                      int q_heads, int dtype, void* out, const luvc_attn_opts* opts);
+
+/* ---- attention to an encoder's states --------------------------------------- */
+
+/* Bytes of workspace luvc_attn_cross needs, whatever the sizes (about 43 MB).  Calls that share one must not overlap (their results are
+ * undefined if they do; calls after them are not affected). */
+size_t luvc_attn_cross_workspace_bytes(void);
+
+typedef struct {
+    void* stream;            /* cudaStream_t; NULL = legacy default stream */
+    void* workspace;         /* as in luvc_attn_opts */
+    size_t workspace_bytes;
+    int32_t* device_status;  /* as in luvc_kv_opts */
+    float scale;             /* factor of the scores; 0 = 1 / sqrt(D) */
+    const float* key_bias;   /* optional DEVICE [k_tokens] fp32, added to the scores of every query: log(size) of merged tokens, or a mask (-inf,
+                                or the lowest finite value) */
+    float* lse;              /* optional DEVICE [q_tokens, q_heads] fp32: log of the sum of exp(score), -inf where no state is left */
+} luvc_attn_cross_opts;
+
+/*
+ * out[t, h, :] = sum_s p_s V[s] / sum_s p_s,  p_s = exp(scale * <q[t, h], K[s]> + key_bias[s]),
+ *
+ * for the tokens t of each of n sequences over all of its states s: the merged and pruned visual tokens that a text, or a set of learned
+ * queries, looks at.  States have no order that masks.  Query head h reads key head h / (q_heads / heads).
+ *
+ * q, out      [q_tokens, q_heads, D] of `dtype` (LUVC_BF16 or LUVC_F32); q_stride: elements from one token to the next (a token's
+ *             q_heads * D elements are contiguous); out is dense
+ * k, v        [k_tokens, heads, D], k_stride / v_stride the same (rows of a fused projection need no copy; of luvc_kv_read)
+ * q_starts    DEVICE [n + 1], ascending, 0 to q_tokens: sequence i has the tokens q_starts[i] .. q_starts[i+1]-1.  NULL: one token each
+ *             (q_tokens = n).  Rows of out (and lse) of no sequence are left as they are
+ * k_starts    DEVICE [n + 1], ascending, 0 to k_tokens: its states are k_starts[i] .. k_starts[i+1]-1
+ * A sequence without states, or whose states are all masked by -inf, gives rows of zeros; a state masked by -inf contributes nothing,
+ * whatever its rows hold.  Scores, softmax and sums are fp32; bf16: a weight enters its product with V rounded to bf16.  A call
+ * repeated gives the same bits; how the work is split, and with it the last bits, depends on all lengths of the call.  The call runs
+ * whatever the status word says.
+ * Limits: D a multiple of 8 (bf16) or 4 (fp32) up to 256; q_heads up to 65536, a multiple of heads; n up to 4096.
+ */
+int luvc_attn_cross(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride, int n,
+                    const int32_t* q_starts, const int32_t* k_starts, int q_tokens, int k_tokens, int q_heads, int heads, int D, int dtype,
+                    void* out, const luvc_attn_cross_opts* opts);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,7 @@ EXPORTS = (
     "luvc_spu_prune_f32", "luvc_spu_prune_ex", "luvc_spu_prune_host", "luvc_spu_prune_static", "luvc_spu_static_status",
     "luvc_spu_cascade", "luvc_kv_workspace_bytes", "luvc_kv_reserve", "luvc_kv_write", "luvc_kv_fork", "luvc_kv_free",
     "luvc_kv_compact", "luvc_attn_workspace_bytes", "luvc_attn_decode", "luvc_rope", "luvc_kv_read",
+    "luvc_attn_cross_workspace_bytes", "luvc_attn_cross",
 )
 
 
@@ -94,6 +95,13 @@ class AttnOpts(ctypes.Structure):
     ]
 
 
+class AttnCrossOpts(ctypes.Structure):
+    _fields_ = [
+        ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("device_status", ctypes.c_void_p), ("scale", ctypes.c_float), ("key_bias", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     path = _build.LIB
     if _build.is_stale():
@@ -147,6 +155,9 @@ def _load() -> ctypes.CDLL:
     L.luvc_attn_workspace_bytes.restype = sz
     L.luvc_attn_workspace_bytes.argtypes = []
     L.luvc_attn_decode.argtypes = [p, ll, cache, i, p, i, i, i, p, ctypes.POINTER(AttnOpts)]
+    L.luvc_attn_cross_workspace_bytes.restype = sz
+    L.luvc_attn_cross_workspace_bytes.argtypes = []
+    L.luvc_attn_cross.argtypes = [p, ll, p, ll, p, ll, i, p, p, i, i, i, i, i, i, p, ctypes.POINTER(AttnCrossOpts)]
     L.luvc_rope.argtypes = [p, ll, p, p, i, i, i, i, i, p, ll, ctypes.POINTER(RopeOpts)]
     return L
 
@@ -477,22 +488,22 @@ def _ints(t: torch.Tensor | None, cache: KvCache, count: int, name: str):
     return t.data_ptr()
 
 
-def _buffers(o, cache: KvCache, workspace, device_status) -> None:
+def _buffers(o, index: int, workspace, device_status) -> None:
     """Enters a caller's workspace and status block (None: the library's) into the options."""
     if workspace is not None:
-        if workspace.get_device() != cache.index or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on %s" % cache.device)
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on cuda:%d" % index)
         o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if device_status is not None:
-        if device_status.dtype is not _INT32 or device_status.numel() < 4 or device_status.get_device() != cache.index \
+        if device_status.dtype is not _INT32 or device_status.numel() < 4 or device_status.get_device() != index \
                 or not device_status.is_contiguous():
-            raise ValueError("device_status must be a contiguous int32 tensor of 4 entries at least on %s" % cache.device)
+            raise ValueError("device_status must be a contiguous int32 tensor of 4 entries at least on cuda:%d" % index)
         o.device_status = device_status.data_ptr()
 
 
 def _kv_opts(cache: KvCache, workspace, device_status) -> KvOpts:
     o = KvOpts(_raw_stream(cache.index))
-    _buffers(o, cache, workspace, device_status)
+    _buffers(o, cache.index, workspace, device_status)
     return o
 
 
@@ -615,7 +626,7 @@ def attn_decode(q: torch.Tensor, cache: KvCache, *, layer: int = 0, seqs: torch.
     o = AttnOpts(_raw_stream(cache.index))
     if scale:
         o.scale = scale
-    _buffers(o, cache, workspace, device_status)
+    _buffers(o, cache.index, workspace, device_status)
     if key_bias is not None:
         if key_bias.dtype is not torch.float32 or key_bias.dim() != 2 or key_bias.shape[0] != n \
                 or key_bias.get_device() != cache.index or (key_bias.shape[1] > 1 and key_bias.stride(1) != 1):
@@ -702,3 +713,63 @@ def rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, *, axis:
     _call_on(index, lib.luvc_rope, x.data_ptr(), stride(x, "x"), positions.data_ptr(), freqs.data_ptr(), tokens, heads, D,
              2 * freqs.numel(), code, out.data_ptr(), stride(out, "out"), o)
     return out
+
+
+# ---- attention to an encoder's states --------------------------------------------------------------
+
+
+def attn_cross_workspace_bytes() -> int:
+    """Bytes a caller's workspace for attn_cross must have (256-byte aligned, zeroed before its first use; one per stream)."""
+    return int(lib.luvc_attn_cross_workspace_bytes())
+
+
+def attn_cross(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, k_starts: torch.Tensor, q_starts: torch.Tensor | None = None,
+               scale: float = 0.0, key_bias: torch.Tensor | None = None, want_lse: bool = False, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None, device_status: torch.Tensor | None = None):
+    """luvc_attn_cross: attention of the tokens q [q_tokens, q_heads, D] of n sequences to their states k, v [k_tokens, heads, D] (bfloat16
+    or float32; all three may be parts of wider tensors whose tokens are contiguous), without a causal mask.
+    q_starts, k_starts: int32 [n+1], sequence i has the tokens q_starts[i] .. q_starts[i+1]-1 (None: one each) and the states
+    k_starts[i] .. k_starts[i+1]-1; key_bias: float32 [k_tokens], added to the scores; scale 0: 1/sqrt(D).
+    workspace: None, the library's own, which calls on other streams must not use at the same time, or attn_cross_workspace_bytes()
+    zeroed bytes.  Returns out [q_tokens, q_heads, D] and, with want_lse, the log-sum-exp of the scores [q_tokens, q_heads] float32."""
+    code = _dtype_code(q)
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("q must be [q_tokens, q_heads, D], k and v [k_tokens, heads, D]")
+    index = q.get_device()
+    q_tokens, q_heads, D = q.shape
+    k_tokens, heads, _ = k.shape
+    strides = []
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if not t.is_cuda or t.get_device() != index:
+            raise ValueError("q, k and v must live on one CUDA device")
+        if t.dtype is not q.dtype:
+            raise TypeError("%s must be %s, got %s" % (name, q.dtype, t.dtype))
+        s0, s1, s2 = t.stride()
+        if (s2 != 1 and D > 1) or (s1 != D and t.shape[1] > 1):
+            raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
+        strides.append(s0 if t.shape[0] > 1 else t.shape[1] * D)        # the stride of a lone token is not used
+    n = q_tokens if q_starts is None else q_starts.numel() - 1
+    for t, name in ((q_starts, "q_starts"), (k_starts, "k_starts")):
+        if t is not None and (t.dtype is not _INT32 or t.dim() != 1 or t.numel() != n + 1 or t.get_device() != index or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous int32 tensor of %d entries on q's device" % (name, n + 1))
+    if key_bias is not None and (key_bias.dtype is not torch.float32 or key_bias.shape != (k_tokens,) or key_bias.get_device() != index
+                                 or not key_bias.is_contiguous()):
+        raise ValueError("key_bias must be a contiguous float32 tensor [k_tokens] on q's device")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_contiguous() or out.device != q.device:
+        raise ValueError("out must be a contiguous tensor of q's shape and type")
+    o = AttnCrossOpts(_raw_stream(index))
+    if scale:
+        o.scale = scale
+    _buffers(o, index, workspace, device_status)
+    if key_bias is not None:
+        o.key_bias = key_bias.data_ptr()
+    lse = None
+    if want_lse:
+        lse = torch.empty((q_tokens, q_heads), dtype=torch.float32, device=q.device)
+        o.lse = lse.data_ptr()
+    _call_on(index, lib.luvc_attn_cross, q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], n,
+             q_starts.data_ptr() if q_starts is not None else None, k_starts.data_ptr(), q_tokens, k_tokens, q_heads, heads, D, code,
+             out.data_ptr(), o)
+    return (out, lse) if want_lse else out

@@ -56,7 +56,7 @@ thread_local cudaStream_t t_stream = nullptr;
 // Library-owned scratch: one growing buffer per purpose and per device (keyed by the ordinal of the
 // device that is current at the call), shared by all threads and streams of the process.  Calls
 // whose GPU work overlaps race on it (documented in luvc.h); the lock only covers (re)allocation.
-enum Slot { kOimWs = 0, kSpuWs, kIoIn, kIoOut, kStatus, kCascade, kIoInSpu, kIoOutSpu, kKvWs, kAttnWs, kSlots };
+enum Slot { kOimWs = 0, kSpuWs, kIoIn, kIoOut, kStatus, kCascade, kIoInSpu, kIoOutSpu, kKvWs, kAttnWs, kCrossWs, kSlots };
 constexpr int kMaxDevices = 64;
 struct Scratch { void* ptr = nullptr; size_t bytes = 0; };
 Scratch g_scratch[kMaxDevices][kSlots];
@@ -125,6 +125,7 @@ void* zeroed_scratch(Slot s, size_t bytes) {
 // The current device's status block, and its attention workspace (which the kernel leaves zeroed where it must be).
 int* status_word() { return static_cast<int*>(zeroed_scratch(kStatus, 256)); }
 void* attn_scratch() { return zeroed_scratch(kAttnWs, attn_workspace_bytes()); }
+void* cross_scratch() { return zeroed_scratch(kCrossWs, attn_cross_workspace_bytes()); }
 
 // Reads (after synchronising the stream) and clears the first word of a status block.
 int read_status_block(int* block, cudaStream_t stream) {
@@ -756,6 +757,40 @@ int luvc_attn_decode(const void* q, long long q_stride, const luvc_kv_cache* cac
     p.scale = o.scale != 0.f ? o.scale : 1.f / std::sqrt((float)cache->D);
     p.stream = static_cast<cudaStream_t>(o.stream);
     return attn_decode(p);
+}
+
+// ---- attention to an encoder's states ----------------------------------------------
+
+size_t luvc_attn_cross_workspace_bytes(void) { return attn_cross_workspace_bytes(); }
+
+int luvc_attn_cross(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride, int n,
+                    const int32_t* q_starts, const int32_t* k_starts, int q_tokens, int k_tokens, int q_heads, int heads, int D, int dtype,
+                    void* out, const luvc_attn_cross_opts* opts) {
+    const luvc_attn_cross_opts o = opts ? *opts : luvc_attn_cross_opts{};
+    if (!k_starts || ((!q || !out) && q_tokens > 0) || ((!k || !v) && k_tokens > 0)) return LUVC_ERR_NULL;
+    if (dtype != LUVC_BF16 && dtype != LUVC_F32) return LUVC_ERR_DTYPE;
+    if (n < 1 || n > kKvMaxSeqs || q_tokens < 0 || k_tokens < 0 || (!q_starts && q_tokens != n) || heads < 1 || q_heads < 1 || q_heads > 65536 ||
+        q_heads % heads || D < 1 || D > 256 || q_stride < (long long)q_heads * D || k_stride < (long long)heads * D ||
+        v_stride < (long long)heads * D || !std::isfinite(o.scale))
+        return LUVC_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if ((D * es) % 16 || (q_stride * es) % 16 || (k_stride * es) % 16 || (v_stride * es) % 16 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
+        !aligned16(out) || !aligned4(q_starts) || !aligned4(k_starts) || !aligned4(o.key_bias) || !aligned4(o.lse) ||
+        (o.device_status && !aligned16(o.device_status)))
+        return LUVC_ERR_ALIGN;
+    CrossProblem p;
+    p.workspace = o.workspace;
+    if (p.workspace && (o.workspace_bytes < attn_cross_workspace_bytes() || (reinterpret_cast<uintptr_t>(p.workspace) & 255u))) return LUVC_ERR_WORKSPACE;
+    if (q_tokens == 0) return LUVC_OK;
+    if (!p.workspace && !(p.workspace = cross_scratch())) return LUVC_ERR_CUDA;
+    p.status = o.device_status ? o.device_status : status_word();
+    if (!p.status) return LUVC_ERR_CUDA;
+    p.q = q; p.k = k; p.v = v; p.out = out; p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+    p.q_starts = q_starts; p.k_starts = k_starts; p.bias = o.key_bias; p.lse = o.lse; p.n = n; p.q_tokens = q_tokens; p.k_tokens = k_tokens;
+    p.q_heads = q_heads; p.heads = heads; p.D = D; p.dtype = dtype;
+    p.scale = o.scale != 0.f ? o.scale : 1.f / std::sqrt((float)D);
+    p.stream = static_cast<cudaStream_t>(o.stream);
+    return attn_cross(p);
 }
 
 }  // extern "C"

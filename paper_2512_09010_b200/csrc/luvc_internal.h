@@ -235,6 +235,24 @@ struct AttnProblem {
 size_t attn_workspace_bytes();
 int attn_decode(const AttnProblem& p);
 
+// ---- attention to an encoder's states (attn_cross.cu) ----------------------------------------------
+
+struct CrossProblem {
+    const void *q, *k, *v;
+    void* out;
+    long long q_stride, k_stride, v_stride;
+    const int32_t *q_starts, *k_starts;
+    const float* bias;
+    float* lse;
+    int n, q_tokens, k_tokens, q_heads, heads, D, dtype;
+    float scale;
+    void* workspace;
+    int* status;
+    cudaStream_t stream;
+};
+size_t attn_cross_workspace_bytes();
+int attn_cross(const CrossProblem& p);
+
 // ---- rotary positions (rope.cu) ---------------------------------------------------------------------
 
 struct RopeProblem {
