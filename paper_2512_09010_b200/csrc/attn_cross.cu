@@ -8,9 +8,10 @@
 // Rows.  The query heads of a key head see the same states, so a row of the products is a (token, query head) pair: all rows of a key head
 // lie one after another, and a tile of 128 of them is one operand, whether it is 128 tokens of one head or one token of seven.
 //
-// Split.  The work is the list of all (sequence, key head, block of rows, tile of states); each CTA, one per SM, takes an equal part of it, whatever
-// the lengths.  What a CTA has of a (sequence, key head, block of rows) that others share goes through the workspace; the CTA that comes last
-// adds the parts, in the order of the list, so that a repeated call gives the same bits.
+// Split.  The work is the list of all (sequence, key head, block of rows, tile of states); each CTA takes an equal part of it, whatever the
+// lengths.  What a CTA has of a (sequence, key head, block of rows) that others share goes through the workspace; the CTA that comes last
+// adds the parts, in the order of the list, so that a repeated call gives the same bits.  Where there is little to do, the parts are whole
+// (sequence, key head, block of rows)s: a join costs as much as some tiles (kJoin).
 //
 // bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums.
 
@@ -20,6 +21,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "luvc_internal.h"
 #include "sm100_ptx.cuh"
@@ -30,22 +32,23 @@ namespace {
 using namespace ptx;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kMaxCtas = 160;                       // CTAs the workspace has room for
-constexpr int kPartFloats = 256 * 130;              // of a partial result: rows of sums, and their (m, l)
-constexpr size_t kCounterBytes = 1024;
+constexpr int kMaxCtas = 320;                       // CTAs there are counters for
+constexpr size_t kCounterBytes = 2048, kPartsBytes = (size_t)160 * 2 * 256 * 130 * sizeof(float);      // 160 CTAs' parts of 256 rows of 128 columns
 static_assert(kMaxCtas * sizeof(unsigned) <= kCounterBytes, "room for the counters");
+constexpr int kJoin = 8;                            // tiles that a join costs as much as
 constexpr int kWaitProbes = 1 << 20;                // probes before a wait gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;               // and with a limit from the status block (a test's)
 
 struct CrossArgs {
     CrossProblem p;
     int group;                                      // query heads per key head
+    int block;                                      // rows of a block
     // Scores are c <q, k> + bias, weights 2^(unit (score - m)), and a score is worth nat in natural units: with biases c = |scale|, unit = log2(e),
     // nat = 1 (a bias of the lowest value times log2(e) would not be finite), without c = |scale| log2(e), unit = 1, nat = ln(2).
     float c, unit, nat;
     float sign;                                     // of the scale; c has its magnitude
     unsigned* counters;                             // [kMaxCtas] arrivals of parts, by the CTA an item begins in
-    float* parts;                                   // [kMaxCtas][2][kPartFloats]
+    float* parts;                                   // two for each CTA
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -53,11 +56,26 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&d);
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     unsigned long long d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d)
         : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)), "l"(*reinterpret_cast<unsigned long long*>(&c)));
     return *reinterpret_cast<float2*>(&d);
+}
+
+// a / b of numbers >= 0: 32 bits where they do (a division of 64 bits takes a tenth of a microsecond).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
 }
 
 // ---- the list of work -----------------------------------------------------------------------------------------------
@@ -71,10 +89,11 @@ struct Item {
     long long first;                                // its first tile's place in the list
 };
 
-template <int BM, int BN>
+template <int BN>
 struct Work {
     const CrossArgs& a;
     long long at = 0, end = 0, per = 0;             // this CTA's part of the list
+    bool whole = false;                             // the list is of blocks, not of tiles
     int seq = 0, head = 0, rb = 0, kb = 0;
     int q0 = 0, qlen = 0, k0 = 0, klen = 0, rbs = 0, kbs = 0;
 
@@ -87,13 +106,9 @@ struct Work {
         k0 = clamped(p.k_starts[i], p.k_tokens);
         klen = max(clamped(p.k_starts[i + 1], p.k_tokens) - k0, 0);
     }
-    __device__ int blocks_of(int qlen) const { return (int)(((long long)qlen * a.group + BM - 1) / BM); }
+    __device__ int blocks_of(int qlen) const { return (int)quotient((long long)qlen * a.group + a.block - 1, a.block); }
     __device__ int tiles_of(int klen) const { return (int)(((long long)klen + BN - 1) / BN); }
-    __device__ long long units(int i) const {
-        int q0, qlen, k0, klen;
-        lengths(i, q0, qlen, k0, klen);
-        return (long long)a.p.heads * blocks_of(qlen) * tiles_of(klen);
-    }
+    __device__ int steps() const { return whole ? min(kbs, 1) : kbs; }          // of the list, of a block
     __device__ void enter(int i) {
         seq = i;
         lengths(i, q0, qlen, k0, klen);
@@ -103,53 +118,73 @@ struct Work {
     // This CTA's part; all NT threads of the CTA call it.
     template <int NT>
     __device__ void begin() {
-        __shared__ long long sums[NT / 32 + 1], found_base;
-        __shared__ int found;
+        constexpr int NW = NT / 32;
+        __shared__ long long sums[NW], blocks[NW], found_in;
+        __shared__ int most[NW], found;
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.p.n;
-        long long mine = 0;
-        for (int i = tid; i < n; i += NT) mine += units(i);
+        // tiles and blocks of NT sequences at a time, and of those before them
+        long long tiles_before = 0, blocks_before = 0, tiles, blocks_mine, total = 0, all_blocks = 0;
+        int longest = 0;
+        auto scan = [&](int i) {
+            int q0, qlen = 0, k0, klen = 0;
+            if (i < n) lengths(i, q0, qlen, k0, klen);
+            const int t = tiles_of(klen);
+            blocks_mine = t ? (long long)a.p.heads * blocks_of(qlen) : 0;
+            tiles = blocks_mine * t;
+            tiles_before = tiles; blocks_before = blocks_mine;
 #pragma unroll
-        for (int d = 16; d; d >>= 1) mine += __shfl_xor_sync(~0u, mine, d);
-        if (lane == 0) sums[warp] = mine;
-        if (tid == 0) found = -1;
-        __syncthreads();
-        long long total = 0;
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long x = __shfl_up_sync(~0u, tiles_before, d), y = __shfl_up_sync(~0u, blocks_before, d);
+                if (lane >= d) { tiles_before += x; blocks_before += y; }
+            }
+            const int m = __reduce_max_sync(~0u, blocks_mine ? t : 0);
+            if (lane == 31) { sums[warp] = tiles_before; blocks[warp] = blocks_before; most[warp] = m; }
+            __syncthreads();
+            tiles_before += total - tiles;
+            blocks_before += all_blocks - blocks_mine;
 #pragma unroll
-        for (int w = 0; w < NT / 32; ++w) total += sums[w];
-        per = (total + gridDim.x - 1) / gridDim.x;
+            for (int w = 0; w < NW; ++w) {
+                if (w < warp) { tiles_before += sums[w]; blocks_before += blocks[w]; }
+                total += sums[w];
+                all_blocks += blocks[w];
+                longest = max(longest, most[w]);
+            }
+        };
+        scan(tid);
+        for (int i0 = NT; i0 < n; i0 += NT) {
+            __syncthreads();                        // the sums have been read
+            scan(i0 + tid);
+        }
+        per = quotient(total + gridDim.x - 1, gridDim.x);
+        const long long rounds = quotient(all_blocks + gridDim.x - 1, gridDim.x);
+        whole = rounds * longest <= per + kJoin;
+        if (whole) { total = all_blocks; per = rounds; }
         at = min(total, per * blockIdx.x);
         end = min(total, at + per);
         if (at < end) {                             // (the same in all threads)
-            long long base = 0;
-            for (int i0 = 0; i0 < n && base <= at; i0 += NT) {
-                const long long x = i0 + tid < n ? units(i0 + tid) : 0;
-                long long upto = x;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const long long y = __shfl_up_sync(~0u, upto, d);
-                    if (lane >= d) upto += y;
+            auto look = [&](int i) {
+                const long long before = whole ? blocks_before : tiles_before, x = whole ? blocks_mine : tiles;
+                if (before <= at && at < before + x) {
+                    found = i;
+                    found_in = at - before;
                 }
-                __syncthreads();                    // the sums have been read
-                if (lane == 31) sums[warp] = upto;
-                __syncthreads();
-                long long before = base, all = base;
-#pragma unroll
-                for (int w = 0; w < NT / 32; ++w) {
-                    if (w < warp) before += sums[w];
-                    all += sums[w];
+            };
+            if (n <= NT) {
+                look(tid);
+            } else {
+                total = all_blocks = 0;
+                for (int i0 = 0; i0 < n && (whole ? all_blocks : total) <= at; i0 += NT) {
+                    __syncthreads();
+                    scan(i0 + tid);
+                    look(i0 + tid);
                 }
-                if (before + upto - x <= at && at < before + upto) {
-                    found = i0 + tid;
-                    found_base = before + upto - x;
-                }
-                base = all;
             }
             __syncthreads();
             enter(found);
-            const long long in = at - found_base, per_head = (long long)rbs * kbs;
-            head = (int)(in / per_head);
-            rb = (int)((in - head * per_head) / kbs);
-            kb = (int)(in % kbs);
+            const long long in = found_in, per_head = (long long)rbs * steps();
+            head = (int)quotient(in, per_head);
+            rb = (int)quotient(in - head * per_head, steps());
+            kb = whole ? 0 : (int)(in - head * per_head - (long long)rb * kbs);
         }
     }
     __device__ bool more() const { return at < end; }
@@ -157,12 +192,12 @@ struct Work {
     __device__ Item next() {
         Item it;
         it.seq = seq; it.head = head; it.rb = rb; it.kb = kb; it.kbs = kbs;
-        it.count = (int)min((long long)(kbs - kb), end - at);
+        it.count = whole ? kbs : (int)min((long long)(kbs - kb), end - at);
         it.q0 = q0;
-        it.rows = (int)min((long long)qlen * a.group - (long long)rb * BM, (long long)BM);
+        it.rows = (int)min((long long)qlen * a.group - (long long)rb * a.block, (long long)a.block);
         it.k0 = k0; it.klen = klen;
         it.first = at - kb;
-        at += it.count;
+        at += whole ? 1 : it.count;
         kb += it.count;
         if (kb == kbs && at < end) {
             kb = 0;
@@ -178,8 +213,8 @@ struct Work {
     }
     // Element of q and of out of a row's first column (in units of tokens' rows: see row_of).
     __device__ static long long token_of(const CrossArgs& a, const Item& it, int r, int& h) {
-        const long long row = (long long)it.rb * BM + r;
-        const long long t = row / a.group;
+        const long long row = (long long)it.rb * a.block + r;
+        const long long t = quotient(row, a.group);
         h = it.head * a.group + (int)(row - t * a.group);
         return it.q0 + t;
     }
@@ -194,8 +229,8 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
 __device__ __forceinline__ float lse_of(const CrossArgs& a, float m, float l) { return l == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.nat, logf(l)); }
 
 // Sequences without states: rows of zeros.
-template <typename T, int BM, int BN, int NT>
-__device__ void empty_sequences(const CrossArgs& a, const Work<BM, BN>& w) {
+template <typename T, int BN, int NT>
+__device__ void empty_sequences(const CrossArgs& a, const Work<BN>& w) {
     for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
         int q0, qlen, k0, klen;
         w.lengths(i, q0, qlen, k0, klen);
@@ -211,12 +246,12 @@ __device__ void empty_sequences(const CrossArgs& a, const Work<BM, BN>& w) {
 // A partial result in the workspace: four columns of a row at o[column / 4 * BM + row], (m, l) of each row.
 template <int BM, int DP>
 struct Part {
+    static constexpr size_t BYTES = BM * (DP + 2) * sizeof(float);
     float4* o;
     float2* ml;
     __device__ Part(const CrossArgs& a, int cta, int slot) {
-        o = reinterpret_cast<float4*>(a.parts + ((size_t)cta * 2 + slot) * kPartFloats);
+        o = reinterpret_cast<float4*>(a.parts + ((size_t)cta * 2 + slot) * (BM * (DP + 2)));
         ml = reinterpret_cast<float2*>(o + BM * (DP / 4));
-        static_assert(BM * (DP + 2) <= kPartFloats, "a part must fit");
     }
 };
 
@@ -227,51 +262,77 @@ __device__ __forceinline__ bool arrive(unsigned* counter, int i, int n) {
     return atomicAdd(counter, x) + x == 0u;
 }
 
-// Adds the parts of an item, which CTAs c0 .. c1 have written, in order, and writes the result.  NT threads.
+// Adds the parts of an item, which CTAs c0 .. c1 have written, in order, and writes the result.  NT threads; each has E groups of four columns
+// at a time, and the parts of all of them on their way.
 template <typename T, int BM, int BN, int DP, int NT>
 __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, int tid) {
-    const int cols = a.p.D / 4;
-    for (int e = tid; e < it.rows * cols; e += NT) {
-        const int r = e % it.rows, c = e / it.rows;
-        float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = c0; k0 <= c1; k0 += 8) {
-            float4 x[8];
-            float2 ml[8];
+    constexpr int E = 4, B = 4;                                 // groups of columns; parts at a time
+    const int all = it.rows * (a.p.D / 4);
+    for (int e0 = tid; e0 < all; e0 += E * NT) {
+        int r[E], c[E];
+        float m[E], l[E];
+        float4 o[E];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {                       // past the last part: that one again, not used
-                const int cta = min(k0 + k, c1);
-                const Part<BM, DP> q(a, cta, cta == c0);
-                ml[k] = __ldcg(q.ml + r);
-                x[k] = __ldcg(q.o + c * BM + r);
-            }
-            float top = m;
+        for (int e = 0; e < E; ++e) {                           // past the last group: that one again, not written
+            const int x = min(e0 + e * NT, all - 1);
+            c[e] = x / it.rows;
+            r[e] = x - c[e] * it.rows;
+            m[e] = -INFINITY;
+            l[e] = 0.f;
+            o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        for (int k0 = c0; k0 <= c1; k0 += B) {
+            float4 x[E][B];
+            float2 ml[E][B];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
-            // o is the mean so far: values near the end of the range stay inside it
-            const float base = top == -INFINITY ? 0.f : top, had = l * exp2_fast((m - base) * a.unit);
-            m = top;
-            l = had;
-            float w[8];
+            for (int k = 0; k < B; ++k)
+                if (k0 + k <= c1) {
+                    const Part<BM, DP> q(a, k0 + k, k0 + k == c0);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                w[k] = k0 + k > c1 ? 0.f : exp2_fast((ml[k].x - base) * a.unit);
-                l = fmaf(w[k], ml[k].y, l);
-            }
-            const float inv = l == 0.f ? 0.f : 1.f / l, f = had * inv;
-            o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+                    for (int e = 0; e < E; ++e) {
+                        ml[e][k] = __ldcg(q.ml + r[e]);
+                        x[e][k] = __ldcg(q.o + c[e] * BM + r[e]);
+                    }
+                } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (k0 + k > c1) continue;
-                const float by = w[k] * inv;
-                o.x = fmaf(by, x[k].x, o.x); o.y = fmaf(by, x[k].y, o.y);
-                o.z = fmaf(by, x[k].z, o.z); o.w = fmaf(by, x[k].w, o.w);
+                    for (int e = 0; e < E; ++e) {
+                        ml[e][k] = make_float2(-INFINITY, 0.f);
+                        x[e][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float top = m[e];
+#pragma unroll
+                for (int k = 0; k < B; ++k) top = fmaxf(top, ml[e][k].x);
+                // o is the mean so far: values near the end of the range stay inside it
+                const float base = top == -INFINITY ? 0.f : top, had = l[e] * exp2_fast((m[e] - base) * a.unit);
+                m[e] = top;
+                l[e] = had;
+                float w[B];
+#pragma unroll
+                for (int k = 0; k < B; ++k) {
+                    w[k] = exp2_fast((ml[e][k].x - base) * a.unit);
+                    l[e] = fmaf(w[k], ml[e][k].y, l[e]);
+                }
+                const float inv = l[e] == 0.f ? 0.f : 1.f / l[e], f = had * inv;
+                o[e].x *= f; o[e].y *= f; o[e].z *= f; o[e].w *= f;
+#pragma unroll
+                for (int k = 0; k < B; ++k) {
+                    const float by = w[k] * inv;
+                    o[e].x = fmaf(by, x[e][k].x, o[e].x); o[e].y = fmaf(by, x[e][k].y, o[e].y);
+                    o[e].z = fmaf(by, x[e][k].z, o[e].z); o[e].w = fmaf(by, x[e][k].w, o[e].w);
+                }
             }
         }
-        int h;
-        const long long row = Work<BM, BN>::token_of(a, it, r, h) * a.p.q_heads + h;
-        put4(static_cast<T*>(a.p.out) + row * a.p.D + 4 * c, l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : o);
-        if (c == 0 && a.p.lse) a.p.lse[row] = lse_of(a, m, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (e0 + e * NT >= all) continue;
+            int h;
+            const long long row = Work<BN>::token_of(a, it, r[e], h) * a.p.q_heads + h;
+            put4(static_cast<T*>(a.p.out) + row * a.p.D + 4 * c[e], l[e] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : o[e]);
+            if (c[e] == 0 && a.p.lse) a.p.lse[row] = lse_of(a, m[e], l[e]);
+        }
     }
 }
 
@@ -283,10 +344,11 @@ template <int BM, int DP>
 struct Cores {
     static constexpr int BN = 64, NT = 256, RT = BM / 16, LD = DP + 4, LP = BN + 4;
     static constexpr size_t SMEM = (size_t)(BM * LD + BN * LD + BN * DP + BM * LP) * sizeof(float);
+    static constexpr int CTAS = DP <= 128 ? 2 : 1;              // of an SM
 };
 
 template <int BM, int DP>
-__global__ void __launch_bounds__(256) attn_cross_f32(const __grid_constant__ CrossArgs a) {
+__global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const __grid_constant__ CrossArgs a) {
     using C = Cores<BM, DP>;
     constexpr int BN = C::BN, NT = C::NT, RT = C::RT, LD = C::LD, LP = C::LP, CG = DP / 64;
     extern __shared__ __align__(16) float smem[];
@@ -300,9 +362,9 @@ __global__ void __launch_bounds__(256) attn_cross_f32(const __grid_constant__ Cr
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, D = p.D;
     pdl_trigger();
     pdl_wait();
-    Work<BM, BN> work(a);
+    Work<BN> work(a);
     work.template begin<NT>();
-    empty_sequences<float, BM, BN, NT>(a, work);
+    empty_sequences<float, BN, NT>(a, work);
     for (int e = tid; e < (BM + BN) * (LD / 4); e += NT) reinterpret_cast<float4*>(qs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);   // columns past D
     for (int e = tid; e < BN * (DP / 4); e += NT) reinterpret_cast<float4*>(vs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
     while (work.more()) {
@@ -324,7 +386,7 @@ __global__ void __launch_bounds__(256) attn_cross_f32(const __grid_constant__ Cr
         for (int e = tid; e < it.rows * (D / 4); e += NT) {
             const int r = e / (D / 4), c = e - r * (D / 4);
             int h;
-            const long long t = Work<BM, BN>::token_of(a, it, r, h);
+            const long long t = Work<BN>::token_of(a, it, r, h);
             const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + t * p.q_stride + (long long)h * D + 4 * c);
             *reinterpret_cast<float4*>(qs + r * LD + 4 * c) = make_float4(x.x * a.sign, x.y * a.sign, x.z * a.sign, x.w * a.sign);
         }
@@ -436,7 +498,7 @@ __global__ void __launch_bounds__(256) attn_cross_f32(const __grid_constant__ Cr
             const int row = ty * RT + r;
             if (row >= it.rows) continue;
             int h;
-            const long long at = Work<BM, BN>::token_of(a, it, row, h) * p.q_heads + h;
+            const long long at = Work<BN>::token_of(a, it, row, h) * p.q_heads + h;
             const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
             for (int g = 0; g < CG; ++g) {
@@ -468,7 +530,7 @@ __global__ void __launch_bounds__(256) attn_cross_f32(const __grid_constant__ Cr
 // ---- bf16 on the tensor cores -----------------------------------------------------------------------------------------
 
 // DP: columns of a row in shared memory (D, rounded up to 64, 128 or 256).  A CTA has TILES tiles of 128 rows, each with four warps that take
-// its weights (a thread has a row), a warp that issues the products and one that brings K and V by TMA.
+// its weights (a thread has a row) and one that issues its products; another one brings K and V by TMA.
 //
 // S = Q K^T lands in tensor memory, the threads read it, and leave the weights, in bf16, in its place, from where they are the first operand of
 // O += P V.  While one tile's weights are worked out, the other tile's products run.  Where there are no more than 128 rows both tiles have
@@ -481,13 +543,16 @@ template <int DP_>
 struct Tc {
     static constexpr int DP = DP_, TILES = DP <= 128 ? 2 : 1, BN = DP <= 128 ? 128 : 64, ROWS = 128 * TILES;
     static constexpr int Q_BYTES = 128 * DP * 2, STAGE = BN * DP * 2, STAGES = DP == 64 ? 8 : 5;
-    static constexpr int THREADS = 320, S_COLS = 128, O_COL = 256, O_COLS = DP <= 128 ? 128 : 256;
+    static constexpr int THREADS = 384, S_COLS = 128, O_COL = 256, O_COLS = DP <= 128 ? 128 : 256;
     static constexpr size_t SMEM = 1024 + TILES * Q_BYTES + STAGES * STAGE;
+    // registers of the threads that have weights, and of the others: together what the launch has, 384 times 168
+    static constexpr int MANY = 208, FEW = 80;
+    static_assert(256 * MANY + 128 * FEW <= THREADS * 168, "more registers than the launch has");
     static_assert(TILES == 1 || 2 * Q_BYTES >= 128 * DP * 4, "a tile's result fits the queries' place");
 };
 
-// The reference of the weights may lag behind the maximum by this much (in powers of two).
-constexpr float kLag = 8.f;
+// Largest sum of a tile's weights before their reference follows the maximum: sums of values up to 2^80 stay in range.
+constexpr float kMost = 0x1p40f;
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -499,11 +564,6 @@ __device__ __forceinline__ void tmem_ld_wait32(uint32_t (&v)[32]) {
                    "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]),
                    "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                 ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-                   "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
                  "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
@@ -511,6 +571,16 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&v)[32]
                    "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
                    "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
+// The same, and whether any of the threads says yes.
+__device__ __forceinline__ bool named_barrier_or(int id, int threads, bool yes) {
+    int any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %3, 0;\n\tbar.red.or.pred q, %1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"(id), "r"(threads), "r"((int)yes) : "memory");
+    return any != 0;
+}
+// Registers of this warpgroup's threads from here on (all four warps call it).
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // Waits for a phase of a barrier.  When one wait of a CTA gives up, all others do at once: what follows runs through without waiting, so that
@@ -532,15 +602,15 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, int parity, volatile in
 }
 
 // A row of an item once more, by a warp, product by product as the formula has them.  An infinity among the values meets weights that bf16 has
-// rounded to 0, and weights above 1, while their reference lags behind, can take values beyond the end of the range; so a
+// rounded to 0, and weights above 1, while their reference lags behind, can take large values beyond the end of the range; so a
 // row that is not finite is worked out again.  It is rare, and need not be fast.
 template <int DP>
-__device__ __noinline__ void plain_row(const CrossArgs& a, const Item& it, int r) {
+__device__ __forceinline__ void plain_row(const CrossArgs& a, const Item& it, int r) {
     constexpr int ROWS = Tc<DP>::ROWS, BN = Tc<DP>::BN;
     const CrossProblem& p = a.p;
     const int lane = threadIdx.x & 31, D = p.D;
     int h;
-    const long long t = Work<ROWS, BN>::token_of(a, it, r, h), row = t * p.q_heads + h;
+    const long long t = Work<BN>::token_of(a, it, r, h), row = t * p.q_heads + h;
     const __nv_bfloat16* const qr = static_cast<const __nv_bfloat16*>(p.q) + t * p.q_stride + (long long)h * D;
     float q[DP / 32], o[DP / 32], m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -598,7 +668,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     using T = Tc<DP>;
     constexpr int TILES = T::TILES, BN = T::BN, ROWS = T::ROWS, STAGES = T::STAGES, CH = BN / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[8 + 2 * STAGES + 1];
+    __shared__ __align__(8) uint64_t bars[8 + 2 * STAGES + 4];
     __shared__ __align__(16) float sb[2][128];                  // biases of a tile of states, for each tile of rows; (m, l) of the second one
     __shared__ uint32_t tmem_at;
     __shared__ int dead_flag, last;
@@ -613,6 +683,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     auto kv_full = [&](int s) { return bar0 + 64 + 8 * s; };
     auto kv_free = [&](int s) { return bar0 + 64 + 8 * (STAGES + s); };
     const uint32_t drained = bar0 + 64 + 16 * STAGES;
+    auto turn = [&](int t) { return drained + 16 + 8 * t; };
     volatile int* const dead = &dead_flag;
     const int segs = (D + 63) / 64, ksteps = (D + 15) / 16;
 
@@ -626,9 +697,12 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
         }
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(kv_full(s), 1);
-            mbar_init(kv_free(s), 1);
+            mbar_init(kv_free(s), 2);                           // for both tiles of rows
         }
         mbar_init(drained, 1);
+        mbar_init(drained + 8, 1);
+        mbar_init(turn(0), 1);
+        mbar_init(turn(1), 1);
         mbar_fence_init();
         dead_flag = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
@@ -636,16 +710,17 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     }
     pdl_trigger();
     pdl_wait();
-    Work<ROWS, BN> work(a);
+    Work<BN> work(a);
     tc_fence_before();
     work.template begin<T::THREADS>();                          // (has barriers of all threads)
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    empty_sequences<__nv_bfloat16, ROWS, BN, T::THREADS>(a, work);
+    empty_sequences<__nv_bfloat16, BN, T::THREADS>(a, work);
 
-    if (warp == 8) {
+    if (warp >= 8) {
+        give_registers<T::FEW>();
         // ---- K and V, tile after tile, through a ring of stages ----
-        if (lane == 0) {
+        if (warp == 8 && lane == 0) {
             int pos = 0;                                        // K of the n-th tile of this CTA is 2 n, V 2 n + 1
             bool ok = true;
             while (ok && work.more()) {
@@ -666,98 +741,119 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             for (int x = max(0, pos - STAGES); x < pos; ++x)
                 for (int probes = 0; !mbar_try_wait(kv_full(x % STAGES), (x / STAGES) & 1) && *dead && probes < kLeastProbes; ++probes) {}
         }
-    } else if (warp == 9) {
-        // ---- products ----
-        const uint32_t idesc_s = make_idesc_bf16(128, BN, false, false), idesc_o = make_idesc_bf16(128, 16 * ksteps, false, true);
-        const uint64_t q0 = make_desc_layout(qs, 16, 1024, 2), k0 = make_desc_layout(ring, 16, 1024, 2), v0 = make_desc_layout(ring, BN * 128, 1024, 2);
-        auto wait = [&](uint32_t bar, int parity) {
+        // ---- products, a warp for each tile of rows ----
+        // (One warp for both takes 2450 cycles for the products of a tile of states with a tile of rows, half of them between the
+        // instructions; the products themselves take 1250.)
+        const int t = warp - 9;
+        if (t >= 0 && t < TILES) {
+            const uint32_t idesc_s = make_idesc_bf16(128, BN, false, false), idesc_o = make_idesc_bf16(128, 16 * ksteps, false, true);
+            const uint64_t q0 = make_desc_layout(qs, 16, 1024, 2), k0 = make_desc_layout(ring, 16, 1024, 2), v0 = make_desc_layout(ring, BN * 128, 1024, 2);
+            // What the loops run on is made the same in all lanes where the compiler can tell, so that descriptors stay in uniform registers: their
+            // lower halves, which hold the address, are handed out before each group of products.
+            auto same = [](int x) { return __shfl_sync(~0u, x, 0); };
+            auto desc = [](uint64_t of, uint32_t lower) { return (of >> 32 << 32) | lower; };
+            const uint32_t s_of = (uint32_t)same((int)tmem) + t * T::S_COLS, o_of = (uint32_t)same((int)tmem) + T::O_COL + t * T::O_COLS;
             bool ok = true;
-            if (lane == 0) ok = wait_phase(bar, parity, dead, p.status);
-            return (bool)__shfl_sync(~0u, (int)ok, 0);
-        };
-        auto full = [&](int pos) { return wait(kv_full(pos % STAGES), (pos / STAGES) & 1); };
-        auto scores = [&](int t, int q_tile, int pos) {         // S of tile t
-            if (elect_one()) {
-                const uint64_t q = q0 + ((uint32_t)(q_tile * T::Q_BYTES) >> 4), k = k0 + ((uint32_t)(pos % STAGES * T::STAGE) >> 4);
-                for (int x = 0; x < ksteps; ++x)
-                    umma_bf16(tmem + t * T::S_COLS, q + ((x >> 2) * (128 * 128) + (x & 3) * 32 >> 4), k + ((x >> 2) * (BN * 128) + (x & 3) * 32 >> 4), idesc_s, x ? 1u : 0u);
-                umma_commit(s_full(t));
-            }
-            __syncwarp();
-        };
-        auto values = [&](int t, int pos, bool first) {         // O of tile t
-            if (elect_one()) {
-                const uint64_t v = v0 + ((uint32_t)(pos % STAGES * T::STAGE) >> 4);
-#pragma unroll
-                for (int x = 0; x < BN / 16; ++x)
-                    umma_bf16_ts(tmem + T::O_COL + t * T::O_COLS, tmem + t * T::S_COLS + 8 * x, v + (2048 * x >> 4), idesc_o, x || !first ? 1u : 0u);
-            }
-            __syncwarp();
-        };
-        auto commit = [&](uint32_t bar) {
-            if (elect_one()) umma_commit(bar);
-            __syncwarp();
-        };
-        int n0 = 0, q_used[2] = {0, 0}, p_used[2] = {0, 0};
-        bool ok = true;
-        while (ok && work.more()) {
-            const Item it = work.next();
-            const bool two = TILES == 2 && it.rows > 128, both = TILES == 2 && !two;        // two tiles of rows; both take the same rows
-            ok = wait(q_full(0), q_used[0]++ & 1);
-            if (ok && two) ok = wait(q_full(1), q_used[1]++ & 1);
-            if (!ok) break;
-            tc_fence_after();
-            if (!both) {
-                const int tiles = two ? 2 : 1;
-                if (!(ok = full(2 * n0))) break;
-                for (int t = 0; t < tiles; ++t) scores(t, t, 2 * n0);
-                commit(kv_free(2 * n0 % STAGES));
-                for (int j = 0; ok && j < it.count; ++j) {
-                    const int v = 2 * (n0 + j) + 1;
-                    ok = full(v);
-                    for (int t = 0; ok && t < tiles; ++t) {
-                        if (!(ok = wait(p_ready(t), p_used[t]++ & 1))) break;
-                        tc_fence_after();
-                        values(t, v, j == 0);
-                        if (j + 1 < it.count) {
-                            if (t == 0 && !(ok = full(v + 1))) break;
-                            scores(t, t, v + 1);
-                        } else {
-                            commit(o_full(t));
-                        }
+            auto wait = [&](uint32_t bar, int parity) {
+                if (__all_sync(~0u, mbar_try_wait(bar, parity)) || !ok) return;
+                bool there = true;
+                if (lane == 0) there = wait_phase(bar, parity, dead, p.status);
+                ok = same(there);
+            };
+            // The next stage of the ring that holds K, or V: every other one.  Each warp waits for all of them in turn and sets all free, also
+            // those that only the other one uses, so that neither misses a phase of a barrier.
+            struct Cursor {
+                int stage, phase;
+                __device__ void advance() {
+                    stage += 2;
+                    if (stage >= STAGES) { stage -= STAGES; phase ^= 1; }
+                }
+            };
+            Cursor kc = {0, 0}, vc = {1, 0};
+            auto pass = [&](Cursor& c) {
+                wait(kv_full(c.stage), c.phase);
+                if (lane == 0) mbar_arrive(kv_free(c.stage));
+                c.advance();
+            };
+            int q_phase = 0, q1_phase = 0, p_phase = 0, turn_phase = 0;
+            // The warps take turns, from one product with V and the scores after it to the next: products of both at once would be done
+            // together, late, and both tiles' weights then be worked out at once.
+            auto take_turn = [&] {
+                wait(turn(t), turn_phase);
+                turn_phase ^= 1;
+            };
+            bool first_turn = t == 0;                               // of all
+            while (ok && same(work.more())) {
+                const Item it = work.next();
+                const int count = same(it.count);
+                const bool two = TILES == 2 && same(it.rows > 128), both = TILES == 2 && !two;  // two tiles of rows; both take the same rows
+                wait(q_full(0), q_phase);
+                q_phase ^= 1;
+                if (two) {
+                    if (t == 1) wait(q_full(1), q1_phase);
+                    q1_phase ^= 1;
+                }
+                const uint32_t q = (uint32_t)same((int)((uint32_t)q0 + ((uint32_t)(both ? 0 : t * T::Q_BYTES) >> 4)));
+                // tiles of states: all of them, or every other one
+                const int step = both ? 2 : 1, mine = both ? (count - t + 1) / 2 : count;
+                const int turns = (both ? (count + 1) / 2 : count) + 1; // of each warp, also where the second one has nothing to do
+                if (both && t == 1) { pass(kc); pass(vc); }
+                for (int j = -1; j < turns - 1; ++j) {
+                    const bool value = j >= 0 && j < mine, score = j < mine - 1;
+                    if (score) {                             // (waited for ahead of the turn)
+                        if (step == 2 && j >= 0) pass(kc);
+                        if (j < 0) wait(kv_full(kc.stage), kc.phase);
                     }
+                    if (value) {                                    // O of the tile of states whose weights are next
+                        wait(kv_full(vc.stage), vc.phase);
+                        wait(p_ready(t), p_phase);
+                        p_phase ^= 1;
+                    }
+                    if (TILES == 2 && !first_turn) take_turn();
+                    first_turn = false;
                     if (!ok) break;
-                    commit(kv_free(v % STAGES));
-                    if (j + 1 < it.count) commit(kv_free((v + 1) % STAGES));
-                }
-            } else {
-                for (int s = 0; ok && s < min(2, it.count); ++s) {
-                    if (!(ok = full(2 * (n0 + s)))) break;
-                    scores(s, 0, 2 * (n0 + s));
-                    commit(kv_free(2 * (n0 + s) % STAGES));
-                }
-                for (int s = 0; ok && s < it.count; ++s) {
-                    const int t = s & 1, v = 2 * (n0 + s) + 1;
-                    if (!(ok = full(v)) || !(ok = wait(p_ready(t), p_used[t]++ & 1))) break;
                     tc_fence_after();
-                    values(t, v, s < 2);
-                    commit(kv_free(v % STAGES));
-                    if (s + 2 < it.count) {
-                        if (!(ok = full(v + 3))) break;
-                        scores(t, 0, v + 3);
-                        commit(kv_free((v + 3) % STAGES));
-                    } else {
-                        commit(o_full(t));
+                    if (value) {
+                        const uint32_t v = (uint32_t)same((int)((uint32_t)v0 + ((uint32_t)(vc.stage * T::STAGE) >> 4)));
+                        if (elect_one()) {
+#pragma unroll
+                            for (int x = 0; x < BN / 16; ++x)
+                                umma_bf16_ts(o_of, s_of + 8 * x, desc(v0, v + (2048 * x >> 4)), idesc_o, x || j ? 1u : 0u);
+                            umma_commit(kv_free(vc.stage));
+                            if (TILES == 1) mbar_arrive(kv_free(vc.stage));
+                            if (j == mine - 1) umma_commit(o_full(t));
+                        }
+                        __syncwarp();
+                        vc.advance();
+                        if (step == 2 && j < mine - 1) pass(vc);
                     }
+                    if (score) {                                    // S of the next
+                        if (j >= 0) wait(kv_full(kc.stage), kc.phase);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t k = (uint32_t)same((int)((uint32_t)k0 + ((uint32_t)(kc.stage * T::STAGE) >> 4)));
+                        if (elect_one()) {
+#pragma unroll
+                            for (int x = 0; x < DP / 16; ++x)
+                                if (x < ksteps)
+                                    umma_bf16(s_of, desc(q0, q + ((x >> 2) * (128 * 128) + (x & 3) * 32 >> 4)), desc(k0, k + ((x >> 2) * (BN * 128) + (x & 3) * 32 >> 4)), idesc_s, x ? 1u : 0u);
+                            umma_commit(s_full(t));
+                        }
+                        __syncwarp();
+                        kc.advance();
+                    }
+                    if (TILES == 2 && lane == 0) mbar_arrive(turn(1 - t));
                 }
+                if (both && ((count - t) & 1) == 0 && count > t) { pass(kc); pass(vc); }        // the other one's last
             }
-            n0 += it.count;
-        }
-        if (!ok) {                                              // tensor memory is given back below: products in flight end first
-            commit(drained);
-            for (int probes = 0; probes < kLeastProbes && !mbar_try_wait(drained, 0); ++probes) {}
+            if (!ok) {                                              // tensor memory is given back below: products in flight end first
+                if (elect_one()) umma_commit(drained + 8 * t);
+                __syncwarp();
+                for (int probes = 0; probes < kLeastProbes && !mbar_try_wait(drained + 8 * t, 0); ++probes) {}
+            }
         }
     } else {
+        take_registers<T::MANY>();
         // ---- weights ----
         const int t = warp >> 2, r = tid & 127;                 // tile; row of it
         const uint32_t rows_at = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_at = rows_at + t * T::S_COLS, o_at = rows_at + T::O_COL + t * T::O_COLS;
@@ -769,18 +865,28 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             const bool mine_live = mine < it.rows;
             if (t == 0 || two) {                                // queries, in the order the products read them
                 int h;
-                const long long tok = Work<ROWS, BN>::token_of(a, it, mine_live ? mine : 0, h);
-                const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + tok * p.q_stride + (long long)h * D);
+                const long long tok = Work<BN>::token_of(a, it, mine_live ? mine : 0, h);
+                const unsigned long long src = mine_live ? reinterpret_cast<unsigned long long>(static_cast<const __nv_bfloat16*>(p.q) + tok * p.q_stride + (long long)h * D) : 0ull;
                 const unsigned flip = a.sign < 0.f ? 0x80008000u : 0u;
-                unsigned char* const dst = base + t * T::Q_BYTES + r * 128;
-#pragma unroll 8
-                for (int c = 0; c < 2 * ksteps; ++c) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (mine_live && 8 * c < D) {
-                        x = __ldg(src + c);
-                        x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+                unsigned char* const dst = base + t * T::Q_BYTES + (warp & 3) * (32 * 128);
+                // a warp brings its 32 rows together, 16 bytes of a lane next to those of the next one
+                const int pieces = 2 * ksteps;
+                const unsigned part = 65536 / pieces + 1;       // piece * part / 65536: exact for 1024 pieces of rows of up to 32
+                for (int x0 = 0; x0 < pieces; x0 += 8) {
+                    uint4 x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const unsigned u = (x0 + e) * 32 + lane, row = u * part >> 16, c = u - row * pieces;
+                        const unsigned long long from = __shfl_sync(~0u, src, row & 31);
+                        x[e] = make_uint4(0u, 0u, 0u, 0u);
+                        if (row < 32 && from && 8 * c < D) x[e] = __ldg(reinterpret_cast<const uint4*>(from) + c);
                     }
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + (((c & 7) ^ (r & 7)) << 4)) = x;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const unsigned u = (x0 + e) * 32 + lane, row = u * part >> 16, c = u - row * pieces;
+                        x[e].x ^= flip; x[e].y ^= flip; x[e].z ^= flip; x[e].w ^= flip;
+                        if (row < 32) *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x[e];
+                    }
                 }
                 fence_proxy_async();
                 mbar_arrive(q_full(t));
@@ -790,87 +896,107 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             const int step = both ? 2 : 1;
             for (int j = both ? t : 0; j < it.count && (t == 0 || TILES == 2); j += step, ++blocks) {
                 const int kb = it.kb + j, keys = min(BN, it.klen - kb * BN);
-                bool gone = r < BN && r >= keys;
+                bool gone = r < BN && r >= keys, masked = keys < BN;
                 if (BIAS) {
                     if (r < BN) {
                         const float b = gone ? -INFINITY : p.bias[it.k0 + (long long)kb * BN + r];
                         gone = b == -INFINITY;
                         sb[t][r] = b;
                     }
-                    named_barrier(2 + t, 128);
+                    masked = named_barrier_or(2 + t, 128, gone);
                 }
                 wait_phase(s_full(t), s_used++ & 1, dead, p.status);
                 tc_fence_after();
-                uint32_t s[CH][32];
+                if (r == 0) {                                   // K has been used
+                    const uint32_t free = kv_free(2 * (n0 + j) % STAGES);
+                    mbar_arrive(free);
+                    if (TILES == 1) mbar_arrive(free);
+                }
+                // the scores; masked ones are -inf whatever the state's rows hold
+                auto each_chunk = [&](auto with_masks, auto use) {
+                    constexpr bool MASKS = decltype(with_masks)::value;
+                    uint32_t s[CH][32];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) tmem_ld32(s_at + 32 * c, s[c]);
+                    for (int c = 0; c < CH; ++c) tmem_ld32(s_at + 32 * c, s[c]);
 #pragma unroll
-                for (int c = 0; c < CH; ++c) tmem_ld_wait32(s[c]);
-                float top = -INFINITY;
-                if (BIAS) {
+                    for (int c = 0; c < CH; ++c) {
+                        tmem_ld_wait32(s[c]);
+                        float2 y[16];
 #pragma unroll
-                    for (int c = 0; c < CH; ++c)
+                        for (int x = 0; x < 16; ++x) y[x] = make_float2(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
+                        if (BIAS) {
 #pragma unroll
-                        for (int x = 0; x < 32; x += 4) {
-                            const float4 b = *reinterpret_cast<const float4*>(&sb[t][32 * c + x]);
-                            const float bs[4] = {b.x, b.y, b.z, b.w};
+                            for (int x = 0; x < 16; x += 2) {
+                                const float4 b = *reinterpret_cast<const float4*>(&sb[t][32 * c + 2 * x]);
+                                y[x] = fma2(y[x], make_float2(a.c, a.c), make_float2(b.x, b.y));
+                                y[x + 1] = fma2(y[x + 1], make_float2(a.c, a.c), make_float2(b.z, b.w));
+                                if (MASKS) {
+                                    if (b.x == -INFINITY) y[x].x = -INFINITY;
+                                    if (b.y == -INFINITY) y[x].y = -INFINITY;
+                                    if (b.z == -INFINITY) y[x + 1].x = -INFINITY;
+                                    if (b.w == -INFINITY) y[x + 1].y = -INFINITY;
+                                }
+                            }
+                        } else if (MASKS) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float y = bs[e] == -INFINITY ? bs[e] : fmaf(__uint_as_float(s[c][x + e]), a.c, bs[e]);
-                                s[c][x + e] = __float_as_uint(y);
+                            for (int x = 0; x < 16; ++x) {
+                                if (32 * c + 2 * x >= keys) y[x].x = -INFINITY;
+                                if (32 * c + 2 * x + 1 >= keys) y[x].y = -INFINITY;
                             }
                         }
-                    named_barrier(2 + t, 128);                  // the biases have been read
-                } else if (keys < BN) {
-#pragma unroll
-                    for (int c = 0; c < CH; ++c)
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (32 * c + x >= keys) s[c][x] = 0xff800000u;
-                }
-                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int x = 0; x < 32; x += 2)
-                        tops[x >> 1 & 3] = fmaxf(tops[x >> 1 & 3], fmaxf(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])));
-                top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                        use(c, y);
+                    }
+                };
                 const float c1 = BIAS ? 1.f : a.c, unit = BIAS ? kLog2e : 1.f;
-                top *= c1;
-                if (__any_sync(~0u, top > m + kLag / unit)) {
-                    const float now = fmaxf(m, top), from = now == -INFINITY ? 0.f : now, f = exp2_fast((m - from) * unit);
-                    m = now;
-                    l *= f;
-                    if (blocks > 0) {                           // the products of the tiles before are done: the scores came after them
-                        for (int c = 0; c < 16 * ksteps; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(o_at + c, o);
-                            tmem_ld_wait32(o);
+                // The reference of the weights is the maximum of the first tile.  It follows later ones only where the sum of a tile's weights
+                // passes kMost: floats, bf16 among them, keep their relative precision up to there, so the maximum need not be known.
+                uint32_t w[BN / 2];
+                float sum;
+                for (bool fresh = __any_sync(~0u, m == -INFINITY);; fresh = true) {
+                    if (fresh) {
+                        float top = -INFINITY;
+                        each_chunk(std::true_type{}, [&](int, const float2 (&y)[16]) {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-                            tmem_st32(o_at + c, o);
+                            for (int x = 0; x < 16; ++x) top = fmaxf(top, fmaxf(y[x].x, y[x].y));
+                        });
+                        const float now = fmaxf(m, top * c1), from = now == -INFINITY ? 0.f : now, f = exp2_fast((m - from) * unit);
+                        m = now;
+                        l *= f;
+                        if (blocks > 0) {                       // the products of the tiles before are done: the scores came after them
+                            for (int c = 0; c < 16 * ksteps; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(o_at + c, o);
+                                tmem_ld_wait32(o);
+#pragma unroll
+                                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                                tmem_st32(o_at + c, o);
+                            }
                         }
                     }
-                }
-                const float from = m == -INFINITY ? 0.f : m;
-                float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const float from = m == -INFINITY ? 0.f : m;
+                    float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    auto weigh = [&](auto with_masks) { each_chunk(with_masks, [&](int c, const float2 (&y)[16]) {
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int x = 0; x < 32; x += 2) {
-                        float2 y;
-                        if (BIAS) y = make_float2((__uint_as_float(s[c][x]) - from) * kLog2e, (__uint_as_float(s[c][x + 1]) - from) * kLog2e);
-                        else y = fma2(make_float2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), make_float2(c1, c1), make_float2(-from, -from));
-                        y = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-                        sums[x >> 1 & 1].x += y.x;
-                        sums[x >> 1 & 1].y += y.y;
-                        const __nv_bfloat162 two16 = __floats2bfloat162_rn(y.x, y.y);
-                        w[x >> 1] = *reinterpret_cast<const uint32_t*>(&two16);
-                    }
-                    tmem_st16(s_at + 16 * c, w);
+                        for (int x = 0; x < 16; ++x) {
+                            float2 z;
+                            if (BIAS) z = mul2(add2(y[x], make_float2(-from, -from)), make_float2(kLog2e, kLog2e));
+                            else z = fma2(y[x], make_float2(c1, c1), make_float2(-from, -from));
+                            z = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+                            sums[x & 1] = add2(sums[x & 1], z);
+                            const __nv_bfloat162 two16 = __floats2bfloat162_rn(z.x, z.y);
+                            w[16 * c + x] = *reinterpret_cast<const uint32_t*>(&two16);
+                        }
+                    }); };
+                    if (masked) weigh(std::true_type{});
+                    else weigh(std::false_type{});
+                    const float2 all = add2(sums[0], sums[1]);
+                    sum = all.x + all.y;
+                    if (fresh || !__any_sync(~0u, sum > kMost)) break;
                 }
-                l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+                l += sum;
+                if (BIAS) named_barrier(2 + t, 128);            // the biases have been read
+#pragma unroll
+                for (int c = 0; c < BN / 64; ++c) tmem_st32(s_at + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(w + 32 * c));
                 if (gone) {                                     // a masked state's values may be anything, and meet a weight of zero
                     const int pos = 2 * (n0 + j) + 1;
                     wait_phase(kv_full(pos % STAGES), (pos / STAGES) & 1, dead, p.status);
@@ -892,13 +1018,18 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             // the result of the thread's row: O f0, plus another part's O f1 of columns [d / 4][row] in shared memory
             auto emit = [&](bool add, float f0, float f1) {
                 int h;
-                const long long row = Work<ROWS, BN>::token_of(a, it, mine_live ? mine : 0, h) * p.q_heads + h;
+                const long long row = Work<BN>::token_of(a, it, mine_live ? mine : 0, h) * p.q_heads + h;
+                const unsigned long long to = mine_live ? reinterpret_cast<unsigned long long>(static_cast<__nv_bfloat16*>(p.out) + row * D) : 0ull;
+                // 32 columns of the warp's rows go through shared memory, four pieces of 16 bytes of a row each 2 KB apart or less: the place
+                // of the warp's own queries, or of what has just been added
                 float bad = l * 0.f;                            // 0, or NaN
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld32(o_at + c, o);
                     tmem_ld_wait32(o);
+                    unsigned char* const stage = add ? base + ((size_t)(c / 4) * 128 + (warp & 3) * 32) * 16 : base + t * T::Q_BYTES + (warp & 3) * (32 * 128);
+                    const int apart = add ? 2048 : 512;
 #pragma unroll
                     for (int x = 0; x < 32; x += 8) {
                         if (c + x >= D) continue;
@@ -915,7 +1046,6 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) bad = fmaf(y[e], 0.f, bad);
-                        if (!mine_live) continue;
                         if (whole) {
                             uint32_t w[4];
 #pragma unroll
@@ -923,11 +1053,22 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                                 const __nv_bfloat162 two16 = __floats2bfloat162_rn(y[2 * e] * inv, y[2 * e + 1] * inv);
                                 w[e] = *reinterpret_cast<const uint32_t*>(&two16);
                             }
-                            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + row * D + c + x) = make_uint4(w[0], w[1], w[2], w[3]);
-                        } else {
+                            *reinterpret_cast<uint4*>(stage + x / 8 * apart + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else if (mine_live) {
                             part.o[(c + x) / 4 * ROWS + mine] = make_float4(y[0], y[1], y[2], y[3]);
                             if (c + x + 4 < D) part.o[((c + x) / 4 + 1) * ROWS + mine] = make_float4(y[4], y[5], y[6], y[7]);
                         }
+                    }
+                    if (whole) {
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {           // 64 bytes of eight rows at a time
+                            const int u = 8 * e + (lane >> 2), x = lane & 3;
+                            const unsigned long long there = __shfl_sync(~0u, to, u);
+                            if (there && c + 8 * x < D)
+                                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(there) + c + 8 * x) = *reinterpret_cast<const uint4*>(stage + x * apart + u * 16);
+                        }
+                        __syncwarp();
                     }
                 }
                 if (mine_live) {
@@ -938,9 +1079,9 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 for (unsigned again = __ballot_sync(~0u, mine_live && bad != 0.f && !*dead); again; again &= again - 1)
                     plain_row<DP>(a, it, __shfl_sync(~0u, mine, __ffs(again) - 1));
             };
-            if (!both || it.count == 1) {
-                if (blocks > 0) emit(false, 1.f, 0.f);
-            } else {
+            const bool merged = both && it.count > 1;
+            float f0 = 1.f, f1 = 0.f;
+            if (merged) {
                 // two results of the same rows: the second one goes through the place of the queries, whose products are done
                 named_barrier(1, 256);
                 if (t == 1) {
@@ -960,13 +1101,14 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 if (t == 0) {
                     const float2 ml = reinterpret_cast<const float2*>(&sb[0][0])[r];
                     const float now = fmaxf(m, ml.x), from = now == -INFINITY ? 0.f : now;
-                    const float f0 = exp2_fast((m - from) * a.unit), f1 = exp2_fast((ml.x - from) * a.unit);
+                    f0 = exp2_fast((m - from) * a.unit);
+                    f1 = exp2_fast((ml.x - from) * a.unit);
                     m = now;
                     l = l * f0 + ml.y * f1;
-                    emit(true, f0, f1);
                 }
-                named_barrier(1, 256);
             }
+            if (blocks > 0 && (t == 0 || !merged)) emit(merged, f0, f1);
+            if (merged) named_barrier(1, 256);
             tc_fence_before();                                  // O has been read before the next item's weights are announced
             if (!whole) {
                 const int c0 = (int)(it.first / work.per), c1 = (int)((it.first + it.kbs - 1) / work.per);
@@ -1001,16 +1143,21 @@ bool allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& set) {
     return true;
 }
 
+// CTAs that there are counters and room for parts of such blocks for.
 template <int BM, int DP>
-int launch_f32(const CrossArgs& a) {
+int max_ctas(int ctas) { return std::min(ctas, std::min(kMaxCtas, (int)(kPartsBytes / (2 * Part<BM, DP>::BYTES)))); }
+
+template <int BM, int DP>
+int launch_f32(CrossArgs& a) {
+    a.block = BM;
     static std::atomic<unsigned long long> set{0};
-    const int sms = std::min(sm_count(), kMaxCtas);
-    if (!sms || !allow_smem(attn_cross_f32<BM, DP>, Cores<BM, DP>::SMEM, set)) return LUVC_ERR_CUDA;
-    return launch_overlapped(attn_cross_f32<BM, DP>, sms, Cores<BM, DP>::NT, Cores<BM, DP>::SMEM, a.p.stream, a);
+    const int ctas = max_ctas<BM, DP>(Cores<BM, DP>::CTAS * sm_count());
+    if (!ctas || !allow_smem(attn_cross_f32<BM, DP>, Cores<BM, DP>::SMEM, set)) return LUVC_ERR_CUDA;
+    return launch_overlapped(attn_cross_f32<BM, DP>, ctas, Cores<BM, DP>::NT, Cores<BM, DP>::SMEM, a.p.stream, a);
 }
 
 template <int BM>
-int launch_f32_wide(const CrossArgs& a) {
+int launch_f32_wide(CrossArgs& a) {
     return a.p.D <= 64 ? launch_f32<BM, 64>(a) : a.p.D <= 128 ? launch_f32<BM, 128>(a) : launch_f32<BM, 256>(a);
 }
 
@@ -1044,10 +1191,12 @@ bool states_map(CUtensorMap* map, const CrossProblem& p, const void* rows, long 
 }
 
 template <int DP, bool BIAS>
-int launch_tc(const CrossArgs& a) {
+int launch_tc(CrossArgs& a) {
     using T = Tc<DP>;
     static std::atomic<unsigned long long> set{0};
-    const int sms = std::min(sm_count(), kMaxCtas);
+    const int sms = max_ctas<T::ROWS, DP>(sm_count());
+    // blocks of two tiles of rows where there are enough for all SMs (of one, and both tiles on the same rows, K and V are brought twice as often)
+    a.block = T::TILES == 2 && (long long)a.p.q_tokens * a.p.q_heads <= 256ll * 2 * sms ? 128 : T::ROWS;
     CUtensorMap kmap, vmap;
     if (!sms || !states_map<T::BN>(&kmap, a.p, a.p.k, a.p.k_stride) || !states_map<T::BN>(&vmap, a.p, a.p.v, a.p.v_stride) ||
         !allow_smem(attn_cross_tc<DP, BIAS>, T::SMEM, set))
@@ -1056,13 +1205,13 @@ int launch_tc(const CrossArgs& a) {
 }
 
 template <int DP>
-int launch_tc_bias(const CrossArgs& a) {
+int launch_tc_bias(CrossArgs& a) {
     return a.p.bias ? launch_tc<DP, true>(a) : launch_tc<DP, false>(a);
 }
 
 }  // namespace
 
-size_t attn_cross_workspace_bytes() { return kCounterBytes + (size_t)kMaxCtas * 2 * kPartFloats * sizeof(float); }
+size_t attn_cross_workspace_bytes() { return kCounterBytes + kPartsBytes; }
 
 int attn_cross(const CrossProblem& p) {
     CrossArgs a;
