@@ -86,13 +86,14 @@ struct Item {
     int q0, rows;                                   // first token of the sequence; rows of the block
     long long k0;                                   // first state
     int klen;
-    long long first;                                // its first tile's place in the list
+    int first;                                      // its first tile's place in the list
 };
 
 template <int BN>
 struct Work {
     const CrossArgs& a;
-    long long at = 0, end = 0, per = 0;             // this CTA's part of the list
+    int at = 0, end = 0;                            // this CTA's part of the list
+    unsigned per = 1;                               // and of all others
     bool whole = false;                             // the list is of blocks, not of tiles
     int seq = 0, head = 0, rb = 0, kb = 0;
     int q0 = 0, qlen = 0, k0 = 0, klen = 0, rbs = 0, kbs = 0;
@@ -115,84 +116,113 @@ struct Work {
         rbs = blocks_of(qlen);
         kbs = tiles_of(klen);
     }
-    // This CTA's part; all NT threads of the CTA call it.
+    // This CTA's part; all NT threads of the CTA call it.  Up to 32 sequences each warp works it out for itself.
     template <int NT>
     __device__ void begin() {
         constexpr int NW = NT / 32;
-        __shared__ long long sums[NW], blocks[NW], found_in;
+        __shared__ unsigned sums[NW], blocks[NW], found_in;
+        __shared__ float sizes[NW];
         __shared__ int most[NW], found;
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.p.n;
-        // tiles and blocks of NT sequences at a time, and of those before them
-        long long tiles_before = 0, blocks_before = 0, tiles, blocks_mine, total = 0, all_blocks = 0;
+        // tiles and blocks of 32 or NT sequences at a time, of all before them, and of all
+        unsigned tiles = 0, tiles_before = 0, total = 0, blocks_mine = 0, blocks_before = 0, all_blocks = 0;
+        float size = 0.f;                           // of the list, which must have less than 2^31 tiles
         int longest = 0;
         auto scan = [&](int i) {
             int q0, qlen = 0, k0, klen = 0;
             if (i < n) lengths(i, q0, qlen, k0, klen);
             const int t = tiles_of(klen);
-            blocks_mine = t ? (long long)a.p.heads * blocks_of(qlen) : 0;
+            const float b = (float)a.p.heads * blocks_of(qlen);
+            blocks_mine = t && b < 2147483648.f ? a.p.heads * (unsigned)blocks_of(qlen) : 0u;
             tiles = blocks_mine * t;
-            tiles_before = tiles; blocks_before = blocks_mine;
+            float x = t ? b * t : 0.f;
+            unsigned s = tiles, c = blocks_mine;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const long long x = __shfl_up_sync(~0u, tiles_before, d), y = __shfl_up_sync(~0u, blocks_before, d);
-                if (lane >= d) { tiles_before += x; blocks_before += y; }
+                const unsigned y = __shfl_up_sync(~0u, s, d), z = __shfl_up_sync(~0u, c, d);
+                x += __shfl_xor_sync(~0u, x, d);
+                if (lane >= d) { s += y; c += z; }
             }
-            const int m = __reduce_max_sync(~0u, blocks_mine ? t : 0);
-            if (lane == 31) { sums[warp] = tiles_before; blocks[warp] = blocks_before; most[warp] = m; }
+            const int m = __reduce_max_sync(~0u, t && qlen ? t : 0);
+            tiles_before = total + s - tiles;
+            blocks_before = all_blocks + c - blocks_mine;
+            if (n <= 32) {
+                total = __shfl_sync(~0u, s, 31);
+                all_blocks = __shfl_sync(~0u, c, 31);
+                longest = m;
+                size = x;
+                return;
+            }
+            if (lane == 31) { sums[warp] = s; blocks[warp] = c; most[warp] = m; sizes[warp] = x; }
             __syncthreads();
-            tiles_before += total - tiles;
-            blocks_before += all_blocks - blocks_mine;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 if (w < warp) { tiles_before += sums[w]; blocks_before += blocks[w]; }
                 total += sums[w];
                 all_blocks += blocks[w];
                 longest = max(longest, most[w]);
+                size += sizes[w];
             }
         };
-        scan(tid);
+        scan(n <= 32 ? lane : tid);
         for (int i0 = NT; i0 < n; i0 += NT) {
             __syncthreads();                        // the sums have been read
             scan(i0 + tid);
         }
-        per = quotient(total + gridDim.x - 1, gridDim.x);
-        const long long rounds = quotient(all_blocks + gridDim.x - 1, gridDim.x);
-        whole = rounds * longest <= per + kJoin;
-        if (whole) { total = all_blocks; per = rounds; }
-        at = min(total, per * blockIdx.x);
-        end = min(total, at + per);
-        if (at < end) {                             // (the same in all threads)
-            auto look = [&](int i) {
-                const long long before = whole ? blocks_before : tiles_before, x = whole ? blocks_mine : tiles;
-                if (before <= at && at < before + x) {
-                    found = i;
-                    found_in = at - before;
-                }
-            };
+        if (size >= 2147000000.f) {
+            if (tid == 0) *a.p.status = LUVC_ERR_SHAPE;
+            return;
+        }
+        per = (total + gridDim.x - 1) / gridDim.x;
+        const unsigned rounds = (all_blocks + gridDim.x - 1) / gridDim.x;
+        whole = (float)rounds * longest <= (float)(per + kJoin);
+        if (whole) per = rounds;
+        unsigned all = whole ? all_blocks : total;
+        at = (int)min((unsigned long long)all, (unsigned long long)per * blockIdx.x);
+        end = (int)min(all, at + per);
+        if (at >= end) return;                      // (the same in all threads)
+        unsigned in = 0;
+        int which = -1;
+        auto look = [&](int i) {
+            const unsigned before = whole ? blocks_before : tiles_before, x = whole ? blocks_mine : tiles;
+            if (before <= (unsigned)at && (unsigned)at < before + x) {
+                which = i;
+                in = at - before;
+            }
+        };
+        if (n <= 32) {
+            look(lane);
+            const int from = __ffs(__ballot_sync(~0u, which >= 0)) - 1;
+            which = __shfl_sync(~0u, which, from);
+            in = __shfl_sync(~0u, in, from);
+        } else {
             if (n <= NT) {
                 look(tid);
             } else {
                 total = all_blocks = 0;
-                for (int i0 = 0; i0 < n && (whole ? all_blocks : total) <= at; i0 += NT) {
+                for (int i0 = 0; i0 < n && (whole ? all_blocks : total) <= (unsigned)at; i0 += NT) {
                     __syncthreads();
                     scan(i0 + tid);
                     look(i0 + tid);
                 }
             }
+            if (which >= 0) { found = which; found_in = in; }
             __syncthreads();
-            enter(found);
-            const long long in = found_in, per_head = (long long)rbs * steps();
-            head = (int)quotient(in, per_head);
-            rb = (int)quotient(in - head * per_head, steps());
-            kb = whole ? 0 : (int)(in - head * per_head - (long long)rb * kbs);
+            which = found;
+            in = found_in;
         }
+        enter(which);
+        const unsigned per_head = (unsigned)rbs * steps();
+        head = in / per_head;
+        rb = (in - head * per_head) / steps();
+        kb = whole ? 0 : (int)(in - head * per_head - (unsigned)rb * kbs);
     }
     __device__ bool more() const { return at < end; }
     // The next item; the list goes on behind it.
     __device__ Item next() {
         Item it;
         it.seq = seq; it.head = head; it.rb = rb; it.kb = kb; it.kbs = kbs;
-        it.count = whole ? kbs : (int)min((long long)(kbs - kb), end - at);
+        it.count = whole ? kbs : min(kbs - kb, end - at);
         it.q0 = q0;
         it.rows = (int)min((long long)qlen * a.group - (long long)rb * a.block, (long long)a.block);
         it.k0 = k0; it.klen = klen;
@@ -514,7 +544,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
             }
         }
         if (!whole) {
-            const int c0 = (int)(it.first / work.per), c1 = (int)((it.first + it.kbs - 1) / work.per);
+            const int c0 = it.first / work.per, c1 = (it.first + it.kbs - 1) / work.per;
             __threadfence();
             __syncthreads();
             if (tid == 0) last = arrive(a.counters + c0, blockIdx.x - c0, c1 - c0 + 1);
@@ -712,7 +742,8 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     pdl_wait();
     Work<BN> work(a);
     tc_fence_before();
-    work.template begin<T::THREADS>();                          // (has barriers of all threads)
+    work.template begin<T::THREADS>();
+    __syncthreads();                                            // barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = tmem_at;
     empty_sequences<__nv_bfloat16, BN, T::THREADS>(a, work);
@@ -1111,7 +1142,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             if (merged) named_barrier(1, 256);
             tc_fence_before();                                  // O has been read before the next item's weights are announced
             if (!whole) {
-                const int c0 = (int)(it.first / work.per), c1 = (int)((it.first + it.kbs - 1) / work.per);
+                const int c0 = it.first / work.per, c1 = (it.first + it.kbs - 1) / work.per;
                 __threadfence();
                 named_barrier(1, 256);
                 if (tid == 0) last = arrive(a.counters + c0, blockIdx.x - c0, c1 - c0 + 1);
