@@ -11,7 +11,7 @@
 // Split.  The work is the list of all (sequence, key head, block of rows, tile of states); each CTA takes an equal part of it, whatever the
 // lengths.  What a CTA has of a (sequence, key head, block of rows) that others share goes through the workspace; the CTA that comes last
 // adds the parts, in the order of the list, so that a repeated call gives the same bits.  Where there is little to do, the parts are whole
-// (sequence, key head, block of rows)s: a join costs as much as some tiles (kJoin).
+// (sequence, key head, block of rows)s: a join costs as much as some tiles (JOIN).
 //
 // bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums.
 
@@ -35,7 +35,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxCtas = 320;                       // CTAs there are counters for
 constexpr size_t kCounterBytes = 2048, kPartsBytes = (size_t)160 * 2 * 256 * 130 * sizeof(float);      // 160 CTAs' parts of 256 rows of 128 columns
 static_assert(kMaxCtas * sizeof(unsigned) <= kCounterBytes, "room for the counters");
-constexpr int kJoin = 8;                            // tiles that a join costs as much as
 constexpr int kWaitProbes = 1 << 20;                // probes before a wait gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;               // and with a limit from the status block (a test's)
 
@@ -89,7 +88,7 @@ struct Item {
     int first;                                      // its first tile's place in the list
 };
 
-template <int BN>
+template <int BN, int JOIN>                         // states of a tile; tiles that a join costs as much as
 struct Work {
     const CrossArgs& a;
     int at = 0, end = 0;                            // this CTA's part of the list
@@ -175,7 +174,7 @@ struct Work {
         }
         per = (total + gridDim.x - 1) / gridDim.x;
         const unsigned rounds = (all_blocks + gridDim.x - 1) / gridDim.x;
-        whole = (float)rounds * longest <= (float)(per + kJoin);
+        whole = (float)rounds * longest <= (float)(per + JOIN);
         if (whole) per = rounds;
         unsigned all = whole ? all_blocks : total;
         at = (int)min((unsigned long long)all, (unsigned long long)per * blockIdx.x);
@@ -241,14 +240,15 @@ struct Work {
         }
         return it;
     }
-    // Element of q and of out of a row's first column (in units of tokens' rows: see row_of).
-    __device__ static long long token_of(const CrossArgs& a, const Item& it, int r, int& h) {
-        const long long row = (long long)it.rb * a.block + r;
-        const long long t = quotient(row, a.group);
-        h = it.head * a.group + (int)(row - t * a.group);
-        return it.q0 + t;
-    }
 };
+
+// Token and query head of row r of an item.
+__device__ __forceinline__ long long token_of(const CrossArgs& a, const Item& it, int r, int& h) {
+    const long long row = (long long)it.rb * a.block + r;
+    const long long t = quotient(row, a.group);
+    h = it.head * a.group + (int)(row - t * a.group);
+    return it.q0 + t;
+}
 
 template <typename T> __device__ __forceinline__ void put4(T* p, float4 x);
 template <> __device__ __forceinline__ void put4<float>(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
@@ -259,8 +259,8 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
 __device__ __forceinline__ float lse_of(const CrossArgs& a, float m, float l) { return l == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.nat, logf(l)); }
 
 // Sequences without states: rows of zeros.
-template <typename T, int BN, int NT>
-__device__ void empty_sequences(const CrossArgs& a, const Work<BN>& w) {
+template <typename T, int NT, typename W>
+__device__ void empty_sequences(const CrossArgs& a, const W& w) {
     for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
         int q0, qlen, k0, klen;
         w.lengths(i, q0, qlen, k0, klen);
@@ -294,7 +294,7 @@ __device__ __forceinline__ bool arrive(unsigned* counter, int i, int n) {
 
 // Adds the parts of an item, which CTAs c0 .. c1 have written, in order, and writes the result.  NT threads; each has E groups of four columns
 // at a time, and the parts of all of them on their way.
-template <typename T, int BM, int BN, int DP, int NT>
+template <typename T, int BM, int DP, int NT>
 __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, int tid) {
     constexpr int E = 4, B = 4;                                 // groups of columns; parts at a time
     const int all = it.rows * (a.p.D / 4);
@@ -359,7 +359,7 @@ __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, i
         for (int e = 0; e < E; ++e) {
             if (e0 + e * NT >= all) continue;
             int h;
-            const long long row = Work<BN>::token_of(a, it, r[e], h) * a.p.q_heads + h;
+            const long long row = token_of(a, it, r[e], h) * a.p.q_heads + h;
             put4(static_cast<T*>(a.p.out) + row * a.p.D + 4 * c[e], l[e] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : o[e]);
             if (c[e] == 0 && a.p.lse) a.p.lse[row] = lse_of(a, m[e], l[e]);
         }
@@ -374,7 +374,7 @@ template <int BM, int DP>
 struct Cores {
     static constexpr int BN = 64, NT = 256, RT = BM / 16, LD = DP + 4, LP = BN + 4;
     static constexpr size_t SMEM = (size_t)(BM * LD + BN * LD + BN * DP + BM * LP) * sizeof(float);
-    static constexpr int CTAS = DP <= 128 ? 2 : 1;              // of an SM
+    static constexpr int CTAS = BM > 64 || DP > 128 ? 1 : 2;    // of an SM
 };
 
 template <int BM, int DP>
@@ -392,9 +392,9 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, D = p.D;
     pdl_trigger();
     pdl_wait();
-    Work<BN> work(a);
+    Work<BN, 2> work(a);
     work.template begin<NT>();
-    empty_sequences<float, BN, NT>(a, work);
+    empty_sequences<float, NT>(a, work);
     for (int e = tid; e < (BM + BN) * (LD / 4); e += NT) reinterpret_cast<float4*>(qs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);   // columns past D
     for (int e = tid; e < BN * (DP / 4); e += NT) reinterpret_cast<float4*>(vs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
     while (work.more()) {
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
         for (int e = tid; e < it.rows * (D / 4); e += NT) {
             const int r = e / (D / 4), c = e - r * (D / 4);
             int h;
-            const long long t = Work<BN>::token_of(a, it, r, h);
+            const long long t = token_of(a, it, r, h);
             const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + t * p.q_stride + (long long)h * D + 4 * c);
             *reinterpret_cast<float4*>(qs + r * LD + 4 * c) = make_float4(x.x * a.sign, x.y * a.sign, x.z * a.sign, x.w * a.sign);
         }
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
             const int row = ty * RT + r;
             if (row >= it.rows) continue;
             int h;
-            const long long at = Work<BN>::token_of(a, it, row, h) * p.q_heads + h;
+            const long long at = token_of(a, it, row, h) * p.q_heads + h;
             const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
             for (int g = 0; g < CG; ++g) {
@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
             __syncthreads();
             if (last) {
                 __threadfence();
-                join_parts<float, BM, BN, DP, NT>(a, it, c0, c1, tid);
+                join_parts<float, BM, DP, NT>(a, it, c0, c1, tid);
             }
         }
     }
@@ -573,6 +573,7 @@ template <int DP_>
 struct Tc {
     static constexpr int DP = DP_, TILES = DP <= 128 ? 2 : 1, BN = DP <= 128 ? 128 : 64, ROWS = 128 * TILES;
     static constexpr int Q_BYTES = 128 * DP * 2, STAGE = BN * DP * 2, STAGES = DP == 64 ? 8 : 5;
+    static constexpr int JOIN = 8;          // (measured: 16 single tokens to 1296 states, 28 / 4 heads, in whole blocks 25 us, in parts 31)
     static constexpr int THREADS = 384, S_COLS = 128, O_COL = 256, O_COLS = DP <= 128 ? 128 : 256;
     static constexpr size_t SMEM = 1024 + TILES * Q_BYTES + STAGES * STAGE;
     // registers of the threads that have weights, and of the others: together what the launch has, 384 times 168
@@ -640,7 +641,7 @@ __device__ __forceinline__ void plain_row(const CrossArgs& a, const Item& it, in
     const CrossProblem& p = a.p;
     const int lane = threadIdx.x & 31, D = p.D;
     int h;
-    const long long t = Work<BN>::token_of(a, it, r, h), row = t * p.q_heads + h;
+    const long long t = token_of(a, it, r, h), row = t * p.q_heads + h;
     const __nv_bfloat16* const qr = static_cast<const __nv_bfloat16*>(p.q) + t * p.q_stride + (long long)h * D;
     float q[DP / 32], o[DP / 32], m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -740,13 +741,13 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     }
     pdl_trigger();
     pdl_wait();
-    Work<BN> work(a);
+    Work<BN, T::JOIN> work(a);
     tc_fence_before();
     work.template begin<T::THREADS>();
     __syncthreads();                                            // barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    empty_sequences<__nv_bfloat16, BN, T::THREADS>(a, work);
+    empty_sequences<__nv_bfloat16, T::THREADS>(a, work);
 
     if (warp >= 8) {
         give_registers<T::FEW>();
@@ -896,7 +897,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             const bool mine_live = mine < it.rows;
             if (t == 0 || two) {                                // queries, in the order the products read them
                 int h;
-                const long long tok = Work<BN>::token_of(a, it, mine_live ? mine : 0, h);
+                const long long tok = token_of(a, it, mine_live ? mine : 0, h);
                 const unsigned long long src = mine_live ? reinterpret_cast<unsigned long long>(static_cast<const __nv_bfloat16*>(p.q) + tok * p.q_stride + (long long)h * D) : 0ull;
                 const unsigned flip = a.sign < 0.f ? 0x80008000u : 0u;
                 unsigned char* const dst = base + t * T::Q_BYTES + (warp & 3) * (32 * 128);
@@ -1049,7 +1050,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             // the result of the thread's row: O f0, plus another part's O f1 of columns [d / 4][row] in shared memory
             auto emit = [&](bool add, float f0, float f1) {
                 int h;
-                const long long row = Work<BN>::token_of(a, it, mine_live ? mine : 0, h) * p.q_heads + h;
+                const long long row = token_of(a, it, mine_live ? mine : 0, h) * p.q_heads + h;
                 const unsigned long long to = mine_live ? reinterpret_cast<unsigned long long>(static_cast<__nv_bfloat16*>(p.out) + row * D) : 0ull;
                 // 32 columns of the warp's rows go through shared memory, four pieces of 16 bytes of a row each 2 KB apart or less: the place
                 // of the warp's own queries, or of what has just been added
@@ -1149,7 +1150,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 named_barrier(1, 256);
                 if (last) {
                     __threadfence();
-                    join_parts<__nv_bfloat16, ROWS, BN, DP, 256>(a, it, c0, c1, tid);
+                    join_parts<__nv_bfloat16, ROWS, DP, 256>(a, it, c0, c1, tid);
                 }
             }
         }
@@ -1257,6 +1258,8 @@ int attn_cross(const CrossProblem& p) {
     if (p.dtype == LUVC_BF16) return p.D <= 64 ? launch_tc_bias<64>(a) : p.D <= 128 ? launch_tc_bias<128>(a) : launch_tc_bias<256>(a);
     // few rows of a key head: small blocks
     const bool few = (long long)p.q_tokens * a.group <= 16ll * p.n;
+    const bool many = p.D <= 128 && (long long)p.q_tokens * a.group >= 96ll * p.n;
+    if (many) return p.D <= 64 ? launch_f32<128, 64>(a) : launch_f32<128, 128>(a);
     return few ? launch_f32_wide<16>(a) : launch_f32_wide<64>(a);
 }
 
