@@ -78,13 +78,6 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// Four bytes into shared memory; and an arrival at the barrier when the copies of this thread have landed.
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -468,7 +461,6 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ unsigned scan_warp[NW];
     __shared__ __align__(16) float core_q[kCores ? NW : 1][kCores ? NH * DP : 4], core_p[kCores ? NW : 1][NH * 16];
     __shared__ float factors[ROWS * (DP / 4) > NTHR ? 64 : 1][ROWS];
-    __shared__ float block_scales[kBlocks ? NW * S : 1][2 * Sh::SUB];      // of a stage's 16-token parts: K, V
     __shared__ int last_flag[2], all_flag;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
@@ -479,7 +471,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
     // ---- the list of tiles ----
     if (lane < S) {
-        mbar_init(smem_u32(&bars[warp * S + lane]), kBlocks ? 1 + 2 * Sh::SUB : 1);     // (and the lanes that bring scales)
+        mbar_init(smem_u32(&bars[warp * S + lane]), 1);
         mbar_fence_init();
     }
     if (lane < 2) piece_off[warp][lane] = 0;
@@ -648,26 +640,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < Sh::SUB; ++j) {
-                bool scaled = false;
                 if (j == 0 || 16 * j < ld_left) {
                     if (ld_page >= pg_first + 32) fetch_pages();
                     const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
                     const int row = (unsigned)page < (unsigned)p.c.pages ? (page * p.c.heads + ld_h) * ps + ld_off : a.rows_total;
                     if (lane < 2 * Sh::SEGS)
                         tma_load_2d(my_dst + stage * Sh::STAGE + j * 2 * Sh::SUBK, my_map, bar, (lane >> 1) * (Sh::PITCH / Sh::ES), row);
-                    if (kBlocks && lane < 2) {                  // its scale arrives with the stage (of no page: 1)
-                        float* const to = &block_scales[warp * S + stage][2 * j + lane];
-                        const float* const from = (is_v ? p.c.v_block_scale : p.c.k_block_scale) + ((size_t)p.layer * a.rows_total + row) / kKvBlock;
-                        scaled = row < a.rows_total;
-                        if (scaled) cp_async4(smem_u32(to), from);
-                        else *to = 1.f;
-                    }
                     ld_off += 16;
                     if (ld_off == ps) { ld_off = 0; ++ld_page; }
-                }
-                if (kBlocks && lane < 2) {
-                    if (scaled) cp_async_arrive(bar);
-                    else mbar_arrive(bar);
                 }
             }
             ld_left -= KT;
@@ -712,6 +692,24 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             const float scale = p.scale * (!kBlocks && p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
             // blocks: the sums O are in units of v_unit, which follows the blocks' scales and is never far below the largest so far
             float v_unit = 0x1p-126f, v_per_unit = 0x1p126f, v_top = 0.f;
+            // their scales, one for each lane: of the 32 blocks from `block0` on, and of the next 32, which are on their way meanwhile
+            float k_block = 1.f, v_block = 1.f, k_next = 1.f, v_next = 1.f;
+            int block0 = at.tile * Sh::SUB;
+            const int blocks_end = kBlocks ? min((at.tile + min(at.tiles - at.tile, left)) * Sh::SUB, (int)(((unsigned)len + 15u) / 16u)) : 0;
+            auto fetch_scales = [&](int first, float& k, float& v) {
+                if (first + lane >= blocks_end) return;
+                const int token = 16 * (first + lane);
+                const int index = a.page_shift >= 0 ? token >> a.page_shift : token / ps;
+                const int page = p.c.table[(long long)slot_of(at.seq) * p.c.max_pages + index];
+                if ((unsigned)page >= (unsigned)p.c.pages) return;                  // (rows of no page are zeros)
+                const size_t block = ((size_t)p.layer * a.rows_total + (page * p.c.heads + h) * ps + (token - index * ps)) / kKvBlock;
+                k = p.c.k_block_scale[block];
+                v = p.c.v_block_scale[block];
+            };
+            if (kBlocks) {
+                fetch_scales(block0, k_block, v_block);
+                fetch_scales(block0 + 32, k_next, v_next);
+            }
             // queries: B operand of S^T = K Q^T, head g of each group of 8
             const TQ* const qrow = static_cast<const TQ*>(p.q) + at.seq * p.q_stride + ((long long)h * a.group + r0) * p.c.D;
             constexpr int KS = DPB / 32;                        // steps of 32 bytes of a row
@@ -838,6 +836,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                 for (int j = 0; j < Sh::SUB; ++j) {
                     if (j > 0 && at.tile * KT + 16 * j >= len) break;
+                    if (kBlocks && at.tile * Sh::SUB + j - block0 >= 32) {
+                        k_block = k_next;
+                        v_block = v_next;
+                        block0 += 32;
+                        fetch_scales(block0 + 32, k_next, v_next);
+                    }
+                    const float k_scale = kBlocks ? __shfl_sync(~0u, k_block, at.tile * Sh::SUB + j - block0) : 1.f;
+                    const float v_scale = kBlocks ? __shfl_sync(~0u, v_block, at.tile * Sh::SUB + j - block0) : 1.f;
                     const uint32_t ks = my_ring_s + stage * Sh::STAGE + j * 2 * Sh::SUBK, vs = ks + Sh::SUBK;
                     if constexpr (kCores) {
                         const unsigned gone = masked ? __ballot_sync(~0u, bias[j][0] == -INFINITY) & 0xffffu : 0u;
@@ -898,7 +904,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 const float x = kF32 ? done[nt][c] + s[nt][c] + (s2[nt][c] + s3[nt][c]) : s[nt][c] + s2[nt][c];
-                                s[nt][c] = fmaf(x, kBlocks ? qmul[nt][c & 1] * block_scales[warp * S + stage][2 * j] : qmul[nt][c & 1], bias[j][c >> 1]);
+                                s[nt][c] = fmaf(x, kBlocks ? qmul[nt][c & 1] * k_scale : qmul[nt][c & 1], bias[j][c >> 1]);
                             }
                         unsigned gone = 0;
                         if (masked) {                               // whatever a masked row holds
@@ -973,7 +979,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             }
                         float w_scale = 1.f;                        // of the weights in their product with V
                         if constexpr (kBlocks) {
-                            float now = block_scales[warp * S + stage][2 * j + 1];
+                            float now = v_scale;
                             if (!(now <= v_unit && now >= kLeastUnit * v_unit)) {
                                 if (!(now > 0.f && now < INFINITY)) now = 0.f;
                                 v_top = fmaxf(v_top, now);

@@ -268,3 +268,22 @@ def test_refusals_of_the_binding(luvc):
     assert luvc.attn_cross(q[:0], k, v, q_starts=ints([0, 0, 0]), k_starts=ks).shape == (0, 4, 64)
     assert not luvc.attn_cross(q, k[:0], v[:0], q_starts=qs, k_starts=ints([0, 0, 0])).any()
     assert luvc.check_status() == 0
+
+
+@pytest.mark.parametrize("hq,heads,D,queries,keys", [(8, 2, 64, [300, 20], [900, 1500]), (4, 1, 128, [1], [5000]), (4, 4, 256, [70], [300])])
+def test_a_wait_that_gives_up(luvc, hq, heads, D, queries, keys):
+    """A copy that is waited for in vain ends the call with a status, in milliseconds; the workspace is as it must be, the next call right."""
+    q, k, v, qs, ks = inputs("bf16", hq, heads, D, queries, keys, seed=9)
+    want = luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks)
+    ws = torch.zeros(luvc.attn_cross_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    call = lambda: luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks, workspace=ws, device_status=status)       # noqa: E731
+    assert torch.equal(call(), want) and luvc.read_status(status) == 0
+    for _ in range(3):
+        assert luvc.lib.luvc_debug_wait_probes(1, 1, status.data_ptr(), stream) == 0
+        call()
+        assert luvc.read_status(status) == 10
+        assert luvc.lib.luvc_debug_wait_probes(0, 0, status.data_ptr(), stream) == 0
+        assert not ws[:2048].any()
+        assert torch.equal(call(), want) and luvc.read_status(status) == 0
