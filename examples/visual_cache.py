@@ -6,7 +6,7 @@ after) enter the cache of a group of decoder layers, their values enhanced by lo
 SPU prunes the visual tokens and the cache closes up; every image is forked into several questions; and all
 questions decode, one token per step, with the step captured in a CUDA graph.
 
-    python examples/visual_cache.py [--images 4] [--questions 3] [--steps 16] [--cache bf16|e4m3|f32]
+    python examples/visual_cache.py [--images 4] [--questions 3] [--steps 16] [--cache bf16|e4m3|e4m3-block|f32]
 
 The last step's attention is compared with dense attention over the tokens that should be in the cache, and the
 largest difference printed.
@@ -31,7 +31,7 @@ def run(images: int = 4, questions: int = 3, steps: int = 16, cache: str = "bf16
     dev = torch.device("cuda")
     g = torch.Generator(device=dev).manual_seed(seed)
     wide = torch.float32 if cache == "f32" else torch.bfloat16
-    pool_type = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}[cache]
+    pool_type = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn, "e4m3-block": torch.float8_e4m3fn}[cache]
     width, page, before, after = q_heads * dim, 16, 9, 17
 
     def normal(*shape, dtype=wide):
@@ -53,8 +53,11 @@ def run(images: int = 4, questions: int = 3, steps: int = 16, cache: str = "bf16
     max_pages = -(-(length + steps) // page)
     pages = images * 2 * -(-length // page) + images * questions * (2 + -(-steps // page))
     pool = torch.zeros((layers, pages, heads, page, dim), device=dev).to(pool_type)
+    # one scale for each layer and head, chosen beforehand, or one for each 16 tokens of a head, which follows from the rows
     scale = torch.full((layers, heads), 0.02, device=dev) if cache == "e4m3" else None
-    kv = luvc.KvCache(pool, pool.clone(), slots, max_pages, k_scale=scale, v_scale=scale)
+    if cache == "e4m3-block":
+        scale = torch.zeros((layers, pages, heads, page // luvc.KV_BLOCK), device=dev)
+    kv = luvc.KvCache(pool, pool.clone(), slots, max_pages, k_scale=scale, v_scale=scale.clone() if cache == "e4m3-block" else scale)
 
     # prompt: one ragged batch; text counts as one token, a merged token as the number it stands for
     count = torch.ones((images, length), dtype=torch.int32, device=dev)
@@ -129,7 +132,7 @@ def main():
     ap.add_argument("--images", type=int, default=4)
     ap.add_argument("--questions", type=int, default=3)
     ap.add_argument("--steps", type=int, default=16)
-    ap.add_argument("--cache", default="bf16", choices=["bf16", "e4m3", "f32"])
+    ap.add_argument("--cache", default="bf16", choices=["bf16", "e4m3", "e4m3-block", "f32"])
     a = ap.parse_args()
     r = run(a.images, a.questions, a.steps, a.cache)
     print("%d questions: %d tokens cached (%d without pruning), %d of %d pages in use, attention within %.2g of dense" % (
