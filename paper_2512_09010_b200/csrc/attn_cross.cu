@@ -258,7 +258,7 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
 }
 __device__ __forceinline__ float lse_of(const CrossArgs& a, float m, float l) { return l == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.nat, logf(l)); }
 
-// Sequences without states: rows of zeros.
+// Sequences without states: rows of zeros.  By a warp, or by a CTA of NT threads.
 template <typename T, int NT, typename W>
 __device__ void empty_sequences(const CrossArgs& a, const W& w) {
     for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
@@ -267,9 +267,9 @@ __device__ void empty_sequences(const CrossArgs& a, const W& w) {
         if (klen > 0) continue;
         const long long row = (long long)a.p.q_heads * a.p.D;
         T* const out = static_cast<T*>(a.p.out) + q0 * row;
-        for (long long e = threadIdx.x; e < qlen * row / 4; e += NT) put4(out + 4 * e, make_float4(0.f, 0.f, 0.f, 0.f));
+        for (long long e = threadIdx.x % NT; e < qlen * row / 4; e += NT) put4(out + 4 * e, make_float4(0.f, 0.f, 0.f, 0.f));
         if (a.p.lse)
-            for (long long e = threadIdx.x; e < (long long)qlen * a.p.q_heads; e += NT) a.p.lse[(long long)q0 * a.p.q_heads + e] = -INFINITY;
+            for (long long e = threadIdx.x % NT; e < (long long)qlen * a.p.q_heads; e += NT) a.p.lse[(long long)q0 * a.p.q_heads + e] = -INFINITY;
     }
 }
 
@@ -293,10 +293,9 @@ __device__ __forceinline__ bool arrive(unsigned* counter, int i, int n) {
 }
 
 // Adds the parts of an item, which CTAs c0 .. c1 have written, in order, and writes the result.  NT threads; each has E groups of four columns
-// at a time, and the parts of all of them on their way.
-template <typename T, int BM, int DP, int NT>
-__device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, int tid) {
-    constexpr int E = 4, B = 4;                                 // groups of columns; parts at a time
+// at a time, and B parts of all of them on their way.
+template <typename T, int BM, int DP, int NT, int E, int B>
+__device__ __forceinline__ void join_groups(const CrossArgs& a, const Item& it, int c0, int c1, int tid) {
     const int all = it.rows * (a.p.D / 4);
     for (int e0 = tid; e0 < all; e0 += E * NT) {
         int r[E], c[E];
@@ -364,6 +363,12 @@ __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, i
             if (c[e] == 0 && a.p.lse) a.p.lse[row] = lse_of(a, m[e], l[e]);
         }
     }
+}
+
+template <typename T, int BM, int DP, int NT>
+__device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, int tid) {
+    if (it.rows * (a.p.D / 4) <= NT) join_groups<T, BM, DP, NT, 1, 16>(a, it, c0, c1, tid);
+    else join_groups<T, BM, DP, NT, 4, 4>(a, it, c0, c1, tid);
 }
 
 // ---- f32 on the CUDA cores --------------------------------------------------------------------------------------------
@@ -747,10 +752,10 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     __syncthreads();                                            // barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    empty_sequences<__nv_bfloat16, T::THREADS>(a, work);
 
     if (warp >= 8) {
         give_registers<T::FEW>();
+        if (warp == 11) empty_sequences<__nv_bfloat16, 32>(a, work);
         // ---- K and V, tile after tile, through a ring of stages ----
         if (warp == 8 && lane == 0) {
             int pos = 0;                                        // K of the n-th tile of this CTA is 2 n, V 2 n + 1
@@ -1054,7 +1059,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 const unsigned long long to = mine_live ? reinterpret_cast<unsigned long long>(static_cast<__nv_bfloat16*>(p.out) + row * D) : 0ull;
                 // 32 columns of the warp's rows go through shared memory, four pieces of 16 bytes of a row each 2 KB apart or less: the place
                 // of the warp's own queries, or of what has just been added
-                float bad = l * 0.f;                            // 0, or NaN
+                float bad[4] = {l * 0.f, 0.f, 0.f, 0.f};        // 0, or NaN
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
@@ -1077,7 +1082,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                             }
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) bad = fmaf(y[e], 0.f, bad);
+                        for (int e = 0; e < 8; ++e) bad[e & 3] = fmaf(y[e], 0.f, bad[e & 3]);
                         if (whole) {
                             uint32_t w[4];
 #pragma unroll
@@ -1108,7 +1113,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                     else if (p.lse) p.lse[row] = lse_of(a, m, l);
                 }
                 __syncwarp();
-                for (unsigned again = __ballot_sync(~0u, mine_live && bad != 0.f && !*dead); again; again &= again - 1)
+                for (unsigned again = __ballot_sync(~0u, mine_live && bad[0] + bad[1] + (bad[2] + bad[3]) != 0.f && !*dead); again; again &= again - 1)
                     plain_row<DP>(a, it, __shfl_sync(~0u, mine, __ffs(again) - 1));
             };
             const bool merged = both && it.count > 1;
