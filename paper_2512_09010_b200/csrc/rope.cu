@@ -5,7 +5,8 @@
 // the inverse turn by -t.  f R(-t) is the transpose of f R(t), so the gradient of x is the inverse turn of the gradient of y.
 //
 // Bound.  Every element is read and written once, with a sine and a cosine for a pair that all heads of a token share: HBM, once there
-// are enough tokens.  16384 tokens of 40 heads of 128 (bf16, 336 MB): 63 us, 0.81 of the copy rate; the smallest calls are a chain of latencies
+// are enough tokens.  16384 tokens of 40 heads of 128 (bf16, 336 MB): 57 us, 0.90 of the copy rate (two CTAs of an SM instead of three,
+// with twice the tokens: 63); the smallest calls are a chain of latencies
 // (launch, position, sine, row).
 //
 // Angles.  A position of a long context times a frequency near 1 has more turns than a float has bits for the rest: the turns,
@@ -93,7 +94,7 @@ template <int W> struct Piece<__nv_bfloat16, W> {
 // INTER: pairs are neighbours, a piece holds W / 2 of them; else a piece of W elements has its partners `half` elements on.  Places past
 // the pairs are copied.
 template <typename T, int W, bool INTER>
-__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(384, 3) rope_kernel(const __grid_constant__ RopeArgs a) {
     // (cos, sin) times the factor, of each token's pairs: pair k of all pieces side by side, so that threads next to one another meet
     // no bank twice
     __shared__ float2 table[kRopeTable];
@@ -186,9 +187,9 @@ int launch(RopeArgs& a, cudaStream_t stream) {
     a.cols = (int)((row + sweeps - 1) / sweeps);
     a.step = a.cols >= 256 ? 1 : 256 / a.cols;
     const int threads = (a.cols * a.step + 31) / 32 * 32;
-    // tokens of a CTA: two rounds of loads each, fewer while that leaves SMs without work, as many as the table has room for
+    // tokens of a CTA: one round of loads each, fewer while that leaves SMs without work, as many as the table has room for
     const long long even = ((long long)a.tokens + 2 * sms - 1) / (2 * sms);
-    const int most = kRopeTable / a.half, full = 2 * kRopeBatch * a.step;
+    const int most = kRopeTable / a.half, full = kRopeBatch * a.step;
     a.per = (int)(even < full ? even : full);
     if (a.per > most) a.per = most;
     return launch_overlapped(rope_kernel<T, W, INTER>, (unsigned)((a.tokens - 1) / a.per + 1), threads, 0, stream, a);
