@@ -681,37 +681,48 @@ def rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, *, axis:
     tensor whose tokens are contiguous) turned by positions * freqs.  positions: int32 [tokens], or [axes, tokens] with
     axis (int32 [len(freqs)]) naming the row that turns each pair.  interleaved: pairs are neighbours, not halves apart;
     inverse: turned back, which is also the gradient; factor: of the turned elements; out: x itself for in place."""
-    code = _dtype_code(x)
-    if x.dim() != 3 or not x.is_cuda:
+    shape, dtype, index = x.shape, x.dtype, x.get_device()
+    if len(shape) != 3 or index < 0:
+        _dtype_code(x)
         raise ValueError("x must be a CUDA tensor [tokens, heads, D]")
-    tokens, heads, D = x.shape
-    index = x.get_device()
-
-    def stride(t, name):
-        s0, s1, s2 = t.stride()
-        if (s2 != 1 and D > 1) or (s1 != D and heads > 1):
-            raise ValueError("%s: the heads * D elements of a token must be contiguous" % name)
-        return s0 if tokens > 1 else heads * D          # the stride of a lone token is not used
-
+    tokens, heads, D = shape
+    s0, s1, s2 = x.stride()
+    if s2 != 1 or (s1 != D and heads > 1):
+        raise ValueError("x: the heads * D elements of a token must be contiguous")
+    dense = heads * D
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index:
-        raise ValueError("out must be a tensor of x's shape, type and device")
-    if freqs.dtype is not torch.float32 or freqs.dim() != 1 or freqs.get_device() != index or not freqs.is_contiguous():
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out_stride = dense
+    else:
+        o0, o1, o2 = out.stride() if out.dim() == 3 else (0, 0, 0)
+        if out.shape != shape or out.dtype is not dtype or out.get_device() != index or o2 != 1 or (o1 != D and heads > 1):
+            raise ValueError("out must be a tensor of x's shape, type and device whose tokens are contiguous")
+        out_stride = o0 if tokens > 1 else dense
+    pairs = freqs.shape
+    if freqs.dtype is not torch.float32 or len(pairs) != 1 or freqs.get_device() != index or not freqs.is_contiguous():
         raise ValueError("freqs must be a contiguous float32 tensor [rotary / 2] on x's device")
-    axes = positions.shape[0] if positions.dim() == 2 else 1
-    if positions.dtype is not _INT32 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or positions.get_device() != index \
+    rows = positions.shape
+    if positions.dtype is not _INT32 or rows[-1:] != shape[:1] or len(rows) > 2 or positions.get_device() != index \
             or (tokens > 1 and positions.stride(-1) != 1):
         raise ValueError("positions must be an int32 tensor [tokens] or [axes, tokens] on x's device, its rows contiguous")
-    if (axis is not None or axes > 1) and (axis is None or axis.dtype is not _INT32 or axis.shape != freqs.shape
-                                           or axis.get_device() != index or not axis.is_contiguous()):
-        raise ValueError("several rows of positions go with axis, a contiguous int32 tensor of freqs' shape")
-    o = RopeOpts(_raw_stream(index), axis.data_ptr() if axis is not None else None, axes,
-                 positions.stride(0) if axes > 1 else 0, int(interleaved), int(inverse), factor)
-    if factor == 0:
-        raise ValueError("factor must not be 0")
-    _call_on(index, lib.luvc_rope, x.data_ptr(), stride(x, "x"), positions.data_ptr(), freqs.data_ptr(), tokens, heads, D,
-             2 * freqs.numel(), code, out.data_ptr(), stride(out, "out"), o)
+    o = RopeOpts(_raw_stream(index))
+    if len(rows) == 2 and rows[0] != 1 or axis is not None:
+        if axis is None or axis.dtype is not _INT32 or axis.shape != pairs or axis.get_device() != index or not axis.is_contiguous():
+            raise ValueError("several rows of positions go with axis, a contiguous int32 tensor of freqs' shape")
+        o.axis = axis.data_ptr()
+        if len(rows) == 2:
+            o.axes, o.position_stride = rows[0], positions.stride(0)
+    if interleaved:
+        o.interleaved = 1
+    if inverse:
+        o.inverse = 1
+    if factor != 1.0:
+        if factor == 0:
+            raise ValueError("factor must not be 0")
+        o.factor = factor
+    # the stride of a lone token is not used
+    _call_on(index, lib.luvc_rope, x.data_ptr(), s0 if tokens > 1 else dense, positions.data_ptr(), freqs.data_ptr(), tokens, heads, D,
+             2 * pairs[0], _dtype_code(x), out.data_ptr(), out_stride, o)
     return out
 
 
