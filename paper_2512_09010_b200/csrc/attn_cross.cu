@@ -1248,9 +1248,22 @@ int launch_tc_bias(CrossArgs& a) {
 
 }  // namespace
 
-size_t attn_cross_workspace_bytes() { return kCounterBytes + kPartsBytes; }
+size_t attn_cross_workspace_bytes() { return align_up(kCounterBytes + kPartsBytes) + attn_workspace_bytes(); }
 
 int attn_cross(const CrossProblem& p) {
+    // No more tokens than sequences (a decode step): each token on its own, in the form that attends from one token to a cache, of 16 rows a
+    // tile where this one has 128 (16 tokens to 1296 states each, 28 / 4 heads of 128: ROWS_US, as tiles of 128 rows 25; f32, 8 tokens to 576
+    // states, 16 / 16 heads of 64: ROWS_F32, 34).
+    if (p.q_tokens <= p.n && p.q_tokens <= kAttnRowsMost && p.k_tokens > 0) {
+        AttnProblem r = {};
+        r.c.k = const_cast<void*>(p.k); r.c.v = const_cast<void*>(p.v); r.c.heads = p.heads; r.c.D = p.D; r.c.dtype = p.dtype;
+        r.c.layers = r.c.pages = r.c.max_pages = r.c.slots = 1; r.c.page_size = kKvBlock;
+        r.q = p.q; r.q_stride = p.q_stride; r.bias = p.bias; r.bias_width = p.bias ? p.k_tokens : 0; r.out = p.out; r.lse = p.lse;
+        r.n = p.q_tokens; r.q_heads = p.q_heads; r.scale = p.scale; r.status = p.status; r.stream = p.stream;
+        r.workspace = static_cast<unsigned char*>(p.workspace) + align_up(kCounterBytes + kPartsBytes);
+        r.q_starts = p.q_starts; r.k_starts = p.k_starts; r.n_seqs = p.n; r.k_tokens = p.k_tokens; r.k_stride = p.k_stride; r.v_stride = p.v_stride;
+        return attn_rows(r);
+    }
     CrossArgs a;
     a.p = p;
     a.group = p.q_heads / p.heads;

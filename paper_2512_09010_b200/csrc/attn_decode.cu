@@ -74,6 +74,10 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(row) : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 // The barrier's phase waits for so many bytes more.
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -398,11 +402,11 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 // a value near the end of the range turns into NaN (inf times the lower part of a weight, which may be 0 or negative; inf - inf), and
 // weights above 1, while their reference lags behind, can take values beyond that end.  So a result that is not finite is worked out
 // again.  It is rare, and need not be fast.
-template <typename T, int DP>
-__device__ __noinline__ void plain_piece(const Args& a, int seq, int h, int r0, int rows, int t0, int t1, float scale, float* os, float2* ml) {
+template <typename T, int DP, bool DENSE>
+__device__ __noinline__ void plain_piece(const Args& a, int seq, int k0, int h, int r0, int rows, int t0, int t1, float scale, float* os, float2* ml) {
     const AttnProblem& p = a.p;
     const int lane = threadIdx.x & 31, ps = p.c.page_size, D = p.c.D;
-    const int32_t* const table = p.c.table + (long long)(p.seqs ? p.seqs[seq] : seq) * p.c.max_pages;
+    const int32_t* const table = DENSE ? nullptr : p.c.table + (long long)(p.seqs ? p.seqs[seq] : seq) * p.c.max_pages;
     const T* const q0 = static_cast<const T*>(p.q) + seq * p.q_stride + ((long long)h * a.group + r0) * D;
     const size_t layer = (size_t)p.layer * a.rows_total;
     for (int r = 0; r < rows; ++r) {
@@ -413,11 +417,12 @@ __device__ __noinline__ void plain_piece(const Args& a, int seq, int h, int r0, 
             o[j] = 0.f;
         }
         for (int t = t0; t < t1; ++t) {
-            const float bias = t < p.bias_width ? p.bias[seq * p.bias_stride + t] : 0.f;
-            const int page = table[t / ps];
+            const float bias = t < p.bias_width ? p.bias[DENSE ? (long long)k0 + t : seq * p.bias_stride + t] : 0.f;
+            const int page = DENSE ? 0 : table[t / ps];
             if (bias == -INFINITY) continue;
-            const bool held = (unsigned)page < (unsigned)p.c.pages;         // as in the tiles: rows of no page are zeros
-            const size_t at = (layer + (held ? (page * p.c.heads + h) * ps + t % ps : 0)) * D;
+            const bool held = DENSE || (unsigned)page < (unsigned)p.c.pages;        // as in the tiles: rows of no page are zeros
+            const size_t row = DENSE ? 0 : (layer + (held ? (page * p.c.heads + h) * ps + t % ps : 0)) * D;
+            const size_t at = DENSE ? ((size_t)k0 + t) * p.k_stride + h * D : row, v_at = DENSE ? ((size_t)k0 + t) * p.v_stride + h * D : row;
             float s = 0.f, v[DP / 32];
 #pragma unroll
             for (int j = 0; j < DP / 32; ++j) {
@@ -425,27 +430,37 @@ __device__ __noinline__ void plain_piece(const Args& a, int seq, int h, int r0, 
                 v[j] = 0.f;
                 if (held && d < D) {
                     s = fmaf(q[j], as_float(static_cast<const T*>(p.c.k)[at + d]), s);
-                    v[j] = as_float(static_cast<const T*>(p.c.v)[at + d]);
+                    v[j] = as_float(static_cast<const T*>(p.c.v)[v_at + d]);
                 }
             }
 #pragma unroll
             for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
             s = fmaf(s, scale, bias);
             const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-            const float f = exp2_fast((m - base) * kLog2e), w = exp2_fast((s - base) * kLog2e);
+            float f = exp2_fast((m - base) * kLog2e), w = exp2_fast((s - base) * kLog2e);
             m = top;
-            l = fmaf(l, f, w);
+            const float sum = fmaf(l, f, w);
+            if constexpr (DENSE) {                              // o is the mean so far: values near the end of the range stay inside it
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                f *= l * inv;
+                w *= inv;
+            }
+            l = sum;
 #pragma unroll
             for (int j = 0; j < DP / 32; ++j) o[j] = lane + 32 * j < D ? fmaf(o[j], f, w * v[j]) : 0.f;
         }
+        // the mean as a partial result whose weights sum to 2^-20: joins add up many of them
+        const float of_sum = DENSE ? 0x1p-20f : 1.f;
 #pragma unroll
-        for (int j = 0; j < DP / 32; ++j) os[o_index(r, lane + 32 * j, DP)] = o[j];
-        if (lane == 0) ml[r] = make_float2(m, l);
+        for (int j = 0; j < DP / 32; ++j) os[o_index(r, lane + 32 * j, DP)] = o[j] * of_sum;
+        if (lane == 0) ml[r] = DENSE && l > 0.f ? make_float2(m + logf(l) + 13.862944f, of_sum) : make_float2(m, l);
     }
     __syncwarp();
 }
 
-template <typename TQ, typename TC, int DPB, int NT>
+// DENSE: the "sequences" are tokens, each of a sequence whose keys and values are not in pages but consecutive rows (luvc_attn_cross with
+// few tokens).
+template <typename TQ, typename TC, int DPB, int NT, bool DENSE>
 __global__ void __launch_bounds__(32 * Shape<TC, DPB, NT>::NW, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ Args a) {
     using Sh = Shape<TC, DPB, NT>;
@@ -464,6 +479,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __shared__ int last_flag[2], all_flag;
     unsigned char* const ring = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* const prefix = reinterpret_cast<int*>(ring + NW * S * Sh::STAGE);      // [n + 1] tiles of the sequences before i
+    int* const dense_len = prefix + a.p.n + 1;                  // DENSE: [n] rows of a token's sequence, -1: of none; the first one
+    int* const dense_first = dense_len + a.p.n;
 
     const AttnProblem& p = a.p;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n, ps = p.c.page_size;
@@ -490,7 +507,27 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int segs = p.c.heads * a.groups;
     bool fits;
     int base, lane_tiles = 0, lane_first = 0;                   // tiles of all sequences; up to 32 of them: those of lane, and before it
+    auto len_at = [&](int i) { return DENSE ? max(dense_len[i], 0) : length_of(slot_of(i)); };
     auto tiles_of = [&](int i) {
+        if constexpr (DENSE) {
+            auto inside = [](int x, int most) { return min(max(x, 0), most); };
+            int s = i;                                          // mostly each token is its sequence's only one
+            bool owned = true;
+            if (p.q_starts && !(i < p.n_seqs && p.q_starts[i] == i && p.q_starts[i + 1] == i + 1)) {
+                int lo = 0, hi = p.n_seqs;                      // q_starts[lo] <= i < q_starts[hi]
+                owned = p.q_starts[0] <= i && i < p.q_starts[hi];
+                while (owned && hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (p.q_starts[mid] <= i) lo = mid; else hi = mid;
+                }
+                s = lo;
+            }
+            const int first = owned ? inside(p.k_starts[s], p.k_tokens) : 0;
+            const int len = owned ? max(inside(p.k_starts[s + 1], p.k_tokens) - first, 0) : -1;
+            dense_len[i] = len;
+            dense_first[i] = first;
+            return (int)(((unsigned)max(len, 0) + (KT - 1u)) / (unsigned)KT);
+        }
         const int slot = slot_of(i);
         if (slot < 0 || slot >= p.c.slots) *p.status = LUVC_ERR_SHAPE;
         return (int)(((unsigned)length_of(slot) + (KT - 1u)) / (unsigned)KT);       // (up to 2^31 - 1 tokens)
@@ -542,7 +579,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
     // sequences without tokens
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
-        if (prefix[i + 1] != prefix[i]) continue;
+        if (prefix[i + 1] != prefix[i] || (DENSE && dense_len[i] < 0)) continue;
         for (int e = tid; e < p.q_heads * (p.c.D / 4); e += NTHR)
             put4(static_cast<TQ*>(p.out) + (long long)i * p.q_heads * p.c.D + 4 * e, make_float4(0.f, 0.f, 0.f, 0.f));
         if (p.lse)
@@ -606,7 +643,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         // what is to be loaded next
         Place ld = place_of(wa);
         int to_load = wb - wa;
-        int ld_left = 0, ld_page = 0, ld_off = 0, ld_len = 0, ld_h = 0, pg_first = 0, pg = -1;
+        int ld_left = 0, ld_page = 0, ld_off = 0, ld_len = 0, ld_h = 0, pg_first = 0, pg = -1, ld_first = 0;
         const int32_t* ld_row = nullptr;
         auto fetch_pages = [&] {
             pg_first = ld_page;
@@ -614,15 +651,19 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         };
         auto load_start = [&](bool new_seq) {                   // at a new (sequence, head), or at the warp's first tile
             if (new_seq) {
-                const int slot = slot_of(ld.seq);
-                ld_len = length_of(slot);
-                ld_row = p.c.table + (long long)slot * p.c.max_pages;
+                ld_len = len_at(ld.seq);
+                if constexpr (DENSE) ld_first = dense_first[ld.seq];
+                else ld_row = p.c.table + (long long)slot_of(ld.seq) * p.c.max_pages;
             }
             const int token = ld.tile * KT;
             ld_left = ld_len - token;
-            ld_page = a.page_shift >= 0 ? token >> a.page_shift : token / ps;
-            ld_off = token - ld_page * ps;
-            if (new_seq || ld_page < pg_first || ld_page >= pg_first + 32) fetch_pages();
+            if constexpr (DENSE) {
+                ld_off = token;
+            } else {
+                ld_page = a.page_shift >= 0 ? token >> a.page_shift : token / ps;
+                ld_off = token - ld_page * ps;
+                if (new_seq || ld_page < pg_first || ld_page >= pg_first + 32) fetch_pages();
+            }
             ld_h = a.groups == 1 ? ld.seg : ld.seg / a.groups;
             // its queries are wanted soon
             const int r0 = (ld.seg - ld_h * a.groups) * ROWS;
@@ -640,7 +681,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < Sh::SUB; ++j) {
-                if (j == 0 || 16 * j < ld_left) {
+                if (DENSE && (j == 0 || 16 * j < ld_left)) {
+                    if (lane < 2 * Sh::SEGS)
+                        tma_load_3d(my_dst + stage * Sh::STAGE + j * 2 * Sh::SUBK, my_map, bar, (lane >> 1) * (Sh::PITCH / Sh::ES), ld_h, ld_first + ld_off);
+                    ld_off += 16;
+                } else if (j == 0 || 16 * j < ld_left) {
                     if (ld_page >= pg_first + 32) fetch_pages();
                     const int page = __shfl_sync(~0u, pg, ld_page - pg_first);
                     const int row = (unsigned)page < (unsigned)p.c.pages ? (page * p.c.heads + ld_h) * ps + ld_off : a.rows_total;
@@ -687,7 +732,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         while (left > 0) {
             const int h = a.groups == 1 ? at.seg : at.seg / a.groups, r0 = (at.seg - h * a.groups) * ROWS;
             const int rows = min(ROWS, a.group - r0);
-            const int len = length_of(slot_of(at.seq));
+            const int len = len_at(at.seq);
             const float vscale = !kBlocks && p.c.v_scale ? p.c.v_scale[p.layer * p.c.heads + h] : 1.f;
             const float scale = p.scale * (!kBlocks && p.c.k_scale ? p.c.k_scale[p.layer * p.c.heads + h] : 1.f);
             // blocks: the sums O are in units of v_unit, which follows the blocks' scales and is never far below the largest so far
@@ -813,7 +858,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         for (int x = 0; x < 2; ++x) {
                             const int token = at.tile * KT + 16 * j + (kCores ? lane & 15 : 8 * x + g);
                             if (token >= len) bias[j][x] = -INFINITY;
-                            else if (token < p.bias_width) bias[j][x] = p.bias[at.seq * p.bias_stride + token];
+                            else if (token < p.bias_width) bias[j][x] = p.bias[DENSE ? (long long)dense_first[at.seq] + token : at.seq * p.bias_stride + token];
                         }
                 if (!dead) {
                     const uint32_t bar = my_bar + 8 * stage;
@@ -1174,7 +1219,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                         for (int j = 0; j < DP / 32; ++j) z[j & 3] = fmaf(core_o[r][j], 0.f, z[j & 3]);
                 if (__any_sync(~0u, z[0] + z[1] + (z[2] + z[3]) != 0.f) && !dead)
-                    plain_piece<TC, DP>(a, at.seq, h, r0, rows, (at.tile - count) * KT, min(at.tile * KT, len), scale, os, ml_of[warp][which]);
+                    plain_piece<TC, DP, DENSE>(a, at.seq, DENSE ? dense_first[at.seq] : 0, h, r0, rows, (at.tile - count) * KT, min(at.tile * KT, len), scale, os, ml_of[warp][which]);
             }
             const long long row0 = (long long)at.seq * p.q_heads + h * a.group + r0;
             if (whole) {
@@ -1439,7 +1484,20 @@ bool layer_map(CUtensorMap* map, const luvc_kv_cache& c, void* pool, int layer, 
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename TQ, typename TC, int DPB, int NT>
+// Consecutive rows of all heads, [k_tokens][heads][D], fetched in boxes of 16 rows of a head by PITCH bytes.
+template <typename TC, int PITCH>
+bool dense_map(CUtensorMap* map, const AttnProblem& p, void* rows, long long stride) {
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)p.c.D, (cuuint64_t)p.c.heads, (cuuint64_t)p.k_tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)p.c.D * sizeof(TC), (cuuint64_t)stride * sizeof(TC)};
+    const cuuint32_t box[3] = {PITCH / (cuuint32_t)sizeof(TC), 1u, 16u}, ones[3] = {1u, 1u, 1u};
+    return encode(map, sizeof(TC) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, rows, dims, strides, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, PITCH == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename TQ, typename TC, int DPB, int NT, bool DENSE>
 int launch(const AttnProblem& p) {
     using Sh = Shape<TC, DPB, NT>;
     Args a;
@@ -1455,36 +1513,51 @@ int launch(const AttnProblem& p) {
     a.counters = static_cast<unsigned*>(p.workspace);
     a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kCounterBytes);
     CUtensorMap kmap, vmap;
-    if (!layer_map<TC, Sh::PITCH>(&kmap, p.c, p.c.k, p.layer, a.rows_total) ||
-        !layer_map<TC, Sh::PITCH>(&vmap, p.c, p.c.v, p.layer, a.rows_total))
+    if constexpr (DENSE) {
+        if (!dense_map<TC, Sh::PITCH>(&kmap, p, p.c.k, p.k_stride) || !dense_map<TC, Sh::PITCH>(&vmap, p, p.c.v, p.v_stride)) return LUVC_ERR_CUDA;
+    } else if (!layer_map<TC, Sh::PITCH>(&kmap, p.c, p.c.k, p.layer, a.rows_total) ||
+               !layer_map<TC, Sh::PITCH>(&vmap, p.c, p.c.v, p.layer, a.rows_total)) {
         return LUVC_ERR_CUDA;
-    const size_t smem = 1024 + (size_t)Sh::NW * Sh::S * Sh::STAGE + (size_t)(p.n + 1) * sizeof(int);
+    }
+    static_assert(3 * kAttnRowsMost <= kKvMaxSeqs, "the attribute below is enough");
+    const size_t smem = 1024 + (size_t)Sh::NW * Sh::S * Sh::STAGE + (size_t)((DENSE ? 3 : 1) * p.n + 1) * sizeof(int);
     static std::atomic<unsigned long long> set{0};              // devices on which the kernel may use this much
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return LUVC_ERR_CUDA;
     if (dev > 63 || !((set.load(std::memory_order_relaxed) >> dev) & 1)) {
-        if (cudaFuncSetAttribute(attn_decode_kernel<TQ, TC, DPB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        if (cudaFuncSetAttribute(attn_decode_kernel<TQ, TC, DPB, NT, DENSE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  1024 + Sh::NW * Sh::S * Sh::STAGE + (kKvMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess) {
             cudaGetLastError();
             return LUVC_ERR_CUDA;
         }
         if (dev <= 63) set.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    return launch_overlapped(attn_decode_kernel<TQ, TC, DPB, NT>, sms, 32 * Sh::NW, smem, p.stream, kmap, vmap, a);
+    return launch_overlapped(attn_decode_kernel<TQ, TC, DPB, NT, DENSE>, sms, 32 * Sh::NW, smem, p.stream, kmap, vmap, a);
 }
 
-template <typename TQ, typename TC, int DPB>
+template <typename TQ, typename TC, int DPB, bool DENSE = false>
 int launch_heads(const AttnProblem& p) {
-    return p.q_heads / p.c.heads <= 8 ? launch<TQ, TC, DPB, 1>(p) : launch<TQ, TC, DPB, 2>(p);
+    return p.q_heads / p.c.heads <= 8 ? launch<TQ, TC, DPB, 1, DENSE>(p) : launch<TQ, TC, DPB, 2, DENSE>(p);
 }
 
 // f32 caches with up to four query heads per key head run on the CUDA cores (measured, against the tensor cores: 32 / 32 heads of
 // 128, 812 MB, 141 and 168 us; 16 / 16 of 64, 203 MB, 42.7 and 42.4, 38 MB 12.3 and 15.3; 32 / 8 of 128, 203 MB, 49 and 52; 8 / 8 of
 // 256, 406 MB, 89 and 141), and all with rows longer than 512 bytes, four heads at a time (79 MB: 12 / 1 heads of 256 64 and 68 us, 8 / 1
 // 50 and 53).  The others do not: 28 / 4 of 128, 158 MB, 63 us in this form, 46 on the tensor cores; 16 / 2 of 64, 40 MB, 24 and 16.
-template <int DPB>
+template <int DPB, bool DENSE>
 int launch_cores(const AttnProblem& p) {
-    return p.q_heads == p.c.heads ? launch<float, float, DPB, -1>(p) : launch<float, float, DPB, -4>(p);
+    return p.q_heads == p.c.heads ? launch<float, float, DPB, -1, DENSE>(p) : launch<float, float, DPB, -4, DENSE>(p);
+}
+
+template <bool DENSE>
+int launch_wide(const AttnProblem& p) {                         // f32 and bf16
+    const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
+    if (p.c.dtype == LUVC_F32 && (p.q_heads <= 4 * p.c.heads || bytes > 512))
+        return bytes <= 256 ? launch_cores<256, DENSE>(p) : bytes <= 512 ? launch_cores<512, DENSE>(p) : launch_cores<1024, DENSE>(p);
+    if (p.c.dtype == LUVC_F32)
+        return bytes <= 256 ? launch_heads<float, float, 256, DENSE>(p) : launch_heads<float, float, 512, DENSE>(p);
+    return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128, DENSE>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256, DENSE>(p)
+                                                                                                   : launch_heads<__nv_bfloat16, __nv_bfloat16, 512, DENSE>(p);
 }
 
 }  // namespace
@@ -1493,18 +1566,14 @@ size_t attn_workspace_bytes() { return kCounterBytes + (size_t)2 * kMaxCtas * 2 
 
 int attn_decode(const AttnProblem& p) {
     const int bytes = p.c.D * (int)kv_elem_size(p.c.dtype);
-    if (p.c.dtype == LUVC_F32 && (p.q_heads <= 4 * p.c.heads || bytes > 512))
-        return bytes <= 256 ? launch_cores<256>(p) : bytes <= 512 ? launch_cores<512>(p) : launch_cores<1024>(p);
-    if (p.c.dtype == LUVC_F32)
-        return bytes <= 256 ? launch_heads<float, float, 256>(p) : launch_heads<float, float, 512>(p);
-    if (p.c.dtype == LUVC_BF16)
-        return bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 128>(p) : bytes <= 256 ? launch_heads<__nv_bfloat16, __nv_bfloat16, 256>(p)
-                                                                                               : launch_heads<__nv_bfloat16, __nv_bfloat16, 512>(p);
+    if (p.c.dtype == LUVC_F32 || p.c.dtype == LUVC_BF16) return launch_wide<false>(p);
     if (p.c.dtype == LUVC_E4M3_BLOCK)
         return bytes <= 64 ? launch_heads<__nv_bfloat16, E4m3Block, 64>(p) : bytes <= 128 ? launch_heads<__nv_bfloat16, E4m3Block, 128>(p)
                                                                                           : launch_heads<__nv_bfloat16, E4m3Block, 256>(p);
     // rows of 64 bytes halve the conversions and products (16 / 16 heads of 64, 79 MB: 28.0 us, as rows of 128 bytes 35.1)
     return bytes <= 64 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 64>(p) : bytes <= 128 ? launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 128>(p) : launch_heads<__nv_bfloat16, __nv_fp8_e4m3, 256>(p);
 }
+
+int attn_rows(const AttnProblem& p) { return launch_wide<true>(p); }
 
 }  // namespace luvc

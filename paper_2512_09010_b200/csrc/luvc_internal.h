@@ -231,9 +231,16 @@ struct AttnProblem {
     void* workspace;
     int* status;
     cudaStream_t stream;
+    // attn_rows: n tokens (at most kAttnRowsMost) of n_seqs sequences, whose keys and values are the rows k_starts[s] .. k_starts[s + 1] - 1
+    // at c.k and c.v (heads, D and dtype are c's); the bias has a value for each row
+    const int32_t *q_starts = nullptr, *k_starts = nullptr;
+    int n_seqs = 0, k_tokens = 0;
+    long long k_stride = 0, v_stride = 0;
 };
+constexpr int kAttnRowsMost = 1024;
 size_t attn_workspace_bytes();
 int attn_decode(const AttnProblem& p);
+int attn_rows(const AttnProblem& p);
 
 // ---- attention to an encoder's states (attn_cross.cu) ----------------------------------------------
 

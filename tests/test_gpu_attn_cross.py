@@ -287,3 +287,34 @@ def test_a_wait_that_gives_up(luvc, hq, heads, D, queries, keys):
         assert luvc.lib.luvc_debug_wait_probes(0, 0, status.data_ptr(), stream) == 0
         assert not ws[:2048].any()
         assert torch.equal(call(), want) and luvc.read_status(status) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_few_tokens(luvc, dtype, shape):
+    """No more tokens than sequences: some have several, some none; rows of no sequence are left as they are."""
+    hq, heads, D = shape
+    if dtype == "bf16" and D % 8:
+        D += 4
+    for queries, keys, more in (([2, 0, 0, 1, 0, 0, 0, 0], [40, 0, 9, 1300, 5, 0, 64, 2], 3), ([0, 0, 5, 0, 0, 0], [1, 2, 777, 0, 3, 3], 0),
+                                ([0, 1, 0, 1], [16, 0, 200, 33], 1), ([1] * 40, [37 * i % 211 for i in range(40)], 0), ([0] * 35 + [30], [3] * 35 + [500], 4)):
+        q, k, v, qs, ks = inputs(dtype, hq, heads, D, queries, keys, seed=D, q_more=more, k_before=2, k_more=5)
+        bias = torch.randn(k.shape[0], generator=torch.Generator().manual_seed(1)).cuda()
+        bias[::5] = -math.inf
+        for b in (None, bias):
+            out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+            out, lse = luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks, key_bias=b, want_lse=True, out=out)
+            assert luvc.check_status() == 0
+            check(q, k, v, qs, ks, out, lse, bias=b)
+            assert more == 0 or bool((out[-more:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_thousand_single_tokens(luvc, dtype):
+    keys = [(53 * i) % 300 for i in range(1024)]
+    for n in (1024, 1025):                                      # in the one form and in the other
+        q, k, v, qs, ks = inputs(dtype, 4, 2, 64, [1] * n, keys + [7] * (n - 1024))
+        out, lse = luvc.attn_cross(q, k, v, k_starts=ks, want_lse=True)
+        assert luvc.check_status() == 0
+        for i in list(range(0, n, 53)) + [n - 1]:
+            check(q, k, v, qs[i:i + 2], ks[i:i + 2], out, lse)
