@@ -1251,10 +1251,15 @@ int launch_tc_bias(CrossArgs& a) {
 size_t attn_cross_workspace_bytes() { return align_up(kCounterBytes + kPartsBytes) + attn_workspace_bytes(); }
 
 int attn_cross(const CrossProblem& p) {
-    // No more tokens than sequences (a decode step): each token on its own, in the form that attends from one token to a cache, of 16 rows a
-    // tile where this one has 128 (16 tokens to 1296 states each, 28 / 4 heads of 128: ROWS_US, as tiles of 128 rows 25; f32, 8 tokens to 576
-    // states, 16 / 16 heads of 64: ROWS_F32, 34).
-    if (p.q_tokens <= p.n && p.q_tokens <= kAttnRowsMost && p.k_tokens > 0) {
+    // Few tokens go each on its own, in the form that attends from one token to a cache (tiles of 16 rows where this file's have 128), which reads
+    // a sequence's states once for each of its tokens.  Where no sequence need have two (a decode step) that is nothing lost: 16 tokens to 1296
+    // states each, 28 / 4 heads of 128, 14.6 us, in blocks of 128 rows 24.8; f32, 8 tokens to 576 states, 16 / 16 heads of 64, 8.8 and 34.
+    // Beyond that it takes a microsecond for 10 MB read, and blocks take two and one for 150 states more than it does for little (8 sequences of
+    // 2, 4, 8 tokens, 1296 states: 15.9, 19.6, 28.0 us, blocks 25; 32 of 4, 300 states: 18.8 and 17.8; one of 4, 16384: 24 and 31); f32 blocks
+    // about twice that (8 of 2 and 4: 40 and 68 us, blocks 67 and 72; 32 / 8 heads of 128).
+    const double states = (double)p.k_tokens / p.n, mb = p.q_tokens * states * p.heads * p.D * (p.dtype == LUVC_F32 ? 8e-6 : 4e-6);
+    const bool alone = p.q_tokens <= p.n || 0.1 * mb <= (p.dtype == LUVC_F32 ? 2. : 1.) * (2. + std::min(states, 2000.) / 150.);
+    if (alone && p.q_tokens <= kAttnRowsMost && p.k_tokens > 0) {
         AttnProblem r = {};
         r.c.k = const_cast<void*>(p.k); r.c.v = const_cast<void*>(p.v); r.c.heads = p.heads; r.c.D = p.D; r.c.dtype = p.dtype;
         r.c.layers = r.c.pages = r.c.max_pages = r.c.slots = 1; r.c.page_size = kKvBlock;
