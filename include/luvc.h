@@ -495,7 +495,8 @@ int luvc_kv_reserve(const luvc_kv_cache* cache, const int32_t* seqs, int n, cons
  * the start of their sequence, or whose slot is out of range, are not written (LUVC_ERR_SHAPE in the status
  * word); all others are, also by the luvc_kv_write calls that follow, until another call finds the word.  (Until
  * luvc_read_status it may hold the status in its low 8 bits.)  Tokens that a fork shares are
- * shared: writing them again writes them for every sequence that holds their page.
+ * shared: writing them again writes them for every sequence that holds their page (into a LUVC_E4M3_BLOCK cache by one sequence of a call
+ * at most: a block and its scale belong together).
  */
 int luvc_kv_write(const luvc_kv_cache* cache, int layer, const int32_t* seqs, int n, const void* k, const void* v,
                   long long k_stride, long long v_stride, int tokens, const int32_t* starts, const int32_t* sizes,
@@ -615,7 +616,8 @@ typedef struct {
  * tokens with 16 bits).  A call
  * repeated gives the same bits; how the work is split, and with it the last bits, depends on all lengths of the call.  The call runs
  * whatever the status word says.
- * Limits: D a multiple of 8 (bf16) or 4 (fp32) up to 256; q_heads up to 65536, a multiple of heads; n up to 4096.
+ * Limits: D a multiple of 8 (bf16) or 4 (fp32) up to 256; q_heads up to 65536, a multiple of heads; n up to 4096.  A call of 2^31 tiles
+ * (16 rows of a key head by 16 states at least) or more does nothing (LUVC_ERR_SHAPE in the status word).
  */
 int luvc_attn_cross(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride, int n,
                     const int32_t* q_starts, const int32_t* k_starts, int q_tokens, int k_tokens, int q_heads, int heads, int D, int dtype,

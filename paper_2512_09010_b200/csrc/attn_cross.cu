@@ -13,7 +13,12 @@
 // adds the parts, in the order of the list, so that a repeated call gives the same bits.  Where there is little to do, the parts are whole
 // (sequence, key head, block of rows)s: a join costs as much as some tiles (JOIN).
 //
-// bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums.
+// Bound.  4 D flops for each row and state: the tensor pipe, where there are many rows.  Two sequences of 1777 to 2048 tokens to 12001 to 16384
+// states, 32 / 8 heads of 128 (970 GFLOP, bf16): 1120 us, 0.51 of the rate of a large matrix product (one of 2048 to 16384: 540 us for 550 GFLOP,
+// 0.60).  Eight questions of 17 to 96 tokens to 1296 states, 28 / 4 heads: 27.5 us, a chain of latencies.  A few tokens are a matter of bytes, and
+// go another way (attn_rows).
+//
+// bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums, 44 TFLOP/s of 73 that packed products reach.
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -373,8 +378,9 @@ __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, i
 
 // ---- f32 on the CUDA cores --------------------------------------------------------------------------------------------
 
-// Tiles of BM rows by 64 states, 256 threads: a thread has RT = BM / 16 rows (ty) and every 16th state or group of four columns (tx).  Products are
-// packed pairs; K and V have one buffer each, and the next tile of K is on its way during the products with V, and the other way round.
+// Tiles of BM rows by 64 states, 256 threads: a thread has RT = BM / 16 rows (ty) and every 16th state or group of four columns (tx): eight rows
+// take half the reads of shared memory per product of four, but one CTA has an SM then (69 GFLOP, 16 / 4 heads of 128: BM = 128 1552 us, two CTAs of
+// 64 2164).  Products are packed pairs; K and V have one buffer each, and the next tile of K is on its way during the products with V, and the other way round.
 template <int BM, int DP>
 struct Cores {
     static constexpr int BN = 64, NT = 256, RT = BM / 16, LD = DP + 4, LP = BN + 4;
@@ -570,6 +576,11 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
 // S = Q K^T lands in tensor memory, the threads read it, and leave the weights, in bf16, in its place, from where they are the first operand of
 // O += P V.  While one tile's weights are worked out, the other tile's products run.  Where there are no more than 128 rows both tiles have
 // the same rows and every other tile of states, and their results are added at the end.
+//
+// What bounds it: the turn from scores to scores of one tile, with 128 columns 3700 cycles: 1700 to take its weights (1024 of them the special
+// function unit's, which does a quarter of a warp's powers of two in a cycle; reading and writing tensor memory, sums and rounding do not
+// overlap with it in one warp), 1400 for its products (16 instructions at 64 cycles, issued at 80), the rest are barriers.  The tiles' turns
+// are kept apart, so the tensor pipe works for 2800 of them.
 //
 // Roundings.  Scores and sums are fp32; a weight is rounded to bf16 for its product with V, 2^-8 of its size at most: the
 // errors of the states' weights are independent, and their mean is below the rounding of the output.  (The pairs of 16-bit floats that the attention
