@@ -46,7 +46,7 @@ constexpr int kLeastProbes = 1 << 12;               // and with a limit from the
 struct CrossArgs {
     CrossProblem p;
     int group;                                      // query heads per key head
-    int block;                                      // rows of a block
+    int block, shift;                               // rows of a block: a power of two
     // Scores are c <q, k> + bias, weights 2^(unit (score - m)), and a score is worth nat in natural units: with biases c = |scale|, unit = log2(e),
     // nat = 1 (a bias of the lowest value times log2(e) would not be finite), without c = |scale| log2(e), unit = 1, nat = ln(2).
     float c, unit, nat;
@@ -111,12 +111,15 @@ struct Work {
         k0 = clamped(p.k_starts[i], p.k_tokens);
         klen = max(clamped(p.k_starts[i + 1], p.k_tokens) - k0, 0);
     }
-    __device__ int blocks_of(int qlen) const { return (int)quotient((long long)qlen * a.group + a.block - 1, a.block); }
+    __device__ int blocks_of(int qlen) const { return (int)(((long long)qlen * a.group + a.block - 1) >> a.shift); }
     __device__ int tiles_of(int klen) const { return (int)(((long long)klen + BN - 1) / BN); }
     __device__ int steps() const { return whole ? min(kbs, 1) : kbs; }          // of the list, of a block
     __device__ void enter(int i) {
-        seq = i;
         lengths(i, q0, qlen, k0, klen);
+        settle(i);
+    }
+    __device__ void settle(int i) {
+        seq = i;
         rbs = blocks_of(qlen);
         kbs = tiles_of(klen);
     }
@@ -133,7 +136,7 @@ struct Work {
         float size = 0.f;                           // of the list, which must have less than 2^31 tiles
         int longest = 0;
         auto scan = [&](int i) {
-            int q0, qlen = 0, k0, klen = 0;
+            q0 = qlen = k0 = klen = 0;
             if (i < n) lengths(i, q0, qlen, k0, klen);
             const int t = tiles_of(klen);
             const float b = (float)a.p.heads * blocks_of(qlen);
@@ -197,8 +200,11 @@ struct Work {
         if (n <= 32) {
             look(lane);
             const int from = __ffs(__ballot_sync(~0u, which >= 0)) - 1;
-            which = __shfl_sync(~0u, which, from);
+            which = from;
             in = __shfl_sync(~0u, in, from);
+            q0 = __shfl_sync(~0u, q0, from); qlen = __shfl_sync(~0u, qlen, from);
+            k0 = __shfl_sync(~0u, k0, from); klen = __shfl_sync(~0u, klen, from);
+            settle(from);
         } else {
             if (n <= NT) {
                 look(tid);
@@ -212,10 +218,9 @@ struct Work {
             }
             if (which >= 0) { found = which; found_in = in; }
             __syncthreads();
-            which = found;
             in = found_in;
+            enter(found);
         }
-        enter(which);
         const unsigned per_head = (unsigned)rbs * steps();
         head = in / per_head;
         rb = (in - head * per_head) / steps();
@@ -914,25 +919,26 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
             if (t == 0 || two) {                                // queries, in the order the products read them
                 int h;
                 const long long tok = token_of(a, it, mine_live ? mine : 0, h);
-                const unsigned long long src = mine_live ? reinterpret_cast<unsigned long long>(static_cast<const __nv_bfloat16*>(p.q) + tok * p.q_stride + (long long)h * D) : 0ull;
+                const unsigned long long src = reinterpret_cast<unsigned long long>(static_cast<const __nv_bfloat16*>(p.q) + tok * p.q_stride + (long long)h * D);
+                const unsigned live = __ballot_sync(~0u, mine_live);
                 const unsigned flip = a.sign < 0.f ? 0x80008000u : 0u;
                 unsigned char* const dst = base + t * T::Q_BYTES + (warp & 3) * (32 * 128);
-                // a warp brings its 32 rows together, 16 bytes of a lane next to those of the next one
+                // a warp brings its 32 rows together, 16 bytes of a lane next to those of the next one (where there are none, those of another
+                // place are read and not used)
                 const int pieces = 2 * ksteps;
                 const unsigned part = 65536 / pieces + 1;       // piece * part / 65536: exact for 1024 pieces of rows of up to 32
-                for (int x0 = 0; x0 < pieces; x0 += 8) {
-                    uint4 x[8];
+                for (int x0 = 0; x0 < pieces; x0 += 16) {
+                    uint4 x[16];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < 16; ++e) {
                         const unsigned u = (x0 + e) * 32 + lane, row = u * part >> 16, c = u - row * pieces;
-                        const unsigned long long from = __shfl_sync(~0u, src, row & 31);
-                        x[e] = make_uint4(0u, 0u, 0u, 0u);
-                        if (row < 32 && from && 8 * c < D) x[e] = __ldg(reinterpret_cast<const uint4*>(from) + c);
+                        x[e] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(~0u, src, row & 31)) + (8 * c < D ? c : 0));
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < 16; ++e) {
                         const unsigned u = (x0 + e) * 32 + lane, row = u * part >> 16, c = u - row * pieces;
                         x[e].x ^= flip; x[e].y ^= flip; x[e].z ^= flip; x[e].w ^= flip;
+                        if (8 * c >= D || !((live >> (row & 31)) & 1u)) x[e] = make_uint4(0u, 0u, 0u, 0u);
                         if (row < 32) *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x[e];
                     }
                 }
@@ -1070,6 +1076,9 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 const unsigned long long to = mine_live ? reinterpret_cast<unsigned long long>(static_cast<__nv_bfloat16*>(p.out) + row * D) : 0ull;
                 // 32 columns of the warp's rows go through shared memory, four pieces of 16 bytes of a row each 2 KB apart or less: the place
                 // of the warp's own queries, or of what has just been added
+                unsigned long long there[4];                    // where a lane's pieces go: of rows lane / 4 + 8 e, the piece lane % 4
+#pragma unroll
+                for (int e = 0; e < 4; ++e) there[e] = __shfl_sync(~0u, to, 8 * e + (lane >> 2));
                 float bad[4] = {l * 0.f, 0.f, 0.f, 0.f};        // 0, or NaN
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int c = 0; c < D; c += 32) {
@@ -1109,13 +1118,12 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                     }
                     if (whole) {
                         __syncwarp();
+                        uint4 out[4];                           // 64 bytes of eight rows at a time
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {           // 64 bytes of eight rows at a time
-                            const int u = 8 * e + (lane >> 2), x = lane & 3;
-                            const unsigned long long there = __shfl_sync(~0u, to, u);
-                            if (there && c + 8 * x < D)
-                                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(there) + c + 8 * x) = *reinterpret_cast<const uint4*>(stage + x * apart + u * 16);
-                        }
+                        for (int e = 0; e < 4; ++e) out[e] = *reinterpret_cast<const uint4*>(stage + (lane & 3) * apart + (8 * e + (lane >> 2)) * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (there[e] && c + 8 * (lane & 3) < D) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(there[e]) + c + 8 * (lane & 3)) = out[e];
                         __syncwarp();
                     }
                 }
@@ -1198,6 +1206,7 @@ int max_ctas(int ctas) { return std::min(ctas, std::min(kMaxCtas, (int)(kPartsBy
 template <int BM, int DP>
 int launch_f32(CrossArgs& a) {
     a.block = BM;
+    a.shift = BM == 16 ? 4 : BM == 64 ? 6 : 7;
     static std::atomic<unsigned long long> set{0};
     const int ctas = max_ctas<BM, DP>(Cores<BM, DP>::CTAS * sm_count());
     if (!ctas || !allow_smem(attn_cross_f32<BM, DP>, Cores<BM, DP>::SMEM, set)) return LUVC_ERR_CUDA;
@@ -1245,6 +1254,7 @@ int launch_tc(CrossArgs& a) {
     const int sms = max_ctas<T::ROWS, DP>(sm_count());
     // blocks of two tiles of rows where there are enough for all SMs (of one, and both tiles on the same rows, K and V are brought twice as often)
     a.block = T::TILES == 2 && (long long)a.p.q_tokens * a.p.q_heads <= 256ll * 2 * sms ? 128 : T::ROWS;
+    a.shift = a.block == 128 ? 7 : 8;
     CUtensorMap kmap, vmap;
     if (!sms || !states_map<T::BN>(&kmap, a.p, a.p.k, a.p.k_stride) || !states_map<T::BN>(&vmap, a.p, a.p.v, a.p.v_stride) ||
         !allow_smem(attn_cross_tc<DP, BIAS>, T::SMEM, set))
