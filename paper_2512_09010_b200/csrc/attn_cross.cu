@@ -396,7 +396,7 @@ struct Cores {
 template <int BM, int DP>
 __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const __grid_constant__ CrossArgs a) {
     using C = Cores<BM, DP>;
-    constexpr int BN = C::BN, NT = C::NT, RT = C::RT, LD = C::LD, LP = C::LP, CG = DP / 64;
+    constexpr int BN = C::BN, NT = C::NT, LD = C::LD, LP = C::LP, CG = DP / 64;
     extern __shared__ __align__(16) float smem[];
     float* const qs = smem;
     float* const ks = qs + BM * LD;
@@ -413,8 +413,9 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
     empty_sequences<float, NT>(a, work);
     for (int e = tid; e < (BM + BN) * (LD / 4); e += NT) reinterpret_cast<float4*>(qs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);   // columns past D
     for (int e = tid; e < BN * (DP / 4); e += NT) reinterpret_cast<float4*>(vs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-    while (work.more()) {
-        const Item it = work.next();
+    // An item, with `rt` rows for each thread: no more than it needs, so that the few rows of a ragged end take little.
+    auto process = [&](const Item& it, auto rt) {
+        constexpr int RT = decltype(rt)::value;
         __syncthreads();                                        // the item before, or the zeros
         // rows past the item's last are left as they are: their results are not written
         auto load = [&](const float* src, long long stride, float* dst, int ld, int kb) {
@@ -570,6 +571,26 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
                 join_parts<float, BM, DP, NT>(a, it, c0, c1, tid);
             }
         }
+    };
+    while (work.more()) {
+        const Item it = work.next();
+        if constexpr (C::RT >= 8) {
+            if (it.rows > 64) {
+                process(it, std::integral_constant<int, 8>{});
+                continue;
+            }
+        }
+        if constexpr (C::RT >= 4) {
+            if (it.rows > 32) {
+                process(it, std::integral_constant<int, 4>{});
+                continue;
+            }
+            if (it.rows > 16) {
+                process(it, std::integral_constant<int, 2>{});
+                continue;
+            }
+        }
+        process(it, std::integral_constant<int, 1>{});
     }
 }
 
