@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kRowsThreads, NC > 8 ? 2 : 4) kv_write_block_k
             if (behind >= 1 && pos >= 0 && pos / ps < c.max_pages) page = c.table[(long long)slot * c.max_pages + pos / ps];
             if (page >= 0 && page < c.pages) {
                 b.front = pos % kKvBlock;
-                b.count = min(behind, kKvBlock - b.front);
+                b.count = min(min(behind, a.tokens - t), kKvBlock - b.front);        // (starts may say more rows than there are)
                 b.token = t;
                 b.row = (long long)page * c.heads * ps + pos % ps - b.front;
                 b.scale = page * c.heads * (ps / kKvBlock) + pos % ps / kKvBlock;

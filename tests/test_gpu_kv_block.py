@@ -332,6 +332,26 @@ def test_write_reports_rows_it_cannot_place(luvc):
     assert luvc.check_status() == 0
 
 
+@pytest.mark.parametrize("given", [1, 15, 16, 24, 33, 39])
+def test_starts_past_the_rows_write_the_rows_there_are(luvc, given):
+    """starts names 40 rows, the call has fewer: those are written, and no scale, stored row or read depends on what lies behind them."""
+    r = Rig(luvc, 3, 64, 32, 1, 64)
+    k, v = rows(torch.Generator("cuda").manual_seed(given), 1, 64, 3, 64)
+    k[0, given:] = v[0, given:] = 1e6                        # behind the rows of the call, in the same memory
+    luvc.kv_reserve(r.cache, ints([40]), seqs=ints([0]))
+    table = r.cache.table[0].tolist()
+    luvc.kv_write(r.cache, k[0, :given], v[0, :given], starts=ints([0, 40]), seqs=ints([0]))
+    luvc.check_status()
+    for pool, scale, x in ((r.cache.k, r.cache.k_scale, k), (r.cache.v, r.cache.v_scale, v)):
+        model = Sequence(3, 64)
+        model.write(x[0, :given].float())
+        got = torch.cat([pool[0, page] for page in table[:2]], dim=1).float()
+        assert torch.equal(got[:, :given], model.x) and got[:, given:].isnan().all()
+        got = torch.cat([scale[0, page] for page in table[:2]], dim=1)
+        blocks = -(-given // 16)
+        assert torch.equal(got[:, :blocks], model.s) and got[:, blocks:].isnan().all()
+
+
 def test_captured(luvc):
     """Steps of a captured graph give what the calls give."""
     g = torch.Generator(device="cuda").manual_seed(8)
