@@ -70,6 +70,12 @@ constexpr float kRise = 11.f, kFall = 6.f, kLead = 8.f, kGone = 60.f, kMostGain 
 // Blocks: a block's scale is at least this part of the unit of the sums O, or the unit becomes the block's scale (neighbours mostly differ
 // by a factor of two; the product with V keeps two bits less of a weight at most).
 constexpr float kLeastUnit = 0.25f;
+// The unit goes down to this part of the largest scale so far at most: a lane's weights sum to 2^kMostGain, a head's to eight times that, a value is
+// at most 448 of its scale, so |O| stays below 2^(60 + 3 + 9 + 50).  (With 2^-60, scores that fall by 34 to 68 along with a block of zeros,
+// whose scale is 2^-60, took it past the range.)
+constexpr float kLowestUnit = 0x1p-50f;
+// At the end of a warp's part, a sum of weights beyond this is brought to about one, and O with it, which leaves its units then: scales go up to 2^60.
+constexpr float kMostSum = 0x1p30f;
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;           // and with a limit from the status block (a test's), so that copies which do come are waited for
 
@@ -1033,7 +1039,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                             if (!(now <= v_unit && now >= kLeastUnit * v_unit)) {
                                 if (!(now > 0.f && now < INFINITY)) now = 0.f;
                                 v_top = fmaxf(v_top, now);
-                                const float unit = fmaxf(now, fmaxf(v_top * 0x1p-60f, 0x1p-126f)), f = v_unit / unit;
+                                const float unit = fmaxf(now, fmaxf(v_top * kLowestUnit, 0x1p-126f)), f = v_unit / unit;
                                 v_unit = unit;
                                 v_per_unit = 1.f / unit;
 #pragma unroll
@@ -1188,6 +1194,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     for (int j = 0; j < DP / 32; ++j) os[o_index(r, f32_column<DP>(lane, j), DP)] = core_o[r][j];
                 }
             }
+            float o_unit[NTX][2];                               // blocks: of O, for each head
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -1196,7 +1203,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     x += __shfl_xor_sync(~0u, x, 4);
                     x += __shfl_xor_sync(~0u, x, 8);
                     x += __shfl_xor_sync(~0u, x, 16);
-                    if (g == 0) ml_of[warp][which][nt * 8 + 2 * t4 + b] = make_float2(m[nt][b], x);
+                    float to = m[nt][b];
+                    if constexpr (kBlocks) {
+                        const unsigned e = x > kMostSum ? (__float_as_uint(x) >> 23) - 127u : 0u;
+                        const float f = __uint_as_float((127u - e) << 23);              // 2^-e
+                        to = fmaf((float)e, 1.f / kLog2e, to);
+                        x *= f;
+                        o_unit[nt][b] = v_unit * f;
+                    }
+                    if (g == 0) ml_of[warp][which][nt * 8 + 2 * t4 + b] = make_float2(to, x);
                 }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
@@ -1205,7 +1220,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int d = 16 * mt + (kF8 ? 2 * g + (c >> 1) : g + 8 * (c >> 1));
-                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = kBlocks ? o[mt][nt][c] * v_unit : o[mt][nt][c];
+                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = kBlocks ? o[mt][nt][c] * o_unit[nt][c & 1] : o[mt][nt][c];
                     }
             __syncwarp();
             if constexpr (!kF8) {                               // (an e4m3 cache has no infinities, and its rows are not split)
