@@ -1037,9 +1037,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         if constexpr (kBlocks) {
                             float now = v_scale;
                             if (!(now <= v_unit && now >= kLeastUnit * v_unit)) {
-                                if (!(now > 0.f && now < INFINITY)) now = 0.f;
+                                // of a block that is masked as a whole it may be anything, and must not set the unit
+                                if (!(now > 0.f && now < INFINITY) || __all_sync(~0u, bias[j][0] == -INFINITY && bias[j][1] == -INFINITY)) now = 0.f;
                                 v_top = fmaxf(v_top, now);
-                                const float unit = fmaxf(now, fmaxf(v_top * kLowestUnit, 0x1p-126f)), f = v_unit / unit;
+                                const float unit = now > 0.f ? fmaxf(now, fmaxf(v_top * kLowestUnit, 0x1p-126f)) : v_unit, f = v_unit / unit;
                                 v_unit = unit;
                                 v_per_unit = 1.f / unit;
 #pragma unroll

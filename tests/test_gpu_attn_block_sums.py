@@ -56,3 +56,21 @@ def test_zeros_far_below_without_biases(luvc):  # noqa: F811
     assert luvc.check_status() == 0
     assert bool(out.isfinite().all())
     check(c, q, out, lse, scale=1.0)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127, 2.0 ** 100, 2.0 ** 60, 2.0 ** -60, 2.0 ** -126, 0.0, -1.0])
+@pytest.mark.parametrize("lengths", [[30011], [100, 40]])
+def test_scales_of_masked_blocks_count_for_nothing(luvc, lengths, scale):  # noqa: F811
+    """Not for the precision of the others either: the same bits, whatever a masked block's scales are."""
+    c = build(luvc, lengths, 4, 128, 16, seed=12)
+    q = queries(len(lengths), 28, 128)
+    bias = torch.zeros((len(lengths), -(-max(lengths) // 16), 16), device="cuda")
+    bias[:, 1::3] = -float("inf")
+    bias = bias.view(len(lengths), -1)[:, :max(lengths)].contiguous()
+    want = luvc.attn_decode(q, c, key_bias=bias)
+    check(c, q, want, None, bias=bias)
+    for i, n in enumerate(lengths):
+        masked = c.table[i, 1:-(-n // 16):3].long()
+        c.k_scale[0, masked], c.v_scale[0, masked] = scale, scale
+    assert torch.equal(luvc.attn_decode(q, c, key_bias=bias), want)
+    assert luvc.check_status() == 0
