@@ -22,7 +22,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
-#include <math.h>
+#include <cmath>
 
 #include <algorithm>
 #include <atomic>
@@ -51,6 +51,9 @@ struct CrossArgs {
     // nat = 1 (a bias of the lowest value times log2(e) would not be finite), without c = |scale| log2(e), unit = 1, nat = ln(2).
     float c, unit, nat;
     float sign;                                     // of the scale; c has its magnitude
+    // f32: weights are `down` at most, a power of two below 1 / the number of states: so their sum stays below 1, and sums of values below the
+    // largest value (results below 2^-126 / down lose bits).  up = 1 / down.  bf16: both 1.
+    float down, up;
     unsigned* counters;                             // [kMaxCtas] arrivals of parts, by the CTA an item begins in
     float* parts;                                   // two for each CTA
 };
@@ -266,7 +269,7 @@ template <> __device__ __forceinline__ void put4<__nv_bfloat16>(__nv_bfloat16* p
     const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-__device__ __forceinline__ float lse_of(const CrossArgs& a, float m, float l) { return l == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.nat, logf(l)); }
+__device__ __forceinline__ float lse_of(const CrossArgs& a, float m, float l) { return l == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.nat, logf(l * a.up)); }
 
 // Sequences without states: rows of zeros.  By a warp, or by a CTA of NT threads.
 template <typename T, int NT, typename W>
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
                 }
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float w = exp2_fast((s[x] - base) * a.unit);
+                    const float w = exp2_fast((s[x] - base) * a.unit) * a.down;
                     l[r] += w;
                     ps[(ty * RT + r) * LP + tx + 16 * x] = w;
                 }
@@ -1319,6 +1322,10 @@ int attn_cross(const CrossProblem& p) {
     a.unit = p.bias ? kLog2e : 1.f;
     a.nat = p.bias ? 1.f : kLn2;
     a.sign = p.scale < 0.f ? -1.f : 1.f;
+    int bits = 0;                                               // 2^bits: more than there are states
+    if (p.dtype == LUVC_F32) std::frexp((float)p.k_tokens, &bits);
+    a.down = std::ldexp(1.f, -bits);
+    a.up = std::ldexp(1.f, bits);
     a.counters = static_cast<unsigned*>(p.workspace);
     a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(p.workspace) + kCounterBytes);
     if (p.dtype == LUVC_BF16) return p.D <= 64 ? launch_tc_bias<64>(a) : p.D <= 128 ? launch_tc_bias<128>(a) : launch_tc_bias<256>(a);
