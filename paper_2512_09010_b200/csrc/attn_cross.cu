@@ -51,9 +51,9 @@ struct CrossArgs {
     // nat = 1 (a bias of the lowest value times log2(e) would not be finite), without c = |scale| log2(e), unit = 1, nat = ln(2).
     float c, unit, nat;
     float sign;                                     // of the scale; c has its magnitude
-    // f32: weights are `down` at most, a power of two below 1 / the number of states: so their sum stays below 1, and sums of values below the
-    // largest value (results below 2^-126 / down lose bits).  up = 1 / down.  bf16: both 1.
-    float down, up;
+    // All weights are multiplied by down = 2^-below, so that the sum of a row's weights stays below 1, and sums of values below the largest value
+    // (results below 2^-126 / down lose bits).  up = 1 / down.
+    float below, down, up;
     unsigned* counters;                             // [kMaxCtas] arrivals of parts, by the CTA an item begins in
     float* parts;                                   // two for each CTA
 };
@@ -66,11 +66,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     unsigned long long d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
-    return *reinterpret_cast<float2*>(&d);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    unsigned long long d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
     return *reinterpret_cast<float2*>(&d);
 }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -628,8 +623,8 @@ struct Tc {
     static_assert(TILES == 1 || 2 * Q_BYTES >= 128 * DP * 4, "a tile's result fits the queries' place");
 };
 
-// Largest sum of a tile's weights before their reference follows the maximum: sums of values up to 2^80 stay in range.
-constexpr float kMost = 0x1p40f;
+// Largest sum of a tile's weights, but for CrossArgs::down, before their reference follows the maximum.
+constexpr int kMostBits = 16;
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -676,67 +671,6 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, int parity, volatile in
     *dead = 1;
     *status = LUVC_ERR_TIMEOUT;
     return false;
-}
-
-// A row of an item once more, by a warp, product by product as the formula has them.  An infinity among the values meets weights that bf16 has
-// rounded to 0, and weights above 1, while their reference lags behind, can take large values beyond the end of the range; so a
-// row that is not finite is worked out again.  It is rare, and need not be fast.
-template <int DP>
-__device__ __forceinline__ void plain_row(const CrossArgs& a, const Item& it, int r) {
-    constexpr int ROWS = Tc<DP>::ROWS, BN = Tc<DP>::BN;
-    const CrossProblem& p = a.p;
-    const int lane = threadIdx.x & 31, D = p.D;
-    int h;
-    const long long t = token_of(a, it, r, h), row = t * p.q_heads + h;
-    const __nv_bfloat16* const qr = static_cast<const __nv_bfloat16*>(p.q) + t * p.q_stride + (long long)h * D;
-    float q[DP / 32], o[DP / 32], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int j = 0; j < DP / 32; ++j) {
-        q[j] = lane + 32 * j < D ? __bfloat162float(qr[lane + 32 * j]) * a.sign : 0.f;
-        o[j] = 0.f;
-    }
-    const long long k1 = it.k0 + min((long long)(it.kb + it.count) * BN, (long long)it.klen);
-    for (long long k = it.k0 + (long long)it.kb * BN; k < k1; ++k) {
-        const float bias = p.bias ? p.bias[k] : 0.f;
-        if (bias == -INFINITY) continue;
-        const __nv_bfloat16* const kr = static_cast<const __nv_bfloat16*>(p.k) + k * p.k_stride + (long long)it.head * D;
-        const __nv_bfloat16* const vr = static_cast<const __nv_bfloat16*>(p.v) + k * p.v_stride + (long long)it.head * D;
-        float s = 0.f, v[DP / 32];
-#pragma unroll
-        for (int j = 0; j < DP / 32; ++j) {
-            const int d = lane + 32 * j;
-            v[j] = 0.f;
-            if (d < D) {
-                s = fmaf(q[j], __bfloat162float(kr[d]), s);
-                v[j] = __bfloat162float(vr[d]);
-            }
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-        s = fmaf(s, a.c, bias);
-        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-        // o is the mean so far: values near the end of the range stay inside it
-        const float had = l * exp2_fast((m - base) * a.unit), w = exp2_fast((s - base) * a.unit);
-        m = top;
-        l = had + w;
-        const float inv = l == 0.f ? 0.f : 1.f / l, f = had * inv, by = w * inv;
-#pragma unroll
-        for (int j = 0; j < DP / 32; ++j) o[j] = lane + 32 * j < D ? fmaf(o[j], f, by * v[j]) : 0.f;
-    }
-    const bool whole = it.count == it.kbs;
-    const Part<ROWS, DP> part(a, blockIdx.x, it.kb == 0);
-#pragma unroll
-    for (int j = 0; j < DP / 32; ++j) {
-        const int d = lane + 32 * j;
-        if (d >= D) continue;
-        if (whole) static_cast<__nv_bfloat16*>(p.out)[row * D + d] = __float2bfloat16_rn(l == 0.f ? 0.f : o[j]);
-        else reinterpret_cast<float*>(part.o + d / 4 * ROWS + r)[d & 3] = o[j];
-    }
-    if (lane == 0) {
-        if (!whole) part.ml[r] = make_float2(l == 0.f ? m : m + __log2f(l) / a.unit, l == 0.f ? 0.f : 1.f);      // weights that sum to one
-        else if (p.lse) p.lse[row] = lse_of(a, m, l);
-    }
-    __syncwarp();
 }
 
 template <int DP, bool BIAS>
@@ -1028,7 +962,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 };
                 const float c1 = BIAS ? 1.f : a.c, unit = BIAS ? kLog2e : 1.f;
                 // The reference of the weights is the maximum of the first tile.  It follows later ones only where the sum of a tile's weights
-                // passes kMost: floats, bf16 among them, keep their relative precision up to there, so the maximum need not be known.
+                // passes 2^kMostBits: floats, bf16 among them, keep their relative precision up to there, so the maximum need not be known.
                 uint32_t w[BN / 2];
                 float sum;
                 for (bool fresh = __any_sync(~0u, m == -INFINITY);; fresh = true) {
@@ -1052,13 +986,13 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                             }
                         }
                     }
-                    const float from = m == -INFINITY ? 0.f : m;
+                    const float from = BIAS ? (m == -INFINITY ? 0.f : m) : (m == -INFINITY ? 0.f : m) + a.below;
                     float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     auto weigh = [&](auto with_masks) { each_chunk(with_masks, [&](int c, const float2 (&y)[16]) {
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
                             float2 z;
-                            if (BIAS) z = mul2(add2(y[x], make_float2(-from, -from)), make_float2(kLog2e, kLog2e));
+                            if (BIAS) z = fma2(add2(y[x], make_float2(-from, -from)), make_float2(kLog2e, kLog2e), make_float2(-a.below, -a.below));
                             else z = fma2(y[x], make_float2(c1, c1), make_float2(-from, -from));
                             z = make_float2(exp2_fast(z.x), exp2_fast(z.y));
                             sums[x & 1] = add2(sums[x & 1], z);
@@ -1070,7 +1004,7 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                     else weigh(std::false_type{});
                     const float2 all = add2(sums[0], sums[1]);
                     sum = all.x + all.y;
-                    if (fresh || !__any_sync(~0u, sum > kMost)) break;
+                    if (fresh || !__any_sync(~0u, sum > a.down * (float)(1 << kMostBits))) break;
                 }
                 l += sum;
                 if (BIAS) named_barrier(2 + t, 128);            // the biases have been read
@@ -1104,7 +1038,6 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                 unsigned long long there[4];                    // where a lane's pieces go: of rows lane / 4 + 8 e, the piece lane % 4
 #pragma unroll
                 for (int e = 0; e < 4; ++e) there[e] = __shfl_sync(~0u, to, 8 * e + (lane >> 2));
-                float bad[4] = {l * 0.f, 0.f, 0.f, 0.f};        // 0, or NaN
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
@@ -1126,8 +1059,6 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                                 y[e + 2] = fmaf(z.z, f1, y[e + 2] * f0); y[e + 3] = fmaf(z.w, f1, y[e + 3] * f0);
                             }
                         }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) bad[e & 3] = fmaf(y[e], 0.f, bad[e & 3]);
                         if (whole) {
                             uint32_t w[4];
 #pragma unroll
@@ -1156,9 +1087,6 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
                     if (!whole) part.ml[mine] = make_float2(m, l);
                     else if (p.lse) p.lse[row] = lse_of(a, m, l);
                 }
-                __syncwarp();
-                for (unsigned again = __ballot_sync(~0u, mine_live && bad[0] + bad[1] + (bad[2] + bad[3]) != 0.f && !*dead); again; again &= again - 1)
-                    plain_row<DP>(a, it, __shfl_sync(~0u, mine, __ffs(again) - 1));
             };
             const bool merged = both && it.count > 1;
             float f0 = 1.f, f1 = 0.f;
@@ -1322,8 +1250,11 @@ int attn_cross(const CrossProblem& p) {
     a.unit = p.bias ? kLog2e : 1.f;
     a.nat = p.bias ? 1.f : kLn2;
     a.sign = p.scale < 0.f ? -1.f : 1.f;
-    int bits = 0;                                               // 2^bits: more than there are states
-    if (p.dtype == LUVC_F32) std::frexp((float)p.k_tokens, &bits);
+    // f32: a weight is 1 at most; bf16: those of a tile of 64 states or more sum to 2^kMostBits at most
+    int bits = 0;                                               // 2^bits: more than there are states, or tiles of them
+    std::frexp((float)(p.dtype == LUVC_F32 ? p.k_tokens : p.k_tokens / 64 + 1), &bits);
+    if (p.dtype == LUVC_BF16) bits += kMostBits;
+    a.below = (float)bits;
     a.down = std::ldexp(1.f, -bits);
     a.up = std::ldexp(1.f, bits);
     a.counters = static_cast<unsigned*>(p.workspace);

@@ -54,3 +54,31 @@ def test_infinities_in_f32_with_many_tokens(luvc, queries, keys):  # noqa: F811
     assert bool((got[..., 3] == math.inf).all()) and bool(got[..., 5].isnan().all())
     rest = [d for d in range(64) if d not in (3, 5)]
     assert bool(got[..., rest].isfinite().all())
+
+
+@pytest.mark.parametrize("hq,D,queries,keys", [(2, 64, 700, 16500), (8, 128, 40, 33000), (2, 256, 200, 9000)])
+def test_nan_and_infinities_take_no_longer(luvc, hq, D, queries, keys):  # noqa: F811
+    """Waits that give up early (a few thousand probes, far more than a tile takes) do not: nothing in the call is worked out at length, once more."""
+    q, k, v, qs, ks = inputs("bf16", hq, 1, D, [queries], [keys], seed=6)
+    k.mul_(0.25)
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    call = lambda: luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks, device_status=status)             # noqa: E731
+    want = call()
+    assert bool(want.isfinite().all()) and luvc.read_status(status) == 0
+    assert luvc.lib.luvc_debug_wait_probes(1, 0, status.data_ptr(), stream) == 0
+    v[5, 0, 3], v[keys - 1, 0, 7], v[keys // 2, 0, 9], v[11, 0, 9] = math.inf, math.nan, math.inf, -math.inf
+    got = call()
+    assert luvc.read_status(status) == 0
+    assert bool((got[..., 3] == math.inf).all()) and bool(got[..., 7].isnan().all()) and bool(got[..., 9].isnan().all())
+    rest = [d for d in range(D) if d not in (3, 7, 9)]
+    assert torch.equal(got[..., rest], want[..., rest])
+    k[keys // 3, 0, 1] = math.nan
+    got = call()
+    assert luvc.read_status(status) == 0 and bool(got.isnan().all())
+    k[keys // 3, 0, 1], q[queries // 2, 1, 0] = 0.0, math.nan
+    got = call()
+    assert luvc.read_status(status) == 0
+    assert bool(got[queries // 2, 1].isnan().all())
+    got[queries // 2, 1] = 0.0
+    assert bool(got[..., rest].isfinite().all())
