@@ -54,6 +54,7 @@ struct CrossArgs {
     // All weights are multiplied by down = 2^-below, so that the sum of a row's weights stays below 1, and sums of values below the largest value
     // (results below 2^-126 / down lose bits).  up = 1 / down.
     float below, down, up;
+    const int* gate;                                // not NULL: attn_rows has done the call where this is 0
     unsigned* counters;                             // [kMaxCtas] arrivals of parts, by the CTA an item begins in
     float* parts;                                   // two for each CTA
 };
@@ -406,6 +407,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, D = p.D;
     pdl_trigger();
     pdl_wait();
+    if (a.gate && *a.gate == 0) return;
     Work<BN, 2> work(a);
     work.template begin<NT>();
     empty_sequences<float, NT>(a, work);
@@ -721,6 +723,11 @@ attn_cross_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ 
     }
     pdl_trigger();
     pdl_wait();
+    if (a.gate && *a.gate == 0) {
+        __syncthreads();
+        if (warp == 9) tmem_dealloc(tmem_at, 512);
+        return;
+    }
     Work<BN, T::JOIN> work(a);
     tc_fence_before();
     work.template begin<T::THREADS>();
@@ -1222,17 +1229,20 @@ int launch_tc_bias(CrossArgs& a) {
 
 }  // namespace
 
-size_t attn_cross_workspace_bytes() { return align_up(kCounterBytes + kPartsBytes) + attn_workspace_bytes(); }
+// This file's counters and parts, attn_rows' workspace, what it says to the kernel behind it.
+size_t attn_cross_workspace_bytes() { return align_up(kCounterBytes + kPartsBytes) + align_up(attn_workspace_bytes()) + 256; }
 
 int attn_cross(const CrossProblem& p) {
     // Few tokens go each on its own, in the form that attends from one token to a cache (tiles of 16 rows where this file's have 128), which reads
-    // a sequence's states once for each of its tokens.  Where no sequence need have two (a decode step) that is nothing lost: 16 tokens to 1296
+    // a sequence's states once for each of its tokens.  Where no sequence has two (a decode step) that is nothing lost: 16 tokens to 1296
     // states each, 28 / 4 heads of 128, 14.6 us, in blocks of 128 rows 24.8; f32, 8 tokens to 576 states, 16 / 16 heads of 64, 8.8 and 34.
     // Beyond that it takes a microsecond for 10 MB read, and blocks take two and one for 150 states more than it does for little (8 sequences of
     // 2, 4, 8 tokens, 1296 states: 15.9, 19.6, 28.0 us, blocks 25; 32 of 4, 300 states: 18.8 and 17.8; one of 4, 16384: 24 and 31); f32 blocks
     // about twice that (8 of 2 and 4: 40 and 68 us, blocks 67 and 72; 32 / 8 heads of 128).
-    const double states = (double)p.k_tokens / p.n, mb = p.q_tokens * states * p.heads * p.D * (p.dtype == LUVC_F32 ? 8e-6 : 4e-6);
+    const double states = (double)p.k_tokens / p.n, state_mb = p.heads * p.D * (p.dtype == LUVC_F32 ? 8e-6 : 4e-6), mb = p.q_tokens * states * state_mb;
     const bool alone = p.q_tokens <= p.n || 0.1 * mb <= (p.dtype == LUVC_F32 ? 2. : 1.) * (2. + std::min(states, 2000.) / 150.);
+    CrossArgs a;
+    a.gate = nullptr;
     if (alone && p.q_tokens <= kAttnRowsMost && p.k_tokens > 0) {
         AttnProblem r = {};
         r.c.k = const_cast<void*>(p.k); r.c.v = const_cast<void*>(p.v); r.c.heads = p.heads; r.c.D = p.D; r.c.dtype = p.dtype;
@@ -1241,9 +1251,20 @@ int attn_cross(const CrossProblem& p) {
         r.n = p.q_tokens; r.q_heads = p.q_heads; r.scale = p.scale; r.status = p.status; r.stream = p.stream;
         r.workspace = static_cast<unsigned char*>(p.workspace) + align_up(kCounterBytes + kPartsBytes);
         r.q_starts = p.q_starts; r.k_starts = p.k_starts; r.n_seqs = p.n; r.k_tokens = p.k_tokens; r.k_stride = p.k_stride; r.v_stride = p.v_stride;
-        return attn_rows(r);
+        // That is for lengths near their means, which are all that is known here.  If all tokens can be of one sequence that has all states, and that is
+        // much, the lengths decide: attn_rows leaves the call to the blocks where it would read more than three times as much as it was
+        // chosen for, and 100 MB; they return at once where it has done it.  (1024 tokens of one of 1024 sequences to 16384 states, 8 / 8 heads of 128:
+        // 105 us, each on its own 5746; 60 of one of 64 to 58000, 28 / 4: 124 and 712; the second launch costs 32 sequences of one token
+        // and 1296 states 0.9 us of 19.3, 64 of 1000 2.5 of 33.3.)
+        const double most = 3. * mb + 100., worst = p.q_starts ? p.q_tokens * (double)p.k_tokens * state_mb : 0.;
+        if (worst > 500. && worst > most) {
+            r.left = reinterpret_cast<int*>(static_cast<unsigned char*>(p.workspace) + attn_cross_workspace_bytes() - 256);
+            r.most_states = (long long)(most / state_mb);
+            a.gate = r.left;
+        }
+        const int status = attn_rows(r);
+        if (status != LUVC_OK || !a.gate) return status;
     }
-    CrossArgs a;
     a.p = p;
     a.group = p.q_heads / p.heads;
     a.c = fabsf(p.scale) * (p.bias ? 1.f : kLog2e);

@@ -189,6 +189,7 @@ struct Args {
     int group, groups;          // query heads per key head; head groups of ROWS
     int page_shift;             // log2 of the page size, -1 if it is no power of two
     int limit;                  // tiles of all sequences up to which the list can be numbered in 32 bits
+    int most;                   // DENSE: and up to which the call is not left to another kernel
     float one_grid;             // 1 / CTAs
     int rows_total;             // rows of the layer's pool (a row number beyond it reads as zeros)
     unsigned* counters;         // [5][kMaxCtas]: arrivals of (sequence, head)s, of their first groups, of the other groups; groups that
@@ -582,7 +583,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             __syncthreads();
         }
     }
-    if (!fits) {                                                // more than 2^31 tiles, a TB at least
+    if constexpr (DENSE) {                                      // the kernel behind this one has the call if it is left
+        if (p.left) {
+            const bool leave = !fits || base > a.most;
+            if (blockIdx.x == 0 && tid == 0) *p.left = leave;
+            if (leave) return;
+        }
+    }
+    if (!fits) {                                                // more than 2^31 tiles, a TB at least (DENSE: attn_cross sees to it)
         if (tid == 0) *p.status = LUVC_ERR_SHAPE;
         return;
     }
@@ -1528,6 +1536,7 @@ int launch(const AttnProblem& p) {
     const int sms = std::min(sm_count(), kMaxCtas);
     if (!sms) return LUVC_ERR_CUDA;
     a.limit = (2147483647 - Sh::SNAP) / (p.c.heads * a.groups);
+    a.most = (int)std::min<long long>(p.most_states / Sh::KT + p.n, 2147483647);        // (a token's last tile need not be full)
     a.one_grid = 1.f / sms;
     a.page_shift = (p.c.page_size & (p.c.page_size - 1)) ? -1 : __builtin_ctz(p.c.page_size);
     a.rows_total = p.c.pages * p.c.heads * p.c.page_size;

@@ -236,6 +236,9 @@ struct AttnProblem {
     const int32_t *q_starts = nullptr, *k_starts = nullptr;
     int n_seqs = 0, k_tokens = 0;
     long long k_stride = 0, v_stride = 0;
+    // attn_rows: where (not NULL) it writes 1, and nothing else, if its tokens read more than so many rows of states in all, or 0
+    int* left = nullptr;
+    long long most_states = 0;
 };
 constexpr int kAttnRowsMost = 1024;
 size_t attn_workspace_bytes();
