@@ -432,7 +432,8 @@ typedef struct {
     union {
         const float* k_scale;    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; else NULL */
         float* k_block_scale;    /* LUVC_E4M3_BLOCK: [layers, pages, heads, page_size / LUVC_KV_BLOCK], a stored key x stands for x
-                                    times the scale of its block; written along with the rows */
+                                    times the scale of its block; written along with the rows, so
+                                    that keys and values must not share scales */
     };
     union {
         const float* v_scale;    /* the same for the values */

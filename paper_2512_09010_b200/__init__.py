@@ -426,7 +426,7 @@ class KvCache:
     k, v: the caller's pools, CUDA tensors [layers, pages, heads, page_size, D] in bfloat16, float32 or
     float8_e4m3fn (then with k_scale / v_scale, float32: a stored x stands for x * scale).  Scales [layers, heads] are the caller's and
     stay as they are; scales [layers, pages, heads, page_size // KV_BLOCK], one for each KV_BLOCK tokens of a page and head, are
-    written along with the rows.
+    written along with the rows, and must not share memory.
     slots: sequences; max_pages: pages a sequence may have.  meta: optional int32 tensor of
     slots + pages + slots * max_pages entries that holds the books (made empty if not given); `lengths`, `refs`
     and `table` are views of it, so that one copy of `meta` is a snapshot of all three."""
@@ -453,6 +453,9 @@ class KvCache:
                                   or s.shape != k_scale.shape or not s.is_contiguous() or s.device != k.device):
                 raise ValueError("scales must be contiguous float32 [layers, heads] or [layers, pages, heads, page_size // %d] tensors on the "
                                  "pools' device" % KV_BLOCK)
+        # (scales for heads are only read, and may be one tensor)
+        if k_scale is not None and k_scale.dim() == 4 and abs(k_scale.data_ptr() - v_scale.data_ptr()) < 4 * k_scale.numel():
+            raise ValueError("k_scale and v_scale are written along with the rows: they must not share memory")
         self.k, self.v, self.meta, self.k_scale, self.v_scale = k, v, meta, k_scale, v_scale
         self.lengths = meta[:slots]
         self.refs = meta[slots:slots + pages]
