@@ -3,8 +3,8 @@
 With seeded random weights in a model's place: OIM merges each image's patch tokens; a merged token stands at the mean row and column
 of its patches, and its key is turned by them (luvc.rope, frame, row and column each for its own frequencies); keys and values, enhanced
 by log(size), are quantised into a paged cache with a scale for each 16 tokens of a head; the rows are read back as the states that the
-tokens of each question look at (luvc.attn_cross, merged tokens weighed by log(size)); and one more token of each question decodes over
-the same cache.
+tokens of each question look at (luvc.attn_cross); and one more token of each question decodes over the same cache.  A merged token's size
+counts once, in its values; with values as they are it would be the key_bias of both calls instead.
 
     python examples/visual_question.py [--images 4] [--tokens 23] [--heads 28]
 
@@ -72,21 +72,19 @@ def run(images: int = 4, tokens: int = 23, q_heads: int = 28, *, side: int = 24,
     q = luvc.rope(q, asked.expand(3, -1), freqs, axis=axis, factor=factor)
     states = torch.empty_like(kv)
     luvc.kv_read(cache, states[:, :heads], states[:, heads:], starts=starts)
-    bias = sizes.view(-1).float().log()
-    seen = luvc.attn_cross(q, states[:, :heads], states[:, heads:], q_starts=ints([tokens * i for i in range(images + 1)]),
-                           k_starts=starts, key_bias=bias)
+    seen = luvc.attn_cross(q, states[:, :heads], states[:, heads:], q_starts=ints([tokens * i for i in range(images + 1)]), k_starts=starts)
     # one more token of each decodes over the cache as it is
     last = q.view(images, tokens, q_heads, dim)[:, -1]
-    answer = luvc.attn_decode(last, cache, key_bias=bias.view(images, merged))
+    answer = luvc.attn_decode(last, cache)
     if luvc.check_status() != 0:
         raise RuntimeError("a call reported a condition")
 
     # the same, densely
     ks, vs = (states.view(images, merged, 2, heads, dim)[:, :, j].double() for j in (0, 1))
     score = torch.einsum("nthgd,nshd->nhgts", q.double().view(images, tokens, heads, -1, dim), ks) * dim ** -0.5
-    p = torch.softmax(score + bias.double().view(images, 1, 1, 1, merged), dim=-1)
+    p = torch.softmax(score, dim=-1)
     want = torch.einsum("nhgts,nshd->nthgd", p, vs).reshape(images, tokens, q_heads, dim)
-    exact = v.double() + bias.double()[:, None, None]
+    exact = v.double() + sizes.view(-1).double().log()[:, None, None]
     return {"cross_error": float((seen.double().view_as(want) - want).norm() / want.norm()),
             "decode_error": float((answer.double() - want[:, -1]).norm() / want[:, -1].norm()),
             "cache_error": float((states[:, heads:].double() - exact).norm() / exact.norm()),
