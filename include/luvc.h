@@ -429,16 +429,24 @@ typedef struct {
     int32_t* lengths;        /* [slots] tokens of each sequence; 0: the slot is empty */
     int32_t* refs;           /* [pages] sequences that hold the page; 0: the page is free */
     int32_t* table;          /* [slots, max_pages] page of each run of page_size tokens, -1 past the sequence */
+    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; v_scale: the same for the values.
+     * LUVC_E4M3_BLOCK: [layers, pages, heads, page_size / LUVC_KV_BLOCK], a stored key x stands for x times the scale of its block; written
+     * along with the rows, so that keys and values must not share scales.  They have names of their own where the language
+     * has unnamed unions (C11, C++); in C99 they are k_scale and v_scale too.
+     * Else NULL. */
+#if defined(__cplusplus) || (defined(__STDC_VERSION__) && __STDC_VERSION__ >= 201112L)
     union {
-        const float* k_scale;    /* LUVC_E4M3: [layers, heads], a stored key x stands for x * k_scale; else NULL */
-        float* k_block_scale;    /* LUVC_E4M3_BLOCK: [layers, pages, heads, page_size / LUVC_KV_BLOCK], a stored key x stands for x
-                                    times the scale of its block; written along with the rows, so
-                                    that keys and values must not share scales */
+        const float* k_scale;
+        float* k_block_scale;
     };
     union {
-        const float* v_scale;    /* the same for the values */
+        const float* v_scale;
         float* v_block_scale;
     };
+#else
+    const float* k_scale;
+    const float* v_scale;
+#endif
     int layers, pages, heads, page_size, D, slots, max_pages;
     int dtype;               /* LUVC_BF16, LUVC_F32, LUVC_E4M3 or LUVC_E4M3_BLOCK */
 } luvc_kv_cache;
