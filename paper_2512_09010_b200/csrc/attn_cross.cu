@@ -408,7 +408,8 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
     pdl_trigger();
     pdl_wait();
     if (a.gate && *a.gate == 0) return;
-    Work<BN, 2> work(a);
+    Work<BN, 2> work(a);            // (parts, nearly always: eight sequences of 8 tokens, 32 / 8 heads of 128, 1296 states 100 us, whole blocks 152; four of 40,
+                                    // 16 / 16 of 64, 2000 states 82 and 271; six of 33 to 257 tokens to 64 to 576 states 103 and 153)
     work.template begin<NT>();
     empty_sequences<float, NT>(a, work);
     for (int e = tid; e < (BM + BN) * (LD / 4); e += NT) reinterpret_cast<float4*>(qs)[e] = make_float4(0.f, 0.f, 0.f, 0.f);   // columns past D
@@ -616,7 +617,11 @@ template <int DP_>
 struct Tc {
     static constexpr int DP = DP_, TILES = DP <= 128 ? 2 : 1, BN = DP <= 128 ? 128 : 64, ROWS = 128 * TILES;
     static constexpr int Q_BYTES = 128 * DP * 2, STAGE = BN * DP * 2, STAGES = DP == 64 ? 8 : 5;
-    static constexpr int JOIN = 8;          // (measured: 16 single tokens to 1296 states, 28 / 4 heads, in whole blocks 25 us, in parts 31)
+    // Tiles that a join costs as much as.  28 / 4 heads of 128, four sequences of 33 tokens to 700, 1296, 2600 and 4000 states (whole blocks have 4, 8, 16 and
+    // 25 tiles more in a CTA): 17.8, 23.5, 33.5 and 44.5 us, in parts 24.3, 39.9, 42.3 and 45.4; 16 / 16 of 64, 128 tokens to 1024 and 2048 (7
+    // and 14 more): 16.4 and 24.1, in parts 18.9 and 20.0; 12 / 1 of 256, four of 100 to 1000, 2000 and 3000 (11, 23, 34 more): 35.7, 60.1 and 81.6, in
+    // parts 50.3, 63.5 and 68.6.
+    static constexpr int JOIN = DP == 64 ? 10 : 18;
     static constexpr int THREADS = 384, S_COLS = 128, O_COL = 256, O_COLS = DP <= 128 ? 128 : 256;
     static constexpr size_t SMEM = 1024 + TILES * Q_BYTES + STAGES * STAGE;
     // registers of the threads that have weights, and of the others: together what the launch has, 384 times 168
