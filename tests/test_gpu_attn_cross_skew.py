@@ -71,3 +71,16 @@ def test_a_list_that_tokens_alone_would_make_too_long(luvc):  # noqa: F811
     assert luvc.check_status() == 0
     some = [0, 1, 700, 2047]
     check(q[:, some], k[:, some], v[:, some], qs[-2:], ks[-2:], out[:, some], None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("queries,keys", [([2048, 60], [0, 300]), ([60] + [300] * 8, [1296] + [0] * 8), ([700], [0]), ([33] + [9, 0] * 100 + [70], [40] + [0] * 201),
+                                          ([20] * 147 + [500], [0] * 100 + [60] * 47 + [0]), ([10] * 320 + [90], [30, 0] * 160 + [0])])
+def test_many_tokens_without_states(luvc, dtype, queries, keys):  # noqa: F811
+    """Beside others that have some, or alone."""
+    q, k, v, qs, ks = inputs(dtype, 6, 2, 64, queries, keys, seed=3, q_more=2, k_more=1)
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    out, lse = luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks, want_lse=True, out=out)
+    assert luvc.check_status() == 0
+    check(q, k, v, qs, ks, out, lse)
+    assert bool((out[-2:] == 7.0).all())
