@@ -622,7 +622,8 @@ typedef struct {
  * k_starts    DEVICE [n + 1], ascending, 0 to k_tokens: its states are k_starts[i] .. k_starts[i+1]-1
  * A sequence without states, or whose states are all masked by -inf, gives rows of zeros; a state masked by -inf contributes nothing,
  * whatever its rows hold.  Scores, softmax and sums are fp32; bf16: a weight enters its product with V rounded to bf16 (of few
- * tokens with 16 bits).  A call
+ * tokens with 16 bits).  Sums of values stay in range where the values are; results below 2^-126 times the number of states (bf16: 2^16 times that)
+ * may lose bits.  A call
  * repeated gives the same bits; how the work is split, and with it the last bits, depends on all lengths of the call.  The call runs
  * whatever the status word says.
  * Limits: D a multiple of 8 (bf16) or 4 (fp32) up to 256; q_heads up to 65536, a multiple of heads; n up to 4096.  A call of 2^31 tiles

@@ -14,11 +14,12 @@
 // (sequence, key head, block of rows)s: a join costs as much as some tiles (JOIN).
 //
 // Bound.  4 D flops for each row and state: the tensor pipe, where there are many rows.  Two sequences of 1777 to 2048 tokens to 12001 to 16384
-// states, 32 / 8 heads of 128 (970 GFLOP, bf16): 1059 to 1089 us, 0.53 of the rate of a large matrix product (one of 2048 to 16384: 524 us for 550
-// GFLOP, 0.62).  Eight questions of 17 to 96 tokens to 1296 states, 28 / 4 heads: 26.4 us, a chain of latencies.  A few tokens are a matter of bytes, and
-// go another way (attn_rows).
+// states, 32 / 8 heads of 128 (970 GFLOP, bf16): 984 us in a short loop, 0.59 of the rate of a large matrix product, 1083 in a long one, where the power
+// limit brings the clock down (one of 2048 to 16384: 530 us for 550 GFLOP, 0.62).  Eight questions of 17 to 96 tokens to 1296 states, 28 / 4 heads:
+// 26.4 us, a chain of latencies.  A few tokens are a matter of bytes, and go another way (attn_rows).
 //
-// bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums, 44 TFLOP/s of 73 that packed products reach.
+// bf16: tensor cores (attn_cross_tc).  f32: CUDA cores (attn_cross_f32), 32-bit products and sums, 44 TFLOP/s of 73 that packed products reach (a
+// choice: pairs of tf32 on the tensor cores are not built).
 
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -385,7 +386,7 @@ __device__ void join_parts(const CrossArgs& a, const Item& it, int c0, int c1, i
 // ---- f32 on the CUDA cores --------------------------------------------------------------------------------------------
 
 // Tiles of BM rows by 64 states, 256 threads: a thread has RT = BM / 16 rows (ty) and every 16th state or group of four columns (tx): eight rows
-// take half the reads of shared memory per product of four, but one CTA has an SM then (69 GFLOP, 16 / 4 heads of 128: BM = 128 1559 us, two CTAs of
+// take half the reads of shared memory per product of four, but one CTA has an SM then (69 GFLOP, 16 / 4 heads of 128: BM = 128 1547 us, two CTAs of
 // 64 2164).  Products are packed pairs; K and V have one buffer each, and the next tile of K is on its way during the products with V, and the other way round.
 template <int BM, int DP>
 struct Cores {
@@ -576,7 +577,7 @@ __global__ void __launch_bounds__(256, Cores<BM, DP>::CTAS) attn_cross_f32(const
         }
     };
     while (work.more()) {
-        // as many rows of a thread as the block needs (six ragged texts of 33 to 257 tokens: always eight 101.8 us, by the block's rows 96.0)
+        // as many rows of a thread as the block needs (six ragged texts of 33 to 257 tokens: always eight 101.8 us, by the block's rows 97.0)
         const Item it = work.next();
         if constexpr (C::RT >= 8) {
             if (it.rows > 64) {

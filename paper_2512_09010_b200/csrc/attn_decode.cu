@@ -36,8 +36,8 @@
 //
 // Scales for blocks (LUVC_E4M3_BLOCK).  A 16-token part of a tile has one scale for K, which the scores are multiplied by, and one for V, which
 // the weights are: O is held in units that follow the scales of V, so that a weight loses two bits at most.  A lane holds
-// the scales of one block, of 32 blocks at a time; the next 32 are on their way meanwhile (249 MB: 55.7 us, with one scale for a head
-// 50.5, with scales that are copied along with each tile 57.9).
+// the scales of one block, of 32 blocks at a time; the next 32 are on their way meanwhile (249 MB: 56.0 us, with one scale for a head
+// 50.8, with scales that are copied along with each tile 57.9).
 
 #include <cuda.h>
 #include <cuda_bf16.h>

@@ -8,8 +8,8 @@
 // old rows are brought to it.
 //
 // Bound.  A bf16 row is read once and written with half its bytes, or the other way round: HBM, once there are enough tokens.  Prompts of
-// 34780 tokens, 8 heads of 128: 42.5 us with sizes, 39.5 without, 0.75 and 0.80 of the copy rate (issue slots 68 % busy); read back
-// 42.4 us, 0.84.
+// 33947 tokens, 8 heads of 128: 42.5 us with sizes, 39.5 without, 0.75 and 0.80 of the copy rate (issue slots 68 % busy); 37861 read back
+// 42.3 us, 0.84.
 //
 // Split.  A CTA takes up to 32 tokens.  Its first warp finds the blocks that begin among them (a token that is the first of the call in its
 // block leads it, wherever the block ends); then each warp takes one (block, head, K or V) after the other, all of it in
