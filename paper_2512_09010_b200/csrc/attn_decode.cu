@@ -76,6 +76,8 @@ constexpr float kLeastUnit = 0.25f;
 constexpr float kLowestUnit = 0x1p-50f;
 // At the end of a warp's part, a sum of weights beyond this is brought to about one, and O with it, which leaves its units then: scales go up to 2^60.
 constexpr float kMostSum = 0x1p30f;
+// DENSE: a warp's part leaves it as this part of its sums, so that the parts of all warps, 2^12 at most, add up to no more than the range has.
+constexpr float kPartDown = 0x1p-12f;
 constexpr int kWaitProbes = 1 << 20;            // probes before a wait for a copy gives up (seconds)
 constexpr int kLeastProbes = 1 << 12;           // and with a limit from the status block (a test's), so that copies which do come are waited for
 
@@ -299,15 +301,15 @@ __device__ __forceinline__ void join4(int count, bool last, Factor factor, Colum
         }
     }
 }
-__device__ __forceinline__ float lse_of(float2 ml) { return ml.y == 0.f ? -INFINITY : (ml.x == -INFINITY ? 0.f : ml.x) + logf(ml.y); }
+__device__ __forceinline__ float lse_of(float2 ml, float up) { return ml.y == 0.f ? -INFINITY : (ml.x == -INFINITY ? 0.f : ml.x) + logf(ml.y * up); }
 
 // Final values of four columns of a row of out; no key left: zeros, -inf.
 template <typename TQ>
-__device__ __forceinline__ void emit4(const AttnProblem& p, long long row, int d, float vscale, float m, float l, float4 o) {
+__device__ __forceinline__ void emit4(const AttnProblem& p, long long row, int d, float vscale, float m, float l, float4 o, float up) {
     const float f = vscale / l;
     put4(static_cast<TQ*>(p.out) + row * p.c.D + d,
          l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-    if (p.lse && d == 0) p.lse[row] = lse_of(make_float2(m, l));
+    if (p.lse && d == 0) p.lse[row] = lse_of(make_float2(m, l), up);
 }
 
 // What is joined in a CTA: the parts of warps first_warp .. first_warp + count - 1 of one (sequence, head).
@@ -461,11 +463,11 @@ __device__ __noinline__ void plain_piece(const Args& a, int seq, int k0, int h, 
 #pragma unroll
             for (int j = 0; j < DP / 32; ++j) o[j] = lane + 32 * j < D ? fmaf(o[j], f, w * v[j]) : 0.f;
         }
-        // the mean as a partial result whose weights sum to 2^-20: joins add up many of them
-        const float of_sum = DENSE ? 0x1p-20f : 1.f;
+        // the mean as a partial result whose weights sum to one
+        const float of_sum = DENSE ? kPartDown : 1.f;
 #pragma unroll
         for (int j = 0; j < DP / 32; ++j) os[o_index(r, lane + 32 * j, DP)] = o[j] * of_sum;
-        if (lane == 0) ml[r] = DENSE && l > 0.f ? make_float2(m + logf(l) + 13.862944f, of_sum) : make_float2(m, l);
+        if (lane == 0) ml[r] = DENSE && l > 0.f ? make_float2(m + logf(l), of_sum) : make_float2(m, l);
     }
     __syncwarp();
 }
@@ -478,6 +480,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     using Sh = Shape<TC, DPB, NT>;
     constexpr int NW = Sh::NW, S = Sh::S, MT = Sh::MT, DP = Sh::DP, ROWS = Sh::ROWS, KT = Sh::KT, NTHR = 32 * NW;
     constexpr bool kF32 = Sh::ES == 4, kF8 = Sh::ES == 1, kCores = Sh::CORES, kBlocks = std::is_same<TC, E4m3Block>::value;
+    constexpr float kDown = DENSE ? kPartDown : 1.f, kUp = 1.f / kDown;
     constexpr int NTX = kCores ? 1 : NT, NH = kCores ? -NT : 1; // sizes of arrays that are not used otherwise
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[NW * S];
@@ -1198,9 +1201,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                     float x = core_l[r];
 #pragma unroll
                     for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-                    if (lane == 0) ml_of[warp][which][r] = make_float2(core_m[r], x);
+                    if (lane == 0) ml_of[warp][which][r] = make_float2(core_m[r], x * kDown);
 #pragma unroll
-                    for (int j = 0; j < DP / 32; ++j) os[o_index(r, f32_column<DP>(lane, j), DP)] = core_o[r][j];
+                    for (int j = 0; j < DP / 32; ++j) os[o_index(r, f32_column<DP>(lane, j), DP)] = core_o[r][j] * kDown;
                 }
             }
             float o_unit[NTX][2];                               // blocks: of O, for each head
@@ -1220,7 +1223,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                         x *= f;
                         o_unit[nt][b] = v_unit * f;
                     }
-                    if (g == 0) ml_of[warp][which][nt * 8 + 2 * t4 + b] = make_float2(to, x);
+                    if (g == 0) ml_of[warp][which][nt * 8 + 2 * t4 + b] = make_float2(to, x * kDown);
                 }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
@@ -1229,7 +1232,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int d = 16 * mt + (kF8 ? 2 * g + (c >> 1) : g + 8 * (c >> 1));
-                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = kBlocks ? o[mt][nt][c] * o_unit[nt][c & 1] : o[mt][nt][c];
+                        os[o_index(nt * 8 + 2 * t4 + (c & 1), d, DP)] = kBlocks ? o[mt][nt][c] * o_unit[nt][c & 1] : o[mt][nt][c] * kDown;
                     }
             __syncwarp();
             if constexpr (!kF8) {                               // (an e4m3 cache has no infinities, and its rows are not split)
@@ -1254,7 +1257,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             if (whole) {
                 if (lane < rows) {                              // the factor takes the maximum's place
                     const float2 ml = ml_of[warp][1][lane];
-                    if (p.lse) p.lse[row0 + lane] = lse_of(ml);
+                    if (p.lse) p.lse[row0 + lane] = lse_of(ml, kUp);
                     ml_of[warp][1][lane].x = ml.y == 0.f ? 0.f : vscale / ml.y;
                 }
                 __syncwarp();
@@ -1328,7 +1331,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                   [&](int k) { return reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring + piece_off[w0 + k][k ? 0 : ch.from]) + at); },
                   m, l, o);
             if (ch.c0 == ch.c1) {
-                emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o);
+                emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o, kUp);
             } else {
                 const Part q = global_part(blockIdx.x, ch.s0 >= cta_a);
                 *reinterpret_cast<float4*>(q.o + at) = o;
@@ -1345,7 +1348,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                 const float2 all = join_factors(ch.count, ml, [&](int k, float f) { ml(k).x = f; }, final, ch.vscale, lane);
                 if (lane == 0) {
                     if (!final) global_part(blockIdx.x, ch.s0 >= cta_a).ml[r] = all;
-                    else if (p.lse) p.lse[ch.row0 + r] = lse_of(all);
+                    else if (p.lse) p.lse[ch.row0 + r] = lse_of(all, kUp);
                 }
             }
         }
@@ -1425,7 +1428,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                                                     [&](int k, float f) { factors[k][r] = f; }, final, ch.vscale, lane);
                     if (lane == 0) {
                         if (!final) to.ml[r] = all;
-                        else if (p.lse) p.lse[ch.row0 + r] = lse_of(all);
+                        else if (p.lse) p.lse[ch.row0 + r] = lse_of(all, kUp);
                     }
                 }
             cp_async_wait<0>();
@@ -1449,7 +1452,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             const int e = tid + x * NTHR, r = e / (DP / 4), d = e % (DP / 4) * 4;
             if (r >= ch.rows || d >= p.c.D) continue;
             if (final) {
-                if constexpr (E == 1) emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o[x]);
+                if constexpr (E == 1) emit4<TQ>(p, ch.row0 + r, d, ch.vscale, m, l, o[x], kUp);
                 else put4(out_row(ch.row0 + r) + d, o[x]);
             } else {
                 *reinterpret_cast<float4*>(to.o + o_index(r, d, DP)) = o[x];

@@ -82,3 +82,20 @@ def test_nan_and_infinities_take_no_longer(luvc, hq, D, queries, keys):  # noqa:
     assert bool(got[queries // 2, 1].isnan().all())
     got[queries // 2, 1] = 0.0
     assert bool(got[..., rest].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,heads,D", [(4, 2, 64), (28, 4, 128), (16, 1, 128), (3, 1, 256)])
+@pytest.mark.parametrize("queries,keys", [([1], [40000]), ([2], [300]), ([1, 0, 2, 1], [700, 30, 5000, 16]), ([30], [200])])
+def test_one_state_of_each_tile_counts(luvc, dtype, hq, heads, D, queries, keys):  # noqa: F811
+    """So that every part of a sum is in range, and the parts together are not."""
+    q, k, v, qs, ks = inputs(dtype, hq, heads, D, queries, keys, seed=D)
+    k.zero_()
+    v.fill_(3e38)
+    bias = torch.full((k.shape[0],), -math.inf, device="cuda")
+    for i, n in enumerate(keys):
+        bias[int(ks[i]):int(ks[i]) + n:16] = 0.0
+    out, lse = luvc.attn_cross(q, k, v, q_starts=qs, k_starts=ks, key_bias=bias, want_lse=True)
+    assert luvc.check_status() == 0
+    assert bool(out.isfinite().all())
+    check(q, k, v, qs, ks, out, lse, bias=bias)
